@@ -280,6 +280,46 @@ int oq_adaln_linear(const void* X_bf16, int n_tokens, int ldx, const void* Wq, c
  * bf16 bit patterns [m][dim / 64]. */
 int oq_adaln_unpack(const void* Wq, const void* scales, int m, int dim, void* q_int8, void* scale_bf16, void* stream);
 
+/* ---- queries and keys between the QKV projection and attention ------------------------------------------- */
+
+/* Rotation by position with 1 to 4 axes (time, height, width, ...): axis a owns axis_dims[a] adjacent coordinates of a
+ * head, in the order given, and turns pair i of them by pos[a] * theta^(-2 i / axis_dims[a]).  OQ_ROPE_PAIRS: pair i is
+ * the adjacent coordinates (2i, 2i + 1) of the axis; OQ_ROPE_HALVES: coordinates (i, i + axis_dims[a] / 2).
+ * Coordinates of a head beyond the axes' sum are not turned.  max_pos[a]: positions 0 .. max_pos[a] - 1 are held in a
+ * table of cosines and sines (computed in fp64 on the host, stored in fp32, uploaded on first use to the device that
+ * is current then).  axis_dims even (halves layout: multiples of 16), their sum at most 256.  *out is owned by the
+ * caller (oq_rope_destroy).  Errors: OQ_ERR_INVALID_ARG, OQ_ERR_UNSUPPORTED, OQ_ERR_NOMEM. */
+typedef struct oq_rope oq_rope;
+enum { OQ_ROPE_PAIRS = 0, OQ_ROPE_HALVES = 1 };
+int oq_make_rope(int n_axes, const int* axis_dims, const int* max_pos, double theta, int layout, oq_rope** out);
+int oq_rope_dim(const oq_rope* rope);
+void oq_rope_destroy(oq_rope* rope);
+
+/* Norms of queries and keys and their rotation, one pass:
+ *   n = x * rsqrt(mean(x^2) + eps) * w, then the rotation of `rope` at pos[token]
+ * with the mean over one head (OQ_NORM_HEAD, w has head_dim values) or over all heads of the token (OQ_NORM_ROW, w has
+ * n_heads * head_dim values); OQ_NORM_NONE only turns.  Arithmetic in fp32, one rounding when y_dtype is OQ_BF16.
+ *   oq_qk_side   X dev, element (token, head, c) at X[token * ld_token + head * ld_head + c], of x_dtype (OQ_BF16 or
+ *                OQ_F32); Y dev, laid out by ldy_*, of y_dtype; w_bf16 dev or NULL (no weights).  Y may be X with the
+ *                same strides and type; otherwise the two must not overlap.  All strides are in elements.
+ *   q, k         either may be NULL (cross attention, where queries and keys come from different tokens).
+ *   pos          dev int32, pos[token * ldpos + axis]; NULL with rope == NULL.  A token with a position outside the
+ *                table gets NaN in the coordinates of that axis.
+ * head_dim 32, 64, 128 or 256; pointers 16-byte aligned, strides multiples of 16 bytes; OQ_NORM_ROW: at most 32768
+ * values a row.  Asynchronous on `stream`.  n_tokens == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED,
+ * ALIGNMENT, CUDA. */
+enum { OQ_NORM_NONE = 0, OQ_NORM_HEAD = 1, OQ_NORM_ROW = 2 };
+typedef struct {
+  const void* X;
+  long long ld_token, ld_head;
+  int n_heads;
+  const void* w_bf16;
+  void* Y;
+  long long ldy_token, ldy_head;
+} oq_qk_side;
+int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int head_dim, const oq_rope* rope, const int* pos,
+                    int ldpos, int norm, float eps, int x_dtype, int y_dtype, void* stream);
+
 /* Self-test of the bounded device-side waits the GEMM pipeline is built on: launches one thread that waits
  * about a millisecond on a barrier nobody arrives at.  The wait gives up by itself (the kernel ends
  * normally, nothing hangs or traps) and records code 9; the following oq_device_status() must return

@@ -60,6 +60,9 @@ def lib():
             "oq_adaln_linear": (i, [vp, i, i, vp, vp, i, i, vp, i, i, vp]),
             "oq_adaln_unpack": (i, [vp, vp, i, i, vp, vp, vp]),
             "oq_block_forward": (i, [i, vp, i, vp, i, vp]),
+            "oq_make_rope": (i, [i, vp, vp, C.c_double, i, pp]),
+            "oq_rope_dim": (i, [vp]), "oq_rope_destroy": (None, [vp]),
+            "oq_qk_norm_rope": (i, [vp, vp, i, i, vp, vp, i, i, C.c_float, i, i, vp]),
             "oq_last_error": (C.c_char_p, []), "oq_version": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -119,6 +122,28 @@ class Rpbh:
     def __del__(self):
         if getattr(self, "handle", None) and _lib is not None:
             _lib.oq_rpbh_destroy(self.handle)
+            self.handle = None
+
+
+class Rope:
+    """Owns an oq_rope handle."""
+
+    LAYOUTS = {"pairs": 0, "halves": 1}
+
+    def __init__(self, axis_dims, max_pos, theta, layout):
+        dims, top = np.asarray(axis_dims, np.int32), np.asarray(max_pos, np.int32)
+        if dims.ndim != 1 or dims.shape != top.shape:
+            raise OqError(1, "oq_make_rope: axis_dims and max_pos must be lists of one length")
+        if layout not in self.LAYOUTS:
+            raise OqError(1, f"oq_make_rope: layout must be one of {sorted(self.LAYOUTS)}")
+        h = C.c_void_p()
+        _check(lib().oq_make_rope(len(dims), dims.ctypes.data, top.ctypes.data, float(theta), self.LAYOUTS[layout], C.byref(h)))
+        self.handle, self.axis_dims, self.max_pos = h, dims.tolist(), top.tolist()
+        self.theta, self.layout, self.dim = theta, layout, int(dims.sum())
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.oq_rope_destroy(self.handle)
             self.handle = None
 
 
@@ -346,6 +371,73 @@ def oq_adaln_unpack(Wq, Sc, m, dim):
     s = torch.empty((m, dim // 64), dtype=torch.bfloat16, device=Wq.device)
     _check(lib().oq_adaln_unpack(_ptr(Wq), _ptr(Sc), m, dim, _ptr(q), _ptr(s), _stream()))
     return q, s
+
+
+def oq_make_rope(axis_dims, max_pos, theta=10000.0, layout="pairs"):
+    """Rotation by position with len(axis_dims) axes; positions 0 .. max_pos[a] - 1 on axis a."""
+    return Rope(axis_dims, max_pos, theta, layout)
+
+
+def _dtype_code(t, what):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return OQ_BF16
+    if t.dtype == torch.float32:
+        return OQ_F32
+    raise OqError(1, f"{what}: bf16 or fp32 expected, got {t.dtype}")
+
+
+def _stride(t, dim):
+    return t.stride(dim) if t.shape[dim] > 1 else 0       # the stride of a single row is free in torch
+
+
+class _QkSide(C.Structure):              # oq_qk_side
+    _fields_ = [("X", C.c_void_p), ("ld_token", C.c_longlong), ("ld_head", C.c_longlong), ("n_heads", C.c_int),
+                ("w_bf16", C.c_void_p), ("Y", C.c_void_p), ("ldy_token", C.c_longlong), ("ldy_head", C.c_longlong)]
+
+
+NORMS = {"none": 0, "head": 1, "row": 2}
+
+
+def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", eps=1e-6, out_q=None, out_k=None, out_dtype=None):
+    """Q, K: CUDA [T, heads, head_dim] (bf16 or fp32, any token and head strides, unit stride inside a head); K may be
+    None.  pos: CUDA int32 [T, axes].  wq, wk: CUDA bf16, head_dim values (norm="head") or heads * head_dim (norm="row").
+    Returns (Q', K'), of out_dtype (the inputs' by default); out_q, out_k may be Q and K themselves."""
+    import torch
+    n, head_dim = Q.shape[0], Q.shape[2]
+    if norm not in NORMS:
+        raise OqError(1, f"oq_qk_norm_rope: norm must be one of {sorted(NORMS)}")
+    sides, outs, given = [], [], [(Q, wq, out_q), (K, wk, out_k)]
+    for X, w, Y in given:
+        if X is None:
+            sides.append(None), outs.append(None)
+            continue
+        if X.dim() != 3 or X.shape[0] != n or X.shape[2] != head_dim or X.dtype != Q.dtype:
+            raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim] of one T, head_dim and type")
+        if Y is None:
+            Y = torch.empty(X.shape, dtype=out_dtype or X.dtype, device=X.device)
+        if Y.shape != X.shape or (outs and Y.dtype != outs[0].dtype):
+            raise OqError(1, "oq_qk_norm_rope: outputs must have the inputs' shape and one type")
+        if X.numel() and (X.stride(2) != 1 or Y.stride(2) != 1):
+            raise OqError(3, "oq_qk_norm_rope: the coordinates of a head must be adjacent")
+        heads = X.shape[1]
+        if w is not None and (w.dtype != torch.bfloat16 or w.numel() != (head_dim if norm == "head" else heads * head_dim) or not w.is_contiguous()):
+            raise OqError(1, "oq_qk_norm_rope: weights must be contiguous bf16, one for each normed coordinate")
+        sides.append(_QkSide(X.data_ptr(), _stride(X, 0), _stride(X, 1), heads, w.data_ptr() if w is not None else None,
+                             Y.data_ptr(), _stride(Y, 0), _stride(Y, 1)))
+        outs.append(Y)
+    ldpos = 0
+    if rope is not None:
+        if pos is None or pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape != (n, len(rope.axis_dims)):
+            raise OqError(1, "oq_qk_norm_rope: pos must be int32 [T, axes]")
+        if n and pos.shape[1] > 1 and pos.stride(1) != 1:
+            raise OqError(3, "oq_qk_norm_rope: the positions of a token must be adjacent")
+        ldpos = pos.stride(0) if n > 1 else pos.shape[1]
+    _check(lib().oq_qk_norm_rope(C.byref(sides[0]), C.byref(sides[1]) if sides[1] is not None else None, n, head_dim,
+                                 rope.handle if rope is not None else None, pos.data_ptr() if rope is not None else None, ldpos,
+                                 NORMS[norm], eps, _dtype_code(Q, "oq_qk_norm_rope"), _dtype_code(outs[0], "oq_qk_norm_rope"),
+                                 _stream()))
+    return outs[0], outs[1]
 
 
 def oq_version():

@@ -1,0 +1,417 @@
+// Norms of queries and keys and their rotation by position, in one pass (between the QKV projection and attention).
+//
+//   n = x * rsqrt(mean(x^2) + eps) * w              the mean over one head, or over all heads of the token
+//   angle(a, i) = pos[a] * theta^(-2 i / d_a)       axis a (time, height, width, ...) owns d_a coordinates of a head
+//   (u, v) -> (u cos - v sin, u sin + v cos)        for the pair (u, v) that belongs to (a, i)
+//
+// Bound: memory.  Every value is read once and written once, and there are about 8 operations per value.  A lane owns
+// 8 adjacent coordinates of a head (one 16-byte access in bf16), a warp 256 / head_dim heads at a time; it requests
+// all of its ITERS rows before it uses the first one, so that 2 KB per warp are in flight while the rotation's table is
+// looked up (pos -> table is the only dependent pair of loads).  The lane's cosines and sines depend on the token alone
+// and serve all of its ITERS heads.  The table (fp64 on the host, rounded once) replaces the sine and cosine of
+// an angle that fp32 could not hold: at position 32760 half a unit in the last place is already 1e-3.
+//
+// Measured (B200): 4608 tokens x (24 + 24) heads of 128 and 32760 tokens x (40 + 40) heads: see the launch rule below.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include <mutex>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "oq_internal.h"
+
+struct oq_rope {
+  int n_axes = 0, dim = 0, layout = 0;
+  std::vector<int> axis_dim, max_pos;
+  std::vector<float> table;          // (cos, sin) pairs: [axis][pos][d_a / 2]
+  std::vector<long long> base;       // first pair of an axis in the table
+  mutable std::mutex mutex;
+  mutable float2* d_table = nullptr; // device copy, created on first GPU use
+  mutable int device = -1;
+};
+
+namespace oq {
+namespace qk {
+
+constexpr int ITERS = 4;            // rows of 256 coordinates one warp holds at a time
+constexpr int WARPS = 8;            // warps of a CTA when the norm stays inside a head
+constexpr int MAX_AXES = 4;
+constexpr int MAX_ROW_WARPS = 32;
+
+struct Side {
+  const void* X;
+  void* Y;
+  const __nv_bfloat16* w;
+  long long ld_token, ld_head, ldy_token, ldy_head;
+  int heads, chunks;                // chunks of ITERS * (256 / head_dim) heads
+};
+struct Params {
+  Side side[2];
+  int tokens, lanes_per_head, head_dim, rot_dim, n_axes, norm;
+  float eps;
+  const int* pos;
+  long long ldpos;
+  const float2* table;
+  int axis_end[MAX_AXES];           // in coordinates of the head
+  int max_pos[MAX_AXES];
+  long long base[MAX_AXES];
+};
+
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = load16(p); }
+  __device__ __forceinline__ void get(float (&x)[8]) const { unpack8(a, x); }
+};
+template <>
+struct Raw<float> {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = load16(p);
+    b = load16(p + 4);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+  }
+};
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+  uint4 v;
+  __nv_bfloat162 h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+  v.x = *reinterpret_cast<uint32_t*>(&h[0]); v.y = *reinterpret_cast<uint32_t*>(&h[1]);
+  v.z = *reinterpret_cast<uint32_t*>(&h[2]); v.w = *reinterpret_cast<uint32_t*>(&h[3]);
+  *reinterpret_cast<uint4*>(p) = v;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// ROW: the norm runs over all heads of a token; a CTA is one (token, side), its warps meet once in shared memory.
+// Otherwise a warp is one (token, side, chunk of heads) and the norm closes inside the lanes of a head.
+// HALVES: the partner of a coordinate lies d_a / 2 further on (in another lane), otherwise right beside it.
+template <typename In, typename Out, bool ROW, bool HALVES>
+__global__ void __launch_bounds__(ROW ? MAX_ROW_WARPS * 32 : WARPS * 32) qk_norm_rope_kernel(const Params p) {
+  __shared__ float red[MAX_ROW_WARPS];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int L = p.lanes_per_head, sub = lane & (L - 1), c0 = 8 * sub;
+  const int per_iter = 32 / L;
+  long long token;
+  int s, chunk;
+  if (ROW) {
+    const int sides = (p.side[0].heads > 0) + (p.side[1].heads > 0);
+    token = blockIdx.x / sides;
+    s = sides == 2 ? (int)(blockIdx.x % 2) : (p.side[0].heads > 0 ? 0 : 1);
+    chunk = warp;
+  } else {
+    const long long item = (long long)blockIdx.x * WARPS + warp;
+    const int per_token = p.side[0].chunks + p.side[1].chunks;
+    token = item / per_token;
+    const int r = (int)(item % per_token);
+    s = r >= p.side[0].chunks;
+    chunk = s ? r - p.side[0].chunks : r;
+    if (token >= p.tokens) return;
+  }
+  const Side& sd = p.side[s];
+  const In* src = reinterpret_cast<const In*>(sd.X) + token * sd.ld_token + c0;
+  const int head0 = chunk * ITERS * per_iter + lane / L;
+  Raw<In> raw[ITERS];
+#pragma unroll
+  for (int i = 0; i < ITERS; ++i) {
+    const int h = head0 + i * per_iter;
+    if (h < sd.heads) raw[i].load(src + (long long)h * sd.ld_head);
+  }
+  // this lane's cosines and sines; (1, 0) where nothing rotates
+  constexpr int NP = HALVES ? 8 : 4;
+  float cs[NP], sn[NP];
+  int partner = lane;
+#pragma unroll
+  for (int e = 0; e < NP; ++e) {
+    const int c = HALVES ? c0 + e : c0 + 2 * e;
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+    if (c < p.rot_dim) {
+      int a = 0, begin = 0;
+      while (a + 1 < p.n_axes && c >= p.axis_end[a]) begin = p.axis_end[a++];
+      const int half = (p.axis_end[a] - begin) >> 1;
+      const int q = __ldg(p.pos + token * p.ldpos + a);
+      int f = HALVES ? c - begin : (c - begin) >> 1;
+      bool upper = false;
+      if (HALVES && f >= half) {
+        f -= half;
+        upper = true;
+      }
+      if (HALVES) partner = upper ? lane - half / 8 : lane + half / 8;
+      float2 t = make_float2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));   // a position outside the table shows as NaN
+      if (q >= 0 && q < p.max_pos[a]) t = __ldg(p.table + p.base[a] + (long long)q * half + f);
+      cs[e] = t.x;
+      sn[e] = HALVES ? (upper ? t.y : -t.y) : t.y;
+    }
+  }
+  float w[8];
+  if (!ROW && sd.w) unpack8(*reinterpret_cast<const uint4*>(sd.w + c0), w);
+  float inv_row = 1.f;
+  if (ROW) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITERS; ++i) {
+      if (head0 + i * per_iter >= sd.heads) continue;
+      float x[8];
+      raw[i].get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) red[warp] = sum;
+    __syncthreads();
+    float total = lane < (int)(blockDim.x >> 5) ? red[lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+    inv_row = rsqrtf(total / (float)(sd.heads * p.head_dim) + p.eps);
+  }
+#pragma unroll
+  for (int i = 0; i < ITERS; ++i) {
+    const int h = head0 + i * per_iter;
+    const bool have = h < sd.heads;                // lanes of another head may still need this lane's shuffles
+    float x[8];
+    if (have) {
+      raw[i].get(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    }
+    float inv = inv_row;
+    if (!ROW && p.norm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+      for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+      inv = rsqrtf(sum / (float)p.head_dim + p.eps);
+    }
+    if (ROW && sd.w && have) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + (long long)h * p.head_dim + c0)), w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = sd.w ? x[e] * inv * w[e] : x[e] * inv;
+    float y[8];
+    if (HALVES) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float other = __shfl_sync(~0u, x[e], partner);
+        y[e] = partner == lane ? x[e] : fmaf(other, sn[e], x[e] * cs[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[2 * e] = fmaf(-x[2 * e + 1], sn[e], x[2 * e] * cs[e]);
+        y[2 * e + 1] = fmaf(x[2 * e], sn[e], x[2 * e + 1] * cs[e]);
+      }
+      if (c0 + 8 > p.rot_dim) {                    // no arithmetic on what does not rotate (an infinity stays one)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c0 + e >= p.rot_dim) y[e] = x[e];
+      }
+    }
+    if (have) store8(reinterpret_cast<Out*>(sd.Y) + token * sd.ldy_token + (long long)h * sd.ldy_head + c0, y);
+  }
+}
+
+template <typename In, typename Out>
+cudaError_t launch(const Params& p, bool row, bool halves, long long ctas, int threads, cudaStream_t st) {
+  void (*kernel)(Params) = row ? (halves ? qk_norm_rope_kernel<In, Out, true, true> : qk_norm_rope_kernel<In, Out, true, false>)
+                               : (halves ? qk_norm_rope_kernel<In, Out, false, true> : qk_norm_rope_kernel<In, Out, false, false>);
+  return launch_dependent(kernel, (int)ctas, threads, 0, st, p);
+}
+
+int ensure_table(const oq_rope* r) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+  std::lock_guard<std::mutex> lock(r->mutex);
+  if (r->d_table && r->device == dev) return OQ_OK;
+  if (r->d_table) return fail(OQ_ERR_INVALID_ARG, "rope handle was first used on another device");
+  float2* d = nullptr;
+  e = cudaMalloc(&d, r->table.size() * sizeof(float));
+  if (e != cudaSuccess) return cuda_fail(e, "cudaMalloc(rope table)");
+  e = cudaMemcpy(d, r->table.data(), r->table.size() * sizeof(float), cudaMemcpyHostToDevice);
+  if (e != cudaSuccess) {
+    cudaFree(d);
+    return cuda_fail(e, "cudaMemcpy(rope table)");
+  }
+  r->device = dev;
+  r->d_table = d;
+  return OQ_OK;
+}
+
+}  // namespace qk
+}  // namespace oq
+
+using namespace oq;
+
+extern "C" {
+
+int oq_make_rope(int n_axes, const int* axis_dims, const int* max_pos, double theta, int layout, oq_rope** out) {
+  if (!out) return fail(OQ_ERR_INVALID_ARG, "oq_make_rope: out is NULL");
+  *out = nullptr;
+  if (!axis_dims || !max_pos) return fail(OQ_ERR_INVALID_ARG, "oq_make_rope: NULL axis_dims or max_pos");
+  if (n_axes < 1 || n_axes > qk::MAX_AXES) return fail(OQ_ERR_UNSUPPORTED, "oq_make_rope: 1 to 4 axes");
+  if (layout != OQ_ROPE_PAIRS && layout != OQ_ROPE_HALVES) return fail(OQ_ERR_INVALID_ARG, "oq_make_rope: unknown layout");
+  if (!(theta > 0.0) || !std::isfinite(theta)) return fail(OQ_ERR_INVALID_ARG, "oq_make_rope: theta must be positive and finite");
+  long long total = 0, dim = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    const int d = axis_dims[a];
+    if (d <= 0 || max_pos[a] <= 0) return fail(OQ_ERR_INVALID_ARG, "oq_make_rope: axis " + std::to_string(a) + ": dims and positions must be positive");
+    if (d % (layout == OQ_ROPE_HALVES ? 16 : 2))
+      return fail(OQ_ERR_UNSUPPORTED, "oq_make_rope: axis " + std::to_string(a) + ": dims must be even (halves layout: a multiple of 16)");
+    dim += d;
+    total += (long long)max_pos[a] * (d / 2);
+  }
+  if (dim > 256) return fail(OQ_ERR_UNSUPPORTED, "oq_make_rope: more than 256 coordinates");
+  if (total > (1ll << 27)) return fail(OQ_ERR_UNSUPPORTED, "oq_make_rope: table above 1 GB");
+  try {
+    oq_rope* r = new oq_rope;
+    try {
+      r->n_axes = n_axes;
+      r->dim = (int)dim;
+      r->layout = layout;
+      r->axis_dim.assign(axis_dims, axis_dims + n_axes);
+      r->max_pos.assign(max_pos, max_pos + n_axes);
+      r->table.resize((size_t)total * 2);
+      size_t at = 0;
+      for (int a = 0; a < n_axes; ++a) {
+        const int half = axis_dims[a] / 2;
+        r->base.push_back((long long)(at / 2));
+        std::vector<double> freq(half);
+        for (int i = 0; i < half; ++i) freq[i] = pow(theta, -2.0 * i / axis_dims[a]);
+        for (int q = 0; q < max_pos[a]; ++q)
+          for (int i = 0; i < half; ++i) {
+            const double angle = q * freq[i];
+            r->table[at++] = (float)cos(angle);
+            r->table[at++] = (float)sin(angle);
+          }
+      }
+    } catch (...) {
+      delete r;
+      throw;
+    }
+    *out = r;
+  } catch (const std::bad_alloc&) {
+    return fail(OQ_ERR_NOMEM, "oq_make_rope: out of host memory");
+  }
+  return OQ_OK;
+}
+
+int oq_rope_dim(const oq_rope* rope) { return rope ? rope->dim : 0; }
+
+void oq_rope_destroy(oq_rope* rope) {
+  if (!rope) return;
+  if (rope->d_table) cudaFree(rope->d_table);
+  delete rope;
+}
+
+int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int head_dim, const oq_rope* rope, const int* pos,
+                    int ldpos, int norm, float eps, int x_dtype, int y_dtype, void* stream) {
+  if (n_tokens < 0) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: n_tokens is negative");
+  if (!q && !k) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: neither queries nor keys");
+  if ((x_dtype != OQ_BF16 && x_dtype != OQ_F32) || (y_dtype != OQ_BF16 && y_dtype != OQ_F32))
+    return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: unknown element type");
+  if (norm != OQ_NORM_NONE && norm != OQ_NORM_HEAD && norm != OQ_NORM_ROW) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: unknown norm");
+  if (!(eps >= 0.f)) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: eps must not be negative");
+  if (head_dim != 32 && head_dim != 64 && head_dim != 128 && head_dim != 256)
+    return fail(OQ_ERR_UNSUPPORTED, "oq_qk_norm_rope: head_dim must be 32, 64, 128 or 256");
+  qk::Params p = {};
+  if (rope) {
+    if (rope->dim > head_dim) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: the rotation has more coordinates than a head");
+    if (n_tokens > 0 && !pos) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: a rotation without positions");
+    if (ldpos < rope->n_axes) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: ldpos is smaller than the number of axes");
+  }
+  const int per_chunk = qk::ITERS * 256 / head_dim;
+  const oq_qk_side* in[2] = {q, k};
+  const int xa = x_dtype == OQ_F32 ? 4 : 8, ya = y_dtype == OQ_F32 ? 4 : 8;       // elements of 16 bytes
+  for (int s = 0; s < 2; ++s) {
+    if (!in[s]) continue;
+    const std::string who = std::string("oq_qk_norm_rope: ") + (s ? "keys: " : "queries: ");
+    if (in[s]->n_heads <= 0) return fail(OQ_ERR_INVALID_ARG, who + "n_heads must be positive");
+    if (norm == OQ_NORM_ROW && in[s]->n_heads > per_chunk * qk::MAX_ROW_WARPS) return fail(OQ_ERR_UNSUPPORTED, who + "a row above 32768 values");
+    if (n_tokens == 0) continue;
+    if (!in[s]->X || !in[s]->Y) return fail(OQ_ERR_INVALID_ARG, who + "NULL buffer");
+    if (in[s]->w_bf16 && norm == OQ_NORM_NONE) return fail(OQ_ERR_INVALID_ARG, who + "weights without a norm");
+    if (!aligned16(in[s]->X) || !aligned16(in[s]->Y) || !aligned16(in[s]->w_bf16) || in[s]->ld_token % xa || in[s]->ld_head % xa ||
+        in[s]->ldy_token % ya || in[s]->ldy_head % ya)
+      return fail(OQ_ERR_ALIGNMENT, who + "pointers must be 16-byte aligned and strides multiples of 16 bytes");
+    qk::Side& d = p.side[s];
+    d.X = in[s]->X;
+    d.Y = in[s]->Y;
+    d.w = reinterpret_cast<const __nv_bfloat16*>(in[s]->w_bf16);
+    d.ld_token = in[s]->ld_token; d.ld_head = in[s]->ld_head;
+    d.ldy_token = in[s]->ldy_token; d.ldy_head = in[s]->ldy_head;
+    d.heads = in[s]->n_heads;
+    d.chunks = (d.heads + per_chunk - 1) / per_chunk;
+  }
+  if (n_tokens == 0) return OQ_OK;
+  p.tokens = n_tokens;
+  p.head_dim = head_dim;
+  p.lanes_per_head = head_dim / 8;
+  p.norm = norm;
+  p.eps = eps;
+  bool halves = false;
+  if (rope) {
+    const int rc = qk::ensure_table(rope);
+    if (rc != OQ_OK) return rc;
+    p.pos = pos;
+    p.ldpos = ldpos;
+    p.table = rope->d_table;
+    p.n_axes = rope->n_axes;
+    p.rot_dim = rope->dim;
+    halves = rope->layout == OQ_ROPE_HALVES;
+    int end = 0;
+    for (int a = 0; a < rope->n_axes; ++a) {
+      p.axis_end[a] = (end += rope->axis_dim[a]);
+      p.max_pos[a] = rope->max_pos[a];
+      p.base[a] = rope->base[a];
+    }
+  }
+  const bool row = norm == OQ_NORM_ROW;
+  long long ctas;
+  int threads;
+  if (row) {
+    const int chunks = p.side[0].chunks > p.side[1].chunks ? p.side[0].chunks : p.side[1].chunks;
+    ctas = (long long)n_tokens * ((p.side[0].heads > 0) + (p.side[1].heads > 0));
+    threads = 32 * chunks;
+  } else {
+    ctas = ((long long)n_tokens * (p.side[0].chunks + p.side[1].chunks) + qk::WARPS - 1) / qk::WARPS;
+    threads = 32 * qk::WARPS;
+  }
+  if (ctas > 0x7FFFFFFFll) return fail(OQ_ERR_UNSUPPORTED, "oq_qk_norm_rope: too many tokens for one launch");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e =
+      x_dtype == OQ_BF16 ? (y_dtype == OQ_BF16 ? qk::launch<__nv_bfloat16, __nv_bfloat16>(p, row, halves, ctas, threads, st)
+                                               : qk::launch<__nv_bfloat16, float>(p, row, halves, ctas, threads, st))
+                         : (y_dtype == OQ_BF16 ? qk::launch<float, __nv_bfloat16>(p, row, halves, ctas, threads, st)
+                                               : qk::launch<float, float>(p, row, halves, ctas, threads, st));
+  if (e != cudaSuccess) return cuda_fail(e, "oq_qk_norm_rope");
+  return OQ_OK;
+}
+
+}  // extern "C"
