@@ -320,6 +320,43 @@ typedef struct {
 int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int head_dim, const oq_rope* rope, const int* pos,
                     int ldpos, int norm, float eps, int x_dtype, int y_dtype, void* stream);
 
+/* ---- attention ---------------------------------------------------------------------------------------------- */
+
+/* Softmax attention over packed sequences, with a sliding window and first keys that stay visible.  Query i of a
+ * sequence of nq queries and nk keys stands at place p = i + nk - nq (the ends are aligned: new queries see the cached
+ * keys before them) and sees key j iff
+ *     j <= p + right   (right < 0: no limit)   and   (j >= p - left  (left < 0: no limit)  or  j < sinks)
+ * out = sum_j softmax_j(scale * q . k_j) v_j over the keys seen, lse = log sum_j exp(scale * q . k_j).  A query that
+ * sees no key gets out = 0 and lse = -inf.  Keys and values that a query does not see do not reach it, whatever they
+ * hold (NaN and infinities included).  causal: right = 0; joint attention: left = right = -1.
+ *   Q, K, V  dev bf16, element (token, head, c) at X[token * ld_token + head * ld_head + c]; strides in elements,
+ *            multiples of 8, at least head_dim where there is more than one token or head; 16-byte aligned
+ *   out      dev bf16, laid out by ldo_*; must not overlap the inputs.   lse  dev fp32 [n_heads][total_q], or NULL
+ *   q_start, k_start  dev int32 [n_seqs + 1]: sequence s owns the queries q_start[s] .. q_start[s + 1] - 1 and the keys
+ *            k_start[s] .. k_start[s + 1] - 1 (either may be empty).  NULL, both: one sequence.  Values are cut to
+ *            0 .. total_q / total_k; queries that no sequence owns are not written when the call does not split (see
+ *            below) and are undefined when it does.
+ *   n_heads  a multiple of n_kv_heads; query head h reads the key and value head h / (n_heads / n_kv_heads)
+ *   scale    0: 1 / sqrt(head_dim).   head_dim 64 or 128.  n_seqs <= 256.
+ * The products run on the tensor cores with fp32 accumulation; the softmax weights are rounded to bf16 for the product
+ * with V, everything else is fp32.  When there are too few queries to fill the GPU the keys are cut into parts whose
+ * results are joined in a second kernel: the workspace (dev, 16-byte aligned, oq_attention_workspace_bytes bytes, 0
+ * when nothing is cut) holds them.  Results are bit-reproducible.  Asynchronous on `stream`.  total_q == 0 launches
+ * nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */
+typedef struct {
+  const void *Q, *K, *V;
+  long long ldq_token, ldq_head, ldk_token, ldk_head, ldv_token, ldv_head;
+  void* out;
+  long long ldo_token, ldo_head;
+  float* lse;
+  const int *q_start, *k_start;
+  int n_seqs, total_q, total_k, n_heads, n_kv_heads, head_dim;
+  int left, right, sinks;
+  float scale;
+} oq_attention_args;
+int oq_attention_workspace_bytes(const oq_attention_args* args, size_t* bytes);
+int oq_attention(const oq_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Self-test of the bounded device-side waits the GEMM pipeline is built on: launches one thread that waits
  * about a millisecond on a barrier nobody arrives at.  The wait gives up by itself (the kernel ends
  * normally, nothing hangs or traps) and records code 9; the following oq_device_status() must return

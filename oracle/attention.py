@@ -35,3 +35,40 @@ def norm_rope(x, w, norm, eps, pos=None, axis_dims=(), theta=1.0, layout="pairs"
             y[:, :, hi] = x[:, :, lo] * s + x[:, :, hi] * c
         at += d
     return y
+
+
+def visible(nq, nk, left, right, sinks):
+    """bool [nq, nk]: which keys a query sees."""
+    p = np.arange(nq)[:, None] + (nk - nq)
+    j = np.arange(nk)[None, :]
+    ok = np.ones((nq, nk), bool)
+    if right >= 0:
+        ok &= j <= p + right
+    if left >= 0:
+        ok &= (j >= p - left) | (j < sinks)
+    return ok
+
+
+def attention(q, k, v, q_lens, k_lens, left=-1, right=-1, sinks=0, scale=None):
+    """q [Tq, H, D], k, v [Tk, Hk, D] float64 -> (out [Tq, H, D], lse [H, Tq]); what a query does not see is never read."""
+    Tq, H, D = q.shape
+    group = H // k.shape[1]
+    scale = scale or 1.0 / np.sqrt(D)
+    out, lse = np.zeros((Tq, H, D)), np.full((H, Tq), -np.inf)
+    q0 = k0 = 0
+    for nq, nk in zip(q_lens, k_lens):
+        ok = visible(nq, nk, left, right, sinks)
+        for h in range(H):
+            kk, vv = k[k0:k0 + nk, h // group], v[k0:k0 + nk, h // group]
+            for i in range(nq):
+                see = ok[i]
+                if not see.any():
+                    continue
+                with np.errstate(invalid="ignore", over="ignore"):
+                    z = (kk[see] @ q[q0 + i, h]) * scale
+                    m = z.max()
+                    e = np.exp(z - m)
+                    lse[h, q0 + i] = m + np.log(e.sum())
+                    out[q0 + i, h] = (e @ vv[see]) / e.sum()
+        q0, k0 = q0 + nq, k0 + nk
+    return out, lse

@@ -63,6 +63,8 @@ def lib():
             "oq_make_rope": (i, [i, vp, vp, C.c_double, i, pp]),
             "oq_rope_dim": (i, [vp]), "oq_rope_destroy": (None, [vp]),
             "oq_qk_norm_rope": (i, [vp, vp, i, i, vp, vp, i, i, C.c_float, i, i, vp]),
+            "oq_attention_workspace_bytes": (i, [vp, C.POINTER(sz)]),
+            "oq_attention": (i, [vp, vp, sz, vp]),
             "oq_last_error": (C.c_char_p, []), "oq_version": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -438,6 +440,56 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
                                  NORMS[norm], eps, _dtype_code(Q, "oq_qk_norm_rope"), _dtype_code(outs[0], "oq_qk_norm_rope"),
                                  _stream()))
     return outs[0], outs[1]
+
+
+class _AttentionArgs(C.Structure):       # oq_attention_args
+    _fields_ = [(n, C.c_void_p) for n in ("Q", "K", "V")] + \
+               [(n, C.c_longlong) for n in ("ldq_token", "ldq_head", "ldk_token", "ldk_head", "ldv_token", "ldv_head")] + \
+               [("out", C.c_void_p), ("ldo_token", C.c_longlong), ("ldo_head", C.c_longlong), ("lse", C.c_void_p),
+                ("q_start", C.c_void_p), ("k_start", C.c_void_p)] + \
+               [(n, C.c_int) for n in ("n_seqs", "total_q", "total_k", "n_heads", "n_kv_heads", "head_dim", "left", "right", "sinks")] + \
+               [("scale", C.c_float)]
+
+
+def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0, scale=0.0, out=None, want_lse=False,
+                 workspace=None):
+    """Q: CUDA bf16 [Tq, heads, head_dim], K, V: [Tk, kv_heads, head_dim] (any token and head strides, unit stride inside
+    a head); q_start, k_start: CUDA int32 [sequences + 1], or None for one sequence.  left, right, sinks: see oq.h.
+    Returns out [Tq, heads, head_dim], or (out, lse fp32 [heads, Tq]) with want_lse.  workspace: CUDA uint8 tensor, by
+    default one is taken from torch's allocator when the call needs it."""
+    import torch
+    if Q.dim() != 3 or K.dim() != 3 or K.shape != V.shape or Q.shape[2] != K.shape[2]:
+        raise OqError(1, "oq_attention: Q must be [Tq, heads, head_dim], K and V [Tk, kv_heads, head_dim]")
+    if not (Q.dtype == K.dtype == V.dtype == torch.bfloat16):
+        raise OqError(1, "oq_attention: bf16 expected")
+    if Q.numel() and Q.stride(2) != 1 or K.numel() and (K.stride(2) != 1 or V.stride(2) != 1):
+        raise OqError(3, "oq_attention: the coordinates of a head must be adjacent")
+    tq, heads, head_dim = Q.shape
+    n_seqs = 1
+    for t in (q_start, k_start):
+        if t is not None:
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() < 2 or not t.is_cuda:
+                raise OqError(1, "oq_attention: q_start and k_start must be contiguous CUDA int32 [sequences + 1]")
+            n_seqs = t.numel() - 1
+    if q_start is not None and k_start is not None and q_start.numel() != k_start.numel():
+        raise OqError(1, "oq_attention: q_start and k_start must have one length")
+    if out is None:
+        out = torch.empty((tq, heads, head_dim), dtype=torch.bfloat16, device=Q.device)
+    elif out.shape != Q.shape or out.dtype != torch.bfloat16 or out.numel() and out.stride(2) != 1:
+        raise OqError(1, "oq_attention: out must be bf16, shaped like Q, with adjacent coordinates")
+    lse = torch.empty((heads, tq), dtype=torch.float32, device=Q.device) if want_lse else None
+    a = _AttentionArgs(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _stride(Q, 0), _stride(Q, 1), _stride(K, 0), _stride(K, 1),
+                       _stride(V, 0), _stride(V, 1), out.data_ptr(), _stride(out, 0), _stride(out, 1),
+                       lse.data_ptr() if want_lse else None, q_start.data_ptr() if q_start is not None else None,
+                       k_start.data_ptr() if k_start is not None else None, n_seqs, tq, K.shape[0], heads, K.shape[1], head_dim,
+                       left, right, sinks, scale)
+    need = C.c_size_t()
+    _check(lib().oq_attention_workspace_bytes(C.byref(a), C.byref(need)))
+    if workspace is None and need.value:
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=Q.device)
+    _check(lib().oq_attention(C.byref(a), workspace.data_ptr() if workspace is not None else None,
+                              workspace.numel() if workspace is not None else 0, _stream()))
+    return (out, lse) if want_lse else out
 
 
 def oq_version():

@@ -1,0 +1,732 @@
+// Softmax attention with a sliding window and first keys that stay visible, over packed sequences.
+//
+//   query i of a sequence (nq queries, nk keys) stands at place p = i + nk - nq among the keys;
+//   it sees key j iff  j <= p + right (right < 0: no limit)  and  (j >= p - left (left < 0: no limit) or j < sinks)
+//   z_j = scale * q . k_j,   lse = log sum_j exp(z_j),   out = sum_j exp(z_j - lse) v_j     (sees nothing: 0, -inf)
+//
+// One pass over the keys with a running reference m and a running sum: with c = scale * log2(e) the kernel holds
+//   l = sum_j 2^(c (s_j - m)),   O = sum_j 2^(c (s_j - m)) v_j
+// for ANY m that keeps the powers in range, so m follows the running maximum only when that has moved by more than
+// 2^SLACK; then O and l are multiplied by 2^(c (m - m')).  The sums are fp32; the powers are rounded once, to bf16, as
+// the tensor cores' operand for the product with V (l sums the unrounded ones), which costs about as much as the one rounding of the
+// output.
+//
+// Bound: the tensor cores and the exponentials alike.  A tile of 128 queries x 128 keys takes 2 * 128^3 multiply-adds
+// for each of the two products at head_dim 128 and 16384 exponentials: both about 1000 cycles of an SM.  So a CTA
+// carries two query tiles in turn: while the tensor cores multiply for one, the other's threads exponentiate.
+//
+//   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of 128 keys through one ring of shared-memory slots
+//   mma warp    (1 thread)   S_t = Q_t K^T into tensor memory; O_t += P_t V with P_t from tensor memory
+//   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16) over S
+//
+// In the order in which one thread issues them, P_t V of a tile comes before the next S_t, so "S_t of tile j is there"
+// also says that O_t holds the tiles before j: O can be rescaled without another wait, and P can lie over S.
+// Tensor memory: S_0 | S_1 | O_0 | O_1, 128 columns each.
+//
+// NaN and infinities in keys and values that a row does not see must not reach it, but 0 * NaN is NaN: a row whose
+// result is not finite (checked once, at the end) is computed again key by key over what it sees.
+#include <cuda_bf16.h>
+
+#include <string>
+
+#include "oq_internal.h"
+#include "oq_sm100.cuh"
+
+namespace oq {
+namespace attn {
+
+constexpr int THREADS = 384;              // 8 softmax warps; the load warp, the mma warp and two that only fill their group
+// Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S (128 values) and grow to
+// 208; the last group shrinks to 80: 256 * 208 + 128 * 80 = 63488.
+constexpr int LOAD_WARP = 8, MMA_WARP = 9;
+constexpr int BM = 128, BN = 128;         // query rows of a tile, keys of a tile
+constexpr int MAX_SEQS = 256;
+constexpr int MAX_SPLITS = 32;
+constexpr float SLACK = 8.f;              // powers stay below 2^8
+constexpr uint32_t ATOM = 128 * 128;      // 64 coordinates of 128 rows
+constexpr uint32_t COL_S = 0, COL_O = 256;
+enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46, W_OFREE = 47, W_DRAIN = 48 };
+
+template <int D>
+struct Shape {
+  static constexpr uint32_t ATOMS = D / 64;
+  static constexpr uint32_t TILE = ATOMS * ATOM;
+  static constexpr int SLOTS = D == 128 ? 5 : 8;
+  static constexpr uint32_t SMEM = 1024 + 2 * TILE + SLOTS * TILE;
+};
+
+struct Params {
+  const __nv_bfloat16 *Q, *K, *V;         // (the tensor maps read them; these serve the rows that are computed again)
+  long long ldq, hdq, ldk, hdk, ldv, hdv;
+  __nv_bfloat16* out;
+  long long ldo, hdo;
+  float* lse;                             // [heads][total_q] or NULL
+  float* part_o;                          // [splits][heads][total_q][D]: unnormalised sums, scaled to a sum of one
+  float* part_lse;                        // [splits][heads][total_q], base 2
+  const int *q_start, *k_start;           // n_seqs + 1, or NULL: one sequence
+  int total_q, total_k, n_seqs, heads, group, splits;
+  int left, right, sinks;
+  float scale, scale_log2;
+  int* status;
+};
+
+// What one CTA works on at a time: up to 256 queries of one head, and a run of their key tiles.
+struct Item {
+  int q_base, k_base;      // first query and key of the sequence
+  int nq, nk;
+  int q0;                  // first query of the item inside the sequence
+  int rows0, rows1;        // queries of the two tiles
+  int head, split;
+  int tiles, n_sink, win0; // key tiles: j < n_sink -> j, else win0 + j - n_sink
+  int first;               // first tile of this split
+  __device__ __forceinline__ int key0(int j) const {
+    j += first;
+    return BN * (j < n_sink ? j : win0 + (j - n_sink));
+  }
+};
+
+__device__ __forceinline__ int row_hi(const Params& p, const Item& it, int qi) {       // last visible key
+  return p.right < 0 ? it.nk - 1 : min(it.nk - 1, qi + it.nk - it.nq + p.right);
+}
+__device__ __forceinline__ int row_lo(const Params& p, const Item& it, int qi) {       // first key of the window
+  return p.left < 0 ? 0 : max(0, qi + it.nk - it.nq - p.left);
+}
+
+// prefix[s]: blocks of 256 queries before sequence s
+__device__ __forceinline__ Item make_item(const Params& p, const int* prefix, int index) {
+  Item it;
+  it.split = index % p.splits;
+  index /= p.splits;
+  const int blocks = prefix[p.n_seqs];
+  it.head = index / blocks;
+  int b = blocks - 1 - index % blocks;         // the last queries see the most keys under a causal mask: first
+  int s = 0, e = p.n_seqs;
+  while (e - s > 1) {
+    const int m = (s + e) >> 1;
+    if (prefix[m] <= b) s = m; else e = m;
+  }
+  b -= prefix[s];
+  if (p.q_start) {
+    it.q_base = min(max(__ldg(p.q_start + s), 0), p.total_q);
+    it.nq = min(max(__ldg(p.q_start + s + 1), it.q_base), p.total_q) - it.q_base;
+    it.k_base = min(max(__ldg(p.k_start + s), 0), p.total_k);
+    it.nk = min(max(__ldg(p.k_start + s + 1), it.k_base), p.total_k) - it.k_base;
+  } else {
+    it.q_base = it.k_base = 0;
+    it.nq = p.total_q;
+    it.nk = p.total_k;
+  }
+  it.q0 = 2 * BM * b;
+  const int rows = min(2 * BM, it.nq - it.q0);
+  it.rows0 = min(rows, BM);
+  it.rows1 = rows - it.rows0;
+  const int hi = row_hi(p, it, it.q0 + rows - 1), lo = row_lo(p, it, it.q0);
+  it.tiles = it.n_sink = it.win0 = 0;
+  if (hi >= 0) {
+    it.win0 = lo / BN;
+    it.n_sink = min((min(p.sinks, hi + 1) + BN - 1) / BN, it.win0);
+    it.tiles = it.n_sink + hi / BN - it.win0 + 1;
+  }
+  it.first = (int)((long long)it.tiles * it.split / p.splits);
+  it.tiles = (int)((long long)it.tiles * (it.split + 1) / p.splits) - it.first;
+  return it;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// bits 0 .. n-1 of a word, n clamped to 0 .. 32
+__device__ __forceinline__ uint32_t ones_below(int n) {
+  return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u);
+}
+
+// One row again, key by key over the keys it sees, by a whole warp (each lane holds D / 32 coordinates).
+template <int D>
+__device__ __noinline__ void exact_row(const Params& p, const Item& it, int qi) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31, hk = it.head / p.group;
+  const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
+  float q[N], o[N], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    q[i] = __bfloat162float(p.Q[(long long)(it.q_base + qi) * p.ldq + it.head * p.hdq + lane * N + i]);
+    o[i] = 0.f;
+  }
+  for (int j = 0; j < it.tiles; ++j) {
+    const int k0 = it.key0(j);
+    for (int key = k0; key < k0 + BN && key <= hi; ++key) {
+      if (key < lo && key >= p.sinks) continue;
+      const long long at = it.k_base + key;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s = fmaf(q[i], __bfloat162float(p.K[at * p.ldk + hk * p.hdk + lane * N + i]), s);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+      s *= p.scale_log2;
+      const float mn = fmaxf(m, s), a = m == mn ? 1.f : exp2f(m - mn), w = s == -INFINITY ? 0.f : exp2f(s - mn);
+      m = mn;
+      l = l * a + w;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float v = __bfloat162float(p.V[at * p.ldv + hk * p.hdv + lane * N + i]);
+        o[i] = o[i] * a + w * v;
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+  const long long row = (long long)it.head * p.total_q + it.q_base + qi;
+  if (p.splits > 1) {
+    const long long at = (long long)it.split * p.heads * p.total_q + row;
+#pragma unroll
+    for (int i = 0; i < N; ++i) p.part_o[at * D + lane * N + i] = o[i] * inv;
+    if (lane == 0) p.part_lse[at] = lse2;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      p.out[(long long)(it.q_base + qi) * p.ldo + it.head * p.hdo + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
+    if (lane == 0 && p.lse) p.lse[row] = lse2 * 0.69314718055994531f;
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ Params p) {
+  using S = Shape<D>;
+  constexpr int SLOTS = S::SLOTS;
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) unsigned long long bars[2 + 2 + 2 * SLOTS + 8];
+  __shared__ int prefix[MAX_SEQS + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  const uint32_t smem_q = smem, smem_kv = smem + 2 * S::TILE;
+  const uint32_t b0 = smem_u32(bars);
+  auto q_full = [&](int t) { return b0 + 8u * (uint32_t)t; };
+  auto q_free = [&](int t) { return b0 + 8u * (uint32_t)(2 + t); };
+  auto s_full = [&](int t) { return b0 + 8u * (uint32_t)(4 + t); };
+  auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };
+  auto o_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };
+  auto o_free = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };
+  auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(12 + s); };
+  auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(12 + SLOTS + s); };
+
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full(t), 1);
+      mbar_init(q_free(t), 1);
+      mbar_init(s_full(t), 1);
+      mbar_init(p_full(t), 4);
+      mbar_init(o_full(t), 1);
+      mbar_init(o_free(t), 4);
+    }
+    for (int s = 0; s < SLOTS; ++s) {
+      mbar_init(kv_full(s), 1);
+      mbar_init(kv_free(s), 1);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (warp == 0) {
+    // blocks of 256 queries before each sequence
+    int before = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+      const int s = s0 + lane;
+      int n = 0;
+      if (s < p.n_seqs) {
+        n = p.total_q;
+        if (p.q_start) {
+          const int b = min(max(__ldg(p.q_start + s), 0), p.total_q);
+          n = min(max(__ldg(p.q_start + s + 1), b), p.total_q) - b;
+        }
+        n = (n + 2 * BM - 1) / (2 * BM);
+      }
+      int sum = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, sum, d);
+        if (lane >= d) sum += o;
+      }
+      if (s < p.n_seqs) prefix[s] = before + sum - n;
+      before += __shfl_sync(~0u, sum, 31);
+    }
+    if (lane == 0) prefix[p.n_seqs] = before;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const int n_items = prefix[p.n_seqs] * p.heads * p.splits;
+
+  if (warp >= LOAD_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  if (warp == LOAD_WARP) {
+    if (lane == 0) {
+      uint32_t slot = 0, round = 0, q_use[2] = {0, 0};
+      auto load_q = [&](const Item& it, int t) {
+        if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
+        ++q_use[t];
+        mbar_expect_tx(q_full(t), S::TILE);
+        for (uint32_t a = 0; a < S::ATOMS; ++a)
+          tma_load_3d(smem_q + (uint32_t)t * S::TILE + a * ATOM, &map_q, 64 * (int)a, it.head, it.q_base + it.q0 + t * BM, q_full(t));
+      };
+      auto load_kv = [&](const Item& it, const CUtensorMap* map, int key0) {
+        if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
+        mbar_expect_tx(kv_full(slot), S::TILE);
+        for (uint32_t a = 0; a < S::ATOMS; ++a)
+          tma_load_3d(smem_kv + slot * S::TILE + a * ATOM, map, 64 * (int)a, it.head / p.group, it.k_base + key0, kv_full(slot));
+        if (++slot == SLOTS) {
+          slot = 0;
+          ++round;
+        }
+      };
+      for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
+        const Item it = make_item(p, prefix, i);
+        if (it.tiles == 0) continue;
+        load_q(it, 0);
+        load_kv(it, &map_k, it.key0(0));
+        if (it.rows1 > 0) load_q(it, 1);
+        for (int j = 0; j < it.tiles && !abort_flag; ++j) {
+          load_kv(it, &map_v, it.key0(j));
+          if (j + 1 < it.tiles) load_kv(it, &map_k, it.key0(j + 1));
+        }
+      }
+      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
+      for (uint32_t s = 0; s < SLOTS; ++s) {
+        const uint32_t fills = round + (s < slot ? 1u : 0u);
+        for (int n = 0; fills > 0 && n < (1 << 20) && !mbar_try(kv_full((int)s), (fills - 1) & 1); ++n) {}
+      }
+      for (int t = 0; t < 2; ++t)
+        for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
+    }
+  } else if (warp == MMA_WARP) {
+    if (lane == 0) {
+      constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
+      constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
+      constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
+      uint32_t slot = 0, round = 0, q_use[2] = {0, 0}, p_use[2] = {0, 0}, o_use[2] = {0, 0};
+      auto next_kv = [&]() {
+        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
+        const uint32_t s = slot;
+        if (++slot == SLOTS) {
+          slot = 0;
+          ++round;
+        }
+        return s;
+      };
+      auto issue_s = [&](int t, uint32_t k_slot) {
+        const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::TILE), b = smem_desc(smem_kv + k_slot * S::TILE);
+#pragma unroll
+        for (uint32_t k = 0; k < D / 16; ++k) {
+          const uint64_t step = (uint64_t)((k >> 2) * (ATOM >> 4) + 2 * (k & 3));
+          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0);
+        }
+        mma_commit(s_full(t));
+      };
+      auto issue_o = [&](int t, uint32_t v_slot, bool first) {
+        const uint64_t b = smem_desc_mn(smem_kv + v_slot * S::TILE, ATOM, 1024);
+#pragma unroll
+        for (uint32_t k = 0; k < BN / 16; ++k)
+          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0));
+      };
+      // the item whose S comes next runs one key tile ahead of the one whose O is accumulated
+      int i = blockIdx.x;
+      Item cur;
+      cur.tiles = 0;
+      auto next_item = [&](Item& it) {
+        for (; i < n_items; i += gridDim.x) {
+          it = make_item(p, prefix, i);
+          if (it.tiles > 0) {
+            i += gridDim.x;
+            return true;
+          }
+        }
+        return false;
+      };
+      bool have = next_item(cur);
+      if (have) {
+        const uint32_t k_slot = next_kv();
+        for (int t = 0; t < (cur.rows1 > 0 ? 2 : 1); ++t) {
+          mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
+          tc_fence_after();
+          issue_s(t, k_slot);
+          if (cur.tiles == 1) mma_commit(q_free(t));
+        }
+        mma_commit(kv_free(k_slot));
+      }
+      while (have && !abort_flag) {
+        Item nxt;
+        const bool more = next_item(nxt);
+        for (int j = 0; j < cur.tiles && !abort_flag; ++j) {
+          const bool last = j + 1 == cur.tiles;
+          const bool ahead = !last || more;            // a tile whose S is to be issued
+          const uint32_t v_slot = next_kv();
+          uint32_t k_slot = 0;
+          bool k_there = false;
+          const bool two_now = cur.rows1 > 0, two_next = last ? (more && nxt.rows1 > 0) : two_now;
+          for (int t = 0; t < 2; ++t) {
+            if (t == 0 || two_now) {
+              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
+              if (j == 0 && o_use[t] > 0) mbar_spin(o_free(t), (o_use[t] - 1) & 1, &abort_flag, p.status, W_OFREE);
+              tc_fence_after();
+              issue_o(t, v_slot, j == 0);
+              if (last) {
+                mma_commit(o_full(t));
+                ++o_use[t];
+              }
+            }
+            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot));
+            if (ahead && (t == 0 || two_next)) {
+              if (!k_there) {
+                k_slot = next_kv();
+                k_there = true;
+              }
+              if (last) mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
+              tc_fence_after();
+              issue_s(t, k_slot);
+              // the query tile is free once its last S is there
+              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t));
+            }
+          }
+          if (k_there) mma_commit(kv_free(k_slot));
+        }
+        cur = nxt;
+        have = more;
+      }
+    }
+  } else if (warp < LOAD_WARP) {
+    // ------------------------------------------------ softmax ------------------------------------------------
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t col_s = tmem + lane_base + COL_S + 128u * (uint32_t)t, col_o = tmem + lane_base + COL_O + 128u * (uint32_t)t;
+    const float c = p.scale_log2;
+    uint32_t s_use = 0, o_use = 0;
+    auto warp_wait = [&](uint32_t bar, uint32_t parity, int code) {
+      mbar_spin(bar, parity, &abort_flag, p.status, code);
+      __syncwarp();
+    };
+    for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
+      const Item it = make_item(p, prefix, i);
+      const int rows = t ? it.rows1 : it.rows0;
+      if (rows == 0) continue;
+      const int r0 = it.q0 + t * BM, qi = r0 + row;
+      const bool mine = row < rows;
+      const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
+      const int full_hi = row_hi(p, it, r0), full_lo = row_lo(p, it, r0 + rows - 1);     // what every row of the tile sees
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < it.tiles && !abort_flag; ++j) {
+        const int k0 = it.key0(j);
+        warp_wait(s_full(t), s_use++ & 1, W_S);
+        tc_fence_after();
+        uint32_t sr[128];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_load32_nowait(col_s + 32u * q, sr + 32 * q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_use32(sr + 32 * q);
+        if (!(k0 + BN - 1 <= full_hi && (k0 >= full_lo || k0 + BN <= p.sinks))) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int b = k0 + 32 * q;
+            const uint32_t keep = ones_below(hi + 1 - b) & (~ones_below(lo - b) | ones_below(p.sinks - b));
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!((keep >> e) & 1u)) sr[32 * q + e] = 0xFF800000u;
+          }
+        }
+        float mx4[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          mx4[q] = __uint_as_float(sr[q]);
+#pragma unroll
+          for (int e = 1; e < 32; ++e) mx4[q] = fmaxf(mx4[q], __uint_as_float(sr[4 * e + q]));
+        }
+        const float mn = fmaxf(m, fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])));
+        if (j == 0) {
+          m = mn;
+        } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
+          // (S_t of tile j is there, so O_t holds the tiles before j and nothing is writing it)
+          const float a = m == mn ? 1.f : exp2_fast((m - mn) * c);
+          m = mn;
+          l *= a;
+#pragma unroll
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t o[32];
+            tmem_load32(col_o + 32u * q, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+            tmem_store32(col_o + 32u * q, o);
+          }
+        }
+        const float shift = m == -INFINITY ? 0.f : -m * c;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float a = exp2_fast(fmaf(__uint_as_float(sr[32 * q + 2 * e]), c, shift));
+            const float b = exp2_fast(fmaf(__uint_as_float(sr[32 * q + 2 * e + 1]), c, shift));
+            sum[e & 1] += a;
+            sum[2 + (e & 1)] += b;
+            pk[e] = pack_bf16(a, b);
+          }
+          tmem_store16(col_s + 16u * q, pk);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(t));
+      }
+      // ------------------------------------------- the item's result -------------------------------------------
+      uint32_t o[D];
+      const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
+      float nan_probe = 0.f;
+      if (it.tiles > 0) {
+        warp_wait(o_full(t), o_use++ & 1, W_O);
+        tc_fence_after();
+#pragma unroll
+        for (int q = 0; q < D / 32; ++q) tmem_load32_nowait(col_o + 32u * q, o + 32 * q);
+#pragma unroll
+        for (int q = 0; q < D / 32; ++q) tmem_use32(o + 32 * q);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_free(t));
+      } else {
+#pragma unroll
+        for (int e = 0; e < D; ++e) o[e] = 0u;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int e = 0; e < D; ++e) {
+        const float v = __uint_as_float(o[e]) * inv;
+        nan_probe = fmaf(v, 0.f, nan_probe);
+        o[e] = __float_as_uint(v);
+      }
+      const bool bad = mine && !(nan_probe == 0.f);
+      const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c, log2f(l));
+      if (mine && !bad) {
+        if (p.splits > 1) {
+          const long long at = (long long)it.split * p.heads * p.total_q + out_row;
+          float4* dst = reinterpret_cast<float4*>(p.part_o + at * D);
+#pragma unroll
+          for (int e = 0; e < D / 4; ++e)
+            dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+          p.part_lse[at] = lse2;
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + (long long)(it.q_base + qi) * p.ldo + it.head * p.hdo);
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            uint4 v;
+            v.x = pack_bf16(__uint_as_float(o[8 * e]), __uint_as_float(o[8 * e + 1]));
+            v.y = pack_bf16(__uint_as_float(o[8 * e + 2]), __uint_as_float(o[8 * e + 3]));
+            v.z = pack_bf16(__uint_as_float(o[8 * e + 4]), __uint_as_float(o[8 * e + 5]));
+            v.w = pack_bf16(__uint_as_float(o[8 * e + 6]), __uint_as_float(o[8 * e + 7]));
+            dst[e] = v;
+          }
+          if (p.lse) p.lse[out_row] = lse2 * 0.69314718055994531f;
+        }
+      }
+      uint32_t again = __ballot_sync(~0u, bad);
+      while (again) {
+        const int r = __ffs(again) - 1;
+        again &= again - 1;
+        exact_row<D>(p, it, r0 + (warp & 3) * 32 + r);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// Joins the splits of a row: weights 2^(lse_i - max) over their sum.  One warp per (token, head).
+template <int D>
+__global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ Params p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31;
+  const long long rows = (long long)p.heads * p.total_q;
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const float mine = lane < p.splits ? p.part_lse[lane * rows + row] : -INFINITY;
+  float top = mine;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  const float w = mine == -INFINITY ? 0.f : exp2f(mine - top);
+  float total = w;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
+  float o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = 0.f;
+  for (int s = 0; s < p.splits; ++s) {
+    const float ws = __shfl_sync(~0u, w, s);
+    if (ws == 0.f) continue;                       // an empty split, or one whose share is below 2^-126
+    const float* src = p.part_o + (s * rows + row) * D + lane * N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = fmaf(ws, src[i], o[i]);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const int head = (int)(row / p.total_q), tok = (int)(row % p.total_q);
+  __nv_bfloat16* dst = p.out + (long long)tok * p.ldo + head * p.hdo + lane * N;
+#pragma unroll
+  for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16(o[i] * inv, o[i + 1] * inv);
+  if (lane == 0 && p.lse) p.lse[row] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+}
+
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  return sms;
+}
+
+// How many parts the keys of a block of queries are cut into.  Blocks of 256 queries times heads are the items; when
+// they do not fill the SMs, or fill them unevenly, each is cut along its keys.  The time of a cut is estimated as
+// (rounds of items over the SMs) x (key tiles of an item + 3, what an item costs besides its tiles).
+int choose_splits(long long total_q, long long total_k, int n_seqs, int heads, int left, int right, int sinks, int sms) {
+  const long long blocks = (total_q + 2LL * BM * n_seqs - 1) / (2 * BM) ;      // between all full and one more per sequence
+  const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
+  long long keys = total_k / n_seqs;
+  if (left >= 0 && right >= 0) {
+    const long long window = (long long)left + right + 2 * BM + sinks;
+    if (window < keys) keys = window;
+  }
+  const long long tiles = (keys + BN - 1) / BN;
+  if (items >= 2LL * sms) return 1;
+  int best = 1;
+  double best_cost = 1e30;
+  for (int n = 1; n <= MAX_SPLITS && (n == 1 || n * 2 <= tiles); ++n) {
+    const double cost = (double)((items * n + sms - 1) / sms) * (double)((tiles + n - 1) / n + 3) + (n > 1 ? 4.0 : 0.0);
+    if (cost < best_cost * 0.97) {
+      best_cost = cost;
+      best = n;
+    }
+  }
+  return best;
+}
+
+template <int D>
+cudaError_t launch(const Params& p, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, int sms, cudaStream_t st) {
+  // (the attribute belongs to the device that is current, so it is set every time)
+  cudaError_t e = cudaFuncSetAttribute(attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D>::SMEM);
+  if (e != cudaSuccess) return e;
+  const long long most = ((long long)(p.total_q + 2 * BM - 1) / (2 * BM) + p.n_seqs) * p.heads * p.splits;
+  e = launch_dependent(attention_kernel<D>, (int)(most < sms ? most : sms), THREADS, Shape<D>::SMEM, st, mq, mk, mv, p);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  return launch_dependent(attention_join_kernel<D>, (int)(((long long)p.heads * p.total_q + 7) / 8), 256, 0, st, p);
+}
+
+}  // namespace attn
+}  // namespace oq
+
+using namespace oq;
+
+static int attention_check(const oq_attention_args* a) {
+  if (!a) return fail(OQ_ERR_INVALID_ARG, "oq_attention: NULL arguments");
+  if (a->total_q < 0 || a->total_k < 0 || a->n_seqs < 1) return fail(OQ_ERR_INVALID_ARG, "oq_attention: bad sizes");
+  if (a->total_q > (1 << 30) || a->total_k > (1 << 30)) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: more than 2^30 tokens");
+  if (a->n_seqs > attn::MAX_SEQS) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: more than 256 sequences");
+  if (a->n_heads <= 0 || a->n_kv_heads <= 0 || a->n_heads % a->n_kv_heads)
+    return fail(OQ_ERR_INVALID_ARG, "oq_attention: n_heads must be a positive multiple of n_kv_heads");
+  if (a->head_dim != 64 && a->head_dim != 128) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: head_dim must be 64 or 128");
+  if ((!a->q_start) != (!a->k_start)) return fail(OQ_ERR_INVALID_ARG, "oq_attention: q_start and k_start go together");
+  if (a->n_seqs > 1 && !a->q_start) return fail(OQ_ERR_INVALID_ARG, "oq_attention: several sequences need q_start and k_start");
+  if (a->sinks < 0) return fail(OQ_ERR_INVALID_ARG, "oq_attention: sinks must not be negative");
+  if (!(a->scale >= 0.f) || !(a->scale < 1e30f)) return fail(OQ_ERR_INVALID_ARG, "oq_attention: scale must be positive, or 0 for 1 / sqrt(head_dim)");
+  if ((long long)a->total_q * a->n_heads > (1ll << 31) * 8) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: too many rows for one launch");
+  return OQ_OK;
+}
+
+static int attention_splits(const oq_attention_args* a) {
+  if (a->total_q == 0 || a->total_k == 0) return 1;
+  return attn::choose_splits(a->total_q, a->total_k, a->n_seqs, a->n_heads, a->left, a->right, a->sinks, attn::sm_count());
+}
+
+extern "C" {
+
+int oq_attention_workspace_bytes(const oq_attention_args* a, size_t* bytes) {
+  if (!bytes) return fail(OQ_ERR_INVALID_ARG, "oq_attention_workspace_bytes: bytes is NULL");
+  *bytes = 0;
+  const int rc = attention_check(a);
+  if (rc != OQ_OK) return rc;
+  const int n = attention_splits(a);
+  if (n > 1) *bytes = (size_t)n * a->n_heads * (size_t)a->total_q * (size_t)(a->head_dim + 4) * sizeof(float);
+  return OQ_OK;
+}
+
+int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = attention_check(a);
+  if (rc != OQ_OK) return rc;
+  if (a->total_q == 0) return OQ_OK;
+  if (!a->Q || !a->out || (a->total_k > 0 && (!a->K || !a->V))) return fail(OQ_ERR_INVALID_ARG, "oq_attention: NULL buffer");
+  if (!aligned16(a->Q) || !aligned16(a->K) || !aligned16(a->V) || !aligned16(a->out) || a->ldq_token % 8 || a->ldq_head % 8 ||
+      a->ldk_token % 8 || a->ldk_head % 8 || a->ldv_token % 8 || a->ldv_head % 8 || a->ldo_token % 8 || a->ldo_head % 8)
+    return fail(OQ_ERR_ALIGNMENT, "oq_attention: pointers must be 16-byte aligned and strides multiples of 8");
+  if (a->ldq_token < 0 || a->ldq_head < 0 || a->ldk_token < 0 || a->ldk_head < 0 || a->ldv_token < 0 || a->ldv_head < 0)
+    return fail(OQ_ERR_INVALID_ARG, "oq_attention: strides must not be negative");
+  attn::Params p = {};
+  p.splits = attention_splits(a);
+  size_t need = 0;
+  rc = oq_attention_workspace_bytes(a, &need);
+  if (rc != OQ_OK) return rc;
+  if (need > workspace_bytes || (need && (!workspace || !aligned16(workspace))))
+    return fail(OQ_ERR_NOMEM, "oq_attention: workspace of " + std::to_string(need) + " bytes (16-byte aligned) needed");
+  p.Q = reinterpret_cast<const __nv_bfloat16*>(a->Q);
+  p.K = reinterpret_cast<const __nv_bfloat16*>(a->K);
+  p.V = reinterpret_cast<const __nv_bfloat16*>(a->V);
+  p.ldq = a->ldq_token; p.hdq = a->ldq_head;
+  p.ldk = a->ldk_token; p.hdk = a->ldk_head;
+  p.ldv = a->ldv_token; p.hdv = a->ldv_head;
+  p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
+  p.ldo = a->ldo_token; p.hdo = a->ldo_head;
+  p.lse = a->lse;
+  p.part_o = reinterpret_cast<float*>(workspace);
+  p.part_lse = p.part_o + (size_t)p.splits * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim;
+  p.q_start = a->q_start; p.k_start = a->k_start;
+  p.total_q = a->total_q; p.total_k = a->total_k;
+  p.n_seqs = a->n_seqs; p.heads = a->n_heads; p.group = a->n_heads / a->n_kv_heads;
+  const int far = 1 << 30;                         // no sequence is longer
+  p.left = a->left < 0 ? -1 : (a->left > far ? far : a->left);
+  p.right = a->right < 0 ? -1 : (a->right > far ? far : a->right);
+  p.sinks = a->sinks > far ? far : a->sinks;
+  p.scale = a->scale > 0.f ? a->scale : (a->head_dim == 128 ? 0.08838834764831845f : 0.125f);
+  p.scale_log2 = p.scale * 1.4426950408889634f;
+  p.status = device_status_word();
+  if (!p.status) return fail(OQ_ERR_CUDA, "oq_attention: cannot allocate the device status word");
+  CUtensorMap mq, mk, mv;
+  auto make_map = [&](CUtensorMap* map, const void* base, int heads, long long tokens, long long ld, long long hd) {
+    const uint64_t dims[3] = {(uint64_t)a->head_dim, (uint64_t)heads, (uint64_t)tokens};
+    // a stride that is never used (one head, one token) still has to be one that the encoder takes
+    const uint64_t strides[2] = {(uint64_t)(heads > 1 && hd > 0 ? hd : a->head_dim) * 2, (uint64_t)(tokens > 1 && ld > 0 ? ld : (long long)a->head_dim * heads) * 2};
+    const uint32_t box[3] = {64, 1, 128};
+    return encode_tensor_map_bf16(map, base, 3, dims, strides, box, true);
+  };
+  cudaError_t e = make_map(&mq, a->Q, a->n_heads, a->total_q, a->ldq_token, a->ldq_head);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mv, a->V, a->n_kv_heads, a->total_k, a->ldv_token, a->ldv_head);
+  if (e != cudaSuccess) return cuda_fail(e, "oq_attention (tensor map)");
+  if (a->total_k == 0) mk = mv = mq;               // no key tile is ever loaded
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  e = a->head_dim == 128 ? attn::launch<128>(p, mq, mk, mv, attn::sm_count(), st) : attn::launch<64>(p, mq, mk, mv, attn::sm_count(), st);
+  if (e != cudaSuccess) return cuda_fail(e, "oq_attention");
+  return OQ_OK;
+}
+
+}  // extern "C"

@@ -134,9 +134,9 @@ struct CodebookParams {
 CodebookParams codebook_params(const oq_codebook* cb);
 
 // cuTensorMapEncodeTiled through the runtime's driver entry point (no link-time dependency on the driver library).
-// bf16 elements, no interleave, no swizzle, out-of-bounds elements read as zero.  rank <= 3.
+// bf16 elements, no interleave, no swizzle or the 128-byte one, out-of-bounds elements read as zero.  rank <= 3.
 cudaError_t encode_tensor_map_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
-                                   const uint32_t* box);
+                                   const uint32_t* box, bool swizzle128 = false);
 
 // Device status word (bounded waits report here).
 int* device_status_word();   // device pointer (allocated on first use), or nullptr on failure
