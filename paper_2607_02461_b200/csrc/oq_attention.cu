@@ -272,143 +272,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   const uint32_t tmem = tmem_slot;
   const int n_items = prefix[p.n_seqs] * p.heads * p.splits;
 
-  if (warp >= LOAD_WARP) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-  if (warp == LOAD_WARP) {
-    if (lane == 0) {
-      uint32_t slot = 0, round = 0, q_use[2] = {0, 0};
-      auto load_q = [&](const Item& it, int t) {
-        if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
-        ++q_use[t];
-        mbar_expect_tx(q_full(t), S::TILE);
-        for (uint32_t a = 0; a < S::ATOMS; ++a)
-          tma_load_3d(smem_q + (uint32_t)t * S::TILE + a * ATOM, &map_q, 64 * (int)a, it.head, it.q_base + it.q0 + t * BM, q_full(t));
-      };
-      auto load_kv = [&](const Item& it, const CUtensorMap* map, int key0) {
-        if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
-        mbar_expect_tx(kv_full(slot), S::TILE);
-        for (uint32_t a = 0; a < S::ATOMS; ++a)
-          tma_load_3d(smem_kv + slot * S::TILE + a * ATOM, map, 64 * (int)a, it.head / p.group, it.k_base + key0, kv_full(slot));
-        if (++slot == SLOTS) {
-          slot = 0;
-          ++round;
-        }
-      };
-      for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
-        const Item it = make_item(p, prefix, i);
-        if (it.tiles == 0) continue;
-        load_q(it, 0);
-        load_kv(it, &map_k, it.key0(0));
-        if (it.rows1 > 0) load_q(it, 1);
-        for (int j = 0; j < it.tiles && !abort_flag; ++j) {
-          load_kv(it, &map_v, it.key0(j));
-          if (j + 1 < it.tiles) load_kv(it, &map_k, it.key0(j + 1));
-        }
-      }
-      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
-      for (uint32_t s = 0; s < SLOTS; ++s) {
-        const uint32_t fills = round + (s < slot ? 1u : 0u);
-        for (int n = 0; fills > 0 && n < (1 << 20) && !mbar_try(kv_full((int)s), (fills - 1) & 1); ++n) {}
-      }
-      for (int t = 0; t < 2; ++t)
-        for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
-    }
-  } else if (warp == MMA_WARP) {
-    if (lane == 0) {
-      constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
-      constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
-      constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
-      uint32_t slot = 0, round = 0, q_use[2] = {0, 0}, p_use[2] = {0, 0}, o_use[2] = {0, 0};
-      auto next_kv = [&]() {
-        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
-        const uint32_t s = slot;
-        if (++slot == SLOTS) {
-          slot = 0;
-          ++round;
-        }
-        return s;
-      };
-      auto issue_s = [&](int t, uint32_t k_slot) {
-        const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::TILE), b = smem_desc(smem_kv + k_slot * S::TILE);
-#pragma unroll
-        for (uint32_t k = 0; k < D / 16; ++k) {
-          const uint64_t step = (uint64_t)((k >> 2) * (ATOM >> 4) + 2 * (k & 3));
-          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0);
-        }
-        mma_commit(s_full(t));
-      };
-      auto issue_o = [&](int t, uint32_t v_slot, bool first) {
-        const uint64_t b = smem_desc_mn(smem_kv + v_slot * S::TILE, ATOM, 1024);
-#pragma unroll
-        for (uint32_t k = 0; k < BN / 16; ++k)
-          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0));
-      };
-      // the item whose S comes next runs one key tile ahead of the one whose O is accumulated
-      int i = blockIdx.x;
-      Item cur;
-      cur.tiles = 0;
-      auto next_item = [&](Item& it) {
-        for (; i < n_items; i += gridDim.x) {
-          it = make_item(p, prefix, i);
-          if (it.tiles > 0) {
-            i += gridDim.x;
-            return true;
-          }
-        }
-        return false;
-      };
-      bool have = next_item(cur);
-      if (have) {
-        const uint32_t k_slot = next_kv();
-        for (int t = 0; t < (cur.rows1 > 0 ? 2 : 1); ++t) {
-          mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
-          tc_fence_after();
-          issue_s(t, k_slot);
-          if (cur.tiles == 1) mma_commit(q_free(t));
-        }
-        mma_commit(kv_free(k_slot));
-      }
-      while (have && !abort_flag) {
-        Item nxt;
-        const bool more = next_item(nxt);
-        for (int j = 0; j < cur.tiles && !abort_flag; ++j) {
-          const bool last = j + 1 == cur.tiles;
-          const bool ahead = !last || more;            // a tile whose S is to be issued
-          const uint32_t v_slot = next_kv();
-          uint32_t k_slot = 0;
-          bool k_there = false;
-          const bool two_now = cur.rows1 > 0, two_next = last ? (more && nxt.rows1 > 0) : two_now;
-          for (int t = 0; t < 2; ++t) {
-            if (t == 0 || two_now) {
-              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
-              if (j == 0 && o_use[t] > 0) mbar_spin(o_free(t), (o_use[t] - 1) & 1, &abort_flag, p.status, W_OFREE);
-              tc_fence_after();
-              issue_o(t, v_slot, j == 0);
-              if (last) {
-                mma_commit(o_full(t));
-                ++o_use[t];
-              }
-            }
-            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot));
-            if (ahead && (t == 0 || two_next)) {
-              if (!k_there) {
-                k_slot = next_kv();
-                k_there = true;
-              }
-              if (last) mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
-              tc_fence_after();
-              issue_s(t, k_slot);
-              // the query tile is free once its last S is there
-              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t));
-            }
-          }
-          if (k_there) mma_commit(kv_free(k_slot));
-        }
-        cur = nxt;
-        have = more;
-      }
-    }
-  } else if (warp < LOAD_WARP) {
+  if (warp < LOAD_WARP) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax ------------------------------------------------
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -548,6 +413,143 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         exact_row<D>(p, it, r0 + (warp & 3) * 32 + r);
       }
     }
+  } else {
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+   if (warp == LOAD_WARP) {
+    if (lane == 0) {
+      uint32_t slot = 0, round = 0, q_use[2] = {0, 0};
+      auto load_q = [&](const Item& it, int t) {
+        if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
+        ++q_use[t];
+        mbar_expect_tx(q_full(t), S::TILE);
+        for (uint32_t a = 0; a < S::ATOMS; ++a)
+          tma_load_3d(smem_q + (uint32_t)t * S::TILE + a * ATOM, &map_q, 64 * (int)a, it.head, it.q_base + it.q0 + t * BM, q_full(t));
+      };
+      auto load_kv = [&](const Item& it, const CUtensorMap* map, int key0) {
+        if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
+        mbar_expect_tx(kv_full(slot), S::TILE);
+        for (uint32_t a = 0; a < S::ATOMS; ++a)
+          tma_load_3d(smem_kv + slot * S::TILE + a * ATOM, map, 64 * (int)a, it.head / p.group, it.k_base + key0, kv_full(slot));
+        if (++slot == SLOTS) {
+          slot = 0;
+          ++round;
+        }
+      };
+      for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
+        const Item it = make_item(p, prefix, i);
+        if (it.tiles == 0) continue;
+        load_q(it, 0);
+        load_kv(it, &map_k, it.key0(0));
+        if (it.rows1 > 0) load_q(it, 1);
+        for (int j = 0; j < it.tiles && !abort_flag; ++j) {
+          load_kv(it, &map_v, it.key0(j));
+          if (j + 1 < it.tiles) load_kv(it, &map_k, it.key0(j + 1));
+        }
+      }
+      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
+      for (uint32_t s = 0; s < SLOTS; ++s) {
+        const uint32_t fills = round + (s < slot ? 1u : 0u);
+        for (int n = 0; fills > 0 && n < (1 << 20) && !mbar_try(kv_full((int)s), (fills - 1) & 1); ++n) {}
+      }
+      for (int t = 0; t < 2; ++t)
+        for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
+    }
+  } else if (warp == MMA_WARP) {
+    if (lane == 0) {
+      constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
+      constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
+      constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
+      uint32_t slot = 0, round = 0, q_use[2] = {0, 0}, p_use[2] = {0, 0}, o_use[2] = {0, 0};
+      auto next_kv = [&]() {
+        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
+        const uint32_t s = slot;
+        if (++slot == SLOTS) {
+          slot = 0;
+          ++round;
+        }
+        return s;
+      };
+      auto issue_s = [&](int t, uint32_t k_slot) {
+        const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::TILE), b = smem_desc(smem_kv + k_slot * S::TILE);
+#pragma unroll
+        for (uint32_t k = 0; k < D / 16; ++k) {
+          const uint64_t step = (uint64_t)((k >> 2) * (ATOM >> 4) + 2 * (k & 3));
+          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0);
+        }
+        mma_commit(s_full(t));
+      };
+      auto issue_o = [&](int t, uint32_t v_slot, bool first) {
+        const uint64_t b = smem_desc_mn(smem_kv + v_slot * S::TILE, ATOM, 1024);
+#pragma unroll
+        for (uint32_t k = 0; k < BN / 16; ++k)
+          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0));
+      };
+      // the item whose S comes next runs one key tile ahead of the one whose O is accumulated
+      int i = blockIdx.x;
+      Item cur;
+      cur.tiles = 0;
+      auto next_item = [&](Item& it) {
+        for (; i < n_items; i += gridDim.x) {
+          it = make_item(p, prefix, i);
+          if (it.tiles > 0) {
+            i += gridDim.x;
+            return true;
+          }
+        }
+        return false;
+      };
+      bool have = next_item(cur);
+      if (have) {
+        const uint32_t k_slot = next_kv();
+        for (int t = 0; t < (cur.rows1 > 0 ? 2 : 1); ++t) {
+          mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
+          tc_fence_after();
+          issue_s(t, k_slot);
+          if (cur.tiles == 1) mma_commit(q_free(t));
+        }
+        mma_commit(kv_free(k_slot));
+      }
+      while (have && !abort_flag) {
+        Item nxt;
+        const bool more = next_item(nxt);
+        for (int j = 0; j < cur.tiles && !abort_flag; ++j) {
+          const bool last = j + 1 == cur.tiles;
+          const bool ahead = !last || more;            // a tile whose S is to be issued
+          const uint32_t v_slot = next_kv();
+          uint32_t k_slot = 0;
+          bool k_there = false;
+          const bool two_now = cur.rows1 > 0, two_next = last ? (more && nxt.rows1 > 0) : two_now;
+          for (int t = 0; t < 2; ++t) {
+            if (t == 0 || two_now) {
+              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
+              if (j == 0 && o_use[t] > 0) mbar_spin(o_free(t), (o_use[t] - 1) & 1, &abort_flag, p.status, W_OFREE);
+              tc_fence_after();
+              issue_o(t, v_slot, j == 0);
+              if (last) {
+                mma_commit(o_full(t));
+                ++o_use[t];
+              }
+            }
+            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot));
+            if (ahead && (t == 0 || two_next)) {
+              if (!k_there) {
+                k_slot = next_kv();
+                k_there = true;
+              }
+              if (last) mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
+              tc_fence_after();
+              issue_s(t, k_slot);
+              // the query tile is free once its last S is there
+              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t));
+            }
+          }
+          if (k_there) mma_commit(kv_free(k_slot));
+        }
+        cur = nxt;
+        have = more;
+      }
+    }
+   }
   }
   tc_fence_before();
   __syncthreads();
