@@ -357,6 +357,27 @@ typedef struct {
 int oq_attention_workspace_bytes(const oq_attention_args* args, size_t* bytes);
 int oq_attention(const oq_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- low-rank adapters beside a shared projection ------------------------------------------------------------ */
+
+/* Adds the low-rank updates of several requests to a projection's output.  A quantized weight cannot take an update
+ * B A without being quantized anew, so a fine-tuned variant is served beside the shared layer:
+ *     Y[t] = base[t] + scale[a] * B_a (A_a X[t]),   a = seg_adapter[s] for the tokens seg_start[s] .. seg_start[s + 1] - 1
+ * and Y[t] = base[t] where a is outside 0 .. n_adapters - 1 (-1: no adapter).
+ *   X_bf16   dev [n_tokens][ldx]: the tokens as they enter the projection (not rotated)
+ *   A_bf16   dev [n_adapters][rank][dim], B_bf16 dev [n_adapters][m][rank], both dense; scale dev fp32 [n_adapters].
+ *            Adapters of smaller rank are filled up with zeros.  rank: a multiple of 8, at most 128
+ *   seg_start dev int32 [n_segs + 1], seg_adapter dev int32 [n_segs].  Values are cut to 0 .. n_tokens; a segment may be
+ *            empty, tokens in no segment are left alone, none may be in two
+ *   base, Y  dev [n_tokens][ldb] / [n_tokens][ldy] of dtype (OQ_BF16 or OQ_F32).  Y may be base (in place, ldy == ldb);
+ *            otherwise the two must not overlap
+ * dim and m multiples of 8, leading dimensions multiples of 16 bytes, pointers 16-byte aligned.  Both products run on the
+ * tensor cores with fp32 accumulation; A x is carried between them in 16 bits for bf16 outputs (two bf16 pieces) and
+ * 24 for fp32 (three).  Results are bit-reproducible.  Asynchronous on `stream`; nothing is allocated.  n_tokens == 0 or
+ * n_segs == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const void* A_bf16, const void* B_bf16, int n_adapters,
+                   int rank, const float* scale, const int* seg_start, const int* seg_adapter, int n_segs, const void* base,
+                   int ldb, void* Y, int ldy, int m, int dtype, void* stream);
+
 /* Self-test of the bounded device-side waits the GEMM pipeline is built on: launches one thread that waits
  * about a millisecond on a barrier nobody arrives at.  The wait gives up by itself (the kernel ends
  * normally, nothing hangs or traps) and records code 9; the following oq_device_status() must return

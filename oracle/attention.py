@@ -72,3 +72,13 @@ def attention(q, k, v, q_lens, k_lens, left=-1, right=-1, sinks=0, scale=None):
                     out[q0 + i, h] = (e @ vv[see]) / e.sum()
         q0, k0 = q0 + nq, k0 + nk
     return out, lse
+
+
+def adapter_add(x, a, b, scale, lens, ids, base):
+    """base + scale_i b_i (a_i x) segment by segment; ids outside the adapters leave base as it is."""
+    y, at = np.array(base, np.float64), 0
+    for n, i in zip(lens, ids):
+        if 0 <= i < len(a):
+            y[at:at + n] += scale[i] * ((x[at:at + n] @ a[i].T) @ b[i].T)
+        at += n
+    return y

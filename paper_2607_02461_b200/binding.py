@@ -65,6 +65,7 @@ def lib():
             "oq_qk_norm_rope": (i, [vp, vp, i, i, vp, vp, i, i, C.c_float, i, i, vp]),
             "oq_attention_workspace_bytes": (i, [vp, C.POINTER(sz)]),
             "oq_attention": (i, [vp, vp, sz, vp]),
+            "oq_adapter_add": (i, [vp, i, i, i, vp, vp, i, i, vp, vp, vp, i, vp, i, vp, i, i, i, vp]),
             "oq_last_error": (C.c_char_p, []), "oq_version": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -490,6 +491,37 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     _check(lib().oq_attention(C.byref(a), workspace.data_ptr() if workspace is not None else None,
                               workspace.numel() if workspace is not None else 0, _stream()))
     return (out, lse) if want_lse else out
+
+
+def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None):
+    """base + scale_a B_a (A_a x) for the tokens of each segment.  X: CUDA bf16 [T, d]; A: bf16 [adapters, rank, d]; Bm: bf16
+    [adapters, m, rank]; scale: fp32 [adapters]; seg_start: int32 [segments + 1]; seg_adapter: int32 [segments] (-1: none);
+    base: bf16 or fp32 [T, m].  Returns out (new by default; out=base adds in place)."""
+    import torch
+    if X.dim() != 2 or A.dim() != 3 or Bm.dim() != 3 or base.dim() != 2:
+        raise OqError(1, "oq_adapter_add: X [T, d], A [adapters, rank, d], B [adapters, m, rank], base [T, m] expected")
+    n, d = X.shape
+    na, rank, m = A.shape[0], A.shape[1], Bm.shape[1]
+    if A.shape[2] != d or Bm.shape[0] != na or Bm.shape[2] != rank or base.shape != (n, m) or scale.shape != (na,):
+        raise OqError(1, "oq_adapter_add: sizes do not match")
+    if not (X.dtype == A.dtype == Bm.dtype == torch.bfloat16) or scale.dtype != torch.float32:
+        raise OqError(1, "oq_adapter_add: X, A, B must be bf16 and scale fp32")
+    if seg_start.dtype != torch.int32 or seg_adapter.dtype != torch.int32 or seg_start.shape != (seg_adapter.shape[0] + 1,):
+        raise OqError(1, "oq_adapter_add: seg_start int32 [segments + 1], seg_adapter int32 [segments] expected")
+    if not (A.is_contiguous() and Bm.is_contiguous() and scale.is_contiguous() and seg_start.is_contiguous() and seg_adapter.is_contiguous()):
+        raise OqError(1, "oq_adapter_add: adapters, scales and segment tables must be contiguous")
+    if out is None:
+        out = torch.empty((n, m), dtype=base.dtype, device=base.device)
+    if out.shape != base.shape or out.dtype != base.dtype:
+        raise OqError(1, "oq_adapter_add: out must have base's shape and type")
+    if n and (X.stride(1) != 1 or base.stride(1) != 1 or out.stride(1) != 1):
+        raise OqError(3, "oq_adapter_add: the elements of a row must be adjacent")
+    many = n > 1
+    _check(lib().oq_adapter_add(X.data_ptr(), n, X.stride(0) if many else d, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(),
+                                seg_start.data_ptr(), seg_adapter.data_ptr(), seg_adapter.shape[0], base.data_ptr(),
+                                base.stride(0) if many else m, out.data_ptr(), out.stride(0) if many else m, m,
+                                _dtype_code(base, "oq_adapter_add"), _stream()))
+    return out
 
 
 def oq_version():

@@ -17,7 +17,7 @@ OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "liboq.so")
 SOURCES = ["oq_host.cu", "oq_rotate_quantize.cu", "oq_rq_mm.cu", "oq_qlinear.cu", "oq_forward_host.cu", "oq_noalloc.cu",
            "oq_adaln.cu", "oq_block.cu", "oq_qk.cu",
-           "oq_attention.cu"]
+           "oq_attention.cu", "oq_adapter.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 
 

@@ -718,7 +718,7 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
     // a stride that is never used (one head, one token) still has to be one that the encoder takes
     const uint64_t strides[2] = {(uint64_t)(heads > 1 && hd > 0 ? hd : a->head_dim) * 2, (uint64_t)(tokens > 1 && ld > 0 ? ld : (long long)a->head_dim * heads) * 2};
     const uint32_t box[3] = {64, 1, 128};
-    return encode_tensor_map_bf16(map, base, 3, dims, strides, box, true);
+    return encode_tensor_map_sw128(map, base, false, 3, dims, strides, box);
   };
   cudaError_t e = make_map(&mq, a->Q, a->n_heads, a->total_q, a->ldq_token, a->ldq_head);
   if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head);

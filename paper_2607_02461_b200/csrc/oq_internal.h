@@ -134,9 +134,12 @@ struct CodebookParams {
 CodebookParams codebook_params(const oq_codebook* cb);
 
 // cuTensorMapEncodeTiled through the runtime's driver entry point (no link-time dependency on the driver library).
-// bf16 elements, no interleave, no swizzle or the 128-byte one, out-of-bounds elements read as zero.  rank <= 3.
+// No interleave, out-of-bounds elements read as zero, rank <= 3: bf16 elements without a swizzle, and bf16 or fp32
+// elements with the 128-byte swizzle (a box is 128 bytes wide).
 cudaError_t encode_tensor_map_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
-                                   const uint32_t* box, bool swizzle128 = false);
+                                   const uint32_t* box);
+cudaError_t encode_tensor_map_sw128(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims,
+                                    const uint64_t* strides_bytes, const uint32_t* box);
 
 // Device status word (bounded waits report here).
 int* device_status_word();   // device pointer (allocated on first use), or nullptr on failure

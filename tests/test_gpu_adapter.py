@@ -1,0 +1,145 @@
+"""GPU parity of the low-rank adapters against the fp64 form, through the C ABI, and their refusals.
+
+Tolerances, derived: the update is two fp32 accumulations of products that are exact in fp32 (at most 8192 + 128 terms,
+added by the tensor cores in blocks: below 2^-18 of the sums of absolute products), and A x is carried in 16 bits (bf16
+output, 2^-16) or 24 (fp32).  With S = |scale| sum |B| (sum |A| |x|): |error| <= 2^-17 S + 2^-23 |Y| for fp32, and for
+bf16 (2^-16 + 2^-17) S before the one rounding of the output (2^-8 |Y|)."""
+import numpy as np
+import pytest
+
+from oracle import attention as oat
+from paper_2607_02461_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(n, d, m, rank, adapters, dtype, seed, pad=0):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, d + pad, generator=g).bfloat16().cuda()[:, :d]
+    a = (torch.randn(adapters, rank, d, generator=g) / np.sqrt(d)).bfloat16().cuda()
+    b = (0.3 * torch.randn(adapters, m, rank, generator=g)).bfloat16().cuda()
+    scale = (0.5 + torch.rand(adapters, generator=g)).cuda()
+    base = torch.randn(n, m + pad, generator=g).to(dtype).cuda()[:, :m]
+    return x, a, b, scale, base
+
+
+def _tables(lens, ids):
+    import torch
+    return (torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda"),
+            torch.tensor(ids, dtype=torch.int32, device="cuda"))
+
+
+def _verify(out, x, a, b, scale, base, lens, ids):
+    import torch
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    ref = oat.adapter_add(f(x), f(a), f(b), f(scale), lens, ids, f(base))
+    size = oat.adapter_add(np.abs(f(x)), np.abs(f(a)), np.abs(f(b)), f(scale), lens, ids, np.zeros(base.shape))
+    err = np.abs(f(out) - ref)
+    tol = 2.0 ** -17 * size + 2.0 ** -23 * np.abs(ref) if out.dtype == torch.float32 else \
+        (2.0 ** -16 + 2.0 ** -17) * size + 2.0 ** -8 * np.abs(ref) * 1.01
+    assert np.all(err <= tol + 1e-30), (err / (tol + 1e-30)).max()
+    at = 0
+    for n, i in zip(lens, ids):                                  # rows without an adapter are the base, bit for bit
+        if not 0 <= i < a.shape[0]:
+            assert torch.equal(out[at:at + n], base[at:at + n])
+        at += n
+
+
+CASES = [
+    # lengths, adapters of the segments, adapters, rank, d, m
+    ([1], [0], 1, 8, 8, 8),
+    ([1, 1, 1], [2, 0, 1], 3, 16, 200, 136),
+    ([130], [0], 1, 32, 64, 72),
+    ([5, 0, 300, 1, 127, 128], [1, 0, -1, 0, 1, 7], 2, 24, 1000, 520),
+    ([129, 257], [1, 0], 2, 64, 3072, 328),
+    ([64, 200], [0, 1], 2, 128, 1024, 264),
+    ([40], [0], 1, 72, 328, 64),
+    ([2, 3], [0, 1], 2, 40, 2048, 9216),
+    ([700], [1], 2, 16, 16, 2048),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,ids,adapters,rank,d,m", CASES)
+def test_matches_fp64(lens, ids, adapters, rank, d, m, dtype):
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, a, b, scale, base = _inputs(sum(lens), d, m, rank, adapters, t, rank + d, pad=16)
+    start, seg = _tables(lens, ids)
+    out = B.oq_adapter_add(x, a, b, scale, start, seg, base)
+    torch.cuda.synchronize()
+    assert B.oq_device_status() == 0
+    _verify(out, x, a, b, scale, base, lens, ids)
+    # in place, into a wider buffer; a second call gives the same bits
+    wide = torch.full((sum(lens), m + 24), 7.0, dtype=t, device="cuda")
+    B.oq_adapter_add(x, a, b, scale, start, seg, base, out=wide[:, :m])
+    assert torch.equal(wide[:, :m], out) and torch.all(wide[:, m:] == 7.0)
+    held = base.clone()
+    B.oq_adapter_add(x, a, b, scale, start, seg, held, out=held)
+    assert torch.equal(held, out)
+
+
+def test_many_small_segments_and_streams():
+    import torch
+    rng = np.random.default_rng(3)
+    lens, ids = rng.integers(0, 4, 300).tolist(), rng.integers(-1, 5, 300).tolist()
+    x, a, b, scale, base = _inputs(sum(lens), 256, 384, 16, 5, torch.bfloat16, 9)
+    start, seg = _tables(lens, ids)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = B.oq_adapter_add(x, a, b, scale, start, seg, base)
+    side.synchronize()
+    _verify(out, x, a, b, scale, base, lens, ids)
+
+
+def test_tokens_in_no_segment_are_left_alone():
+    import torch
+    x, a, b, scale, base = _inputs(300, 128, 192, 16, 2, torch.float32, 4)
+    start = torch.tensor([10, 60, 200], dtype=torch.int32, device="cuda")
+    out = torch.full_like(base, 7.0)
+    B.oq_adapter_add(x, a, b, scale, start, torch.tensor([1, 0], dtype=torch.int32, device="cuda"), base, out=out)
+    assert torch.all(out[:10] == 7.0) and torch.all(out[200:] == 7.0)
+    _verify(out[10:200], x[10:200], a, b, scale, base[10:200], [50, 140], [1, 0])
+
+
+def test_other_segments_values_do_not_leak():
+    """NaN and infinities in a neighbouring segment's tokens or base stay there, although its rows share a tile's loads."""
+    import torch
+    lens, ids = [70, 20, 60], [0, 1, 0]
+    x, a, b, scale, base = _inputs(150, 256, 320, 32, 2, torch.bfloat16, 6)
+    start, seg = _tables(lens, ids)
+    want = B.oq_adapter_add(x, a, b, scale, start, seg, base)
+    x2, base2 = x.clone(), base.clone()
+    x2[75], base2[80], x2[85] = float("nan"), float("inf"), float("inf")
+    got = B.oq_adapter_add(x2, a, b, scale, start, seg, base2)
+    assert torch.equal(got[:70], want[:70]) and torch.equal(got[90:], want[90:]) and torch.equal(got[70:75], want[70:75])
+    assert torch.all(torch.isnan(got[75]))
+
+
+def test_empty_and_refusals():
+    import torch
+    x, a, b, scale, base = _inputs(4, 64, 64, 16, 2, torch.bfloat16, 1)
+    start, seg = _tables([4], [0])
+    assert B.oq_adapter_add(x[:0], a, b, scale, start, seg, base[:0]).shape == (0, 64)
+
+    def code(*args, **kw):
+        with pytest.raises(B.OqError) as e:
+            B.oq_adapter_add(*args, **kw)
+        return e.value.code
+
+    assert code(x, a[:, :12].contiguous(), b[:, :, :12].contiguous(), scale, start, seg, base) == 2           # rank 12
+    big = _inputs(4, 64, 64, 136, 1, torch.bfloat16, 1)
+    assert code(big[0], big[1], big[2], big[3], start, seg, big[4]) == 2                                      # rank 136
+    assert code(x[:, :60], a[:, :, :60].contiguous(), b, scale, start, seg, base) == 2                        # d 60
+    assert code(x, a, b, scale, start, seg, base[:, :32]) == 1
+    assert code(x.float(), a, b, scale, start, seg, base) == 1
+    assert code(x, a, b, scale.double(), start, seg, base) == 1
+    assert code(x, a, b, scale, start.long(), seg, base) == 1
+    assert code(x, a, b, scale, start, seg, base.half()) == 1
+    assert code(x, a, b, scale, start, seg, base, out=base.float()) == 1
+    wide = torch.zeros(4, 72, dtype=torch.bfloat16, device="cuda")
+    assert code(wide[:, 4:68], a, b, scale, start, seg, base) == 3
+    odd = torch.zeros(4, 68, dtype=torch.bfloat16, device="cuda")
+    assert code(x, a, b, scale, start, seg, odd[:, :64]) == 3
