@@ -5,6 +5,7 @@ the library's kernels.  There is no fallback: if liboq.so is missing or a call f
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -88,6 +89,12 @@ def _ptr(t):
 def _stream():
     import torch
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _raw_stream(device_index):
+    """The current stream's handle without a stream object: 0.2 us instead of 3.5, which counts in calls of a few us."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device_index)
 
 
 class Codebook:
@@ -381,25 +388,38 @@ def oq_make_rope(axis_dims, max_pos, theta=10000.0, layout="pairs"):
     return Rope(axis_dims, max_pos, theta, layout)
 
 
-def _dtype_code(t, what):
+def _dtype_code(dtype, what):
     import torch
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return OQ_BF16
-    if t.dtype == torch.float32:
+    if dtype == torch.float32:
         return OQ_F32
-    raise OqError(1, f"{what}: bf16 or fp32 expected, got {t.dtype}")
+    raise OqError(1, f"{what}: bf16 or fp32 expected, got {dtype}")
 
 
-def _stride(t, dim):
-    return t.stride(dim) if t.shape[dim] > 1 else 0       # the stride of a single row is free in torch
-
-
-class _QkSide(C.Structure):              # oq_qk_side
-    _fields_ = [("X", C.c_void_p), ("ld_token", C.c_longlong), ("ld_head", C.c_longlong), ("n_heads", C.c_int),
-                ("w_bf16", C.c_void_p), ("Y", C.c_void_p), ("ldy_token", C.c_longlong), ("ldy_head", C.c_longlong)]
-
-
+_QK_SIDE = struct.Struct("@PqqiPPqq")               # oq_qk_side
 NORMS = {"none": 0, "head": 1, "row": 2}
+
+
+def _qk_side(X, w, Y, norm, n, head_dim, dtype):
+    """Checks one side of oq_qk_norm_rope and packs its oq_qk_side."""
+    import torch
+    shape = X.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != head_dim or X.dtype != dtype:
+        raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim] of one T, head_dim and type")
+    if Y.shape != shape:
+        raise OqError(1, "oq_qk_norm_rope: outputs must have the inputs' shape")
+    (lt, lh, lc), (yt, yh, yc) = X.stride(), Y.stride()
+    if (lc != 1 or yc != 1) and n and shape[1]:
+        raise OqError(3, "oq_qk_norm_rope: the coordinates of a head must be adjacent")
+    heads = shape[1]
+    if w is not None and (w.dtype != torch.bfloat16 or w.numel() != (head_dim if norm == "head" else heads * head_dim) or not w.is_contiguous()):
+        raise OqError(1, "oq_qk_norm_rope: weights must be contiguous bf16, one for each normed coordinate")
+    if n == 1:                                       # torch leaves the stride of a single row or head free
+        lt = yt = 0
+    if heads == 1:
+        lh = yh = 0
+    return _QK_SIDE.pack(X.data_ptr(), lt, lh, heads, w.data_ptr() if w is not None else 0, Y.data_ptr(), yt, yh)
 
 
 def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", eps=1e-6, out_q=None, out_k=None, out_dtype=None):
@@ -407,49 +427,40 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
     None.  pos: CUDA int32 [T, axes].  wq, wk: CUDA bf16, head_dim values (norm="head") or heads * head_dim (norm="row").
     Returns (Q', K'), of out_dtype (the inputs' by default); out_q, out_k may be Q and K themselves."""
     import torch
-    n, head_dim = Q.shape[0], Q.shape[2]
+    shape, dtype = Q.shape, Q.dtype
+    if len(shape) != 3:
+        raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim]")
+    n, head_dim = shape[0], shape[2]
     if norm not in NORMS:
         raise OqError(1, f"oq_qk_norm_rope: norm must be one of {sorted(NORMS)}")
-    sides, outs, given = [], [], [(Q, wq, out_q), (K, wk, out_k)]
-    for X, w, Y in given:
-        if X is None:
-            sides.append(None), outs.append(None)
-            continue
-        if X.dim() != 3 or X.shape[0] != n or X.shape[2] != head_dim or X.dtype != Q.dtype:
-            raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim] of one T, head_dim and type")
-        if Y is None:
-            Y = torch.empty(X.shape, dtype=out_dtype or X.dtype, device=X.device)
-        if Y.shape != X.shape or (outs and Y.dtype != outs[0].dtype):
-            raise OqError(1, "oq_qk_norm_rope: outputs must have the inputs' shape and one type")
-        if X.numel() and (X.stride(2) != 1 or Y.stride(2) != 1):
-            raise OqError(3, "oq_qk_norm_rope: the coordinates of a head must be adjacent")
-        heads = X.shape[1]
-        if w is not None and (w.dtype != torch.bfloat16 or w.numel() != (head_dim if norm == "head" else heads * head_dim) or not w.is_contiguous()):
-            raise OqError(1, "oq_qk_norm_rope: weights must be contiguous bf16, one for each normed coordinate")
-        sides.append(_QkSide(X.data_ptr(), _stride(X, 0), _stride(X, 1), heads, w.data_ptr() if w is not None else None,
-                             Y.data_ptr(), _stride(Y, 0), _stride(Y, 1)))
-        outs.append(Y)
-    ldpos = 0
+    x_code = _dtype_code(dtype, "oq_qk_norm_rope")
+    if out_q is None:
+        out_q = Q.new_empty(shape) if out_dtype is None else Q.new_empty(shape, dtype=out_dtype)
+    y_code = _dtype_code(out_q.dtype, "oq_qk_norm_rope")
+    q_side, k_side = _qk_side(Q, wq, out_q, norm, n, head_dim, dtype), None
+    if K is not None:
+        if out_k is None:
+            out_k = K.new_empty(K.shape) if out_dtype is None else K.new_empty(K.shape, dtype=out_dtype)
+        if out_k.dtype != out_q.dtype:
+            raise OqError(1, "oq_qk_norm_rope: outputs must have one type")
+        k_side = _qk_side(K, wk, out_k, norm, n, head_dim, dtype)
+    ldpos, table, at = 0, None, None
     if rope is not None:
-        if pos is None or pos.dtype != torch.int32 or pos.dim() != 2 or pos.shape != (n, len(rope.axis_dims)):
+        axes = len(rope.axis_dims)
+        if pos is None or pos.dtype != torch.int32 or pos.shape != (n, axes):
             raise OqError(1, "oq_qk_norm_rope: pos must be int32 [T, axes]")
-        if n and pos.shape[1] > 1 and pos.stride(1) != 1:
+        ldpos, step = pos.stride()
+        if step != 1 and axes > 1 and n:
             raise OqError(3, "oq_qk_norm_rope: the positions of a token must be adjacent")
-        ldpos = pos.stride(0) if n > 1 else pos.shape[1]
-    _check(lib().oq_qk_norm_rope(C.byref(sides[0]), C.byref(sides[1]) if sides[1] is not None else None, n, head_dim,
-                                 rope.handle if rope is not None else None, pos.data_ptr() if rope is not None else None, ldpos,
-                                 NORMS[norm], eps, _dtype_code(Q, "oq_qk_norm_rope"), _dtype_code(outs[0], "oq_qk_norm_rope"),
-                                 _stream()))
-    return outs[0], outs[1]
+        if n <= 1:
+            ldpos = axes
+        table, at = rope.handle, pos.data_ptr()
+    _check(lib().oq_qk_norm_rope(q_side, k_side, n, head_dim, table, at, ldpos, NORMS[norm], eps, x_code, y_code,
+                                 _raw_stream(Q.get_device())))
+    return out_q, out_k if K is not None else None
 
 
-class _AttentionArgs(C.Structure):       # oq_attention_args
-    _fields_ = [(n, C.c_void_p) for n in ("Q", "K", "V")] + \
-               [(n, C.c_longlong) for n in ("ldq_token", "ldq_head", "ldk_token", "ldk_head", "ldv_token", "ldv_head")] + \
-               [("out", C.c_void_p), ("ldo_token", C.c_longlong), ("ldo_head", C.c_longlong), ("lse", C.c_void_p),
-                ("q_start", C.c_void_p), ("k_start", C.c_void_p)] + \
-               [(n, C.c_int) for n in ("n_seqs", "total_q", "total_k", "n_heads", "n_kv_heads", "head_dim", "left", "right", "sinks")] + \
-               [("scale", C.c_float)]
+_ATTENTION_ARGS = struct.Struct("@PPPqqqqqqPqqPPPiiiiiiiiif")      # oq_attention_args
 
 
 def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0, scale=0.0, out=None, want_lse=False,
@@ -459,37 +470,51 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     Returns out [Tq, heads, head_dim], or (out, lse fp32 [heads, Tq]) with want_lse.  workspace: CUDA uint8 tensor, by
     default one is taken from torch's allocator when the call needs it."""
     import torch
-    if Q.dim() != 3 or K.dim() != 3 or K.shape != V.shape or Q.shape[2] != K.shape[2]:
+    bf16 = torch.bfloat16
+    qs, ks = Q.shape, K.shape
+    if len(qs) != 3 or len(ks) != 3 or ks != V.shape or qs[2] != ks[2]:
         raise OqError(1, "oq_attention: Q must be [Tq, heads, head_dim], K and V [Tk, kv_heads, head_dim]")
-    if not (Q.dtype == K.dtype == V.dtype == torch.bfloat16):
+    if Q.dtype != bf16 or K.dtype != bf16 or V.dtype != bf16:
         raise OqError(1, "oq_attention: bf16 expected")
-    if Q.numel() and Q.stride(2) != 1 or K.numel() and (K.stride(2) != 1 or V.stride(2) != 1):
-        raise OqError(3, "oq_attention: the coordinates of a head must be adjacent")
-    tq, heads, head_dim = Q.shape
-    n_seqs = 1
-    for t in (q_start, k_start):
-        if t is not None:
-            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() < 2 or not t.is_cuda:
-                raise OqError(1, "oq_attention: q_start and k_start must be contiguous CUDA int32 [sequences + 1]")
-            n_seqs = t.numel() - 1
-    if q_start is not None and k_start is not None and q_start.numel() != k_start.numel():
-        raise OqError(1, "oq_attention: q_start and k_start must have one length")
+    tq, heads, head_dim = qs
+    tk, kv_heads = ks[0], ks[1]
+    n_seqs, starts = 1, [0, 0]
+    if q_start is not None or k_start is not None:
+        for i, t in enumerate((q_start, k_start)):
+            if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+                raise OqError(1, "oq_attention: q_start and k_start must both be contiguous CUDA int32 [sequences + 1]")
+            n_seqs, starts[i] = t.shape[0] - 1, t.data_ptr()
+        if q_start.shape[0] != k_start.shape[0]:
+            raise OqError(1, "oq_attention: q_start and k_start must have one length")
     if out is None:
-        out = torch.empty((tq, heads, head_dim), dtype=torch.bfloat16, device=Q.device)
-    elif out.shape != Q.shape or out.dtype != torch.bfloat16 or out.numel() and out.stride(2) != 1:
-        raise OqError(1, "oq_attention: out must be bf16, shaped like Q, with adjacent coordinates")
+        out = Q.new_empty(qs)
+    elif out.shape != qs or out.dtype != bf16:
+        raise OqError(1, "oq_attention: out must be bf16, shaped like Q")
+    (qt, qh, qc), (kt, kh, kc), (vt, vh, vc), (ot, oh, oc) = Q.stride(), K.stride(), V.stride(), out.stride()
+    if (qc != 1 or oc != 1) and Q.numel() or (kc != 1 or vc != 1) and K.numel():
+        raise OqError(3, "oq_attention: the coordinates of a head must be adjacent")
+    if tq <= 1:                                      # torch leaves the stride of a single row or head free
+        qt = ot = 0
+    if heads == 1:
+        qh = oh = 0
+    if tk <= 1:
+        kt = vt = 0
+    if kv_heads == 1:
+        kh = vh = 0
     lse = torch.empty((heads, tq), dtype=torch.float32, device=Q.device) if want_lse else None
-    a = _AttentionArgs(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _stride(Q, 0), _stride(Q, 1), _stride(K, 0), _stride(K, 1),
-                       _stride(V, 0), _stride(V, 1), out.data_ptr(), _stride(out, 0), _stride(out, 1),
-                       lse.data_ptr() if want_lse else None, q_start.data_ptr() if q_start is not None else None,
-                       k_start.data_ptr() if k_start is not None else None, n_seqs, tq, K.shape[0], heads, K.shape[1], head_dim,
-                       left, right, sinks, scale)
-    need = C.c_size_t()
-    _check(lib().oq_attention_workspace_bytes(C.byref(a), C.byref(need)))
-    if workspace is None and need.value:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=Q.device)
-    _check(lib().oq_attention(C.byref(a), workspace.data_ptr() if workspace is not None else None,
-                              workspace.numel() if workspace is not None else 0, _stream()))
+    args = _ATTENTION_ARGS.pack(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qt, qh, kt, kh, vt, vh, out.data_ptr(), ot, oh,
+                                lse.data_ptr() if want_lse else 0, starts[0], starts[1], n_seqs, tq, tk, heads, kv_heads, head_dim,
+                                left, right, sinks, scale)
+    space = size = 0
+    if workspace is not None:
+        space, size = workspace.data_ptr(), workspace.numel()
+    else:
+        need = C.c_size_t()
+        _check(lib().oq_attention_workspace_bytes(args, C.byref(need)))
+        if need.value:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=Q.device)
+            space, size = workspace.data_ptr(), need.value
+    _check(lib().oq_attention(args, space, size, _raw_stream(Q.get_device())))
     return (out, lse) if want_lse else out
 
 
@@ -498,29 +523,33 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None):
     [adapters, m, rank]; scale: fp32 [adapters]; seg_start: int32 [segments + 1]; seg_adapter: int32 [segments] (-1: none);
     base: bf16 or fp32 [T, m].  Returns out (new by default; out=base adds in place)."""
     import torch
-    if X.dim() != 2 or A.dim() != 3 or Bm.dim() != 3 or base.dim() != 2:
+    bf16, i32 = torch.bfloat16, torch.int32
+    xs, sa, sb, shape = X.shape, A.shape, Bm.shape, base.shape
+    if len(xs) != 2 or len(sa) != 3 or len(sb) != 3 or len(shape) != 2:
         raise OqError(1, "oq_adapter_add: X [T, d], A [adapters, rank, d], B [adapters, m, rank], base [T, m] expected")
-    n, d = X.shape
-    na, rank, m = A.shape[0], A.shape[1], Bm.shape[1]
-    if A.shape[2] != d or Bm.shape[0] != na or Bm.shape[2] != rank or base.shape != (n, m) or scale.shape != (na,):
+    n, d = xs
+    na, rank, m = sa[0], sa[1], sb[1]
+    segs = seg_adapter.shape[0]
+    if sa[2] != d or sb[0] != na or sb[2] != rank or shape[0] != n or shape[1] != m or scale.shape != (na,):
         raise OqError(1, "oq_adapter_add: sizes do not match")
-    if not (X.dtype == A.dtype == Bm.dtype == torch.bfloat16) or scale.dtype != torch.float32:
+    if X.dtype != bf16 or A.dtype != bf16 or Bm.dtype != bf16 or scale.dtype != torch.float32:
         raise OqError(1, "oq_adapter_add: X, A, B must be bf16 and scale fp32")
-    if seg_start.dtype != torch.int32 or seg_adapter.dtype != torch.int32 or seg_start.shape != (seg_adapter.shape[0] + 1,):
+    if seg_start.dtype != i32 or seg_adapter.dtype != i32 or seg_start.shape != (segs + 1,):
         raise OqError(1, "oq_adapter_add: seg_start int32 [segments + 1], seg_adapter int32 [segments] expected")
     if not (A.is_contiguous() and Bm.is_contiguous() and scale.is_contiguous() and seg_start.is_contiguous() and seg_adapter.is_contiguous()):
         raise OqError(1, "oq_adapter_add: adapters, scales and segment tables must be contiguous")
     if out is None:
-        out = torch.empty((n, m), dtype=base.dtype, device=base.device)
-    if out.shape != base.shape or out.dtype != base.dtype:
+        out = base.new_empty(shape)
+    elif out.shape != shape or out.dtype != base.dtype:
         raise OqError(1, "oq_adapter_add: out must have base's shape and type")
-    if n and (X.stride(1) != 1 or base.stride(1) != 1 or out.stride(1) != 1):
+    (ldx, xc), (ldb, bc), (ldy, yc) = X.stride(), base.stride(), out.stride()
+    if n and (xc != 1 or bc != 1 or yc != 1):
         raise OqError(3, "oq_adapter_add: the elements of a row must be adjacent")
-    many = n > 1
-    _check(lib().oq_adapter_add(X.data_ptr(), n, X.stride(0) if many else d, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(),
-                                seg_start.data_ptr(), seg_adapter.data_ptr(), seg_adapter.shape[0], base.data_ptr(),
-                                base.stride(0) if many else m, out.data_ptr(), out.stride(0) if many else m, m,
-                                _dtype_code(base, "oq_adapter_add"), _stream()))
+    if n <= 1:
+        ldx, ldb, ldy = d, m, m
+    _check(lib().oq_adapter_add(X.data_ptr(), n, ldx, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(), seg_start.data_ptr(),
+                                seg_adapter.data_ptr(), segs, base.data_ptr(), ldb, out.data_ptr(), ldy, m,
+                                _dtype_code(base.dtype, "oq_adapter_add"), _raw_stream(X.get_device())))
     return out
 
 

@@ -5,13 +5,12 @@
 //   (u, v) -> (u cos - v sin, u sin + v cos)        for the pair (u, v) that belongs to (a, i)
 //
 // Bound: memory.  Every value is read once and written once, and there are about 8 operations per value.  A lane owns
-// 8 adjacent coordinates of a head (one 16-byte access in bf16), a warp 256 / head_dim heads at a time; it requests
-// all of its ITERS rows before it uses the first one, so that 2 KB per warp are in flight while the rotation's table is
-// looked up (pos -> table is the only dependent pair of loads).  The lane's cosines and sines depend on the token alone
-// and serve all of its ITERS heads.  The table (fp64 on the host, rounded once) replaces the sine and cosine of
-// an angle that fp32 could not hold: at position 32760 half a unit in the last place is already 1e-3.
-//
-// Measured (B200): 4608 tokens x (24 + 24) heads of 128 and 32760 tokens x (40 + 40) heads: see the launch rule below.
+// 8 adjacent coordinates of a head (one 16-byte access in bf16), a warp 256 / head_dim heads at a time and ITERS such
+// rows together.  Warps (with a norm over all heads: CTAs) stay and walk over the tokens, and request the next rows, the
+// table entries of the next token and the positions of the one after it before they work on the present ones: three
+// dependent latencies (position, table, rows) overlap with the arithmetic, and 2 KB a warp are always in flight.
+// The table (fp64 on the host, rounded once) replaces the sine and cosine of an angle that fp32 could not hold: at
+// position 32760 half a unit in the last place is already 1e-3.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -26,7 +25,7 @@ struct oq_rope {
   int n_axes = 0, dim = 0, layout = 0;
   std::vector<int> axis_dim, max_pos;
   std::vector<float> table;          // (cos, sin) pairs: [axis][pos][d_a / 2]
-  std::vector<long long> base;       // first pair of an axis in the table
+  std::vector<int> base;             // first (cos, sin) pair of an axis in the table
   mutable std::mutex mutex;
   mutable float2* d_table = nullptr; // device copy, created on first GPU use
   mutable int device = -1;
@@ -56,7 +55,7 @@ struct Params {
   const float2* table;
   int axis_end[MAX_AXES];           // in coordinates of the head
   int max_pos[MAX_AXES];
-  long long base[MAX_AXES];
+  int base[MAX_AXES];               // first table entry of an axis
 };
 
 __device__ __forceinline__ uint4 load16(const void* p) {
@@ -107,141 +106,198 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
+enum { HEAD = 0, ROW = 1, WIDE_ROW = 2 };      // WIDE_ROW: more than WARPS warps for a row, fewer registers each
+
 // ROW: the norm runs over all heads of a token; a CTA is one (token, side), its warps meet once in shared memory.
-// Otherwise a warp is one (token, side, chunk of heads) and the norm closes inside the lanes of a head.
+// HEAD: a warp is one (token, side, chunk of heads) and the norm closes inside the lanes of a head.
 // HALVES: the partner of a coordinate lies d_a / 2 further on (in another lane), otherwise right beside it.
-template <typename In, typename Out, bool ROW, bool HALVES>
-__global__ void __launch_bounds__(ROW ? MAX_ROW_WARPS * 32 : WARPS * 32) qk_norm_rope_kernel(const Params p) {
-  __shared__ float red[MAX_ROW_WARPS];
+template <typename In, typename Out, int MODE, bool HALVES>
+__global__ void __launch_bounds__(MODE == WIDE_ROW ? MAX_ROW_WARPS * 32 : WARPS * 32, MODE == WIDE_ROW ? 1 : 2)
+qk_norm_rope_kernel(const __grid_constant__ Params p) {
+  constexpr int NP = HALVES ? 8 : 4;           // pairs a lane has a part in
+  __shared__ float red[2][MAX_ROW_WARPS];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int L = p.lanes_per_head, sub = lane & (L - 1), c0 = 8 * sub;
-  const int per_iter = 32 / L;
-  long long token;
-  int s, chunk;
-  if (ROW) {
-    const int sides = (p.side[0].heads > 0) + (p.side[1].heads > 0);
-    token = blockIdx.x / sides;
-    s = sides == 2 ? (int)(blockIdx.x % 2) : (p.side[0].heads > 0 ? 0 : 1);
-    chunk = warp;
-  } else {
-    const long long item = (long long)blockIdx.x * WARPS + warp;
-    const int per_token = p.side[0].chunks + p.side[1].chunks;
-    token = item / per_token;
-    const int r = (int)(item % per_token);
-    s = r >= p.side[0].chunks;
-    chunk = s ? r - p.side[0].chunks : r;
-    if (token >= p.tokens) return;
-  }
-  const Side& sd = p.side[s];
-  const In* src = reinterpret_cast<const In*>(sd.X) + token * sd.ld_token + c0;
-  const int head0 = chunk * ITERS * per_iter + lane / L;
-  Raw<In> raw[ITERS];
-#pragma unroll
-  for (int i = 0; i < ITERS; ++i) {
-    const int h = head0 + i * per_iter;
-    if (h < sd.heads) raw[i].load(src + (long long)h * sd.ld_head);
-  }
-  // this lane's cosines and sines; (1, 0) where nothing rotates
-  constexpr int NP = HALVES ? 8 : 4;
-  float cs[NP], sn[NP];
+  const int L = p.lanes_per_head, sub = lane & (L - 1), c0 = 8 * sub, per_iter = 32 / L;
+
+  // which table entries the lane's pairs have, apart from the position
+  int axis[NP], half[NP], entry[NP];
   int partner = lane;
+  bool upper = false;
 #pragma unroll
   for (int e = 0; e < NP; ++e) {
     const int c = HALVES ? c0 + e : c0 + 2 * e;
-    cs[e] = 1.f;
-    sn[e] = 0.f;
+    axis[e] = -1;
+    half[e] = entry[e] = 0;
     if (c < p.rot_dim) {
       int a = 0, begin = 0;
       while (a + 1 < p.n_axes && c >= p.axis_end[a]) begin = p.axis_end[a++];
-      const int half = (p.axis_end[a] - begin) >> 1;
-      const int q = __ldg(p.pos + token * p.ldpos + a);
+      axis[e] = a;
+      half[e] = (p.axis_end[a] - begin) >> 1;
       int f = HALVES ? c - begin : (c - begin) >> 1;
-      bool upper = false;
-      if (HALVES && f >= half) {
-        f -= half;
-        upper = true;
+      if (HALVES) {                            // (the same for the lane's 8 coordinates: an axis' half is a multiple of 8)
+        upper = f >= half[e];
+        if (upper) f -= half[e];
+        partner = upper ? lane - half[e] / 8 : lane + half[e] / 8;
       }
-      if (HALVES) partner = upper ? lane - half / 8 : lane + half / 8;
-      float2 t = make_float2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));   // a position outside the table shows as NaN
-      if (q >= 0 && q < p.max_pos[a]) t = __ldg(p.table + p.base[a] + (long long)q * half + f);
-      cs[e] = t.x;
-      sn[e] = HALVES ? (upper ? t.y : -t.y) : t.y;
+      entry[e] = p.base[a] + f;
     }
   }
-  float w[8];
-  if (!ROW && sd.w) unpack8(*reinterpret_cast<const uint4*>(sd.w + c0), w);
-  float inv_row = 1.f;
-  if (ROW) {
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITERS; ++i) {
-      if (head0 + i * per_iter >= sd.heads) continue;
-      float x[8];
-      raw[i].get(x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+
+  const int sides = (p.side[0].heads > 0) + (p.side[1].heads > 0);
+  const int per_token = MODE == HEAD ? p.side[0].chunks + p.side[1].chunks : sides;
+  const unsigned unit = MODE == HEAD ? blockIdx.x * WARPS + warp : blockIdx.x;
+  const unsigned units = MODE == HEAD ? gridDim.x * WARPS : gridDim.x;
+  const int step_token = (int)(units / per_token), step_r = (int)(units % per_token);
+  struct Place {
+    int token, r;
+  };
+  auto next = [&](Place a) {
+    a.token += step_token;
+    a.r += step_r;
+    if (a.r >= per_token) {
+      a.r -= per_token;
+      ++a.token;
     }
+    return a;
+  };
+  auto side_of = [&](const Place& a) { return MODE == HEAD ? (int)(a.r >= p.side[0].chunks) : (sides == 2 ? a.r : (int)(p.side[0].heads == 0)); };
+  auto head_of = [&](const Place& a, int s) { return (MODE == HEAD ? a.r - (s ? p.side[0].chunks : 0) : warp) * ITERS * per_iter + lane / L; };
+  auto load_rows = [&](const Place& a, Raw<In> (&raw)[ITERS]) {
+    if (a.token >= p.tokens) return;
+    const int s = side_of(a), h0 = head_of(a, s);
+    const Side& sd = p.side[s];
+    const In* src = reinterpret_cast<const In*>(sd.X) + a.token * sd.ld_token + c0;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    if (lane == 0) red[warp] = sum;
-    __syncthreads();
-    float total = lane < (int)(blockDim.x >> 5) ? red[lane] : 0.f;
+    for (int i = 0; i < ITERS; ++i)
+      if (h0 + i * per_iter < sd.heads) raw[i].load(src + (long long)(h0 + i * per_iter) * sd.ld_head);
+  };
+  auto load_pos = [&](const Place& a, int (&pos)[MAX_AXES]) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-    inv_row = rsqrtf(total / (float)(sd.heads * p.head_dim) + p.eps);
-  }
+    for (int x = 0; x < MAX_AXES; ++x) pos[x] = x < p.n_axes && a.token < p.tokens ? __ldg(p.pos + a.token * p.ldpos + x) : 0;
+  };
+  auto load_table = [&](const int (&pos)[MAX_AXES], float2 (&t)[NP]) {
 #pragma unroll
-  for (int i = 0; i < ITERS; ++i) {
-    const int h = head0 + i * per_iter;
-    const bool have = h < sd.heads;                // lanes of another head may still need this lane's shuffles
-    float x[8];
-    if (have) {
-      raw[i].get(x);
-    } else {
+    for (int e = 0; e < NP; ++e) {
+      t[e] = make_float2(1.f, 0.f);                                   // nothing rotates
+      if (axis[e] >= 0) {
+        int q = pos[0], top = p.max_pos[0];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        for (int x = 1; x < MAX_AXES; ++x)
+          if (axis[e] == x) {
+            q = pos[x];
+            top = p.max_pos[x];
+          }
+        t[e] = make_float2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));   // a position outside the table shows as NaN
+        if ((unsigned)q < (unsigned)top) t[e] = __ldg(p.table + entry[e] + q * half[e]);
+      }
     }
-    float inv = inv_row;
-    if (!ROW && p.norm) {
+  };
+
+  Place here{(int)(unit / per_token), (int)(unit % per_token)}, there = next(here);
+  Raw<In> raw[ITERS], raw_next[ITERS];
+  float2 turn[NP], turn_next[NP];
+  int pos[MAX_AXES];
+  load_rows(here, raw);
+  load_pos(here, pos);
+  load_table(pos, turn);
+  load_pos(there, pos);
+  for (int n = 0; here.token < p.tokens; ++n) {
+    load_rows(there, raw_next);
+    load_table(pos, turn_next);
+    const Place after = next(there);
+    load_pos(after, pos);
+
+    const int s = side_of(here), head0 = head_of(here, s);
+    const Side& sd = p.side[s];
+    float inv_row = 1.f;
+    if (MODE != HEAD) {
       float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-      for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-      inv = rsqrtf(sum / (float)p.head_dim + p.eps);
+      for (int i = 0; i < ITERS; ++i) {
+        if (head0 + i * per_iter >= sd.heads) continue;
+        float x[8];
+        raw[i].get(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+      if (lane == 0) red[n & 1][warp] = sum;          // (two buffers: one barrier a token is enough)
+      __syncthreads();
+      float total = lane < (int)(blockDim.x >> 5) ? red[n & 1][lane] : 0.f;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+      inv_row = rsqrtf(total / (float)(sd.heads * p.head_dim) + p.eps);
     }
-    if (ROW && sd.w && have) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + (long long)h * p.head_dim + c0)), w);
+    Out* const dst = reinterpret_cast<Out*>(sd.Y) + here.token * sd.ldy_token + c0;
+    float w[8];
+    if (MODE == HEAD && sd.w) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + c0)), w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = sd.w ? x[e] * inv * w[e] : x[e] * inv;
-    float y[8];
-    if (HALVES) {
+    for (int i = 0; i < ITERS; ++i) {
+      const int h = head0 + i * per_iter;
+      const bool have = h < sd.heads;                // lanes of another head may still need this lane's shuffles
+      float x[8];
+      if (have) {
+        raw[i].get(x);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float other = __shfl_sync(~0u, x[e], partner);
-        y[e] = partner == lane ? x[e] : fmaf(other, sn[e], x[e] * cs[e]);
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
       }
-    } else {
+      float inv = inv_row;
+      if (MODE == HEAD && p.norm) {
+        float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[2 * e] = fmaf(-x[2 * e + 1], sn[e], x[2 * e] * cs[e]);
-        y[2 * e + 1] = fmaf(x[2 * e], sn[e], x[2 * e + 1] * cs[e]);
+        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+        for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        inv = rsqrtf(sum / (float)p.head_dim + p.eps);
       }
-      if (c0 + 8 > p.rot_dim) {                    // no arithmetic on what does not rotate (an infinity stays one)
+      if (MODE != HEAD && sd.w && have) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + (long long)h * p.head_dim + c0)), w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c0 + e >= p.rot_dim) y[e] = x[e];
+      for (int e = 0; e < 8; ++e) x[e] = sd.w ? x[e] * inv * w[e] : x[e] * inv;
+      float y[8];
+      if (HALVES) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float other = __shfl_sync(~0u, x[e], partner);
+          y[e] = partner == lane ? x[e] : fmaf(other, upper ? turn[e].y : -turn[e].y, x[e] * turn[e].x);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[2 * e] = fmaf(-x[2 * e + 1], turn[e].y, x[2 * e] * turn[e].x);
+          y[2 * e + 1] = fmaf(x[2 * e], turn[e].y, x[2 * e + 1] * turn[e].x);
+          if (axis[e] < 0) {                         // no arithmetic on what does not rotate (an infinity stays one)
+            y[2 * e] = x[2 * e];
+            y[2 * e + 1] = x[2 * e + 1];
+          }
+        }
       }
+      if (have) store8(dst + (long long)h * sd.ldy_head, y);
     }
-    if (have) store8(reinterpret_cast<Out*>(sd.Y) + token * sd.ldy_token + (long long)h * sd.ldy_head + c0, y);
+    here = there;
+    there = after;
+#pragma unroll
+    for (int i = 0; i < ITERS; ++i) raw[i] = raw_next[i];
+#pragma unroll
+    for (int e = 0; e < NP; ++e) turn[e] = turn_next[e];
   }
 }
 
 template <typename In, typename Out>
-cudaError_t launch(const Params& p, bool row, bool halves, long long ctas, int threads, cudaStream_t st) {
-  void (*kernel)(Params) = row ? (halves ? qk_norm_rope_kernel<In, Out, true, true> : qk_norm_rope_kernel<In, Out, true, false>)
-                               : (halves ? qk_norm_rope_kernel<In, Out, false, true> : qk_norm_rope_kernel<In, Out, false, false>);
-  return launch_dependent(kernel, (int)ctas, threads, 0, st, p);
+cudaError_t launch(const Params& p, int mode, bool halves, long long most_ctas, int threads, cudaStream_t st) {
+  void (*kernel)(Params) =
+      mode == HEAD ? (halves ? qk_norm_rope_kernel<In, Out, HEAD, true> : qk_norm_rope_kernel<In, Out, HEAD, false>)
+      : mode == ROW ? (halves ? qk_norm_rope_kernel<In, Out, ROW, true> : qk_norm_rope_kernel<In, Out, ROW, false>)
+                    : (halves ? qk_norm_rope_kernel<In, Out, WIDE_ROW, true> : qk_norm_rope_kernel<In, Out, WIDE_ROW, false>);
+  int dev = 0, sms = 0, per_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0);
+  if (e != cudaSuccess) return e;
+  const long long slots = (long long)sms * (per_sm < 1 ? 1 : per_sm);
+  return launch_dependent(kernel, (int)(most_ctas < slots ? most_ctas : slots), threads, 0, st, p);
 }
 
 int ensure_table(const oq_rope* r) {
@@ -301,7 +357,7 @@ int oq_make_rope(int n_axes, const int* axis_dims, const int* max_pos, double th
       size_t at = 0;
       for (int a = 0; a < n_axes; ++a) {
         const int half = axis_dims[a] / 2;
-        r->base.push_back((long long)(at / 2));
+        r->base.push_back((int)(at / 2));
         std::vector<double> freq(half);
         for (int i = 0; i < half; ++i) freq[i] = pow(theta, -2.0 * i / axis_dims[a]);
         for (int q = 0; q < max_pos[a]; ++q)
@@ -392,24 +448,21 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
       p.base[a] = rope->base[a];
     }
   }
-  const bool row = norm == OQ_NORM_ROW;
-  long long ctas;
-  int threads;
-  if (row) {
+  // Rows of up to WARPS warps keep two sets of rows in registers; longer ones run with half the registers.
+  int mode = qk::HEAD, threads = 32 * qk::WARPS;
+  long long ctas = ((long long)n_tokens * (p.side[0].chunks + p.side[1].chunks) + qk::WARPS - 1) / qk::WARPS;
+  if (norm == OQ_NORM_ROW) {
     const int chunks = p.side[0].chunks > p.side[1].chunks ? p.side[0].chunks : p.side[1].chunks;
+    mode = chunks <= qk::WARPS ? qk::ROW : qk::WIDE_ROW;
     ctas = (long long)n_tokens * ((p.side[0].heads > 0) + (p.side[1].heads > 0));
     threads = 32 * chunks;
-  } else {
-    ctas = ((long long)n_tokens * (p.side[0].chunks + p.side[1].chunks) + qk::WARPS - 1) / qk::WARPS;
-    threads = 32 * qk::WARPS;
   }
-  if (ctas > 0x7FFFFFFFll) return fail(OQ_ERR_UNSUPPORTED, "oq_qk_norm_rope: too many tokens for one launch");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e =
-      x_dtype == OQ_BF16 ? (y_dtype == OQ_BF16 ? qk::launch<__nv_bfloat16, __nv_bfloat16>(p, row, halves, ctas, threads, st)
-                                               : qk::launch<__nv_bfloat16, float>(p, row, halves, ctas, threads, st))
-                         : (y_dtype == OQ_BF16 ? qk::launch<float, __nv_bfloat16>(p, row, halves, ctas, threads, st)
-                                               : qk::launch<float, float>(p, row, halves, ctas, threads, st));
+      x_dtype == OQ_BF16 ? (y_dtype == OQ_BF16 ? qk::launch<__nv_bfloat16, __nv_bfloat16>(p, mode, halves, ctas, threads, st)
+                                               : qk::launch<__nv_bfloat16, float>(p, mode, halves, ctas, threads, st))
+                         : (y_dtype == OQ_BF16 ? qk::launch<float, __nv_bfloat16>(p, mode, halves, ctas, threads, st)
+                                               : qk::launch<float, float>(p, mode, halves, ctas, threads, st));
   if (e != cudaSuccess) return cuda_fail(e, "oq_qk_norm_rope");
   return OQ_OK;
 }
