@@ -35,7 +35,8 @@ namespace oq {
 namespace qk {
 
 constexpr int ITERS = 4;            // rows of 256 coordinates one warp holds at a time
-constexpr int WARPS = 8;            // warps of a CTA when the norm stays inside a head
+constexpr int WARPS = 4;            // warps of a CTA when the norm stays inside a head
+constexpr int ROW_WARPS = 8;        // and at most when it runs over a row that fits their registers
 constexpr int MAX_AXES = 4;
 constexpr int MAX_ROW_WARPS = 32;
 
@@ -49,7 +50,7 @@ struct Side {
 struct Params {
   Side side[2];
   int tokens, lanes_per_head, head_dim, rot_dim, n_axes, norm;
-  float eps;
+  float eps, inv_dim;
   const int* pos;
   long long ldpos;
   const float2* table;
@@ -106,35 +107,41 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-enum { HEAD = 0, ROW = 1, WIDE_ROW = 2 };      // WIDE_ROW: more than WARPS warps for a row, fewer registers each
+enum { HEAD = 0, ROW = 1, WIDE_ROW = 2 };      // WIDE_ROW: more than ROW_WARPS warps for a row, fewer registers each
 
 // ROW: the norm runs over all heads of a token; a CTA is one (token, side), its warps meet once in shared memory.
 // HEAD: a warp is one (token, side, chunk of heads) and the norm closes inside the lanes of a head.
 // HALVES: the partner of a coordinate lies d_a / 2 further on (in another lane), otherwise right beside it.
-template <typename In, typename Out, int MODE, bool HALVES>
-__global__ void __launch_bounds__(MODE == WIDE_ROW ? MAX_ROW_WARPS * 32 : WARPS * 32, MODE == WIDE_ROW ? 1 : 2)
+// LANES: lanes of a head, 0: read from the parameters.
+// A turned coordinate is y = x * A + partner * B; where the weights are the same for every head (HEAD) they are part of
+// A and B, which are made once for a token and serve all of the warp's heads.  That, and reductions of fixed length,
+// keep the kernel at ~80 instructions for 256 values; at 270 (weights and side read again for every head, loops of run-time
+// length) it was bound by instruction issue, at twice the time.
+template <typename In, typename Out, int MODE, bool HALVES, int LANES>
+__global__ void __launch_bounds__(MODE == WIDE_ROW ? MAX_ROW_WARPS * 32 : (MODE == ROW ? ROW_WARPS : WARPS) * 32, MODE == WIDE_ROW ? 1 : (MODE == ROW ? 2 : 4))
 qk_norm_rope_kernel(const __grid_constant__ Params p) {
   constexpr int NP = HALVES ? 8 : 4;           // pairs a lane has a part in
   __shared__ float red[2][MAX_ROW_WARPS];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int L = p.lanes_per_head, sub = lane & (L - 1), c0 = 8 * sub, per_iter = 32 / L;
+  const int L = LANES ? LANES : p.lanes_per_head, sub = lane & (L - 1), c0 = 8 * sub, per_iter = 32 / L;
 
-  // which table entries the lane's pairs have, apart from the position
-  int axis[NP], half[NP], entry[NP];
+  // which table entries the lane's pairs have, apart from the position; top < 0: not turned
+  int axis[NP], half[NP], entry[NP], top[NP];
   int partner = lane;
   bool upper = false;
 #pragma unroll
   for (int e = 0; e < NP; ++e) {
     const int c = HALVES ? c0 + e : c0 + 2 * e;
-    axis[e] = -1;
-    half[e] = entry[e] = 0;
+    axis[e] = half[e] = entry[e] = 0;
+    top[e] = -1;
     if (c < p.rot_dim) {
       int a = 0, begin = 0;
       while (a + 1 < p.n_axes && c >= p.axis_end[a]) begin = p.axis_end[a++];
       axis[e] = a;
       half[e] = (p.axis_end[a] - begin) >> 1;
+      top[e] = p.max_pos[a];
       int f = HALVES ? c - begin : (c - begin) >> 1;
       if (HALVES) {                            // (the same for the lane's 8 coordinates: an axis' half is a multiple of 8)
         upper = f >= half[e];
@@ -144,6 +151,7 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
       entry[e] = p.base[a] + f;
     }
   }
+  const bool all_turned = p.rot_dim == 8 * L;
 
   const int sides = (p.side[0].heads > 0) + (p.side[1].heads > 0);
   const int per_token = MODE == HEAD ? p.side[0].chunks + p.side[1].chunks : sides;
@@ -163,42 +171,42 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     return a;
   };
   auto side_of = [&](const Place& a) { return MODE == HEAD ? (int)(a.r >= p.side[0].chunks) : (sides == 2 ? a.r : (int)(p.side[0].heads == 0)); };
-  auto head_of = [&](const Place& a, int s) { return (MODE == HEAD ? a.r - (s ? p.side[0].chunks : 0) : warp) * ITERS * per_iter + lane / L; };
+  // rows of this lane that exist: row i is head first + i * per_iter
+  auto first_head = [&](const Place& a, int s) { return (MODE == HEAD ? a.r - (s ? p.side[0].chunks : 0) : warp) * ITERS * per_iter + lane / L; };
   auto load_rows = [&](const Place& a, Raw<In> (&raw)[ITERS]) {
     if (a.token >= p.tokens) return;
-    const int s = side_of(a), h0 = head_of(a, s);
+    const int s = side_of(a);
     const Side& sd = p.side[s];
-    const In* src = reinterpret_cast<const In*>(sd.X) + a.token * sd.ld_token + c0;
+    const int h0 = first_head(a, s);
+    const In* src = reinterpret_cast<const In*>(sd.X) + a.token * sd.ld_token + h0 * sd.ld_head + c0;
+    const long long step = per_iter * sd.ld_head;
 #pragma unroll
-    for (int i = 0; i < ITERS; ++i)
-      if (h0 + i * per_iter < sd.heads) raw[i].load(src + (long long)(h0 + i * per_iter) * sd.ld_head);
+    for (int i = 0; i < ITERS; ++i) {
+      if (h0 + i * per_iter < sd.heads) raw[i].load(src);
+      src += step;
+    }
   };
-  auto load_pos = [&](const Place& a, int (&pos)[MAX_AXES]) {
+  auto load_pos = [&](const Place& a, int (&pos)[NP]) {
+    if (p.rot_dim == 0 || a.token >= p.tokens) return;
+    const int* row = p.pos + a.token * p.ldpos;
 #pragma unroll
-    for (int x = 0; x < MAX_AXES; ++x) pos[x] = x < p.n_axes && a.token < p.tokens ? __ldg(p.pos + a.token * p.ldpos + x) : 0;
+    for (int e = 0; e < NP; ++e) pos[e] = (HALVES && e) ? pos[0] : __ldg(row + axis[e]);
   };
-  auto load_table = [&](const int (&pos)[MAX_AXES], float2 (&t)[NP]) {
+  auto load_table = [&](const int (&pos)[NP], float2 (&t)[NP]) {
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
-      t[e] = make_float2(1.f, 0.f);                                   // nothing rotates
-      if (axis[e] >= 0) {
-        int q = pos[0], top = p.max_pos[0];
-#pragma unroll
-        for (int x = 1; x < MAX_AXES; ++x)
-          if (axis[e] == x) {
-            q = pos[x];
-            top = p.max_pos[x];
-          }
-        t[e] = make_float2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));   // a position outside the table shows as NaN
-        if ((unsigned)q < (unsigned)top) t[e] = __ldg(p.table + entry[e] + q * half[e]);
-      }
+      t[e] = top[e] < 0 ? make_float2(1.f, 0.f)                                          // not turned
+                        : make_float2(__int_as_float(0x7FFFFFFF), __int_as_float(0x7FFFFFFF));   // a position outside the table shows as NaN
+      if (pos[e] >= 0 && pos[e] < top[e]) t[e] = __ldg(p.table + entry[e] + pos[e] * half[e]);
     }
   };
 
   Place here{(int)(unit / per_token), (int)(unit % per_token)}, there = next(here);
   Raw<In> raw[ITERS], raw_next[ITERS];
   float2 turn[NP], turn_next[NP];
-  int pos[MAX_AXES];
+  int pos[NP];
+#pragma unroll
+  for (int e = 0; e < NP; ++e) pos[e] = 0;
   load_rows(here, raw);
   load_pos(here, pos);
   load_table(pos, turn);
@@ -209,14 +217,32 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     const Place after = next(there);
     load_pos(after, pos);
 
-    const int s = side_of(here), head0 = head_of(here, s);
+    const int s = side_of(here);
     const Side& sd = p.side[s];
-    float inv_row = 1.f;
+    const int heads = sd.heads, head0 = first_head(here, s);
+    const __nv_bfloat16* const weights = sd.w;
+    float A[8], Bc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      A[e] = turn[HALVES ? e : e / 2].x;
+      Bc[e] = HALVES ? (upper ? turn[HALVES ? e : 0].y : -turn[HALVES ? e : 0].y) : ((e & 1) ? turn[e / 2].y : -turn[e / 2].y);
+    }
+    if (MODE == HEAD && weights) {
+      float w[8], wp[8];
+      unpack8(__ldg(reinterpret_cast<const uint4*>(weights + c0)), w);
+      if (HALVES) unpack8(__ldg(reinterpret_cast<const uint4*>(weights + 8 * (partner & (L - 1)))), wp);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        A[e] *= w[e];
+        Bc[e] *= HALVES ? wp[e] : w[e ^ 1];
+      }
+    }
+    float inv = 1.f;
     if (MODE != HEAD) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < ITERS; ++i) {
-        if (head0 + i * per_iter >= sd.heads) continue;
+        if (head0 + i * per_iter >= heads) continue;
         float x[8];
         raw[i].get(x);
 #pragma unroll
@@ -229,52 +255,56 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
       float total = lane < (int)(blockDim.x >> 5) ? red[n & 1][lane] : 0.f;
 #pragma unroll
       for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-      inv_row = rsqrtf(total / (float)(sd.heads * p.head_dim) + p.eps);
+      inv = rsqrtf(total / (float)(heads * p.head_dim) + p.eps);
     }
-    Out* const dst = reinterpret_cast<Out*>(sd.Y) + here.token * sd.ldy_token + c0;
-    float w[8];
-    if (MODE == HEAD && sd.w) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + c0)), w);
+    Out* dst = reinterpret_cast<Out*>(sd.Y) + here.token * sd.ldy_token + head0 * sd.ldy_head + c0;
+    const long long step = per_iter * sd.ldy_head;
 #pragma unroll
     for (int i = 0; i < ITERS; ++i) {
       const int h = head0 + i * per_iter;
-      const bool have = h < sd.heads;                // lanes of another head may still need this lane's shuffles
+      const bool have = h < heads;                   // lanes of another head may still need this lane's shuffles
       float x[8];
-      if (have) {
-        raw[i].get(x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      }
-      float inv = inv_row;
+      raw[i].get(x);                                 // (of a row that is not there: never stored, and its lanes meet only their own)
       if (MODE == HEAD && p.norm) {
-        float sum = 0.f;
+        float sum = x[0] * x[0], odd = x[1] * x[1];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-        for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-        inv = rsqrtf(sum / (float)p.head_dim + p.eps);
+        for (int e = 2; e < 8; e += 2) {
+          sum = fmaf(x[e], x[e], sum);
+          odd = fmaf(x[e + 1], x[e + 1], odd);
+        }
+        sum += odd;
+        if (LANES) {
+#pragma unroll
+          for (int o = LANES >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        } else {
+          for (int o = L >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        }
+        inv = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
       }
-      if (MODE != HEAD && sd.w && have) unpack8(__ldg(reinterpret_cast<const uint4*>(sd.w + (long long)h * p.head_dim + c0)), w);
+      if (MODE != HEAD && weights) {
+        float w[8];
+        if (have) {
+          unpack8(__ldg(reinterpret_cast<const uint4*>(weights + (long long)h * p.head_dim + c0)), w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = sd.w ? x[e] * inv * w[e] : x[e] * inv;
+          for (int e = 0; e < 8; ++e) x[e] *= inv * w[e];
+        }
+      } else if (MODE != HEAD || p.norm) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= inv;
+      }
       float y[8];
-      if (HALVES) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float other = __shfl_sync(~0u, x[e], partner);
-          y[e] = partner == lane ? x[e] : fmaf(other, upper ? turn[e].y : -turn[e].y, x[e] * turn[e].x);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          y[2 * e] = fmaf(-x[2 * e + 1], turn[e].y, x[2 * e] * turn[e].x);
-          y[2 * e + 1] = fmaf(x[2 * e], turn[e].y, x[2 * e + 1] * turn[e].x);
-          if (axis[e] < 0) {                         // no arithmetic on what does not rotate (an infinity stays one)
-            y[2 * e] = x[2 * e];
-            y[2 * e + 1] = x[2 * e + 1];
-          }
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float other = HALVES ? __shfl_sync(~0u, x[e], partner) : x[e ^ 1];
+        y[e] = fmaf(other, Bc[e], x[e] * A[e]);
       }
-      if (have) store8(dst + (long long)h * sd.ldy_head, y);
+      if (!all_turned) {                             // no part of a partner in what is not turned (an infinity stays one)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (top[HALVES ? e : e / 2] < 0) y[e] = x[e] * A[e];
+      }
+      if (have) store8(dst, y);
+      dst += step;
     }
     here = there;
     there = after;
@@ -287,10 +317,15 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
 
 template <typename In, typename Out>
 cudaError_t launch(const Params& p, int mode, bool halves, long long most_ctas, int threads, cudaStream_t st) {
-  void (*kernel)(Params) =
-      mode == HEAD ? (halves ? qk_norm_rope_kernel<In, Out, HEAD, true> : qk_norm_rope_kernel<In, Out, HEAD, false>)
-      : mode == ROW ? (halves ? qk_norm_rope_kernel<In, Out, ROW, true> : qk_norm_rope_kernel<In, Out, ROW, false>)
-                    : (halves ? qk_norm_rope_kernel<In, Out, WIDE_ROW, true> : qk_norm_rope_kernel<In, Out, WIDE_ROW, false>);
+  void (*kernel)(Params);
+  if (mode == HEAD) {
+    if (p.head_dim == 128) kernel = halves ? qk_norm_rope_kernel<In, Out, HEAD, true, 16> : qk_norm_rope_kernel<In, Out, HEAD, false, 16>;
+    else kernel = halves ? qk_norm_rope_kernel<In, Out, HEAD, true, 0> : qk_norm_rope_kernel<In, Out, HEAD, false, 0>;
+  } else if (mode == ROW) {
+    kernel = halves ? qk_norm_rope_kernel<In, Out, ROW, true, 0> : qk_norm_rope_kernel<In, Out, ROW, false, 0>;
+  } else {
+    kernel = halves ? qk_norm_rope_kernel<In, Out, WIDE_ROW, true, 0> : qk_norm_rope_kernel<In, Out, WIDE_ROW, false, 0>;
+  }
   int dev = 0, sms = 0, per_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -431,6 +466,7 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
   p.lanes_per_head = head_dim / 8;
   p.norm = norm;
   p.eps = eps;
+  p.inv_dim = 1.f / (float)head_dim;      // (a power of two)
   bool halves = false;
   if (rope) {
     const int rc = qk::ensure_table(rope);
@@ -448,12 +484,12 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
       p.base[a] = rope->base[a];
     }
   }
-  // Rows of up to WARPS warps keep two sets of rows in registers; longer ones run with half the registers.
+  // Rows of up to ROW_WARPS warps keep two sets of rows in registers; longer ones run with half the registers.
   int mode = qk::HEAD, threads = 32 * qk::WARPS;
   long long ctas = ((long long)n_tokens * (p.side[0].chunks + p.side[1].chunks) + qk::WARPS - 1) / qk::WARPS;
   if (norm == OQ_NORM_ROW) {
     const int chunks = p.side[0].chunks > p.side[1].chunks ? p.side[0].chunks : p.side[1].chunks;
-    mode = chunks <= qk::WARPS ? qk::ROW : qk::WIDE_ROW;
+    mode = chunks <= qk::ROW_WARPS ? qk::ROW : qk::WIDE_ROW;
     ctas = (long long)n_tokens * ((p.side[0].heads > 0) + (p.side[1].heads > 0));
     threads = 32 * chunks;
   }
