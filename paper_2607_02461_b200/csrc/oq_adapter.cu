@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
   const int kb0 = (int)((long long)kb_all * rank / ranks), kb1 = (int)((long long)kb_all * (rank + 1) / ranks);
   const int nb0 = (int)((long long)nb_all * rank / ranks), nb1 = (int)((long long)nb_all * (rank + 1) / ranks);
   const int steps = p.rank16 / 16;
+  const uint32_t leader = elect_leader();
   uint32_t st = 0, ph = 0;                                       // stage ring position of the load and mma threads
   auto advance = [&]() {
     if (++st == (uint32_t)S::STAGES) {
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
         tma_load_3d(at + S::BASE, &map_a, k * KB, 0, id, full(st));
         advance();
       }
-    } else if (warp == MMA_WARP && lane == 0) {
+    } else if (warp == MMA_WARP) {
       const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(p.rank16 >> 3) << 17);
       for (int k = kb0; k < kb1 && !abort_flag; ++k) {
         mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
@@ -199,12 +200,12 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
         const uint64_t a = smem_desc(smem_st + st * S::STAGE), b = smem_desc(smem_st + st * S::STAGE + S::BASE);
 #pragma unroll
         for (uint32_t i = 0; i < KB / 16; ++i)
-          mma_ss(tmem + COL_U, a + 2 * i, b + 2 * i, idesc, k > kb0 || i > 0);
-        mma_commit(freed(st));
-        for (int w = 0; w < 4; ++w) mbar_arrive(freed(st));      // no epilogue warp uses a stage while shrinking
+          mma_ss(tmem + COL_U, a + 2 * i, b + 2 * i, idesc, k > kb0 || i > 0, leader);
+        mma_commit(freed(st), leader);
+        if (lane < 4) mbar_arrive(freed(st));      // no epilogue warp uses a stage while shrinking
         advance();
       }
-      if (kb1 > kb0) mma_commit(u_full);
+      if (kb1 > kb0) mma_commit(u_full, leader);
     } else if (warp < 4) {
       const int row = warp * 32 + lane;
       unsigned char* dst = smem_p + S::U_BYTES + (uint32_t)row * (uint32_t)(p.rank16 * 4 + 16);
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
       // copies still in flight end before the CTA does (after an abort nobody else waits for them)
       for (int s = 0; s < S::STAGES; ++s)
         for (int n = 0; abort_flag && n < (1 << 16); ++n) mbar_try(full(s), ph);
-    } else if (warp == MMA_WARP && lane == 0) {
+    } else if (warp == MMA_WARP) {
       constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(BN >> 3) << 17);
       for (int n = nb0; n < nb1 && !abort_flag; ++n) {
         const uint32_t i = (uint32_t)(n - nb0), a = i & 1u;
@@ -295,11 +296,11 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
             for (int s = 0; s < steps; ++s) {
               const uint64_t da = smem_desc(smem_u + (uint32_t)(q * RB + (s >> 2)) * ATOM) + 2u * (uint32_t)(s & 3);
               const uint64_t db = smem_desc(bt + (uint32_t)(s >> 2) * 8192u) + 2u * (uint32_t)(s & 3);
-              mma_ss(tmem + COL_ACC + 64u * a, da, db, IDESC, q > 0 || s > 0);
+              mma_ss(tmem + COL_ACC + 64u * a, da, db, IDESC, q > 0 || s > 0, leader);
             }
         }
-        mma_commit(acc_full((int)a));
-        mma_commit(freed(st));
+        mma_commit(acc_full((int)a), leader);
+        mma_commit(freed(st), leader);
         advance();
       }
     } else if (warp < 4) {

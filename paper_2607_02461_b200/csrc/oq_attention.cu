@@ -16,7 +16,7 @@
 // carries two query tiles in turn: while the tensor cores multiply for one, the other's threads exponentiate.
 //
 //   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of 128 keys through one ring of shared-memory slots
-//   mma warp    (1 thread)   S_t = Q_t K^T into tensor memory; O_t += P_t V with P_t from tensor memory
+//   mma warp                 S_t = Q_t K^T into tensor memory; O_t += P_t V with P_t from tensor memory
 //   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16) over S
 //
 // In the order in which one thread issues them, P_t V of a tile comes before the next S_t, so "S_t of tile j is there"
@@ -142,6 +142,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// two fp32 lanes in one instruction
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
+  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n mov.b64 c, {%5, %5};\n fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}"
+      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
+  asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n mov.b64 d, {%0, %1};\n add.rn.f32x2 d, d, a;\n mov.b64 {%0, %1}, d;\n}"
+      : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1));
+}
 // bits 0 .. n-1 of a word, n clamped to 0 .. 32
 __device__ __forceinline__ uint32_t ones_below(int n) {
   return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u);
@@ -201,7 +215,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   using S = Shape<D>;
   constexpr int SLOTS = S::SLOTS;
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) unsigned long long bars[2 + 2 + 2 * SLOTS + 8];
+  __shared__ __align__(8) unsigned long long bars[14 + 2 * SLOTS];
   __shared__ int prefix[MAX_SEQS + 1];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
@@ -215,14 +229,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };
   auto o_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };
   auto o_free = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };
-  auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(12 + s); };
-  auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(12 + SLOTS + s); };
+  auto p_part = [&](int t) { return b0 + 8u * (uint32_t)(12 + t); };
+  auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(14 + s); };
+  auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(14 + SLOTS + s); };
 
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full(t), 1);
       mbar_init(q_free(t), 1);
       mbar_init(s_full(t), 1);
+      mbar_init(p_part(t), 4);
       mbar_init(p_full(t), 4);
       mbar_init(o_full(t), 1);
       mbar_init(o_free(t), 4);
@@ -312,14 +328,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
               if (!((keep >> e) & 1u)) sr[32 * q + e] = 0xFF800000u;
           }
         }
-        float mx4[4];
+        float mx[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          mx4[q] = __uint_as_float(sr[q]);
+          mx[q] = fmaxf(__uint_as_float(sr[q]), __uint_as_float(sr[4 + q]));
 #pragma unroll
-          for (int e = 1; e < 32; ++e) mx4[q] = fmaxf(mx4[q], __uint_as_float(sr[4 * e + q]));
+          for (int e = 2; e < 32; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
         }
-        const float mn = fmaxf(m, fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])));
+        const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
         if (j == 0) {
           m = mn;
         } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
@@ -343,19 +359,22 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           uint32_t pk[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float a = exp2_fast(fmaf(__uint_as_float(sr[32 * q + 2 * e]), c, shift));
-            const float b = exp2_fast(fmaf(__uint_as_float(sr[32 * q + 2 * e + 1]), c, shift));
-            sum[e & 1] += a;
-            sum[2 + (e & 1)] += b;
+            float a, b;
+            fma2(a, b, __uint_as_float(sr[32 * q + 2 * e]), __uint_as_float(sr[32 * q + 2 * e + 1]), c, shift);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+            add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], a, b);
             pk[e] = pack_bf16(a, b);
           }
           tmem_store16(col_s + 16u * q, pk);
+          if (q >= 2) {                                   // the first 96 keys, then the rest
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q == 2 ? p_part(t) : p_full(t));
+          }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(t));
       }
       // ------------------------------------------- the item's result -------------------------------------------
       uint32_t o[D];
@@ -455,7 +474,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
     }
   } else if (warp == MMA_WARP) {
-    if (lane == 0) {
+    {
+      const uint32_t leader = elect_leader();       // (the whole warp runs this, one lane issues)
       constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
       constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
       constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
@@ -474,15 +494,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
 #pragma unroll
         for (uint32_t k = 0; k < D / 16; ++k) {
           const uint64_t step = (uint64_t)((k >> 2) * (ATOM >> 4) + 2 * (k & 3));
-          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0);
+          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0, leader);
         }
-        mma_commit(s_full(t));
+        mma_commit(s_full(t), leader);
       };
-      auto issue_o = [&](int t, uint32_t v_slot, bool first) {
+      constexpr uint32_t PART = 6;              // steps of 16 keys whose weights come first
+      auto issue_o = [&](int t, uint32_t v_slot, uint32_t from, uint32_t to, bool first) {
         const uint64_t b = smem_desc_mn(smem_kv + v_slot * S::TILE, ATOM, 1024);
 #pragma unroll
-        for (uint32_t k = 0; k < BN / 16; ++k)
-          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0));
+        for (uint32_t k = from; k < to; ++k)
+          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0), leader);
       };
       // the item whose S comes next runs one key tile ahead of the one whose O is accumulated
       int i = blockIdx.x;
@@ -505,9 +526,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
           tc_fence_after();
           issue_s(t, k_slot);
-          if (cur.tiles == 1) mma_commit(q_free(t));
+          if (cur.tiles == 1) mma_commit(q_free(t), leader);
         }
-        mma_commit(kv_free(k_slot));
+        mma_commit(kv_free(k_slot), leader);
       }
       while (have && !abort_flag) {
         Item nxt;
@@ -519,18 +540,22 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           uint32_t k_slot = 0;
           bool k_there = false;
           const bool two_now = cur.rows1 > 0, two_next = last ? (more && nxt.rows1 > 0) : two_now;
+#pragma unroll
           for (int t = 0; t < 2; ++t) {
             if (t == 0 || two_now) {
-              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
+              mbar_spin(p_part(t), p_use[t] & 1, &abort_flag, p.status, W_P);
               if (j == 0 && o_use[t] > 0) mbar_spin(o_free(t), (o_use[t] - 1) & 1, &abort_flag, p.status, W_OFREE);
               tc_fence_after();
-              issue_o(t, v_slot, j == 0);
+              issue_o(t, v_slot, 0, PART, j == 0);
+              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
+              tc_fence_after();
+              issue_o(t, v_slot, PART, BN / 16, false);
               if (last) {
-                mma_commit(o_full(t));
+                mma_commit(o_full(t), leader);
                 ++o_use[t];
               }
             }
-            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot));
+            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot), leader);
             if (ahead && (t == 0 || two_next)) {
               if (!k_there) {
                 k_slot = next_kv();
@@ -540,10 +565,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
               tc_fence_after();
               issue_s(t, k_slot);
               // the query tile is free once its last S is there
-              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t));
+              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t), leader);
             }
           }
-          if (k_there) mma_commit(kv_free(k_slot));
+          if (k_there) mma_commit(kv_free(k_slot), leader);
         }
         cur = nxt;
         have = more;
