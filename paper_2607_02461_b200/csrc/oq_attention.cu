@@ -11,17 +11,19 @@
 // the tensor cores' operand for the product with V (l sums the unrounded ones), which costs about as much as the one rounding of the
 // output.
 //
-// Bound: the tensor cores and the exponentials alike.  A tile of 128 queries x 128 keys takes 2 * 128^3 multiply-adds
-// for each of the two products at head_dim 128 and 16384 exponentials: both about 1000 cycles of an SM.  So a CTA
-// carries two query tiles in turn: while the tensor cores multiply for one, the other's threads exponentiate.
+// Bound: the tensor cores and the exponentials alike.  128 queries x 128 keys take 128^3 multiply-adds for each of the
+// two products at head_dim 128 and 16384 exponentials: both about 1000 cycles of an SM.  So a CTA carries two query
+// tiles, and neither the tensor cores nor the exponential units wait for a chain S -> softmax -> P V of one tile:
 //
-//   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of 128 keys through one ring of shared-memory slots
-//   mma warp                 S_t = Q_t K^T into tensor memory; O_t += P_t V with P_t from tensor memory
-//   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16) over S
+//   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of BN keys through one ring of shared-memory slots
+//   2 mma warps              one per query tile: S_t = Q_t K^T into tensor memory, one key tile ahead of
+//                            O_t += P_t V with P_t from tensor memory
+//   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16)
 //
-// In the order in which one thread issues them, P_t V of a tile comes before the next S_t, so "S_t of tile j is there"
-// also says that O_t holds the tiles before j: O can be rescaled without another wait, and P can lie over S.
-// Tensor memory: S_0 | S_1 | O_0 | O_1, 128 columns each.
+// S, P and O have columns of their own, so the next S is computed while the softmax of the present one still runs.
+// Of a tile's 256 columns O takes head_dim, which at 128 leaves room for S and P of 80 keys (80 + 40 columns).  Tiles
+// of 128 keys fit only with P laid over S, which chains S, softmax and P V of a tile one after the other: 3200 cycles for 2 x 128
+// queries x 128 keys where the tensor cores and the exponential units need 2048 each.
 //
 // NaN and infinities in keys and values that a row does not see must not reach it, but 0 * NaN is NaN: a row whose
 // result is not finite (checked once, at the end) is computed again key by key over what it sees.
@@ -35,24 +37,26 @@
 namespace oq {
 namespace attn {
 
-constexpr int THREADS = 384;              // 8 softmax warps; the load warp, the mma warp and two that only fill their group
-// Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S (128 values) and grow to
-// 208; the last group shrinks to 80: 256 * 208 + 128 * 80 = 63488.
+constexpr int THREADS = 384;              // 8 softmax warps; the load warp, two mma warps and one that only fills their group
+// Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S and grow to 208; the last
+// group shrinks to 80: 256 * 208 + 128 * 80 = 63488.
 constexpr int LOAD_WARP = 8, MMA_WARP = 9;
-constexpr int BM = 128, BN = 128;         // query rows of a tile, keys of a tile
+constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
 constexpr int MAX_SPLITS = 32;
 constexpr float SLACK = 8.f;              // powers stay below 2^8
-constexpr uint32_t ATOM = 128 * 128;      // 64 coordinates of 128 rows
-constexpr uint32_t COL_S = 0, COL_O = 256;
-enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46, W_OFREE = 47, W_DRAIN = 48 };
+enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_SFREE = 45, W_P = 46, W_O = 47 };
 
 template <int D>
 struct Shape {
+  static constexpr int BN = D == 128 ? 80 : 128;                  // keys of a tile
   static constexpr uint32_t ATOMS = D / 64;
-  static constexpr uint32_t TILE = ATOMS * ATOM;
-  static constexpr int SLOTS = D == 128 ? 5 : 8;
-  static constexpr uint32_t SMEM = 1024 + 2 * TILE + SLOTS * TILE;
+  static constexpr uint32_t Q_ATOM = BM * 128, KV_ATOM = BN * 128;      // 64 coordinates of all rows, 128 bytes each
+  static constexpr uint32_t Q_TILE = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
+  static constexpr int SLOTS = 8;
+  static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE;
+  static constexpr uint32_t COL_S = 0, COL_P = BN, COL_O = 256 - D;     // columns of a query tile's 256
+  static_assert(BN + BN / 2 <= 256 - D, "S and P beside O");
 };
 
 struct Params {
@@ -71,6 +75,7 @@ struct Params {
 };
 
 // What one CTA works on at a time: up to 256 queries of one head, and a run of their key tiles.
+template <int BN>
 struct Item {
   int q_base, k_base;      // first query and key of the sequence
   int nq, nk;
@@ -85,16 +90,19 @@ struct Item {
   }
 };
 
-__device__ __forceinline__ int row_hi(const Params& p, const Item& it, int qi) {       // last visible key
+template <int BN>
+__device__ __forceinline__ int row_hi(const Params& p, const Item<BN>& it, int qi) {       // last visible key
   return p.right < 0 ? it.nk - 1 : min(it.nk - 1, qi + it.nk - it.nq + p.right);
 }
-__device__ __forceinline__ int row_lo(const Params& p, const Item& it, int qi) {       // first key of the window
+template <int BN>
+__device__ __forceinline__ int row_lo(const Params& p, const Item<BN>& it, int qi) {       // first key of the window
   return p.left < 0 ? 0 : max(0, qi + it.nk - it.nq - p.left);
 }
 
 // prefix[s]: blocks of 256 queries before sequence s
-__device__ __forceinline__ Item make_item(const Params& p, const int* prefix, int index) {
-  Item it;
+template <int BN>
+__device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix, int index) {
+  Item<BN> it;
   it.split = index % p.splits;
   index /= p.splits;
   const int blocks = prefix[p.n_seqs];
@@ -163,7 +171,8 @@ __device__ __forceinline__ uint32_t ones_below(int n) {
 
 // One row again, key by key over the keys it sees, by a whole warp (each lane holds D / 32 coordinates).
 template <int D>
-__device__ __noinline__ void exact_row(const Params& p, const Item& it, int qi) {
+__device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>& it, int qi) {
+  constexpr int BN = Shape<D>::BN;
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 31, hk = it.head / p.group;
   const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
@@ -213,39 +222,37 @@ template <int D>
 __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ Params p) {
   using S = Shape<D>;
-  constexpr int SLOTS = S::SLOTS;
+  constexpr int SLOTS = S::SLOTS, BN = S::BN;
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) unsigned long long bars[14 + 2 * SLOTS];
+  __shared__ __align__(8) unsigned long long bars[12 + 2 * SLOTS];
   __shared__ int prefix[MAX_SEQS + 1];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-  const uint32_t smem_q = smem, smem_kv = smem + 2 * S::TILE;
+  const uint32_t smem_q = smem, smem_kv = smem + 2 * S::Q_TILE;
   const uint32_t b0 = smem_u32(bars);
   auto q_full = [&](int t) { return b0 + 8u * (uint32_t)t; };
   auto q_free = [&](int t) { return b0 + 8u * (uint32_t)(2 + t); };
   auto s_full = [&](int t) { return b0 + 8u * (uint32_t)(4 + t); };
-  auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };
-  auto o_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };
-  auto o_free = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };
-  auto p_part = [&](int t) { return b0 + 8u * (uint32_t)(12 + t); };
-  auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(14 + s); };
-  auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(14 + SLOTS + s); };
+  auto s_free = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };     // S has been read into registers
+  auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };     // P is there (and O rescaled, and read at an item's end)
+  auto o_done = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };    // P V has been added: P is free, O may be read
+  auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(12 + s); };
+  auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(12 + SLOTS + s); };
 
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full(t), 1);
       mbar_init(q_free(t), 1);
       mbar_init(s_full(t), 1);
-      mbar_init(p_part(t), 4);
+      mbar_init(s_free(t), 4);
       mbar_init(p_full(t), 4);
-      mbar_init(o_full(t), 1);
-      mbar_init(o_free(t), 4);
+      mbar_init(o_done(t), 1);
     }
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(kv_full(s), 1);
-      mbar_init(kv_free(s), 1);
+      mbar_init(kv_free(s), 2);           // both mma warps
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -287,45 +294,78 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int n_items = prefix[p.n_seqs] * p.heads * p.splits;
+  // All roles walk over the same steps: the key tiles of this CTA's items, one after the other.
+  struct Step {
+    Item<BN> it;
+    int index, j;          // the item's number; the key tile inside it
+  };
+  auto first_from = [&](Step& s, int index) {        // the first step of the first item from `index` on that has a key tile
+    for (; index < n_items; index += gridDim.x) {
+      s.it = make_item<BN>(p, prefix, index);
+      if (s.it.tiles > 0) {
+        s.index = index;
+        s.j = 0;
+        return true;
+      }
+    }
+    return false;
+  };
+  auto next_step = [&](Step& s) {
+    if (++s.j < s.it.tiles) return true;
+    return first_from(s, s.index + (int)gridDim.x);
+  };
 
   if (warp < LOAD_WARP) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------ softmax ------------------------------------------------
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t col_s = tmem + lane_base + COL_S + 128u * (uint32_t)t, col_o = tmem + lane_base + COL_O + 128u * (uint32_t)t;
+    const uint32_t columns = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256u * (uint32_t)t;
+    const uint32_t col_s = columns + S::COL_S, col_p = columns + S::COL_P, col_o = columns + S::COL_O;
     const float c = p.scale_log2;
-    uint32_t s_use = 0, o_use = 0;
+    uint32_t steps = 0;                         // of this tile so far
     auto warp_wait = [&](uint32_t bar, uint32_t parity, int code) {
       mbar_spin(bar, parity, &abort_flag, p.status, code);
       __syncwarp();
     };
     for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
-      const Item it = make_item(p, prefix, i);
+      const Item<BN> it = make_item<BN>(p, prefix, i);
       const int rows = t ? it.rows1 : it.rows0;
       if (rows == 0) continue;
       const int r0 = it.q0 + t * BM, qi = r0 + row;
-      const bool mine = row < rows;
+      const bool mine = row < rows, idle = (warp & 3) * 32 >= rows;      // idle: none of the warp's rows exists
       const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
       const int full_hi = row_hi(p, it, r0), full_lo = row_lo(p, it, r0 + rows - 1);     // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < it.tiles && !abort_flag; ++j) {
+      for (int j = 0; j < it.tiles && !abort_flag; ++j, ++steps) {
         const int k0 = it.key0(j);
-        warp_wait(s_full(t), s_use++ & 1, W_S);
+        warp_wait(s_full(t), steps & 1, W_S);
+        if (idle) {                             // (O's rows are never read: whatever P holds there may stay)
+          if (lane == 0) mbar_arrive(s_free(t));
+          // (a warp arrives for a tile only when the one before it is through: else two arrivals of this warp could
+          // stand for one of a slower warp)
+          if (steps > 0) warp_wait(o_done(t), (steps - 1) & 1, W_O);
+          if (lane == 0) mbar_arrive(p_full(t));
+          continue;
+        }
         tc_fence_after();
-        uint32_t sr[128];
+        uint32_t sr[BN];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_load32_nowait(col_s + 32u * q, sr + 32 * q);
+        for (int q = 0; q < BN / 32; ++q) tmem_load32_nowait(col_s + 32u * q, sr + 32 * q);
+        if (BN % 32) tmem_load16_at(col_s + BN - 16u, sr + BN - 16);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_use32(sr + 32 * q);
+        for (int q = 0; q < BN / 32; ++q) tmem_use32(sr + 32 * q);
+        if (BN % 32) tmem_use16(sr + BN - 16);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free(t));
         if (!(k0 + BN - 1 <= full_hi && (k0 >= full_lo || k0 + BN <= p.sinks))) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int b = k0 + 32 * q;
+          for (int q = 0; q < BN / 16; ++q) {
+            const int b = k0 + 16 * q;
             const uint32_t keep = ones_below(hi + 1 - b) & (~ones_below(lo - b) | ones_below(p.sinks - b));
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!((keep >> e) & 1u)) sr[32 * q + e] = 0xFF800000u;
+            for (int e = 0; e < 16; ++e)
+              if (!((keep >> e) & 1u)) sr[16 * q + e] = 0xFF800000u;
           }
         }
         float mx[4];
@@ -333,68 +373,71 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         for (int q = 0; q < 4; ++q) {
           mx[q] = fmaxf(__uint_as_float(sr[q]), __uint_as_float(sr[4 + q]));
 #pragma unroll
-          for (int e = 2; e < 32; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
+          for (int e = 2; e < BN / 4; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
         }
         const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
-        if (j == 0) {
-          m = mn;
-        } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
-          // (S_t of tile j is there, so O_t holds the tiles before j and nothing is writing it)
-          const float a = m == mn ? 1.f : exp2_fast((m - mn) * c);
+        const bool move = j > 0 && __any_sync(~0u, (mn - m) * c > SLACK);
+        float a = 1.f;
+        if (j == 0) m = mn;
+        if (move) {
+          a = m == mn ? 1.f : exp2_fast((m - mn) * c);
           m = mn;
           l *= a;
-#pragma unroll
-          for (int q = 0; q < D / 32; ++q) {
-            uint32_t o[32];
-            tmem_load32(col_o + 32u * q, o);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
-            tmem_store32(col_o + 32u * q, o);
-          }
         }
         const float shift = m == -INFINITY ? 0.f : -m * c;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t pk[16];
+        for (int q = 0; q < BN / 16; ++q) {
+          uint32_t pk[8];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float a, b;
-            fma2(a, b, __uint_as_float(sr[32 * q + 2 * e]), __uint_as_float(sr[32 * q + 2 * e + 1]), c, shift);
-            a = exp2_fast(a);
-            b = exp2_fast(b);
-            add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], a, b);
-            pk[e] = pack_bf16(a, b);
+          for (int e = 0; e < 8; ++e) {
+            float x, y;
+            fma2(x, y, __uint_as_float(sr[16 * q + 2 * e]), __uint_as_float(sr[16 * q + 2 * e + 1]), c, shift);
+            x = exp2_fast(x);
+            y = exp2_fast(y);
+            add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], x, y);
+            pk[e] = pack_bf16(x, y);
           }
-          tmem_store16(col_s + 16u * q, pk);
-          if (q >= 2) {                                   // the first 96 keys, then the rest
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(q == 2 ? p_part(t) : p_full(t));
+          if (q == 0 && steps > 0) {            // the tile before has been added: its P may be overwritten, and O rescaled
+            warp_wait(o_done(t), (steps - 1) & 1, W_O);
+            tc_fence_after();
+            if (move) {
+#pragma unroll 1
+              for (int x = 0; x < D / 16; ++x) {
+                uint32_t o[16];
+                tmem_load16_at(col_o + 16u * x, o);
+                tmem_use16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+                tmem_store16(col_o + 16u * x, o);
+              }
+            }
           }
+          tmem_store8(col_p + 8u * q, pk);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(t));
       }
       // ------------------------------------------- the item's result -------------------------------------------
+      if (it.tiles > 0) warp_wait(o_done(t), (steps - 1) & 1, W_O);
+      if (idle) continue;
       uint32_t o[D];
-      const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
-      float nan_probe = 0.f;
       if (it.tiles > 0) {
-        warp_wait(o_full(t), o_use++ & 1, W_O);
         tc_fence_after();
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) tmem_load32_nowait(col_o + 32u * q, o + 32 * q);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) tmem_use32(o + 32 * q);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_free(t));
+        tc_fence_before();                      // (the next item's first P, which lets O be overwritten, comes after this)
       } else {
 #pragma unroll
         for (int e = 0; e < D; ++e) o[e] = 0u;
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
+      float nan_probe = 0.f;
 #pragma unroll
       for (int e = 0; e < D; ++e) {
         const float v = __uint_as_float(o[e]) * inv;
@@ -403,6 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       }
       const bool bad = mine && !(nan_probe == 0.f);
       const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c, log2f(l));
+      const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
       if (mine && !bad) {
         if (p.splits > 1) {
           const long long at = (long long)it.split * p.heads * p.total_q + out_row;
@@ -433,148 +477,110 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       }
     }
   } else {
-   asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-   if (warp == LOAD_WARP) {
-    if (lane == 0) {
-      uint32_t slot = 0, round = 0, q_use[2] = {0, 0};
-      auto load_q = [&](const Item& it, int t) {
-        if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
-        ++q_use[t];
-        mbar_expect_tx(q_full(t), S::TILE);
-        for (uint32_t a = 0; a < S::ATOMS; ++a)
-          tma_load_3d(smem_q + (uint32_t)t * S::TILE + a * ATOM, &map_q, 64 * (int)a, it.head, it.q_base + it.q0 + t * BM, q_full(t));
-      };
-      auto load_kv = [&](const Item& it, const CUtensorMap* map, int key0) {
-        if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
-        mbar_expect_tx(kv_full(slot), S::TILE);
-        for (uint32_t a = 0; a < S::ATOMS; ++a)
-          tma_load_3d(smem_kv + slot * S::TILE + a * ATOM, map, 64 * (int)a, it.head / p.group, it.k_base + key0, kv_full(slot));
-        if (++slot == SLOTS) {
-          slot = 0;
-          ++round;
-        }
-      };
-      for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
-        const Item it = make_item(p, prefix, i);
-        if (it.tiles == 0) continue;
-        load_q(it, 0);
-        load_kv(it, &map_k, it.key0(0));
-        if (it.rows1 > 0) load_q(it, 1);
-        for (int j = 0; j < it.tiles && !abort_flag; ++j) {
-          load_kv(it, &map_v, it.key0(j));
-          if (j + 1 < it.tiles) load_kv(it, &map_k, it.key0(j + 1));
-        }
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    uint32_t slot = 0, round = 0;               // position in the ring, the same sequence in all three warps
+    auto advance = [&]() {
+      if (++slot == SLOTS) {
+        slot = 0;
+        ++round;
       }
-      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
-      for (uint32_t s = 0; s < SLOTS; ++s) {
-        const uint32_t fills = round + (s < slot ? 1u : 0u);
-        for (int n = 0; fills > 0 && n < (1 << 20) && !mbar_try(kv_full((int)s), (fills - 1) & 1); ++n) {}
+    };
+    if (warp == LOAD_WARP) {
+      if (lane == 0) {
+        uint32_t q_use[2] = {0, 0};
+        auto load_kv = [&](const Step& s, const CUtensorMap* map) {
+          if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
+          mbar_expect_tx(kv_full(slot), S::KV_TILE);
+          for (uint32_t a = 0; a < S::ATOMS; ++a)
+            tma_load_3d(smem_kv + slot * S::KV_TILE + a * S::KV_ATOM, map, 64 * (int)a, s.it.head / p.group, s.it.k_base + s.it.key0(s.j), kv_full(slot));
+          advance();
+        };
+        auto load_k = [&](const Step& s) {
+          if (s.j == 0) {
+            for (int t = 0; t < (s.it.rows1 > 0 ? 2 : 1); ++t) {
+              if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
+              ++q_use[t];
+              mbar_expect_tx(q_full(t), S::Q_TILE);
+              for (uint32_t a = 0; a < S::ATOMS; ++a)
+                tma_load_3d(smem_q + (uint32_t)t * S::Q_TILE + a * S::Q_ATOM, &map_q, 64 * (int)a, s.it.head, s.it.q_base + s.it.q0 + t * BM, q_full(t));
+            }
+          }
+          load_kv(s, &map_k);
+        };
+        Step now, ahead;
+        bool have = first_from(now, blockIdx.x);
+        if (have) load_k(now);
+        while (have && !abort_flag) {
+          ahead = now;
+          have = next_step(ahead);
+          if (have) load_k(ahead);
+          load_kv(now, &map_v);
+          now = ahead;
+        }
+        // copies still in flight end before the CTA does (after an abort nobody else waits for them)
+        for (uint32_t s = 0; s < SLOTS; ++s) {
+          const uint32_t fills = round + (s < slot ? 1u : 0u);
+          for (int n = 0; fills > 0 && n < (1 << 20) && !mbar_try(kv_full((int)s), (fills - 1) & 1); ++n) {}
+        }
+        for (int t = 0; t < 2; ++t)
+          for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
       }
-      for (int t = 0; t < 2; ++t)
-        for (int n = 0; q_use[t] > 0 && n < (1 << 20) && !mbar_try(q_full(t), (q_use[t] - 1) & 1); ++n) {}
-    }
-  } else if (warp == MMA_WARP) {
-    {
+    } else if (warp < MMA_WARP + 2) {
+      const int t = warp - MMA_WARP;
       const uint32_t leader = elect_leader();       // (the whole warp runs this, one lane issues)
       constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
       constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
       constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
-      uint32_t slot = 0, round = 0, q_use[2] = {0, 0}, p_use[2] = {0, 0}, o_use[2] = {0, 0};
-      auto next_kv = [&]() {
+      const uint32_t columns = tmem + 256u * (uint32_t)t;
+      uint32_t q_use = 0, s_use = 0, p_use = 0;
+      auto active = [&](const Step& s) { return t == 0 || s.it.rows1 > 0; };
+      auto do_s = [&](const Step& s) {
         mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
-        const uint32_t s = slot;
-        if (++slot == SLOTS) {
-          slot = 0;
-          ++round;
-        }
-        return s;
-      };
-      auto issue_s = [&](int t, uint32_t k_slot) {
-        const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::TILE), b = smem_desc(smem_kv + k_slot * S::TILE);
-#pragma unroll
-        for (uint32_t k = 0; k < D / 16; ++k) {
-          const uint64_t step = (uint64_t)((k >> 2) * (ATOM >> 4) + 2 * (k & 3));
-          mma_ss(tmem + COL_S + 128u * t, a + step, b + step, IDESC_S, k > 0, leader);
-        }
-        mma_commit(s_full(t), leader);
-      };
-      constexpr uint32_t PART = 6;              // steps of 16 keys whose weights come first
-      auto issue_o = [&](int t, uint32_t v_slot, uint32_t from, uint32_t to, bool first) {
-        const uint64_t b = smem_desc_mn(smem_kv + v_slot * S::TILE, ATOM, 1024);
-#pragma unroll
-        for (uint32_t k = from; k < to; ++k)
-          mma_ts(tmem + COL_O + 128u * t, tmem + COL_S + 128u * t + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, !(first && k == 0), leader);
-      };
-      // the item whose S comes next runs one key tile ahead of the one whose O is accumulated
-      int i = blockIdx.x;
-      Item cur;
-      cur.tiles = 0;
-      auto next_item = [&](Item& it) {
-        for (; i < n_items; i += gridDim.x) {
-          it = make_item(p, prefix, i);
-          if (it.tiles > 0) {
-            i += gridDim.x;
-            return true;
-          }
-        }
-        return false;
-      };
-      bool have = next_item(cur);
-      if (have) {
-        const uint32_t k_slot = next_kv();
-        for (int t = 0; t < (cur.rows1 > 0 ? 2 : 1); ++t) {
-          mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
+        if (active(s)) {
+          if (s.j == 0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q);
+          if (s_use > 0) mbar_spin(s_free(t), (s_use - 1) & 1, &abort_flag, p.status, W_SFREE);
+          ++s_use;
           tc_fence_after();
-          issue_s(t, k_slot);
-          if (cur.tiles == 1) mma_commit(q_free(t), leader);
-        }
-        mma_commit(kv_free(k_slot), leader);
-      }
-      while (have && !abort_flag) {
-        Item nxt;
-        const bool more = next_item(nxt);
-        for (int j = 0; j < cur.tiles && !abort_flag; ++j) {
-          const bool last = j + 1 == cur.tiles;
-          const bool ahead = !last || more;            // a tile whose S is to be issued
-          const uint32_t v_slot = next_kv();
-          uint32_t k_slot = 0;
-          bool k_there = false;
-          const bool two_now = cur.rows1 > 0, two_next = last ? (more && nxt.rows1 > 0) : two_now;
+          const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::Q_TILE), b = smem_desc(smem_kv + slot * S::KV_TILE);
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (t == 0 || two_now) {
-              mbar_spin(p_part(t), p_use[t] & 1, &abort_flag, p.status, W_P);
-              if (j == 0 && o_use[t] > 0) mbar_spin(o_free(t), (o_use[t] - 1) & 1, &abort_flag, p.status, W_OFREE);
-              tc_fence_after();
-              issue_o(t, v_slot, 0, PART, j == 0);
-              mbar_spin(p_full(t), p_use[t]++ & 1, &abort_flag, p.status, W_P);
-              tc_fence_after();
-              issue_o(t, v_slot, PART, BN / 16, false);
-              if (last) {
-                mma_commit(o_full(t), leader);
-                ++o_use[t];
-              }
-            }
-            if (t == (two_now ? 1 : 0)) mma_commit(kv_free(v_slot), leader);
-            if (ahead && (t == 0 || two_next)) {
-              if (!k_there) {
-                k_slot = next_kv();
-                k_there = true;
-              }
-              if (last) mbar_spin(q_full(t), q_use[t]++ & 1, &abort_flag, p.status, W_Q);
-              tc_fence_after();
-              issue_s(t, k_slot);
-              // the query tile is free once its last S is there
-              if (last ? nxt.tiles == 1 : j + 2 == cur.tiles) mma_commit(q_free(t), leader);
-            }
-          }
-          if (k_there) mma_commit(kv_free(k_slot), leader);
+          for (uint32_t k = 0; k < D / 16; ++k)
+            mma_ss(columns + S::COL_S, a + (uint64_t)((k >> 2) * (S::Q_ATOM >> 4) + 2 * (k & 3)), b + (uint64_t)((k >> 2) * (S::KV_ATOM >> 4) + 2 * (k & 3)),
+                   IDESC_S, k > 0, leader);
+          mma_commit(s_full(t), leader);
+          mma_commit(kv_free(slot), leader);
+          if (s.j + 1 == s.it.tiles) mma_commit(q_free(t), leader);       // the query tile's last S
+        } else if (leader) {
+          mbar_arrive(kv_free(slot));
         }
-        cur = nxt;
-        have = more;
+        advance();
+      };
+      auto do_o = [&](const Step& s) {
+        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
+        if (active(s)) {
+          mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P);
+          tc_fence_after();
+          const uint64_t b = smem_desc_mn(smem_kv + slot * S::KV_TILE, S::KV_ATOM, 1024);
+#pragma unroll
+          for (uint32_t k = 0; k < BN / 16; ++k)
+            mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > 0 || k > 0, leader);
+          mma_commit(o_done(t), leader);
+          mma_commit(kv_free(slot), leader);
+        } else if (leader) {
+          mbar_arrive(kv_free(slot));
+        }
+        advance();
+      };
+      Step now, ahead;
+      bool have = first_from(now, blockIdx.x);
+      if (have) do_s(now);
+      while (have && !abort_flag) {
+        ahead = now;
+        have = next_step(ahead);
+        if (have) do_s(ahead);
+        do_o(now);
+        now = ahead;
       }
     }
-   }
   }
   tc_fence_before();
   __syncthreads();
@@ -635,7 +641,7 @@ int choose_splits(long long total_q, long long total_k, int n_seqs, int heads, i
     const long long window = (long long)left + right + 2 * BM + sinks;
     if (window < keys) keys = window;
   }
-  const long long tiles = (keys + BN - 1) / BN;
+  const long long tiles = (keys + 99) / 100;            // (80 or 128 keys each)
   if (items >= 2LL * sms) return 1;
   int best = 1;
   double best_cost = 1e30;
@@ -738,16 +744,17 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.status = device_status_word();
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_attention: cannot allocate the device status word");
   CUtensorMap mq, mk, mv;
-  auto make_map = [&](CUtensorMap* map, const void* base, int heads, long long tokens, long long ld, long long hd) {
+  auto make_map = [&](CUtensorMap* map, const void* base, int heads, long long tokens, long long ld, long long hd, int rows) {
     const uint64_t dims[3] = {(uint64_t)a->head_dim, (uint64_t)heads, (uint64_t)tokens};
     // a stride that is never used (one head, one token) still has to be one that the encoder takes
     const uint64_t strides[2] = {(uint64_t)(heads > 1 && hd > 0 ? hd : a->head_dim) * 2, (uint64_t)(tokens > 1 && ld > 0 ? ld : (long long)a->head_dim * heads) * 2};
-    const uint32_t box[3] = {64, 1, 128};
+    const uint32_t box[3] = {64, 1, (uint32_t)rows};
     return encode_tensor_map_sw128(map, base, false, 3, dims, strides, box);
   };
-  cudaError_t e = make_map(&mq, a->Q, a->n_heads, a->total_q, a->ldq_token, a->ldq_head);
-  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head);
-  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mv, a->V, a->n_kv_heads, a->total_k, a->ldv_token, a->ldv_head);
+  const int keys = a->head_dim == 128 ? attn::Shape<128>::BN : attn::Shape<64>::BN;
+  cudaError_t e = make_map(&mq, a->Q, a->n_heads, a->total_q, a->ldq_token, a->ldq_head, attn::BM);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head, keys);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mv, a->V, a->n_kv_heads, a->total_k, a->ldv_token, a->ldv_head, keys);
   if (e != cudaSuccess) return cuda_fail(e, "oq_attention (tensor map)");
   if (a->total_k == 0) mk = mv = mq;               // no key tile is ever loaded
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
