@@ -13,17 +13,14 @@
 //
 // Bound: the tensor cores and the exponentials alike.  128 queries x 128 keys take 128^3 multiply-adds for each of the
 // two products at head_dim 128 and 16384 exponentials: both about 1000 cycles of an SM.  So a CTA carries two query
-// tiles, and neither the tensor cores nor the exponential units wait for a chain S -> softmax -> P V of one tile:
+// tiles: while the tensor cores multiply for one, the threads of the other exponentiate.
 //
-//   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of BN keys through one ring of shared-memory slots
-//   2 mma warps              one per query tile: S_t = Q_t K^T into tensor memory, one key tile ahead of
-//                            O_t += P_t V with P_t from tensor memory
-//   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16)
+//   load warp   (1 thread)   TMA: Q tiles, then K and V tiles of 128 keys through one ring of shared-memory slots
+//   2 mma warps              one per query tile: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t from tensor memory
+//   2 x 4 warps              one thread per query row: S from tensor memory, mask, maximum, powers, P (bf16) over S
 //
-// S, P and O have columns of their own, so the next S is computed while the softmax of the present one still runs.
-// Of a tile's 256 columns O takes head_dim, which at 128 leaves room for S and P of 80 keys (80 + 40 columns).  Tiles
-// of 128 keys fit only with P laid over S, which chains S, softmax and P V of a tile one after the other: 3200 cycles for 2 x 128
-// queries x 128 keys where the tensor cores and the exponential units need 2048 each.
+// Of a tile's 256 columns of tensor memory S has 128, over which P lies, and O the rest.  The mma warp issues P_t V of a
+// key tile before the next S_t, so "S_t is there" also says that O_t holds the tiles before it.
 //
 // NaN and infinities in keys and values that a row does not see must not reach it, but 0 * NaN is NaN: a row whose
 // result is not finite (checked once, at the end) is computed again key by key over what it sees.
@@ -45,18 +42,17 @@ constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
 constexpr int MAX_SPLITS = 32;
 constexpr float SLACK = 8.f;              // powers stay below 2^8
-enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_SFREE = 45, W_P = 46, W_O = 47 };
+enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46 };
 
 template <int D>
 struct Shape {
-  static constexpr int BN = D == 128 ? 80 : 128;                  // keys of a tile
+  static constexpr int BN = 128;                                  // keys of a tile
   static constexpr uint32_t ATOMS = D / 64;
   static constexpr uint32_t Q_ATOM = BM * 128, KV_ATOM = BN * 128;      // 64 coordinates of all rows, 128 bytes each
   static constexpr uint32_t Q_TILE = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
-  static constexpr int SLOTS = 8;
+  static constexpr int SLOTS = D == 128 ? 5 : 8;
   static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE;
-  static constexpr uint32_t COL_S = 0, COL_P = BN, COL_O = 256 - D;     // columns of a query tile's 256
-  static_assert(BN + BN / 2 <= 256 - D, "S and P beside O");
+  static constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;           // columns of a query tile's 256: P lies over S
 };
 
 struct Params {
@@ -235,9 +231,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   auto q_full = [&](int t) { return b0 + 8u * (uint32_t)t; };
   auto q_free = [&](int t) { return b0 + 8u * (uint32_t)(2 + t); };
   auto s_full = [&](int t) { return b0 + 8u * (uint32_t)(4 + t); };
-  auto s_free = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };     // S has been read into registers
-  auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };     // P is there (and O rescaled, and read at an item's end)
-  auto o_done = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };    // P V has been added: P is free, O may be read
+  auto p_part = [&](int t) { return b0 + 8u * (uint32_t)(6 + t); };     // P of the first 96 keys is there (and O rescaled, and read at an item's end)
+  auto p_full = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };     // all of P is there
+  auto o_done = [&](int t) { return b0 + 8u * (uint32_t)(10 + t); };    // the item's last P V has been added: O may be read
   auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(12 + s); };
   auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(12 + SLOTS + s); };
 
@@ -246,7 +242,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       mbar_init(q_full(t), 1);
       mbar_init(q_free(t), 1);
       mbar_init(s_full(t), 1);
-      mbar_init(s_free(t), 4);
+      mbar_init(p_part(t), 4);
       mbar_init(p_full(t), 4);
       mbar_init(o_done(t), 1);
     }
@@ -322,12 +318,18 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     const uint32_t columns = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256u * (uint32_t)t;
     const uint32_t col_s = columns + S::COL_S, col_p = columns + S::COL_P, col_o = columns + S::COL_O;
     const float c = p.scale_log2;
-    uint32_t steps = 0;                         // of this tile so far
+    uint32_t steps = 0, items = 0;              // of this tile so far
     auto warp_wait = [&](uint32_t bar, uint32_t parity, int code) {
       mbar_spin(bar, parity, &abort_flag, p.status, code);
       __syncwarp();
     };
-    for (int i = blockIdx.x; i < n_items && !abort_flag; i += gridDim.x) {
+    // Warp w of tile 0 and of tile 1 sit on the same scheduler.  They take turns: left alone they run in step, fight for the
+    // exponential unit and then leave it idle together.  (The turns are counted, so no warp leaves its loops early, not
+    // even when a wait has given up.)
+    const int quarter = warp & 3;
+    auto turn_wait = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + 2 * quarter + t) : "memory"); };
+    auto turn_pass = [&]() { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 2 * quarter - t) : "memory"); };
+    for (int i = blockIdx.x; i < n_items; i += gridDim.x) {
       const Item<BN> it = make_item<BN>(p, prefix, i);
       const int rows = t ? it.rows1 : it.rows0;
       if (rows == 0) continue;
@@ -336,15 +338,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
       const int full_hi = row_hi(p, it, r0), full_lo = row_lo(p, it, r0 + rows - 1);     // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < it.tiles && !abort_flag; ++j, ++steps) {
+      const bool turns = it.rows1 > quarter * 32;       // both warps have rows (tile 0 is full where tile 1 has any)
+      for (int j = 0; j < it.tiles; ++j, ++steps) {
         const int k0 = it.key0(j);
         warp_wait(s_full(t), steps & 1, W_S);
         if (idle) {                             // (O's rows are never read: whatever P holds there may stay)
-          if (lane == 0) mbar_arrive(s_free(t));
-          // (a warp arrives for a tile only when the one before it is through: else two arrivals of this warp could
-          // stand for one of a slower warp)
-          if (steps > 0) warp_wait(o_done(t), (steps - 1) & 1, W_O);
-          if (lane == 0) mbar_arrive(p_full(t));
+          if (lane == 0) {
+            mbar_arrive(p_part(t));
+            mbar_arrive(p_full(t));
+          }
           continue;
         }
         tc_fence_after();
@@ -355,9 +357,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
 #pragma unroll
         for (int q = 0; q < BN / 32; ++q) tmem_use32(sr + 32 * q);
         if (BN % 32) tmem_use16(sr + BN - 16);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(s_free(t));
         if (!(k0 + BN - 1 <= full_hi && (k0 >= full_lo || k0 + BN <= p.sinks))) {
 #pragma unroll
           for (int q = 0; q < BN / 16; ++q) {
@@ -376,53 +375,52 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           for (int e = 2; e < BN / 4; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
         }
         const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
-        const bool move = j > 0 && __any_sync(~0u, (mn - m) * c > SLACK);
-        float a = 1.f;
-        if (j == 0) m = mn;
-        if (move) {
-          a = m == mn ? 1.f : exp2_fast((m - mn) * c);
+        if (j == 0) {
+          m = mn;
+        } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
+          // (S_t of this key tile is there, so O_t holds the tiles before it and nothing is writing it)
+          const float a = m == mn ? 1.f : exp2_fast((m - mn) * c);
           m = mn;
           l *= a;
+#pragma unroll 1
+          for (int x = 0; x < D / 16; ++x) {
+            uint32_t o[16];
+            tmem_load16_at(col_o + 16u * x, o);
+            tmem_use16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+            tmem_store16(col_o + 16u * x, o);
+          }
         }
         const float shift = m == -INFINITY ? 0.f : -m * c;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // one warp of the two that share a scheduler exponentiates while the other does all else
+        if (turns && (t == 1 || j > 0)) turn_wait();
 #pragma unroll
-        for (int q = 0; q < BN / 16; ++q) {
-          uint32_t pk[8];
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
+          for (int e = 0; e < 16; ++e) {
             float x, y;
-            fma2(x, y, __uint_as_float(sr[16 * q + 2 * e]), __uint_as_float(sr[16 * q + 2 * e + 1]), c, shift);
+            fma2(x, y, __uint_as_float(sr[32 * q + 2 * e]), __uint_as_float(sr[32 * q + 2 * e + 1]), c, shift);
             x = exp2_fast(x);
             y = exp2_fast(y);
             add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], x, y);
             pk[e] = pack_bf16(x, y);
           }
-          if (q == 0 && steps > 0) {            // the tile before has been added: its P may be overwritten, and O rescaled
-            warp_wait(o_done(t), (steps - 1) & 1, W_O);
-            tc_fence_after();
-            if (move) {
-#pragma unroll 1
-              for (int x = 0; x < D / 16; ++x) {
-                uint32_t o[16];
-                tmem_load16_at(col_o + 16u * x, o);
-                tmem_use16(o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
-                tmem_store16(col_o + 16u * x, o);
-              }
-            }
+          if (q == 3 && turns && (t == 0 || j + 1 < it.tiles)) turn_pass();
+          tmem_store16(col_p + 16u * q, pk);
+          if (q >= 2) {                                   // the first 96 keys, then the rest
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q == 2 ? p_part(t) : p_full(t));
           }
-          tmem_store8(col_p + 8u * q, pk);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(t));
       }
       // ------------------------------------------- the item's result -------------------------------------------
-      if (it.tiles > 0) warp_wait(o_done(t), (steps - 1) & 1, W_O);
+      if (it.tiles > 0) warp_wait(o_done(t), items++ & 1, W_O);
       if (idle) continue;
       uint32_t o[D];
       if (it.tiles > 0) {
@@ -513,8 +511,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         while (have && !abort_flag) {
           ahead = now;
           have = next_step(ahead);
-          if (have) load_k(ahead);
           load_kv(now, &map_v);
+          if (have) load_k(ahead);
           now = ahead;
         }
         // copies still in flight end before the CTA does (after an abort nobody else waits for them)
@@ -532,14 +530,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
       constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
       const uint32_t columns = tmem + 256u * (uint32_t)t;
-      uint32_t q_use = 0, s_use = 0, p_use = 0;
+      uint32_t q_use = 0, p_use = 0;
       auto active = [&](const Step& s) { return t == 0 || s.it.rows1 > 0; };
       auto do_s = [&](const Step& s) {
         mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
         if (active(s)) {
           if (s.j == 0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q);
-          if (s_use > 0) mbar_spin(s_free(t), (s_use - 1) & 1, &abort_flag, p.status, W_SFREE);
-          ++s_use;
           tc_fence_after();
           const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::Q_TILE), b = smem_desc(smem_kv + slot * S::KV_TILE);
 #pragma unroll
@@ -557,13 +553,18 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       auto do_o = [&](const Step& s) {
         mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
         if (active(s)) {
-          mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P);
+          mbar_spin(p_part(t), p_use & 1, &abort_flag, p.status, W_P);
           tc_fence_after();
           const uint64_t b = smem_desc_mn(smem_kv + slot * S::KV_TILE, S::KV_ATOM, 1024);
 #pragma unroll
-          for (uint32_t k = 0; k < BN / 16; ++k)
+          for (uint32_t k = 0; k < BN / 16; ++k) {
+            if (k == 6) {
+              mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P);
+              tc_fence_after();
+            }
             mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > 0 || k > 0, leader);
-          mma_commit(o_done(t), leader);
+          }
+          if (s.j + 1 == s.it.tiles) mma_commit(o_done(t), leader);
           mma_commit(kv_free(slot), leader);
         } else if (leader) {
           mbar_arrive(kv_free(slot));
@@ -576,8 +577,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       while (have && !abort_flag) {
         ahead = now;
         have = next_step(ahead);
-        if (have) do_s(ahead);
         do_o(now);
+        if (have) do_s(ahead);
         now = ahead;
       }
     }

@@ -194,20 +194,25 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// The bounded wait without sleeping between polls (the try itself suspends the thread for a while): for the barriers
-// on the critical path of a kernel whose other warps do not need the issue slots.
+// The bounded wait for barriers on the critical path: the hardware suspends the thread (for up to `hint` ns a try) instead
+// of this code polling, which would take issue slots from the warps that share its scheduler.
+__device__ __forceinline__ bool mbar_try_for(uint32_t bar, uint32_t parity, uint32_t hint) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(hint)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void mbar_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
-  if (mbar_try(bar, parity)) return;
+  if (mbar_try_for(bar, parity, 20000u)) return;
   const long long t0 = clock64();
-  int polls = 0;
-  while (!mbar_try(bar, parity)) {
-    if (*abort_flag) return;
-    if ((++polls & 255) == 0) {
-      if (*reinterpret_cast<volatile int*>(status) != 0 || clock64() - t0 > WAIT_CYCLES) {
-        atomicCAS(status, 0, code);
-        *abort_flag = 1;
-        return;
-      }
+  while (!*abort_flag && !mbar_try_for(bar, parity, 20000u)) {
+    if (*reinterpret_cast<volatile int*>(status) != 0 || clock64() - t0 > WAIT_CYCLES) {
+      atomicCAS(status, 0, code);
+      *abort_flag = 1;
+      return;
     }
   }
 }
