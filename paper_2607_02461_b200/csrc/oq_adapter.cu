@@ -24,8 +24,13 @@
 namespace oq {
 namespace adapter {
 
-constexpr int THREADS = 192;               // 4 epilogue warps, the load warp, the mma warp
-constexpr int LOAD_WARP = 4, MMA_WARP = 5;
+#ifndef OQ_AD
+#define OQ_AD 592
+#endif
+constexpr int EPI = 8;                     // epilogue warps: two for each 32 rows, 32 columns of an expand tile each
+constexpr int THREADS = (EPI + 2) * 32;
+constexpr int LOAD_WARP = EPI, MMA_WARP = EPI + 1;
+constexpr int FEW = 8;                     // rows up to which a tile runs on the ordinary cores
 constexpr int BM = 128, KB = 64, BN = 64;  // tokens, columns of d in a shrink step, columns of m in an expand step
 constexpr int TMEM_COLS = 256;             // U: 128 columns at most, two accumulators of 64
 constexpr uint32_t COL_U = 0, COL_ACC = 128;
@@ -46,6 +51,9 @@ struct Shape {
 };
 
 struct Params {
+  const __nv_bfloat16 *X, *A, *B;          // (the tensor maps read them; these serve tiles of few rows)
+  const void* base;
+  long long ldx, ldb;
   const float* scale;
   const int *seg_start, *seg_adapter;
   int n_segs, n_tokens, n_adapters, rank, rank16, d, m;
@@ -85,14 +93,111 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* map, int x
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y) : "memory");
 }
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
 
+// A tile of up to FEW rows: a 128-row MMA would multiply padding, and its pipeline of tiles would cost more time than reading
+// the weights once, which is what bounds this case.  CTA k of the cluster takes columns d0 .. d1 - 1 of the first
+// product (a warp for each rank, lanes along d) and columns m0 .. m1 - 1 of the second (a thread for each column).
+template <bool F32>
+__device__ __noinline__ void few_rows(const Params& p, unsigned char* smem, int tok0, int rows, int id, uint32_t rank, uint32_t ranks, int d0, int d1,
+                                      int m0, int m1) {
+  float* const part = reinterpret_cast<float*>(smem);            // [FEW][128] this CTA's share of A x
+  float* const u = part + FEW * 128;                             // [FEW][128] scale * A x
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  if (id >= 0) {
+    const __nv_bfloat16* const A = p.A + (long long)id * p.rank * p.d;
+    for (int r = warp; r < p.rank; r += THREADS / 32) {
+      float sum[FEW];
+#pragma unroll
+      for (int t = 0; t < FEW; ++t) sum[t] = 0.f;
+#pragma unroll 2
+      for (int k = d0 + 8 * lane; k < d1; k += 256) {            // (d is a multiple of 8)
+        float w[8];
+        unpack8(__ldg(reinterpret_cast<const uint4*>(A + (long long)r * p.d + k)), w);
+#pragma unroll
+        for (int t = 0; t < FEW; ++t)
+          if (t < rows) {
+            float x[8];
+            unpack8(__ldg(reinterpret_cast<const uint4*>(p.X + (long long)(tok0 + t) * p.ldx + k)), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[t] = fmaf(w[e], x[e], sum[t]);
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < FEW; ++t)
+        if (t < rows) {
+#pragma unroll
+          for (int o = 16; o; o >>= 1) sum[t] += __shfl_xor_sync(~0u, sum[t], o);
+          if (lane == 0) part[t * 128 + r] = sum[t];
+        }
+    }
+    cluster_sync();
+    const float sc = __ldg(p.scale + id);
+    for (int i = (int)threadIdx.x; i < rows * (p.rank / 4); i += THREADS) {
+      const int t = i / (p.rank / 4), r = 4 * (i % (p.rank / 4));
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t k = 0; k < ranks; ++k) {
+        const float4 o = load_remote(map_rank(smem_u32(part + t * 128 + r), k));
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+      }
+      *reinterpret_cast<float4*>(u + t * 128 + r) = make_float4(v.x * sc, v.y * sc, v.z * sc, v.w * sc);
+    }
+    cluster_sync();                                              // (nobody leaves while its share is being read)
+  }
+  const __nv_bfloat16* const Bw = p.B + (long long)(id >= 0 ? id : 0) * p.m * p.rank;
+#pragma unroll 2
+  for (int col = m0 + (int)threadIdx.x; col < m1; col += THREADS) {
+    float y[FEW];
+#pragma unroll
+    for (int t = 0; t < FEW; ++t) {
+      y[t] = 0.f;
+      if (t < rows) {
+        const long long at = (long long)(tok0 + t) * p.ldb + col;
+        y[t] = F32 ? reinterpret_cast<const float*>(p.base)[at] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p.base)[at]);
+      }
+    }
+    if (id >= 0) {
+      float add[FEW];
+#pragma unroll
+      for (int t = 0; t < FEW; ++t) add[t] = 0.f;
+#pragma unroll 2
+      for (int r = 0; r < p.rank; r += 8) {
+        float w[8];
+        unpack8(__ldg(reinterpret_cast<const uint4*>(Bw + (long long)col * p.rank + r)), w);
+#pragma unroll
+        for (int t = 0; t < FEW; ++t)
+          if (t < rows) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) add[t] = fmaf(w[e], u[t * 128 + r + e], add[t]);
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < FEW; ++t) y[t] += add[t];
+    }
+#pragma unroll
+    for (int t = 0; t < FEW; ++t)
+      if (t < rows) {
+        const long long at = (long long)(tok0 + t) * p.ldy + col;
+        if (F32) reinterpret_cast<float*>(p.Y)[at] = y[t];
+        else reinterpret_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(y[t]);
+      }
+  }
+}
+
 template <bool F32, int RB>
-__global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__(THREADS, F32 || RB == 2 ? 1 : 2) adapter_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
                                                           const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
                                                           const __grid_constant__ Params p) {
   using S = Shape<F32, RB>;
@@ -115,12 +220,12 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::STAGES; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(freed(s), 1 + 4);           // the mma thread's commit, and the four epilogue warps (expanding only)
+      mbar_init(freed(s), 1 + EPI);         // the mma warp's commit, and the epilogue warps (expanding only)
     }
     mbar_init(u_full, 1);
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full(a), 1);
-      mbar_init(acc_free(a), 4);
+      mbar_init(acc_free(a), EPI);
     }
     abort_flag = 0;
     tile_info[1] = 0;
@@ -167,7 +272,8 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int tok0 = tile_info[0], rows = tile_info[1], id = tile_info[2];
-  const bool update = rows > 0 && id >= 0;                       // the same in every CTA of the cluster
+  const bool few = rows <= FEW;                                  // (all of these are the same in every CTA of the cluster)
+  const bool update = rows > 0 && id >= 0 && !few;
   const int kb_all = (p.d + KB - 1) / KB, nb_all = (p.m + BN - 1) / BN;
   const int kb0 = (int)((long long)kb_all * rank / ranks), kb1 = (int)((long long)kb_all * (rank + 1) / ranks);
   const int nb0 = (int)((long long)nb_all * rank / ranks), nb1 = (int)((long long)nb_all * (rank + 1) / ranks);
@@ -185,7 +291,7 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
   if (update) {
     if (warp == LOAD_WARP && lane == 0) {
       for (int k = kb0; k < kb1 && !abort_flag; ++k) {
-        mbar_wait(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
+        mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
         const uint32_t at = smem_st + st * S::STAGE;
         mbar_expect_tx(full(st), ATOM + (uint32_t)p.rank16 * 128u);
         tma_load_2d(at, &map_x, k * KB, tok0, full(st));
@@ -202,15 +308,15 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
         for (uint32_t i = 0; i < KB / 16; ++i)
           mma_ss(tmem + COL_U, a + 2 * i, b + 2 * i, idesc, k > kb0 || i > 0, leader);
         mma_commit(freed(st), leader);
-        if (lane < 4) mbar_arrive(freed(st));      // no epilogue warp uses a stage while shrinking
+        if (lane < EPI) mbar_arrive(freed(st));      // no epilogue warp uses a stage while shrinking
         advance();
       }
       if (kb1 > kb0) mma_commit(u_full, leader);
-    } else if (warp < 4) {
+    } else if (warp < 4) {                   // (one warp for each 32 rows is enough here)
       const int row = warp * 32 + lane;
       unsigned char* dst = smem_p + S::U_BYTES + (uint32_t)row * (uint32_t)(p.rank16 * 4 + 16);
       if (kb1 > kb0) {
-        mbar_wait(u_full, 0, &abort_flag, p.status, W_U);
+        mbar_spin(u_full, 0, &abort_flag, p.status, W_U);
         __syncwarp();
         tc_fence_after();
       }
@@ -230,10 +336,10 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
     }
     __syncwarp();
     cluster_sync();
-    if (warp < 4) {
+    if (warp < EPI) {
       const int part = (BM + (int)ranks - 1) / (int)ranks, r0 = (int)rank * part, quads = p.rank16 / 4;
       const float sc = __ldg(p.scale + id);
-      for (int i = (int)threadIdx.x; i < part * quads; i += 128) {
+      for (int i = (int)threadIdx.x; i < part * quads; i += 32 * EPI) {
         const int row = r0 + i / quads, c = 4 * (i % quads);
         if (row >= BM) break;
         const uint32_t src = smem_st + (uint32_t)row * (uint32_t)(p.rank16 * 4 + 16) + 4u * (uint32_t)c;
@@ -261,17 +367,17 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
     cluster_sync();
     tc_fence_after();
     asm volatile("fence.proxy.async;" ::: "memory");
-    if (warp < 4) {                          // where the other roles' ring stands now
+    if (warp < EPI) {                        // where the other roles' ring stands now
       st = (uint32_t)(kb1 - kb0) % S::STAGES;
       ph = ((uint32_t)(kb1 - kb0) / S::STAGES) & 1u;
     }
   }
 
   // ------------------------------------------------- expand -------------------------------------------------
-  if (update || (rows > 0 && p.copy)) {
+  if (update || (rows > 0 && id < 0 && p.copy)) {
     if (warp == LOAD_WARP && lane == 0) {
       for (int n = nb0; n < nb1 && !abort_flag; ++n) {
-        mbar_wait(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
+        mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
         const uint32_t at = smem_st + st * S::STAGE;
         mbar_expect_tx(full(st), S::BASE + (update ? S::WEIGHTS : 0u));
         tma_load_2d(at, &map_base, n * BN, tok0, full(st));
@@ -303,24 +409,23 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
         mma_commit(freed(st), leader);
         advance();
       }
-    } else if (warp < 4) {
-      constexpr int CH = F32 ? 16 : 8;                           // 16-byte chunks of a row of the tile
-      const int row = warp * 32 + lane;
+    } else if (warp < EPI) {
+      // this warp: 32 rows, half of the tile's columns (CH chunks of 16 bytes from chunk C0 on)
+      constexpr int CH = F32 ? 8 : 4, EL = F32 ? 4 : 8;
+      const int row = (warp & 3) * 32 + lane, half = warp >> 2;
       for (int n = nb0; n < nb1 && !abort_flag; ++n) {
         const uint32_t i = (uint32_t)(n - nb0), a = i & 1u;
-        mbar_wait(full(st), ph, &abort_flag, p.status, W_FULL);
-        mbar_wait(acc_full((int)a), (i >> 1) & 1u, &abort_flag, p.status, W_ACC);
+        mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
+        mbar_spin(acc_full((int)a), (i >> 1) & 1u, &abort_flag, p.status, W_ACC);
         __syncwarp();
         tc_fence_after();
-        unsigned char* const tile = smem_p + S::U_BYTES + st * S::STAGE;
-        unsigned char* const mine = tile + row * 128;
-        uint32_t acc[64];
+        // (fp32: a half is a box of its own; bf16: chunks 0-3 or 4-7 of the one box)
+        unsigned char* const box = smem_p + S::U_BYTES + st * S::STAGE + (F32 ? half * (int)ATOM : 0);
+        const int chunk0 = F32 ? 0 : 4 * half;
+        uint32_t acc[32];
         if (update) {
-          const uint32_t ta = tmem + ((uint32_t)(warp * 32) << 16) + COL_ACC + 64u * a;
-          tmem_load32_nowait(ta, acc);
-          tmem_load32_nowait(ta + 32, acc + 32);
+          tmem_load32_nowait(tmem + ((uint32_t)((warp & 3) * 32) << 16) + COL_ACC + 64u * a + 32u * (uint32_t)half, acc);
           tmem_use32(acc);
-          tmem_use32(acc + 32);
         }
         tc_fence_before();
         __syncwarp();
@@ -328,31 +433,24 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
         if (update) {
 #pragma unroll
           for (int c = 0; c < CH; ++c) {
-            uint4* const at = reinterpret_cast<uint4*>(mine + (c >> 3) * (int)ATOM + (((c & 7) ^ (row & 7)) << 4));
+            uint4* const at = reinterpret_cast<uint4*>(box + row * 128 + (((chunk0 + c) ^ (row & 7)) << 4));
             uint4 v = *at;
-            if (F32) {
-              v.x = __float_as_uint(__uint_as_float(v.x) + __uint_as_float(acc[(4 * c) & 63]));
-              v.y = __float_as_uint(__uint_as_float(v.y) + __uint_as_float(acc[(4 * c + 1) & 63]));
-              v.z = __float_as_uint(__uint_as_float(v.z) + __uint_as_float(acc[(4 * c + 2) & 63]));
-              v.w = __float_as_uint(__uint_as_float(v.w) + __uint_as_float(acc[(4 * c + 3) & 63]));
-            } else {
-              uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                w[e] = pack2(__uint_as_float(w[e] << 16) + __uint_as_float(acc[(8 * c + 2 * e) & 63]),
-                             __uint_as_float(w[e] & 0xFFFF0000u) + __uint_as_float(acc[(8 * c + 2 * e + 1) & 63]));
-              v = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int e = 0; e < 4; ++e) {
+              if (F32) w[e] = __float_as_uint(__uint_as_float(w[e]) + __uint_as_float(acc[(EL * c + e) & 31]));
+              else w[e] = pack2(__uint_as_float(w[e] << 16) + __uint_as_float(acc[(EL * c + 2 * e) & 31]),
+                                __uint_as_float(w[e] & 0xFFFF0000u) + __uint_as_float(acc[(EL * c + 2 * e + 1) & 31]));
             }
-            *at = v;
+            *at = make_uint4(w[0], w[1], w[2], w[3]);
           }
           __syncwarp();
         }
-        // the warp's 32 rows leave as whole 128-byte (bf16) or 256-byte (fp32) pieces
-        constexpr int EL = F32 ? 4 : 8;
+        // the warp's 32 rows leave as whole 64-byte (bf16) or 128-byte (fp32) pieces
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-          const int r = warp * 32 + k * (32 / CH) + lane / CH, c = lane % CH, col = n * BN + c * EL;
-          const uint4 v = *reinterpret_cast<const uint4*>(tile + (c >> 3) * (int)ATOM + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          const int r = (warp & 3) * 32 + k * (32 / CH) + lane / CH, c = chunk0 + lane % CH, col = n * BN + (F32 ? 32 * half : 0) + c * EL;
+          const uint4 v = *reinterpret_cast<const uint4*>(box + r * 128 + ((c ^ (r & 7)) << 4));
           if (r < rows && col < p.m)
             *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(p.Y) + ((long long)(tok0 + r) * p.ldy + col) * (F32 ? 4 : 2)) = v;
         }
@@ -364,6 +462,7 @@ __global__ void __launch_bounds__(THREADS) adapter_kernel(const __grid_constant_
       }
     }
   }
+  if (few && rows > 0 && (id >= 0 || p.copy)) few_rows<F32>(p, smem_p, tok0, rows, id, rank, ranks, kb0 * KB, min(kb1 * KB, p.d), nb0 * BN, min(nb1 * BN, p.m));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -414,6 +513,12 @@ extern "C" int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim
     return fail(OQ_ERR_ALIGNMENT, "oq_adapter_add: pointers must be 16-byte aligned and leading dimensions multiples of 16 bytes");
   if (Y == base && ldy != ldb) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_add: Y is base with another leading dimension");
   adapter::Params p = {};
+  p.X = reinterpret_cast<const __nv_bfloat16*>(X_bf16);
+  p.A = reinterpret_cast<const __nv_bfloat16*>(A_bf16);
+  p.B = reinterpret_cast<const __nv_bfloat16*>(B_bf16);
+  p.base = base;
+  p.ldx = ldx;
+  p.ldb = ldb;
   p.scale = scale;
   p.seg_start = seg_start;
   p.seg_adapter = seg_adapter;
@@ -455,7 +560,7 @@ extern "C" int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim
   const long long most = (n_tokens + adapter::BM - 1) / adapter::BM + (long long)n_segs;
   const int tiles = (int)(most < n_tokens ? most : n_tokens);
   int ranks = 1;
-  while (ranks < 8 && (long long)tiles * ranks < 592) ranks *= 2;
+  while (ranks < 8 && (long long)tiles * ranks < OQ_AD) ranks *= 2;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool wide = rank > 64;
   if (dtype == OQ_F32) e = wide ? adapter::launch<true, 2>(p, mx, ma, mb, mbase, tiles, ranks, st) : adapter::launch<true, 1>(p, mx, ma, mb, mbase, tiles, ranks, st);
