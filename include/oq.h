@@ -372,11 +372,14 @@ int oq_attention(const oq_attention_args* args, void* workspace, size_t workspac
  *            otherwise the two must not overlap
  * dim and m multiples of 8, leading dimensions multiples of 16 bytes, pointers 16-byte aligned.  Both products run on the
  * tensor cores with fp32 accumulation; A x is carried between them in 16 bits for bf16 outputs (two bf16 pieces) and
- * 24 for fp32 (three).  Results are bit-reproducible.  Asynchronous on `stream`; nothing is allocated.  n_tokens == 0 or
- * n_segs == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+ * 24 for fp32 (three); with 8 tokens a segment or fewer on average both run on the ordinary cores in fp32.  The workspace (dev, 16-byte
+ * aligned, oq_adapter_workspace_bytes bytes, 0 for few tokens) carries A x between the two kernels.  Results are
+ * bit-reproducible.  Asynchronous on `stream`; nothing is allocated.  n_tokens == 0 or n_segs == 0 launches nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */
+int oq_adapter_workspace_bytes(int n_tokens, int n_segs, int dim, int rank, size_t* bytes);
 int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const void* A_bf16, const void* B_bf16, int n_adapters,
                    int rank, const float* scale, const int* seg_start, const int* seg_adapter, int n_segs, const void* base,
-                   int ldb, void* Y, int ldy, int m, int dtype, void* stream);
+                   int ldb, void* Y, int ldy, int m, int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Self-test of the bounded device-side waits the GEMM pipeline is built on: launches one thread that waits
  * about a millisecond on a barrier nobody arrives at.  The wait gives up by itself (the kernel ends

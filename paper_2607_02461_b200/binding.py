@@ -66,7 +66,8 @@ def lib():
             "oq_qk_norm_rope": (i, [vp, vp, i, i, vp, vp, i, i, C.c_float, i, i, vp]),
             "oq_attention_workspace_bytes": (i, [vp, C.POINTER(sz)]),
             "oq_attention": (i, [vp, vp, sz, vp]),
-            "oq_adapter_add": (i, [vp, i, i, i, vp, vp, i, i, vp, vp, vp, i, vp, i, vp, i, i, i, vp]),
+            "oq_adapter_workspace_bytes": (i, [i, i, i, i, C.POINTER(sz)]),
+            "oq_adapter_add": (i, [vp, i, i, i, vp, vp, i, i, vp, vp, vp, i, vp, i, vp, i, i, i, vp, sz, vp]),
             "oq_last_error": (C.c_char_p, []), "oq_version": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -518,10 +519,11 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     return (out, lse) if want_lse else out
 
 
-def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None):
+def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, workspace=None):
     """base + scale_a B_a (A_a x) for the tokens of each segment.  X: CUDA bf16 [T, d]; A: bf16 [adapters, rank, d]; Bm: bf16
     [adapters, m, rank]; scale: fp32 [adapters]; seg_start: int32 [segments + 1]; seg_adapter: int32 [segments] (-1: none);
-    base: bf16 or fp32 [T, m].  Returns out (new by default; out=base adds in place)."""
+    base: bf16 or fp32 [T, m].  Returns out (new by default; out=base adds in place).  workspace: CUDA uint8 tensor, by default
+    one is taken from torch's allocator when the call needs it."""
     import torch
     bf16, i32 = torch.bfloat16, torch.int32
     xs, sa, sb, shape = X.shape, A.shape, Bm.shape, base.shape
@@ -547,9 +549,17 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None):
         raise OqError(3, "oq_adapter_add: the elements of a row must be adjacent")
     if n <= 1:
         ldx, ldb, ldy = d, m, m
+    space = size = 0
+    if workspace is None:
+        need = C.c_size_t()
+        _check(lib().oq_adapter_workspace_bytes(n, segs, d, rank, C.byref(need)))
+        if need.value:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=X.device)
+    if workspace is not None:
+        space, size = workspace.data_ptr(), workspace.numel()
     _check(lib().oq_adapter_add(X.data_ptr(), n, ldx, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(), seg_start.data_ptr(),
                                 seg_adapter.data_ptr(), segs, base.data_ptr(), ldb, out.data_ptr(), ldy, m,
-                                _dtype_code(base.dtype, "oq_adapter_add"), _raw_stream(X.get_device())))
+                                _dtype_code(base.dtype, "oq_adapter_add"), space, size, _raw_stream(X.get_device())))
     return out
 
 

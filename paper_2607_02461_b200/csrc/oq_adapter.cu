@@ -3,17 +3,21 @@
 //   Y[t] = base[t] + scale_a B_a (A_a x[t]),   a = the adapter of the segment of tokens that t belongs to (none: base)
 //
 // Bound: memory.  base is read and Y written once (4 or 8 bytes an element) and X read once; the two products are
-// 2 r (d + m) multiply-adds a token, far below what the tensor cores do in that time.  So everything travels by TMA
-// and one kernel does both products: a cluster of up to 8 CTAs takes 128 tokens of one segment,
+// 2 r (d + m) operations a token, far below what the tensor cores do in that time.  Two kernels:
 //
-//   shrink   CTA k multiplies its share of the d columns:  U_k = X A^T  (tcgen05, fp32 in tensor memory);
-//            the shares are added over the cluster's shared memory in CTA order (bit-reproducible), each CTA a part of
-//            the rows, which it scales, cuts into bf16 pieces and hands to all CTAs of the cluster as an MMA operand
-//   expand   CTA k multiplies its share of the m columns, 64 at a time: acc = U B^T, and adds the base's tile
+//   shrink   u = A x by tcgen05 for tiles of 128 tokens of one segment.  The k-blocks (64 columns of d) of all tiles, one after the
+//            other, are one line of steps and every SM takes an equal stretch of it; a stretch leaves its sum of a tile, fp32,
+//            in the workspace (a few per cent of the traffic)
+//   expand   Y = base + u B^T, the column tiles of all token tiles again one line in equal stretches.  At a token tile's
+//            start the parts of u are added in the order of the stretches (bit-reproducible), scaled and cut into pieces of bf16
+//            as an MMA operand: 2 pieces (16 bits) for bf16 outputs, 3 (24 bits) for fp32, each a product of its own, so that
+//            the update is as exact as the output's type can show.  base tiles come by TMA, are added to in shared memory and
+//            leave by TMA
 //
-// The cluster's size only divides the columns: no byte is read twice for it, and no workspace or second launch is
-// needed.  U is cut into 2 pieces of bf16 for bf16 outputs (16 bits) and 3 for fp32 (24 bits), each a product of its own, so that
-// the update is as exact as the output's type can show.
+// (One kernel for both, a cluster of CTAs per token tile that exchanges u through distributed shared memory, needs no
+// workspace, but clusters fill whole groups of SMs only: 38 tiles took 64 to 77 us where equal stretches take half.)
+//
+// Segments of a few tokens (serving one token each) run in a third kernel on the ordinary cores, see few_kernel.
 #include <cuda_bf16.h>
 
 #include <string>
@@ -24,34 +28,16 @@
 namespace oq {
 namespace adapter {
 
-#ifndef OQ_AD
-#define OQ_AD 592
-#endif
-constexpr int EPI = 8;                     // epilogue warps: two for each 32 rows, 32 columns of an expand tile each
-constexpr int THREADS = (EPI + 2) * 32;
-constexpr int LOAD_WARP = EPI, MMA_WARP = EPI + 1;
-constexpr int FEW = 8;                     // rows up to which a tile runs on the ordinary cores
-constexpr int BM = 128, KB = 64, BN = 64;  // tokens, columns of d in a shrink step, columns of m in an expand step
-constexpr int TMEM_COLS = 256;             // U: 128 columns at most, two accumulators of 64
-constexpr uint32_t COL_U = 0, COL_ACC = 128;
+constexpr int BM = 128, KB = 64;           // tokens of a tile, columns of d in a shrink step
 constexpr uint32_t ATOM = BM * 128;        // 128 rows of 128 bytes
-enum { W_FULL = 60, W_FREE = 61, W_U = 62, W_ACC = 63, W_ACCFREE = 64 };
-
-// RB: blocks of 64 ranks; a stage holds an X tile and an A tile while shrinking, a base tile and a B tile while expanding
-template <bool F32, int RB>
-struct Shape {
-  static constexpr int PIECES = F32 ? 3 : 2;
-  static constexpr uint32_t U_BYTES = PIECES * RB * ATOM;
-  static constexpr uint32_t BASE = F32 ? 2 * ATOM : ATOM;
-  static constexpr uint32_t WEIGHTS = RB * 64 * 128;                     // 64 x RB blocks (A), or RB atoms of 64 rows (B)
-  static constexpr uint32_t STAGE = BASE + WEIGHTS;
-  static constexpr int STAGES = F32 && RB == 2 ? 2 : 3;              // (what fits in 227 KB beside U)
-  static constexpr uint32_t PART = BM * (RB * 64 * 4 + 16);              // one CTA's share of U, fp32; lies over the stages
-  static constexpr uint32_t SMEM = 1024 + U_BYTES + (STAGES * STAGE > PART ? STAGES * STAGE : PART);
-};
+constexpr int EPI = 8;                     // epilogue warps of the expand kernel: two groups that take turns at column tiles
+constexpr int EXPAND_THREADS = (EPI + 2) * 32, SHRINK_THREADS = 6 * 32;
+constexpr int FEW = 8;                     // tokens the few-token kernel holds at a time
+constexpr int FEW_THREADS = 256;
+enum { W_FULL = 60, W_FREE = 61, W_U = 62, W_UFREE = 63, W_ACC = 64, W_ACCFREE = 65 };
 
 struct Params {
-  const __nv_bfloat16 *X, *A, *B;          // (the tensor maps read them; these serve tiles of few rows)
+  const __nv_bfloat16 *X, *A, *B;
   const void* base;
   long long ldx, ldb;
   const float* scale;
@@ -60,6 +46,9 @@ struct Params {
   void* Y;
   long long ldy;
   int copy;                                // Y is not base: rows without an adapter are copied
+  float* part;                             // [tiles][parts][128][rank16]
+  int parts;                               // places for them, the most stretches a tile can meet
+  int ctas;                                // stretches of the shrink line, at most
   int* status;
 };
 
@@ -74,6 +63,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return r;
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
@@ -86,12 +76,13 @@ __device__ __forceinline__ float4 load_remote(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void store_remote(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("st.shared::cluster.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
-}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const void* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+               ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(src) : "memory");
 }
 __device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
   const uint32_t u[4] = {v.x, v.y, v.z, v.w};
@@ -107,18 +98,62 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return d;
 }
 
-// A tile of up to FEW rows: a 128-row MMA would multiply padding, and its pipeline of tiles would cost more time than reading
-// the weights once, which is what bounds this case.  CTA k of the cluster takes columns d0 .. d1 - 1 of the first
-// product (a warp for each rank, lanes along d) and columns m0 .. m1 - 1 of the second (a thread for each column).
+// 128 tokens of one segment.  Tiles are counted segment by segment.
+struct Tile {
+  int tok0, rows, id;                      // id: the adapter, or -1
+};
+// By a whole warp: tile `want`; rows = 0 and tok0 = the number of tiles when there are no more than `want`.
+__device__ __forceinline__ Tile find_tile(const Params& p, int want) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int s0 = 0; s0 < p.n_segs; s0 += 32) {
+    const int s = s0 + lane;
+    int b = 0, n = 0, id = -1;
+    if (s < p.n_segs) {
+      b = min(max(__ldg(p.seg_start + s), 0), p.n_tokens);
+      n = min(max(__ldg(p.seg_start + s + 1), b), p.n_tokens) - b;
+      id = __ldg(p.seg_adapter + s);
+      if (id < 0 || id >= p.n_adapters) id = -1;
+    }
+    const int tiles = (n + BM - 1) / BM;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(~0u, sum, d);
+      if (lane >= d) sum += o;
+    }
+    const int at = want - (before + sum - tiles);
+    const uint32_t mine = __ballot_sync(~0u, at >= 0 && at < tiles);
+    if (mine) {
+      const int l = __ffs(mine) - 1;
+      Tile t;
+      t.tok0 = __shfl_sync(~0u, b + at * BM, l);
+      t.rows = __shfl_sync(~0u, min(BM, n - at * BM), l);
+      t.id = __shfl_sync(~0u, id, l);
+      return t;
+    }
+    before += __shfl_sync(~0u, sum, 31);
+  }
+  return Tile{before, 0, -1};
+}
+// Steps of a stretch of the shrink line: an equal share, but so many that the kbs steps of a tile never meet more than
+// p.parts stretches, however few tiles the segments turn out to make: ceil((kbs - 1) / len) + 1 <= parts.
+__device__ __forceinline__ long long shrink_stretch(const Params& p, long long total, int kbs) {
+  return max((total + p.ctas - 1) / p.ctas, (long long)(p.parts > 1 ? (kbs + p.parts - 2) / (p.parts - 1) : 1));
+}
+
+// Up to FEW rows of a segment: a 128-row MMA would multiply padding, and what bounds this case is reading the weights once.
+// CTA k of the cluster takes columns d0 .. d1 - 1 of the first product (a warp for each rank, lanes along d) and
+// columns m0 .. m1 - 1 of the second (a thread for each column); the shares of u meet in distributed shared memory.
 template <bool F32>
-__device__ __noinline__ void few_rows(const Params& p, unsigned char* smem, int tok0, int rows, int id, uint32_t rank, uint32_t ranks, int d0, int d1,
+__device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, int tok0, int rows, int id, uint32_t rank, uint32_t ranks, int d0, int d1,
                                       int m0, int m1) {
   float* const part = reinterpret_cast<float*>(smem);            // [FEW][128] this CTA's share of A x
   float* const u = part + FEW * 128;                             // [FEW][128] scale * A x
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   if (id >= 0) {
     const __nv_bfloat16* const A = p.A + (long long)id * p.rank * p.d;
-    for (int r = warp; r < p.rank; r += THREADS / 32) {
+    for (int r = warp; r < p.rank; r += FEW_THREADS / 32) {
       float sum[FEW];
 #pragma unroll
       for (int t = 0; t < FEW; ++t) sum[t] = 0.f;
@@ -145,7 +180,7 @@ __device__ __noinline__ void few_rows(const Params& p, unsigned char* smem, int 
     }
     cluster_sync();
     const float sc = __ldg(p.scale + id);
-    for (int i = (int)threadIdx.x; i < rows * (p.rank / 4); i += THREADS) {
+    for (int i = (int)threadIdx.x; i < rows * (p.rank / 4); i += FEW_THREADS) {
       const int t = i / (p.rank / 4), r = 4 * (i % (p.rank / 4));
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       for (uint32_t k = 0; k < ranks; ++k) {
@@ -158,7 +193,7 @@ __device__ __noinline__ void few_rows(const Params& p, unsigned char* smem, int 
   }
   const __nv_bfloat16* const Bw = p.B + (long long)(id >= 0 ? id : 0) * p.m * p.rank;
 #pragma unroll 2
-  for (int col = m0 + (int)threadIdx.x; col < m1; col += THREADS) {
+  for (int col = m0 + (int)threadIdx.x; col < m1; col += FEW_THREADS) {
     float y[FEW];
 #pragma unroll
     for (int t = 0; t < FEW; ++t) {
@@ -196,298 +231,432 @@ __device__ __noinline__ void few_rows(const Params& p, unsigned char* smem, int 
   }
 }
 
-template <bool F32, int RB>
-__global__ void __launch_bounds__(THREADS, F32 || RB == 2 ? 1 : 2) adapter_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
-                                                          const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
-                                                          const __grid_constant__ Params p) {
-  using S = Shape<F32, RB>;
+template <bool F32>
+__global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant__ Params p) {
+  __shared__ __align__(16) unsigned char smem[2 * FEW * 128 * 4];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const Tile t = find_tile(p, (int)(blockIdx.x / ranks));        // (the same in every CTA of the cluster)
+  if (t.rows == 0 || (t.id < 0 && !p.copy)) return;
+  const int kb = (p.d + 63) / 64, nb = (p.m + 63) / 64;
+  for (int r = 0; r < t.rows; r += FEW)                          // (a segment that is not short after all: the weights come again)
+    few_rows<F32>(p, smem, t.tok0 + r, min(FEW, t.rows - r), t.id, rank, ranks, 64 * (int)((long long)kb * rank / ranks),
+                  min(64 * (int)((long long)kb * (rank + 1) / ranks), p.d), 64 * (int)((long long)nb * rank / ranks),
+                  min(64 * (int)((long long)nb * (rank + 1) / ranks), p.m));
+}
+
+// ------------------------------------------------- shrink -------------------------------------------------
+template <int RB>
+struct Shrink {
+  static constexpr uint32_t STAGE = ATOM + RB * 8192;           // 128 tokens and up to 64 RB ranks, 64 columns of d each
+  static constexpr int STAGES = RB == 1 ? 9 : 6;
+  static constexpr uint32_t SMEM = 1024 + STAGES * STAGE;
+};
+template <int RB>
+__global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
+                                                                   const __grid_constant__ Params p) {
+  using S = Shrink<RB>;
+  constexpr int STAGES = S::STAGES, LOAD_WARP = 4, MMA_WARP = 5;
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 5];
-  __shared__ int tile_info[3];              // first token, tokens, adapter
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  unsigned char* const smem_p = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
-  const uint32_t smem_u = smem_u32(smem_p), smem_st = smem_u + S::U_BYTES;
-  const uint32_t b0 = smem_u32(bars);
-  auto full = [&](int s) { return b0 + 8u * (uint32_t)s; };
-  auto freed = [&](int s) { return b0 + 8u * (uint32_t)(S::STAGES + s); };
-  const uint32_t u_full = b0 + 8u * (2 * S::STAGES);
-  auto acc_full = [&](int a) { return b0 + 8u * (uint32_t)(2 * S::STAGES + 1 + a); };
-  auto acc_free = [&](int a) { return b0 + 8u * (uint32_t)(2 * S::STAGES + 3 + a); };
-  const uint32_t rank = cluster_rank(), ranks = cluster_size();
-
+  const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u, b0 = smem_u32(bars);
+  auto full = [&](uint32_t s) { return b0 + 8u * s; };
+  auto freed = [&](uint32_t s) { return b0 + 8u * (STAGES + s); };
+  auto u_full = [&](uint32_t a) { return b0 + 8u * (2 * STAGES + a); };
+  auto u_free = [&](uint32_t a) { return b0 + 8u * (2 * STAGES + 2 + a); };
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S::STAGES; ++s) {
+    for (int s = 0; s < STAGES; ++s) {
       mbar_init(full(s), 1);
-      mbar_init(freed(s), 1 + EPI);         // the mma warp's commit, and the epilogue warps (expanding only)
+      mbar_init(freed(s), 1);
     }
-    mbar_init(u_full, 1);
     for (int a = 0; a < 2; ++a) {
-      mbar_init(acc_full(a), 1);
-      mbar_init(acc_free(a), EPI);
+      mbar_init(u_full(a), 1);
+      mbar_init(u_free(a), 4);
     }
     abort_flag = 0;
-    tile_info[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == MMA_WARP) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(TMEM_COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  __syncthreads();
-  if (warp == 0) {
-    // which 128 tokens: tiles are counted segment by segment
-    const int want = (int)(blockIdx.x / ranks);
-    int before = 0;
-    for (int s0 = 0; s0 < p.n_segs && before <= want; s0 += 32) {
-      const int s = s0 + lane;
-      int b = 0, n = 0;
-      if (s < p.n_segs) {
-        b = min(max(__ldg(p.seg_start + s), 0), p.n_tokens);
-        n = min(max(__ldg(p.seg_start + s + 1), b), p.n_tokens) - b;
-      }
-      const int tiles = (n + BM - 1) / BM;
-      int sum = tiles;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, sum, d);
-        if (lane >= d) sum += o;
-      }
-      const int at = want - (before + sum - tiles);
-      if (at >= 0 && at < tiles) {
-        tile_info[0] = b + at * BM;
-        tile_info[1] = min(BM, n - at * BM);
-        const int a = __ldg(p.seg_adapter + s);
-        tile_info[2] = a >= 0 && a < p.n_adapters ? a : -1;
-      }
-      before += __shfl_sync(~0u, sum, 31);
-    }
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int tok0 = tile_info[0], rows = tile_info[1], id = tile_info[2];
-  const bool few = rows <= FEW;                                  // (all of these are the same in every CTA of the cluster)
-  const bool update = rows > 0 && id >= 0 && !few;
-  const int kb_all = (p.d + KB - 1) / KB, nb_all = (p.m + BN - 1) / BN;
-  const int kb0 = (int)((long long)kb_all * rank / ranks), kb1 = (int)((long long)kb_all * (rank + 1) / ranks);
-  const int nb0 = (int)((long long)nb_all * rank / ranks), nb1 = (int)((long long)nb_all * (rank + 1) / ranks);
-  const int steps = p.rank16 / 16;
-  const uint32_t leader = elect_leader();
-  uint32_t st = 0, ph = 0;                                       // stage ring position of the load and mma threads
+  const int kbs = (p.d + KB - 1) / KB;
+  const long long total = (long long)find_tile(p, 0x7FFFFFFF).tok0 * kbs;
+  const long long len = shrink_stretch(p, total, kbs);
+  const int c = (int)blockIdx.x;
+  long long pos = c * len;
+  const long long end = min(pos + len, total);
+  // runs: the k-blocks k .. k + count - 1 of one token tile
+  Tile t;
+  int tile = 0, k = 0, count = 0;
+  auto next_run = [&]() {
+    while (pos < end) {
+      tile = (int)(pos / kbs);
+      k = (int)(pos % kbs);
+      count = (int)min((long long)(kbs - k), end - pos);
+      pos += count;
+      t = find_tile(p, tile);
+      if (t.id >= 0) return true;
+    }
+    return false;
+  };
+  uint32_t st = 0, ph = 0, runs = 0;
   auto advance = [&]() {
-    if (++st == (uint32_t)S::STAGES) {
+    if (++st == (uint32_t)STAGES) {
       st = 0;
       ph ^= 1u;
     }
   };
-
-  // ------------------------------------------------- shrink -------------------------------------------------
-  if (update) {
-    if (warp == LOAD_WARP && lane == 0) {
-      for (int k = kb0; k < kb1 && !abort_flag; ++k) {
-        mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
-        const uint32_t at = smem_st + st * S::STAGE;
-        mbar_expect_tx(full(st), ATOM + (uint32_t)p.rank16 * 128u);
-        tma_load_2d(at, &map_x, k * KB, tok0, full(st));
-        tma_load_3d(at + S::BASE, &map_a, k * KB, 0, id, full(st));
-        advance();
-      }
-    } else if (warp == MMA_WARP) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(p.rank16 >> 3) << 17);
-      for (int k = kb0; k < kb1 && !abort_flag; ++k) {
+  if (warp == LOAD_WARP) {
+    while (next_run()) {
+      if (lane == 0)
+        for (int i = 0; i < count && !abort_flag; ++i) {
+          mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
+          const uint32_t at = smem + st * S::STAGE;
+          mbar_expect_tx(full(st), ATOM + (uint32_t)p.rank16 * 128u);
+          tma_load_2d(at, &map_x, (k + i) * KB, t.tok0, full(st));
+          tma_load_3d(at + ATOM, &map_a, (k + i) * KB, 0, t.id, full(st));
+          advance();
+        }
+      __syncwarp();
+    }
+    // copies still in flight end before the CTA does (after an abort nobody else waits for them)
+    if (lane == 0 && abort_flag)
+      for (uint32_t s = 0; s < (uint32_t)STAGES; ++s)
+        for (int i = 0; i < (1 << 16) && !mbar_try(full(s), (s < st ? ph : ph ^ 1u)); ++i) {}
+  } else if (warp == MMA_WARP) {
+    const uint32_t leader = elect_leader();
+    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(p.rank16 >> 3) << 17);
+    for (; next_run(); ++runs) {
+      const uint32_t a = runs & 1u;
+      if (runs >= 2) mbar_spin(u_free(a), ((runs >> 1) - 1u) & 1u, &abort_flag, p.status, W_UFREE);
+      for (int i = 0; i < count && !abort_flag; ++i) {
         mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
         tc_fence_after();
-        const uint64_t a = smem_desc(smem_st + st * S::STAGE), b = smem_desc(smem_st + st * S::STAGE + S::BASE);
+        const uint64_t da = smem_desc(smem + st * S::STAGE), db = smem_desc(smem + st * S::STAGE + ATOM);
 #pragma unroll
-        for (uint32_t i = 0; i < KB / 16; ++i)
-          mma_ss(tmem + COL_U, a + 2 * i, b + 2 * i, idesc, k > kb0 || i > 0, leader);
+        for (uint32_t q = 0; q < KB / 16; ++q) mma_ss(tmem + 128u * a, da + 2 * q, db + 2 * q, idesc, i > 0 || q > 0, leader);
         mma_commit(freed(st), leader);
-        if (lane < EPI) mbar_arrive(freed(st));      // no epilogue warp uses a stage while shrinking
         advance();
       }
-      if (kb1 > kb0) mma_commit(u_full, leader);
-    } else if (warp < 4) {                   // (one warp for each 32 rows is enough here)
-      const int row = warp * 32 + lane;
-      unsigned char* dst = smem_p + S::U_BYTES + (uint32_t)row * (uint32_t)(p.rank16 * 4 + 16);
-      if (kb1 > kb0) {
-        mbar_spin(u_full, 0, &abort_flag, p.status, W_U);
-        __syncwarp();
-        tc_fence_after();
-      }
-      // (every stage has been read: the MMAs that this barrier follows were the last to read one)
-      for (int c = 0; c < p.rank16; c += 16) {
+      mma_commit(u_full(a), leader);
+    }
+  } else {
+    for (; next_run(); ++runs) {
+      const uint32_t a = runs & 1u;
+      mbar_spin(u_full(a), (runs >> 1) & 1u, &abort_flag, p.status, W_U);
+      __syncwarp();
+      tc_fence_after();
+      const int row = warp * 32 + lane, place = c - (int)((long long)tile * kbs / len);
+      float* dst = p.part + (((long long)tile * p.parts + place) * BM + row) * p.rank16;
+      for (int q = 0; q < p.rank16; q += 16) {
         uint32_t r[16];
-        if (kb1 > kb0) {
-          tmem_load16_nowait(tmem + ((uint32_t)(warp * 32) << 16) + COL_U + (uint32_t)c, r);
-          tmem_wait_ld();
-        } else {
+        tmem_load16_at(tmem + ((uint32_t)(warp * 32) << 16) + 128u * a + (uint32_t)q, r);
+        tmem_use16(r);
+        if (row < t.rows)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) r[i] = 0u;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(dst + 4 * (c + i)) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+          for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(dst + q + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
       }
-    }
-    __syncwarp();
-    cluster_sync();
-    if (warp < EPI) {
-      const int part = (BM + (int)ranks - 1) / (int)ranks, r0 = (int)rank * part, quads = p.rank16 / 4;
-      const float sc = __ldg(p.scale + id);
-      for (int i = (int)threadIdx.x; i < part * quads; i += 32 * EPI) {
-        const int row = r0 + i / quads, c = 4 * (i % quads);
-        if (row >= BM) break;
-        const uint32_t src = smem_st + (uint32_t)row * (uint32_t)(p.rank16 * 4 + 16) + 4u * (uint32_t)c;
-        float4 u = load_remote(map_rank(src, 0));
-        for (uint32_t k = 1; k < ranks; ++k) {
-          const float4 v = load_remote(map_rank(src, k));
-          u.x += v.x; u.y += v.y; u.z += v.z; u.w += v.w;
-        }
-        float x[4] = {u.x * sc, u.y * sc, u.z * sc, u.w * sc};
-        const uint32_t dst = smem_u + (uint32_t)(c >> 6) * ATOM + (uint32_t)row * 128u + (uint32_t)((((c & 63) >> 3) ^ (row & 7)) << 4) + (uint32_t)(c & 4) * 2u;
-#pragma unroll
-        for (int q = 0; q < S::PIECES; ++q) {
-          const uint32_t lo = pack2(x[0], x[1]), hi = pack2(x[2], x[3]);
-          for (uint32_t k = 0; k < ranks; ++k) store_remote(map_rank(dst + (uint32_t)q * RB * ATOM, k), lo, hi);
-          x[0] -= __uint_as_float(lo << 16);
-          x[1] -= __uint_as_float(lo & 0xFFFF0000u);
-          x[2] -= __uint_as_float(hi << 16);
-          x[3] -= __uint_as_float(hi & 0xFFFF0000u);
-        }
-      }
-      asm volatile("fence.proxy.async;" ::: "memory");
-    }
-    tc_fence_before();
-    __syncwarp();
-    cluster_sync();
-    tc_fence_after();
-    asm volatile("fence.proxy.async;" ::: "memory");
-    if (warp < EPI) {                        // where the other roles' ring stands now
-      st = (uint32_t)(kb1 - kb0) % S::STAGES;
-      ph = ((uint32_t)(kb1 - kb0) / S::STAGES) & 1u;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(u_free(a));
     }
   }
-
-  // ------------------------------------------------- expand -------------------------------------------------
-  if (update || (rows > 0 && id < 0 && p.copy)) {
-    if (warp == LOAD_WARP && lane == 0) {
-      for (int n = nb0; n < nb1 && !abort_flag; ++n) {
-        mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
-        const uint32_t at = smem_st + st * S::STAGE;
-        mbar_expect_tx(full(st), S::BASE + (update ? S::WEIGHTS : 0u));
-        tma_load_2d(at, &map_base, n * BN, tok0, full(st));
-        if (F32) tma_load_2d(at + ATOM, &map_base, n * BN + 32, tok0, full(st));
-        if (update)
-          for (int r = 0; r < RB; ++r) tma_load_3d(at + S::BASE + (uint32_t)r * 8192u, &map_b, 64 * r, n * BN, id, full(st));
-        advance();
-      }
-      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
-      for (int s = 0; s < S::STAGES; ++s)
-        for (int n = 0; abort_flag && n < (1 << 16); ++n) mbar_try(full(s), ph);
-    } else if (warp == MMA_WARP) {
-      constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(BN >> 3) << 17);
-      for (int n = nb0; n < nb1 && !abort_flag; ++n) {
-        const uint32_t i = (uint32_t)(n - nb0), a = i & 1u;
-        mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
-        if (i >= 2) mbar_spin(acc_free((int)a), ((i >> 1) - 1u) & 1u, &abort_flag, p.status, W_ACCFREE);
-        tc_fence_after();
-        if (update) {
-          const uint32_t bt = smem_st + st * S::STAGE + S::BASE;
-          for (int q = 0; q < S::PIECES; ++q)
-            for (int s = 0; s < steps; ++s) {
-              const uint64_t da = smem_desc(smem_u + (uint32_t)(q * RB + (s >> 2)) * ATOM) + 2u * (uint32_t)(s & 3);
-              const uint64_t db = smem_desc(bt + (uint32_t)(s >> 2) * 8192u) + 2u * (uint32_t)(s & 3);
-              mma_ss(tmem + COL_ACC + 64u * a, da, db, IDESC, q > 0 || s > 0, leader);
-            }
-        }
-        mma_commit(acc_full((int)a), leader);
-        mma_commit(freed(st), leader);
-        advance();
-      }
-    } else if (warp < EPI) {
-      // this warp: 32 rows, half of the tile's columns (CH chunks of 16 bytes from chunk C0 on)
-      constexpr int CH = F32 ? 8 : 4, EL = F32 ? 4 : 8;
-      const int row = (warp & 3) * 32 + lane, half = warp >> 2;
-      for (int n = nb0; n < nb1 && !abort_flag; ++n) {
-        const uint32_t i = (uint32_t)(n - nb0), a = i & 1u;
-        mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
-        mbar_spin(acc_full((int)a), (i >> 1) & 1u, &abort_flag, p.status, W_ACC);
-        __syncwarp();
-        tc_fence_after();
-        // (fp32: a half is a box of its own; bf16: chunks 0-3 or 4-7 of the one box)
-        unsigned char* const box = smem_p + S::U_BYTES + st * S::STAGE + (F32 ? half * (int)ATOM : 0);
-        const int chunk0 = F32 ? 0 : 4 * half;
-        uint32_t acc[32];
-        if (update) {
-          tmem_load32_nowait(tmem + ((uint32_t)((warp & 3) * 32) << 16) + COL_ACC + 64u * a + 32u * (uint32_t)half, acc);
-          tmem_use32(acc);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(acc_free((int)a));
-        if (update) {
-#pragma unroll
-          for (int c = 0; c < CH; ++c) {
-            uint4* const at = reinterpret_cast<uint4*>(box + row * 128 + (((chunk0 + c) ^ (row & 7)) << 4));
-            uint4 v = *at;
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (F32) w[e] = __float_as_uint(__uint_as_float(w[e]) + __uint_as_float(acc[(EL * c + e) & 31]));
-              else w[e] = pack2(__uint_as_float(w[e] << 16) + __uint_as_float(acc[(EL * c + 2 * e) & 31]),
-                                __uint_as_float(w[e] & 0xFFFF0000u) + __uint_as_float(acc[(EL * c + 2 * e + 1) & 31]));
-            }
-            *at = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          __syncwarp();
-        }
-        // the warp's 32 rows leave as whole 64-byte (bf16) or 128-byte (fp32) pieces
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-          const int r = (warp & 3) * 32 + k * (32 / CH) + lane / CH, c = chunk0 + lane % CH, col = n * BN + (F32 ? 32 * half : 0) + c * EL;
-          const uint4 v = *reinterpret_cast<const uint4*>(box + r * 128 + ((c ^ (r & 7)) << 4));
-          if (r < rows && col < p.m)
-            *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(p.Y) + ((long long)(tok0 + r) * p.ldy + col) * (F32 ? 4 : 2)) = v;
-        }
-        // (the next TMA load into this stage is ordered after these reads and writes by the barrier and a proxy fence)
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(freed(st));
-        advance();
-      }
-    }
-  }
-  if (few && rows > 0 && (id >= 0 || p.copy)) few_rows<F32>(p, smem_p, tok0, rows, id, rank, ranks, kb0 * KB, min(kb1 * KB, p.d), nb0 * BN, min(nb1 * BN, p.m));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS) : "memory");
+  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(256) : "memory");
 }
 
+// ------------------------------------------------- expand -------------------------------------------------
 template <bool F32, int RB>
-cudaError_t launch(const Params& p, const CUtensorMap& mx, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mbase, int tiles,
-                   int ranks, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(adapter_kernel<F32, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<F32, RB>::SMEM);
-  if (e != cudaSuccess) return e;
+struct Expand {
+  static constexpr int BN = F32 ? 32 : 64;                       // columns of a tile: 128 bytes
+  static constexpr int PIECES = F32 ? 3 : 2;
+  static constexpr uint32_t U_BYTES = PIECES * RB * ATOM;
+  static constexpr uint32_t B_ATOM = BN * 128, STAGE = ATOM + RB * B_ATOM;      // a base tile and the rows of B for its columns
+  static constexpr int STAGES = (int)((226 * 1024 - U_BYTES) / STAGE) < 8 ? (int)((226 * 1024 - U_BYTES) / STAGE) : 8;
+  static constexpr uint32_t SMEM = 1024 + U_BYTES + STAGES * STAGE;
+};
+template <bool F32, int RB>
+__global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
+                                                                   const __grid_constant__ CUtensorMap map_y, const __grid_constant__ Params p) {
+  using S = Expand<F32, RB>;
+  constexpr int STAGES = S::STAGES, BN = S::BN, LOAD_WARP = EPI, MMA_WARP = EPI + 1;
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES + 5];
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  unsigned char* const smem_p = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
+  const uint32_t smem_u = smem_u32(smem_p), smem_st = smem_u + S::U_BYTES, b0 = smem_u32(bars);
+  auto full = [&](uint32_t s) { return b0 + 8u * s; };
+  auto freed = [&](uint32_t s) { return b0 + 8u * (STAGES + s); };
+  auto acc_full = [&](uint32_t a) { return b0 + 8u * (2 * STAGES + a); };
+  auto acc_free = [&](uint32_t a) { return b0 + 8u * (2 * STAGES + 2 + a); };
+  const uint32_t u_ready = b0 + 8u * (2 * STAGES + 4);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full(s), 1);
+      mbar_init(freed(s), 1 + 4);           // the mma warp's commit, and the four warps whose tile it is
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full(a), 1);
+      mbar_init(acc_free(a), 4);
+    }
+    mbar_init(u_ready, EPI);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(128) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const int nbs = (p.m + BN - 1) / BN, kbs = (p.d + KB - 1) / KB, steps = p.rank16 / 16;
+  const int tiles = find_tile(p, 0x7FFFFFFF).tok0;
+  const long long total = (long long)tiles * nbs, len = shrink_stretch(p, (long long)tiles * kbs, kbs);
+  long long pos = total * blockIdx.x / gridDim.x;
+  const long long end = total * (blockIdx.x + 1) / gridDim.x;
+  // runs: the column tiles k .. k + count - 1 of one token tile
+  Tile t;
+  int tile = 0, k = 0, count = 0;
+  auto next_run = [&]() {
+    while (pos < end) {
+      tile = (int)(pos / nbs);
+      k = (int)(pos % nbs);
+      count = (int)min((long long)(nbs - k), end - pos);
+      pos += count;
+      t = find_tile(p, tile);
+      if (t.id >= 0 || p.copy) return true;
+    }
+    return false;
+  };
+  uint32_t st = 0, ph = 0, i = 0, updates = 0;                   // stage ring; column tiles so far; runs with an adapter so far
+  auto advance = [&]() {
+    ++i;
+    if (++st == (uint32_t)STAGES) {
+      st = 0;
+      ph ^= 1u;
+    }
+  };
+  if (warp == LOAD_WARP) {
+    while (next_run()) {
+      if (lane == 0)
+        for (int q = 0; q < count && !abort_flag; ++q) {
+          mbar_spin(freed(st), ph ^ 1u, &abort_flag, p.status, W_FREE);
+          const uint32_t at = smem_st + st * S::STAGE;
+          mbar_expect_tx(full(st), ATOM + (t.id >= 0 ? RB * S::B_ATOM : 0u));
+          tma_load_2d(at, &map_base, (k + q) * BN, t.tok0, full(st));
+          if (t.id >= 0)
+            for (uint32_t r = 0; r < RB; ++r) tma_load_3d(at + ATOM + r * S::B_ATOM, &map_b, 64 * (int)r, (k + q) * BN, t.id, full(st));
+          advance();
+        }
+      __syncwarp();
+    }
+    if (lane == 0 && abort_flag)
+      for (uint32_t s = 0; s < (uint32_t)STAGES; ++s)
+        for (int q = 0; q < (1 << 16) && !mbar_try(full(s), (s < st ? ph : ph ^ 1u)); ++q) {}
+  } else if (warp == MMA_WARP) {
+    const uint32_t leader = elect_leader();
+    constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24) | ((uint32_t)(BN >> 3) << 17);
+    while (next_run()) {
+      if (t.id >= 0) mbar_spin(u_ready, updates++ & 1u, &abort_flag, p.status, W_U);
+      for (int x = 0; x < count && !abort_flag; ++x) {
+        const uint32_t a = i & 1u;
+        mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
+        if (i >= 2) mbar_spin(acc_free(a), ((i >> 1) - 1u) & 1u, &abort_flag, p.status, W_ACCFREE);
+        tc_fence_after();
+        if (t.id >= 0) {
+          const uint32_t bt = smem_st + st * S::STAGE + ATOM;
+          for (int q = 0; q < S::PIECES; ++q)
+            for (int s = 0; s < steps; ++s) {
+              const uint64_t da = smem_desc(smem_u + (uint32_t)(q * RB + (s >> 2)) * ATOM) + 2u * (uint32_t)(s & 3);
+              const uint64_t db = smem_desc(bt + (uint32_t)(s >> 2) * S::B_ATOM) + 2u * (uint32_t)(s & 3);
+              mma_ss(tmem + 64u * a, da, db, IDESC, q > 0 || s > 0, leader);
+            }
+        }
+        mma_commit(acc_full(a), leader);
+        mma_commit(freed(st), leader);
+        advance();
+      }
+    }
+  } else {
+    const int group = warp >> 2, row = (warp & 3) * 32 + lane;
+    uint32_t held = 0;                                           // the stage whose tile is still being stored, + 1
+    while (next_run()) {                    // (the groups meet at barriers: no warp leaves early, not even when a wait has given up)
+      if (t.id >= 0) {
+        // u of this token tile as an MMA operand.  (All MMAs that read the last one are done: both groups have had their results.)
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const int parts = (int)(((long long)(tile + 1) * kbs - 1) / len - (long long)tile * kbs / len) + 1;
+        const float sc = __ldg(p.scale + t.id);
+        const int quads = p.rank16 / 4;
+        for (int x = (int)threadIdx.x; x < BM * quads; x += 32 * EPI) {
+          const int r = x / quads, col = 4 * (x % quads);
+          float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r < t.rows) {
+            const float4* src = reinterpret_cast<const float4*>(p.part + ((long long)tile * p.parts * BM + r) * p.rank16 + col);
+            for (int q = 0; q < parts; ++q) {
+              const float4 v = __ldcg(src + (long long)q * BM * p.rank16 / 4);
+              u.x += v.x; u.y += v.y; u.z += v.z; u.w += v.w;
+            }
+          }
+          float w[4] = {u.x * sc, u.y * sc, u.z * sc, u.w * sc};
+          unsigned char* dst = smem_p + (col >> 6) * (int)ATOM + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 4) * 2;
+#pragma unroll
+          for (int q = 0; q < S::PIECES; ++q) {
+            const uint32_t lo = pack2(w[0], w[1]), hi = pack2(w[2], w[3]);
+            *reinterpret_cast<uint2*>(dst + q * RB * (int)ATOM) = make_uint2(lo, hi);
+            w[0] -= __uint_as_float(lo << 16);
+            w[1] -= __uint_as_float(lo & 0xFFFF0000u);
+            w[2] -= __uint_as_float(hi << 16);
+            w[3] -= __uint_as_float(hi & 0xFFFF0000u);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(u_ready);
+      }
+      for (int x = 0; x < count && !abort_flag; ++x) {
+        if ((int)(i & 1u) != group) {                            // the other group's tile
+          advance();
+          continue;
+        }
+        const uint32_t a = i & 1u;
+        mbar_spin(full(st), ph, &abort_flag, p.status, W_FULL);
+        mbar_spin(acc_full(a), (i >> 1) & 1u, &abort_flag, p.status, W_ACC);
+        __syncwarp();
+        tc_fence_after();
+        unsigned char* const box = smem_p + S::U_BYTES + st * S::STAGE;
+        if (t.id >= 0) {
+          uint32_t acc[BN];
+#pragma unroll
+          for (int q = 0; q < BN / 32; ++q) tmem_load32_nowait(tmem + ((uint32_t)((warp & 3) * 32) << 16) + 64u * a + 32u * q, acc + 32 * q);
+#pragma unroll
+          for (int q = 0; q < BN / 32; ++q) tmem_use32(acc + 32 * q);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_free(a));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            uint4* const at = reinterpret_cast<uint4*>(box + row * 128 + ((e ^ (row & 7)) << 4));
+            const uint4 v = *at;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (F32) w[q] = __float_as_uint(__uint_as_float(w[q]) + __uint_as_float(acc[(4 * e + q) % BN]));
+              else w[q] = pack2(__uint_as_float(w[q] << 16) + __uint_as_float(acc[(8 * e + 2 * q) % BN]),
+                                __uint_as_float(w[q] & 0xFFFF0000u) + __uint_as_float(acc[(8 * e + 2 * q + 1) % BN]));
+            }
+            *at = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else if (lane == 0) {
+          mbar_arrive(acc_free(a));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        const int col = (k + x) * BN, r0 = (warp & 3) * 32;
+        if (r0 + 32 <= t.rows) {
+          if (lane == 0) {
+            tma_store_2d(&map_y, col, t.tok0 + r0, smem_st + st * S::STAGE + (uint32_t)r0 * 128u);
+            // the stage before this one has been read by its store
+            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group.read 1;" ::: "memory");
+            if (held) mbar_arrive(freed(held - 1));
+            held = st + 1;
+          }
+        } else {                                                 // the segment ends inside the warp's rows
+          constexpr int EL = F32 ? 4 : 8;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int r = r0 + 4 * e + lane / 8, ch = lane % 8;
+            const uint4 v = *reinterpret_cast<const uint4*>(box + r * 128 + ((ch ^ (r & 7)) << 4));
+            if (r < t.rows && col + ch * EL < p.m)
+              *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(p.Y) + ((long long)(t.tok0 + r) * p.ldy + col + ch * EL) * (F32 ? 4 : 2)) = v;
+          }
+          __syncwarp();
+          if (lane == 0) {
+            if (held) {
+              asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              mbar_arrive(freed(held - 1));
+              held = 0;
+            }
+            mbar_arrive(freed(st));
+          }
+        }
+        advance();
+      }
+    }
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      if (held) mbar_arrive(freed(held - 1));
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(128) : "memory");
+}
+
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  return sms;
+}
+// Segments of 8 tokens or fewer on average: the few-token kernel.
+bool few_tokens(int n_tokens, int n_segs) { return n_tokens <= (long long)FEW * n_segs; }
+int most_tiles(int n_tokens, int n_segs) {
+  const long long most = (n_tokens + BM - 1) / BM + (long long)n_segs;
+  return (int)(most < n_tokens ? most : n_tokens);
+}
+// Stretches that a tile's k-blocks meet when the segments cover all tokens without gaps (shrink_stretch keeps the stretches
+// long enough for this number in every other case).
+int most_parts(int n_tokens, int kbs, int sms) {
+  const long long total = (long long)((n_tokens + BM - 1) / BM) * kbs, len = (total + sms - 1) / sms;
+  const long long parts = (kbs - 1 + len - 1) / len + 1;
+  return (int)(parts < kbs ? parts : kbs);
+}
+
+template <bool F32>
+cudaError_t launch_few(const Params& p, int tiles, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * ranks));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = Shape<F32, RB>::SMEM;
+  cfg.gridDim = dim3((unsigned)tiles * 8);
+  cfg.blockDim = dim3(FEW_THREADS);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)ranks;
+  attr[1].val.clusterDim.x = 8;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, adapter_kernel<F32, RB>, mx, ma, mb, mbase, p);
+  return cudaLaunchKernelEx(&cfg, few_kernel<F32>, p);
+}
+template <bool F32, int RB>
+cudaError_t launch(const Params& p, const CUtensorMap& mx, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mbase, const CUtensorMap& my,
+                   int sms, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(shrink_kernel<RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shrink<RB>::SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(expand_kernel<F32, RB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Expand<F32, RB>::SMEM);
+  if (e == cudaSuccess) e = launch_dependent(shrink_kernel<RB>, p.ctas, SHRINK_THREADS, Shrink<RB>::SMEM, st, mx, ma, p);
+  if (e == cudaSuccess) e = launch_dependent(expand_kernel<F32, RB>, sms, EXPAND_THREADS, Expand<F32, RB>::SMEM, st, mb, mbase, my, p);
+  return e;
 }
 
 }  // namespace adapter
@@ -495,9 +664,22 @@ cudaError_t launch(const Params& p, const CUtensorMap& mx, const CUtensorMap& ma
 
 using namespace oq;
 
-extern "C" int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const void* A_bf16, const void* B_bf16, int n_adapters,
+extern "C" {
+
+int oq_adapter_workspace_bytes(int n_tokens, int n_segs, int dim, int rank, size_t* bytes) {
+  if (!bytes) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_workspace_bytes: bytes is NULL");
+  *bytes = 0;
+  if (n_tokens < 0 || n_segs < 0 || dim <= 0 || rank <= 0) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_workspace_bytes: bad sizes");
+  if (n_tokens == 0 || n_segs == 0 || adapter::few_tokens(n_tokens, n_segs)) return OQ_OK;
+  const int kbs = (dim + adapter::KB - 1) / adapter::KB;
+  *bytes = (size_t)adapter::most_tiles(n_tokens, n_segs) * adapter::most_parts(n_tokens, kbs, adapter::sm_count()) * adapter::BM *
+           (size_t)((rank + 15) / 16 * 16) * sizeof(float);
+  return OQ_OK;
+}
+
+int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const void* A_bf16, const void* B_bf16, int n_adapters,
                               int rank, const float* scale, const int* seg_start, const int* seg_adapter, int n_segs, const void* base,
-                              int ldb, void* Y, int ldy, int m, int dtype, void* stream) {
+                              int ldb, void* Y, int ldy, int m, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (n_tokens < 0 || n_segs < 0) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_add: negative count");
   if (dim <= 0 || m <= 0 || rank <= 0 || n_adapters <= 0) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_add: sizes must be positive");
   if (dtype != OQ_BF16 && dtype != OQ_F32) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_add: unknown dtype");
@@ -531,9 +713,25 @@ extern "C" int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim
   p.copy = Y != base;
   p.status = device_status_word();
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_adapter_add: cannot allocate the device status word");
-  CUtensorMap mx, ma, mb, mbase;
-  const uint64_t size = dtype == OQ_F32 ? 4 : 2;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
+  if (adapter::few_tokens(n_tokens, n_segs)) {
+    const int tiles = adapter::most_tiles(n_tokens, n_segs);
+    e = dtype == OQ_F32 ? adapter::launch_few<true>(p, tiles, st) : adapter::launch_few<false>(p, tiles, st);
+    if (e != cudaSuccess) return cuda_fail(e, "oq_adapter_add");
+    return OQ_OK;
+  }
+  size_t need = 0;
+  const int rc = oq_adapter_workspace_bytes(n_tokens, n_segs, dim, rank, &need);
+  if (rc != OQ_OK) return rc;
+  if (need > workspace_bytes || !workspace || !aligned16(workspace))
+    return fail(OQ_ERR_NOMEM, "oq_adapter_add: workspace of " + std::to_string(need) + " bytes (16-byte aligned) needed");
+  const int sms = adapter::sm_count();
+  p.part = reinterpret_cast<float*>(workspace);
+  p.ctas = sms;
+  p.parts = adapter::most_parts(n_tokens, (dim + adapter::KB - 1) / adapter::KB, sms);
+  CUtensorMap mx, ma, mb, mbase, my;
+  const uint64_t size = dtype == OQ_F32 ? 4 : 2;
   {
     const uint64_t dims[2] = {(uint64_t)dim, (uint64_t)n_tokens}, strides[1] = {(uint64_t)ldx * 2};
     const uint32_t box[2] = {64, 128};
@@ -546,25 +744,26 @@ extern "C" int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim
   }
   if (e == cudaSuccess) {
     const uint64_t dims[3] = {(uint64_t)rank, (uint64_t)m, (uint64_t)n_adapters}, strides[2] = {(uint64_t)rank * 2, (uint64_t)m * rank * 2};
-    const uint32_t box[3] = {64, 64, 1};
+    const uint32_t box[3] = {64, dtype == OQ_F32 ? 32u : 64u, 1};
     e = encode_tensor_map_sw128(&mb, B_bf16, false, 3, dims, strides, box);
   }
+  const uint64_t dims[2] = {(uint64_t)m, (uint64_t)n_tokens};
   if (e == cudaSuccess) {
-    const uint64_t dims[2] = {(uint64_t)m, (uint64_t)n_tokens}, strides[1] = {(uint64_t)ldb * size};
+    const uint64_t strides[1] = {(uint64_t)ldb * size};
     const uint32_t box[2] = {(uint32_t)(128 / size), 128};
     e = encode_tensor_map_sw128(&mbase, base, dtype == OQ_F32, 2, dims, strides, box);
   }
+  if (e == cudaSuccess) {
+    const uint64_t strides[1] = {(uint64_t)ldy * size};
+    const uint32_t box[2] = {(uint32_t)(128 / size), 32};
+    e = encode_tensor_map_sw128(&my, Y, dtype == OQ_F32, 2, dims, strides, box);
+  }
   if (e != cudaSuccess) return cuda_fail(e, "oq_adapter_add (tensor map)");
-  // Tiles of 128 tokens, counted segment by segment (the segments' ends are on the device: an upper bound).  The cluster
-  // grows until there are two rounds of CTAs for every SM, two at a time.
-  const long long most = (n_tokens + adapter::BM - 1) / adapter::BM + (long long)n_segs;
-  const int tiles = (int)(most < n_tokens ? most : n_tokens);
-  int ranks = 1;
-  while (ranks < 8 && (long long)tiles * ranks < OQ_AD) ranks *= 2;
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool wide = rank > 64;
-  if (dtype == OQ_F32) e = wide ? adapter::launch<true, 2>(p, mx, ma, mb, mbase, tiles, ranks, st) : adapter::launch<true, 1>(p, mx, ma, mb, mbase, tiles, ranks, st);
-  else e = wide ? adapter::launch<false, 2>(p, mx, ma, mb, mbase, tiles, ranks, st) : adapter::launch<false, 1>(p, mx, ma, mb, mbase, tiles, ranks, st);
+  if (dtype == OQ_F32) e = wide ? adapter::launch<true, 2>(p, mx, ma, mb, mbase, my, sms, st) : adapter::launch<true, 1>(p, mx, ma, mb, mbase, my, sms, st);
+  else e = wide ? adapter::launch<false, 2>(p, mx, ma, mb, mbase, my, sms, st) : adapter::launch<false, 1>(p, mx, ma, mb, mbase, my, sms, st);
   if (e != cudaSuccess) return cuda_fail(e, "oq_adapter_add");
   return OQ_OK;
 }
+
+}  // extern "C"

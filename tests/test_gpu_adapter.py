@@ -104,6 +104,18 @@ def test_tokens_in_no_segment_are_left_alone():
     _verify(out[10:200], x[10:200], a, b, scale, base[10:200], [50, 140], [1, 0])
 
 
+def test_segments_that_leave_most_tokens_out():
+    """Few tiles where the sizes alone promise many: the products of a tile are cut into more parts."""
+    import torch
+    n, d, m = 20000, 4096, 192
+    x, a, b, scale, base = _inputs(n, d, m, 16, 2, torch.bfloat16, 5)
+    start = torch.tensor([700, 760, 960], dtype=torch.int32, device="cuda")
+    held = base.clone()
+    B.oq_adapter_add(x, a, b, scale, start, torch.tensor([1, 0], dtype=torch.int32, device="cuda"), held, out=held)
+    assert torch.equal(held[:700], base[:700]) and torch.equal(held[960:], base[960:])
+    _verify(held[700:960], x[700:960], a, b, scale, base[700:960], [60, 200], [1, 0])
+
+
 def test_other_segments_values_do_not_leak():
     """NaN and infinities in a neighbouring segment's tokens or base stay there, although its rows share a tile's loads."""
     import torch
@@ -141,5 +153,8 @@ def test_empty_and_refusals():
     assert code(x, a, b, scale, start, seg, base, out=base.float()) == 1
     wide = torch.zeros(4, 72, dtype=torch.bfloat16, device="cuda")
     assert code(wide[:, 4:68], a, b, scale, start, seg, base) == 3
+    many = _inputs(300, 64, 64, 16, 2, torch.bfloat16, 1)
+    small = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    assert code(*many[:4], *_tables([300], [0]), many[4], workspace=small) == 6
     odd = torch.zeros(4, 68, dtype=torch.bfloat16, device="cuda")
     assert code(x, a, b, scale, start, seg, odd[:, :64]) == 3
