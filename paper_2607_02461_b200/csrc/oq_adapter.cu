@@ -33,7 +33,7 @@ constexpr uint32_t ATOM = BM * 128;        // 128 rows of 128 bytes
 constexpr int EPI = 8;                     // epilogue warps of the expand kernel: two groups that take turns at column tiles
 constexpr int EXPAND_THREADS = (EPI + 2) * 32, SHRINK_THREADS = 6 * 32;
 constexpr int FEW = 8;                     // tokens the few-token kernel holds at a time
-constexpr int FEW_THREADS = 256;
+constexpr int FEW_THREADS = 256, FEW_RANKS = 8;      // and its cluster
 enum { W_FULL = 60, W_FREE = 61, W_U = 62, W_UFREE = 63, W_ACC = 64, W_ACCFREE = 65 };
 
 struct Params {
@@ -55,11 +55,6 @@ struct Params {
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
 __device__ __forceinline__ void cluster_sync() {
@@ -145,24 +140,27 @@ __device__ __forceinline__ long long shrink_stretch(const Params& p, long long t
 // Up to FEW rows of a segment: a 128-row MMA would multiply padding, and what bounds this case is reading the weights once.
 // CTA k of the cluster takes columns d0 .. d1 - 1 of the first product (a warp for each rank, lanes along d) and
 // columns m0 .. m1 - 1 of the second (a thread for each column); the shares of u meet in distributed shared memory.
-template <bool F32>
-__device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, int tok0, int rows, int id, uint32_t rank, uint32_t ranks, int d0, int d1,
-                                      int m0, int m1) {
+template <bool F32, int ROWS>
+__device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, int tok0, int rows, int id, int d0, int d1, int m0, int m1) {
   float* const part = reinterpret_cast<float*>(smem);            // [FEW][128] this CTA's share of A x
   float* const u = part + FEW * 128;                             // [FEW][128] scale * A x
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const __nv_bfloat16* const Bw = p.B + (long long)(id >= 0 ? id : 0) * p.m * p.rank;
   if (id >= 0) {
+    // the second product's weights travel to L2 while the first one runs
+    for (long long i = (long long)m0 * p.rank * 2 + 128 * threadIdx.x; i < (long long)m1 * p.rank * 2; i += 128 * FEW_THREADS)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(Bw) + i));
     const __nv_bfloat16* const A = p.A + (long long)id * p.rank * p.d;
     for (int r = warp; r < p.rank; r += FEW_THREADS / 32) {
-      float sum[FEW];
+      float sum[ROWS];
 #pragma unroll
-      for (int t = 0; t < FEW; ++t) sum[t] = 0.f;
+      for (int t = 0; t < ROWS; ++t) sum[t] = 0.f;
 #pragma unroll 2
       for (int k = d0 + 8 * lane; k < d1; k += 256) {            // (d is a multiple of 8)
         float w[8];
         unpack8(__ldg(reinterpret_cast<const uint4*>(A + (long long)r * p.d + k)), w);
 #pragma unroll
-        for (int t = 0; t < FEW; ++t)
+        for (int t = 0; t < ROWS; ++t)
           if (t < rows) {
             float x[8];
             unpack8(__ldg(reinterpret_cast<const uint4*>(p.X + (long long)(tok0 + t) * p.ldx + k)), x);
@@ -171,7 +169,7 @@ __device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, i
           }
       }
 #pragma unroll
-      for (int t = 0; t < FEW; ++t)
+      for (int t = 0; t < ROWS; ++t)
         if (t < rows) {
 #pragma unroll
           for (int o = 16; o; o >>= 1) sum[t] += __shfl_xor_sync(~0u, sum[t], o);
@@ -183,20 +181,23 @@ __device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, i
     for (int i = (int)threadIdx.x; i < rows * (p.rank / 4); i += FEW_THREADS) {
       const int t = i / (p.rank / 4), r = 4 * (i % (p.rank / 4));
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t k = 0; k < ranks; ++k) {
-        const float4 o = load_remote(map_rank(smem_u32(part + t * 128 + r), k));
-        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+      float4 o[FEW_RANKS];
+#pragma unroll
+      for (uint32_t k = 0; k < FEW_RANKS; ++k) o[k] = load_remote(map_rank(smem_u32(part + t * 128 + r), k));
+#pragma unroll
+      for (uint32_t k = 0; k < FEW_RANKS; ++k) {
+        v.x += o[k].x; v.y += o[k].y; v.z += o[k].z; v.w += o[k].w;
       }
       *reinterpret_cast<float4*>(u + t * 128 + r) = make_float4(v.x * sc, v.y * sc, v.z * sc, v.w * sc);
     }
     cluster_sync();                                              // (nobody leaves while its share is being read)
   }
-  const __nv_bfloat16* const Bw = p.B + (long long)(id >= 0 ? id : 0) * p.m * p.rank;
-#pragma unroll 2
+  constexpr int COLS = ROWS == 1 ? 4 : 1;                        // columns a thread has in flight
+#pragma unroll COLS
   for (int col = m0 + (int)threadIdx.x; col < m1; col += FEW_THREADS) {
-    float y[FEW];
+    float y[ROWS];
 #pragma unroll
-    for (int t = 0; t < FEW; ++t) {
+    for (int t = 0; t < ROWS; ++t) {
       y[t] = 0.f;
       if (t < rows) {
         const long long at = (long long)(tok0 + t) * p.ldb + col;
@@ -204,25 +205,25 @@ __device__ __forceinline__ void few_rows(const Params& p, unsigned char* smem, i
       }
     }
     if (id >= 0) {
-      float add[FEW];
+      float add[ROWS];
 #pragma unroll
-      for (int t = 0; t < FEW; ++t) add[t] = 0.f;
+      for (int t = 0; t < ROWS; ++t) add[t] = 0.f;
 #pragma unroll 2
       for (int r = 0; r < p.rank; r += 8) {
         float w[8];
         unpack8(__ldg(reinterpret_cast<const uint4*>(Bw + (long long)col * p.rank + r)), w);
 #pragma unroll
-        for (int t = 0; t < FEW; ++t)
+        for (int t = 0; t < ROWS; ++t)
           if (t < rows) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) add[t] = fmaf(w[e], u[t * 128 + r + e], add[t]);
           }
       }
 #pragma unroll
-      for (int t = 0; t < FEW; ++t) y[t] += add[t];
+      for (int t = 0; t < ROWS; ++t) y[t] += add[t];
     }
 #pragma unroll
-    for (int t = 0; t < FEW; ++t)
+    for (int t = 0; t < ROWS; ++t)
       if (t < rows) {
         const long long at = (long long)(tok0 + t) * p.ldy + col;
         if (F32) reinterpret_cast<float*>(p.Y)[at] = y[t];
@@ -236,14 +237,18 @@ __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant_
   __shared__ __align__(16) unsigned char smem[2 * FEW * 128 * 4];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t rank = cluster_rank(), ranks = cluster_size();
-  const Tile t = find_tile(p, (int)(blockIdx.x / ranks));        // (the same in every CTA of the cluster)
+  const uint32_t rank = cluster_rank();
+  const Tile t = find_tile(p, (int)blockIdx.x / FEW_RANKS);        // (the same in every CTA of the cluster)
   if (t.rows == 0 || (t.id < 0 && !p.copy)) return;
   const int kb = (p.d + 63) / 64, nb = (p.m + 63) / 64;
+  const int d0 = 64 * (kb * (int)rank / FEW_RANKS), d1 = min(64 * (kb * ((int)rank + 1) / FEW_RANKS), p.d);
+  const int m0 = 64 * (nb * (int)rank / FEW_RANKS), m1 = min(64 * (nb * ((int)rank + 1) / FEW_RANKS), p.m);
+  if (t.rows == 1) {
+    few_rows<F32, 1>(p, smem, t.tok0, 1, t.id, d0, d1, m0, m1);
+    return;
+  }
   for (int r = 0; r < t.rows; r += FEW)                          // (a segment that is not short after all: the weights come again)
-    few_rows<F32>(p, smem, t.tok0 + r, min(FEW, t.rows - r), t.id, rank, ranks, 64 * (int)((long long)kb * rank / ranks),
-                  min(64 * (int)((long long)kb * (rank + 1) / ranks), p.d), 64 * (int)((long long)nb * rank / ranks),
-                  min(64 * (int)((long long)nb * (rank + 1) / ranks), p.m));
+    few_rows<F32, FEW>(p, smem, t.tok0 + r, min(FEW, t.rows - r), t.id, d0, d1, m0, m1);
 }
 
 // ------------------------------------------------- shrink -------------------------------------------------
@@ -508,26 +513,38 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
         const int parts = (int)(((long long)(tile + 1) * kbs - 1) / len - (long long)tile * kbs / len) + 1;
         const float sc = __ldg(p.scale + t.id);
         const int quads = p.rank16 / 4;
-        for (int x = (int)threadIdx.x; x < BM * quads; x += 32 * EPI) {
-          const int r = x / quads, col = 4 * (x % quads);
-          float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (r < t.rows) {
-            const float4* src = reinterpret_cast<const float4*>(p.part + ((long long)tile * p.parts * BM + r) * p.rank16 + col);
-            for (int q = 0; q < parts; ++q) {
-              const float4 v = __ldcg(src + (long long)q * BM * p.rank16 / 4);
-              u.x += v.x; u.y += v.y; u.z += v.z; u.w += v.w;
-            }
-          }
-          float w[4] = {u.x * sc, u.y * sc, u.z * sc, u.w * sc};
-          unsigned char* dst = smem_p + (col >> 6) * (int)ATOM + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 4) * 2;
+        for (int x0 = (int)threadIdx.x; x0 < BM * quads; x0 += 4 * 32 * EPI) {       // 4 values a thread, their parts requested together
+          float4 u[4];
+          const float4* src[4];
 #pragma unroll
-          for (int q = 0; q < S::PIECES; ++q) {
-            const uint32_t lo = pack2(w[0], w[1]), hi = pack2(w[2], w[3]);
-            *reinterpret_cast<uint2*>(dst + q * RB * (int)ATOM) = make_uint2(lo, hi);
-            w[0] -= __uint_as_float(lo << 16);
-            w[1] -= __uint_as_float(lo & 0xFFFF0000u);
-            w[2] -= __uint_as_float(hi << 16);
-            w[3] -= __uint_as_float(hi & 0xFFFF0000u);
+          for (int e = 0; e < 4; ++e) {
+            const int x = x0 + e * 32 * EPI, r = x / quads;
+            u[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            src[e] = r < t.rows ? reinterpret_cast<const float4*>(p.part + ((long long)tile * p.parts * BM + r) * p.rank16 + 4 * (x % quads)) : nullptr;
+          }
+#pragma unroll 4
+          for (int q = 0; q < parts; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (src[e]) {
+                const float4 v = __ldcg(src[e] + (long long)q * BM * quads);
+                u[e].x += v.x; u[e].y += v.y; u[e].z += v.z; u[e].w += v.w;
+              }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int x = x0 + e * 32 * EPI, r = x / quads, col = 4 * (x % quads);
+            if (r >= BM) break;
+            float w[4] = {u[e].x * sc, u[e].y * sc, u[e].z * sc, u[e].w * sc};
+            unsigned char* dst = smem_p + (col >> 6) * (int)ATOM + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 4) * 2;
+#pragma unroll
+            for (int q = 0; q < S::PIECES; ++q) {
+              const uint32_t lo = pack2(w[0], w[1]), hi = pack2(w[2], w[3]);
+              *reinterpret_cast<uint2*>(dst + q * RB * (int)ATOM) = make_uint2(lo, hi);
+              w[0] -= __uint_as_float(lo << 16);
+              w[1] -= __uint_as_float(lo & 0xFFFF0000u);
+              w[2] -= __uint_as_float(hi << 16);
+              w[3] -= __uint_as_float(hi & 0xFFFF0000u);
+            }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -636,14 +653,14 @@ int most_parts(int n_tokens, int kbs, int sms) {
 template <bool F32>
 cudaError_t launch_few(const Params& p, int tiles, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)tiles * 8);
+  cfg.gridDim = dim3((unsigned)tiles * FEW_RANKS);
   cfg.blockDim = dim3(FEW_THREADS);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 8;
+  attr[1].val.clusterDim.x = FEW_RANKS;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
