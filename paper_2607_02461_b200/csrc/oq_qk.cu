@@ -73,6 +73,36 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
   }
 }
 
+// Two fp32 values in one instruction (the kernel is bound by instruction issue wherever it is not bound by memory).  A lane's
+// 8 coordinates are held as 4 pairs, so that a value and its partner in the turn are the same half of two pairs:
+// PAIRS layout (0 2) (4 6) (1 3) (5 7), HALVES layout (0 1) (2 3) (4 5) (6 7).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+template <bool HALVES>
+__device__ __forceinline__ void to_pairs(const float (&x)[8], float2 (&p)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    p[i] = HALVES ? make_float2(x[2 * i], x[2 * i + 1]) : make_float2(x[4 * (i & 1) + (i >> 1)], x[4 * (i & 1) + 2 + (i >> 1)]);
+}
+template <bool HALVES>
+__device__ __forceinline__ void from_pairs(const float2 (&p)[4], float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[HALVES ? 2 * i : 4 * (i & 1) + (i >> 1)] = p[i].x;
+    x[HALVES ? 2 * i + 1 : 4 * (i & 1) + 2 + (i >> 1)] = p[i].y;
+  }
+}
+
 template <typename T>
 struct Raw;
 template <>
@@ -201,6 +231,19 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     }
   };
 
+  // A CTA of a row norm stays on one side (the grid is even where there are two), and a warp on its heads: their weights
+  // are loaded once.
+  uint4 row_weights[MODE == HEAD ? 1 : ITERS];
+  if (MODE != HEAD) {
+    const Place first{0, (int)(unit % per_token)};
+    const int s = side_of(first), h0 = first_head(first, s);
+#pragma unroll
+    for (int i = 0; i < ITERS; ++i) {
+      row_weights[MODE == HEAD ? 0 : i] = make_uint4(0u, 0u, 0u, 0u);
+      if (p.side[s].w && h0 + i * per_iter < p.side[s].heads)
+        row_weights[MODE == HEAD ? 0 : i] = __ldg(reinterpret_cast<const uint4*>(p.side[s].w + (long long)(h0 + i * per_iter) * p.head_dim + c0));
+    }
+  }
   Place here{(int)(unit / per_token), (int)(unit % per_token)}, there = next(here);
   Raw<In> raw[ITERS], raw_next[ITERS];
   float2 turn[NP], turn_next[NP];
@@ -221,36 +264,45 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     const Side& sd = p.side[s];
     const int heads = sd.heads, head0 = first_head(here, s);
     const __nv_bfloat16* const weights = sd.w;
-    float A[8], Bc[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      A[e] = turn[HALVES ? e : e / 2].x;
-      Bc[e] = HALVES ? (upper ? turn[HALVES ? e : 0].y : -turn[HALVES ? e : 0].y) : ((e & 1) ? turn[e / 2].y : -turn[e / 2].y);
-    }
-    if (MODE == HEAD && weights) {
-      float w[8], wp[8];
-      unpack8(__ldg(reinterpret_cast<const uint4*>(weights + c0)), w);
-      if (HALVES) unpack8(__ldg(reinterpret_cast<const uint4*>(weights + 8 * (partner & (L - 1)))), wp);
+    // y = x * A + partner * B
+    float2 A[4], Bc[4];
+    {
+      float c[8], d[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        A[e] *= w[e];
-        Bc[e] *= HALVES ? wp[e] : w[e ^ 1];
+        c[e] = turn[HALVES ? e : e / 2].x;
+        d[e] = HALVES ? (upper ? turn[HALVES ? e : 0].y : -turn[HALVES ? e : 0].y) : ((e & 1) ? turn[e / 2].y : -turn[e / 2].y);
       }
+      if (MODE == HEAD && weights) {
+        float w[8], wp[8];
+        unpack8(__ldg(reinterpret_cast<const uint4*>(weights + c0)), w);
+        if (HALVES) unpack8(__ldg(reinterpret_cast<const uint4*>(weights + 8 * (partner & (L - 1)))), wp);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          c[e] *= w[e];
+          d[e] *= HALVES ? wp[e] : w[e ^ 1];
+        }
+      }
+      to_pairs<HALVES>(c, A);
+      to_pairs<HALVES>(d, Bc);
     }
     float inv = 1.f;
     if (MODE != HEAD) {
-      float sum = 0.f;
+      float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < ITERS; ++i) {
         if (head0 + i * per_iter >= heads) continue;
         float x[8];
+        float2 v[4];
         raw[i].get(x);
+        to_pairs<HALVES>(x, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+        for (int e = 0; e < 4; ++e) sum = fma2(v[e], v[e], sum);
       }
+      float all = sum.x + sum.y;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-      if (lane == 0) red[n & 1][warp] = sum;          // (two buffers: one barrier a token is enough)
+      for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(~0u, all, o);
+      if (lane == 0) red[n & 1][warp] = all;          // (two buffers: one barrier a token is enough)
       __syncthreads();
       float total = lane < (int)(blockDim.x >> 5) ? red[n & 1][lane] : 0.f;
 #pragma unroll
@@ -261,18 +313,16 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     const long long step = per_iter * sd.ldy_head;
 #pragma unroll
     for (int i = 0; i < ITERS; ++i) {
-      const int h = head0 + i * per_iter;
-      const bool have = h < heads;                   // lanes of another head may still need this lane's shuffles
+      const bool have = head0 + i * per_iter < heads;      // lanes of another head may still need this lane's shuffles
       float x[8];
+      float2 v[4], y[4];
       raw[i].get(x);                                 // (of a row that is not there: never stored, and its lanes meet only their own)
+      to_pairs<HALVES>(x, v);
       if (MODE == HEAD && p.norm) {
-        float sum = x[0] * x[0], odd = x[1] * x[1];
+        float2 sq = mul2(v[0], v[0]);
 #pragma unroll
-        for (int e = 2; e < 8; e += 2) {
-          sum = fmaf(x[e], x[e], sum);
-          odd = fmaf(x[e + 1], x[e + 1], odd);
-        }
-        sum += odd;
+        for (int e = 1; e < 4; ++e) sq = fma2(v[e], v[e], sq);
+        float sum = sq.x + sq.y;
         if (LANES) {
 #pragma unroll
           for (int o = LANES >> 1; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
@@ -283,27 +333,32 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
       }
       if (MODE != HEAD && weights) {
         float w[8];
-        if (have) {
-          unpack8(__ldg(reinterpret_cast<const uint4*>(weights + (long long)h * p.head_dim + c0)), w);
+        float2 wv[4];
+        unpack8(row_weights[MODE == HEAD ? 0 : i], w);
+        to_pairs<HALVES>(w, wv);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= inv * w[e];
-        }
+        for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], mul2(wv[e], make_float2(inv, inv)));
       } else if (MODE != HEAD || p.norm) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= inv;
+        for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], make_float2(inv, inv));
       }
-      float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float other = HALVES ? __shfl_sync(~0u, x[e], partner) : x[e ^ 1];
-        y[e] = fmaf(other, Bc[e], x[e] * A[e]);
+      for (int e = 0; e < 4; ++e) {
+        const float2 other = HALVES ? make_float2(__shfl_sync(~0u, v[e].x, partner), __shfl_sync(~0u, v[e].y, partner)) : v[e ^ 2];
+        y[e] = fma2(other, Bc[e], mul2(v[e], A[e]));
       }
       if (!all_turned) {                             // no part of a partner in what is not turned (an infinity stays one)
+        float z[8], u[8], a[8];
+        from_pairs<HALVES>(y, z);
+        from_pairs<HALVES>(v, u);
+        from_pairs<HALVES>(A, a);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (top[HALVES ? e : e / 2] < 0) y[e] = x[e] * A[e];
+          if (top[HALVES ? e : e / 2] < 0) z[e] = u[e] * a[e];
+        to_pairs<HALVES>(z, y);
       }
-      if (have) store8(dst, y);
+      from_pairs<HALVES>(y, x);
+      if (have) store8(dst, x);
       dst += step;
     }
     here = there;
@@ -331,7 +386,7 @@ cudaError_t launch(const Params& p, int mode, bool halves, long long most_ctas, 
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0);
   if (e != cudaSuccess) return e;
-  const long long slots = (long long)sms * (per_sm < 1 ? 1 : per_sm);
+  const long long slots = ((long long)sms * (per_sm < 1 ? 1 : per_sm)) & ~1ll;      // (even: a CTA of a row norm keeps its side)
   return launch_dependent(kernel, (int)(most_ctas < slots ? most_ctas : slots), threads, 0, st, p);
 }
 
