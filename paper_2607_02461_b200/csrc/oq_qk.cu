@@ -45,6 +45,7 @@ struct Side {
   void* Y;
   const __nv_bfloat16* w;
   long long ld_token, ld_head, ldy_token, ldy_head;
+  float inv_count;                  // 1 / values of a row
   int heads, chunks;                // chunks of ITERS * (256 / head_dim) heads
 };
 struct Params {
@@ -151,7 +152,7 @@ template <typename In, typename Out, int MODE, bool HALVES, int LANES>
 __global__ void __launch_bounds__(MODE == WIDE_ROW ? MAX_ROW_WARPS * 32 : (MODE == ROW ? ROW_WARPS : WARPS) * 32, MODE == WIDE_ROW ? 1 : (MODE == ROW ? 2 : 4))
 qk_norm_rope_kernel(const __grid_constant__ Params p) {
   constexpr int NP = HALVES ? 8 : 4;           // pairs a lane has a part in
-  __shared__ float red[2][MAX_ROW_WARPS];
+  __shared__ __align__(16) float red[2][MAX_ROW_WARPS];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -231,6 +232,10 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
     }
   };
 
+  if (MODE == ROW) {
+    if (threadIdx.x < 2 * ROW_WARPS) red[threadIdx.x / ROW_WARPS][threadIdx.x % ROW_WARPS] = 0.f;
+    __syncthreads();
+  }
   // A CTA of a row norm stays on one side (the grid is even where there are two), and a warp on its heads: their weights
   // are loaded once.
   uint4 row_weights[MODE == HEAD ? 1 : ITERS];
@@ -304,10 +309,16 @@ qk_norm_rope_kernel(const __grid_constant__ Params p) {
       for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(~0u, all, o);
       if (lane == 0) red[n & 1][warp] = all;          // (two buffers: one barrier a token is enough)
       __syncthreads();
-      float total = lane < (int)(blockDim.x >> 5) ? red[n & 1][lane] : 0.f;
+      float total;
+      if (MODE == ROW) {                              // (places of warps that do not exist hold zero)
+        const float4 a = *reinterpret_cast<const float4*>(&red[n & 1][0]), b = *reinterpret_cast<const float4*>(&red[n & 1][4]);
+        total = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+      } else {
+        total = lane < (int)(blockDim.x >> 5) ? red[n & 1][lane] : 0.f;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-      inv = rsqrtf(total / (float)(heads * p.head_dim) + p.eps);
+        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+      }
+      inv = rsqrtf(fmaf(total, sd.inv_count, p.eps));
     }
     Out* dst = reinterpret_cast<Out*>(sd.Y) + here.token * sd.ldy_token + head0 * sd.ldy_head + c0;
     const long long step = per_iter * sd.ldy_head;
@@ -513,6 +524,7 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
     d.ld_token = in[s]->ld_token; d.ld_head = in[s]->ld_head;
     d.ldy_token = in[s]->ldy_token; d.ldy_head = in[s]->ldy_head;
     d.heads = in[s]->n_heads;
+    d.inv_count = 1.f / ((float)d.heads * (float)head_dim);
     d.chunks = (d.heads + per_chunk - 1) / per_chunk;
   }
   if (n_tokens == 0) return OQ_OK;
