@@ -40,7 +40,7 @@ constexpr int THREADS = 384;              // 8 softmax warps; the load warp, two
 constexpr int LOAD_WARP = 8, MMA_WARP = 9;
 constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
-constexpr int MAX_SPLITS = 32;
+constexpr int MAX_PARTS = 32;
 constexpr float SLACK = 8.f;              // powers stay below 2^8
 enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46 };
 
@@ -61,16 +61,21 @@ struct Params {
   __nv_bfloat16* out;
   long long ldo, hdo;
   float* lse;                             // [heads][total_q] or NULL
-  float* part_o;                          // [splits][heads][total_q][D]: unnormalised sums, scaled to a sum of one
-  float* part_lse;                        // [splits][heads][total_q], base 2
+  float* part_o;                          // [parts][heads][total_q][D]: sums scaled to weights that add up to one
+  float* part_lse;                        // [parts][heads][total_q], base 2
   const int *q_start, *k_start;           // n_seqs + 1, or NULL: one sequence
-  int total_q, total_k, n_seqs, heads, group, splits;
+  int total_q, total_k, n_seqs, heads, group;
+  int splits;                             // runs that an item's key tiles are cut into
+  int dual;                               // see below
+  int parts;                              // results of a row to be joined: splits, twice as many when dual
   int left, right, sinks;
   float scale, scale_log2;
   int* status;
 };
 
-// What one CTA works on at a time: up to 256 queries of one head, and a run of their key tiles.
+// What one CTA works on at a time: a block of queries of one head and a run of their key tiles.  A block is 256 queries, one
+// tile of 128 after the other.  With few queries (dual) it is 128, both query tiles hold the same ones, and each takes
+// every other key tile: two chains S -> softmax -> P V run where one would leave everything waiting for the other stages.
 template <int BN>
 struct Item {
   int q_base, k_base;      // first query and key of the sequence
@@ -79,7 +84,7 @@ struct Item {
   int rows0, rows1;        // queries of the two tiles
   int head, split;
   int tiles, n_sink, win0; // key tiles: j < n_sink -> j, else win0 + j - n_sink
-  int first;               // first tile of this split
+  int first;               // first tile of this run
   __device__ __forceinline__ int key0(int j) const {
     j += first;
     return BN * (j < n_sink ? j : win0 + (j - n_sink));
@@ -95,7 +100,10 @@ __device__ __forceinline__ int row_lo(const Params& p, const Item<BN>& it, int q
   return p.left < 0 ? 0 : max(0, qi + it.nk - it.nq - p.left);
 }
 
-// prefix[s]: blocks of 256 queries before sequence s
+__device__ __forceinline__ int block_rows(const Params& p) { return p.dual ? BM : 2 * BM; }
+// whether query tile t takes step j of an item that it has rows of
+__device__ __forceinline__ bool takes(const Params& p, int t, int j) { return !p.dual || (j & 1) == t; }
+// prefix[s]: blocks of queries before sequence s
 template <int BN>
 __device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix, int index) {
   Item<BN> it;
@@ -120,10 +128,10 @@ __device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix
     it.nq = p.total_q;
     it.nk = p.total_k;
   }
-  it.q0 = 2 * BM * b;
-  const int rows = min(2 * BM, it.nq - it.q0);
+  it.q0 = block_rows(p) * b;
+  const int rows = min(block_rows(p), it.nq - it.q0);
   it.rows0 = min(rows, BM);
-  it.rows1 = rows - it.rows0;
+  it.rows1 = p.dual ? rows : rows - it.rows0;
   const int hi = row_hi(p, it, it.q0 + rows - 1), lo = row_lo(p, it, it.q0);
   it.tiles = it.n_sink = it.win0 = 0;
   if (hi >= 0) {
@@ -167,7 +175,7 @@ __device__ __forceinline__ uint32_t ones_below(int n) {
 
 // One row again, key by key over the keys it sees, by a whole warp (each lane holds D / 32 coordinates).
 template <int D>
-__device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>& it, int qi) {
+__device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>& it, int qi, int t) {
   constexpr int BN = Shape<D>::BN;
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 31, hk = it.head / p.group;
@@ -179,6 +187,7 @@ __device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>
     o[i] = 0.f;
   }
   for (int j = 0; j < it.tiles; ++j) {
+    if (!takes(p, t, j)) continue;
     const int k0 = it.key0(j);
     for (int key = k0; key < k0 + BN && key <= hi; ++key) {
       if (key < lo && key >= p.sinks) continue;
@@ -201,8 +210,8 @@ __device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>
   }
   const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
   const long long row = (long long)it.head * p.total_q + it.q_base + qi;
-  if (p.splits > 1) {
-    const long long at = (long long)it.split * p.heads * p.total_q + row;
+  if (p.parts > 1) {
+    const long long at = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + row;
 #pragma unroll
     for (int i = 0; i < N; ++i) p.part_o[at * D + lane * N + i] = o[i] * inv;
     if (lane == 0) p.part_lse[at] = lse2;
@@ -248,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     }
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(kv_full(s), 1);
-      mbar_init(kv_free(s), 2);           // both mma warps
+      mbar_init(kv_free(s), 2);           // both mma warps, also when one of them does not use the slot (see below)
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -272,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           const int b = min(max(__ldg(p.q_start + s), 0), p.total_q);
           n = min(max(__ldg(p.q_start + s + 1), b), p.total_q) - b;
         }
-        n = (n + 2 * BM - 1) / (2 * BM);
+        n = (n + block_rows(p) - 1) / block_rows(p);
       }
       int sum = n;
 #pragma unroll
@@ -333,13 +342,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       const Item<BN> it = make_item<BN>(p, prefix, i);
       const int rows = t ? it.rows1 : it.rows0;
       if (rows == 0) continue;
-      const int r0 = it.q0 + t * BM, qi = r0 + row;
+      const int r0 = it.q0 + (p.dual ? 0 : t * BM), qi = r0 + row;
       const bool mine = row < rows, idle = (warp & 3) * 32 >= rows;      // idle: none of the warp's rows exists
       const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
       const int full_hi = row_hi(p, it, r0), full_lo = row_lo(p, it, r0 + rows - 1);     // what every row of the tile sees
       float m = -INFINITY, l = 0.f;
-      const bool turns = it.rows1 > quarter * 32;       // both warps have rows (tile 0 is full where tile 1 has any)
-      for (int j = 0; j < it.tiles; ++j, ++steps) {
+      const bool turns = !p.dual && it.rows1 > quarter * 32;       // both warps have rows (tile 0 is full where tile 1 has any)
+      const int j0 = p.dual ? t : 0, jd = p.dual ? 2 : 1;
+      for (int j = j0; j < it.tiles; j += jd, ++steps) {
         const int k0 = it.key0(j);
         warp_wait(s_full(t), steps & 1, W_S);
         if (idle) {                             // (O's rows are never read: whatever P holds there may stay)
@@ -375,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           for (int e = 2; e < BN / 4; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
         }
         const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
-        if (j == 0) {
+        if (j == j0) {
           m = mn;
         } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
           // (S_t of this key tile is there, so O_t holds the tiles before it and nothing is writing it)
@@ -420,10 +430,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       // ------------------------------------------- the item's result -------------------------------------------
-      if (it.tiles > 0) warp_wait(o_done(t), items++ & 1, W_O);
+      const bool any = it.tiles > j0;
+      if (any) warp_wait(o_done(t), items++ & 1, W_O);
       if (idle) continue;
       uint32_t o[D];
-      if (it.tiles > 0) {
+      if (any) {
         tc_fence_after();
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) tmem_load32_nowait(col_o + 32u * q, o + 32 * q);
@@ -446,8 +457,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c, log2f(l));
       const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
       if (mine && !bad) {
-        if (p.splits > 1) {
-          const long long at = (long long)it.split * p.heads * p.total_q + out_row;
+        if (p.parts > 1) {
+          const long long at = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + out_row;
           float4* dst = reinterpret_cast<float4*>(p.part_o + at * D);
 #pragma unroll
           for (int e = 0; e < D / 4; ++e)
@@ -471,7 +482,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       while (again) {
         const int r = __ffs(again) - 1;
         again &= again - 1;
-        exact_row<D>(p, it, r0 + (warp & 3) * 32 + r);
+        exact_row<D>(p, it, r0 + (warp & 3) * 32 + r, t);
       }
     }
   } else {
@@ -495,12 +506,13 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         };
         auto load_k = [&](const Step& s) {
           if (s.j == 0) {
-            for (int t = 0; t < (s.it.rows1 > 0 ? 2 : 1); ++t) {
+            for (int t = 0; t < 2; ++t) {
+              if (t == 1 && (s.it.rows1 == 0 || (p.dual && s.it.tiles == 1))) continue;      // no step of this tile
               if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
               ++q_use[t];
               mbar_expect_tx(q_full(t), S::Q_TILE);
               for (uint32_t a = 0; a < S::ATOMS; ++a)
-                tma_load_3d(smem_q + (uint32_t)t * S::Q_TILE + a * S::Q_ATOM, &map_q, 64 * (int)a, s.it.head, s.it.q_base + s.it.q0 + t * BM, q_full(t));
+                tma_load_3d(smem_q + (uint32_t)t * S::Q_TILE + a * S::Q_ATOM, &map_q, 64 * (int)a, s.it.head, s.it.q_base + s.it.q0 + (p.dual ? 0 : t * BM), q_full(t));
             }
           }
           load_kv(s, &map_k);
@@ -531,11 +543,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);      // V is N-major
       const uint32_t columns = tmem + 256u * (uint32_t)t;
       uint32_t q_use = 0, p_use = 0;
-      auto active = [&](const Step& s) { return t == 0 || s.it.rows1 > 0; };
+      auto active = [&](const Step& s) { return (t == 0 || s.it.rows1 > 0) && takes(p, t, s.j); };
+      const int jd = p.dual ? 2 : 1, j0 = p.dual ? t : 0;        // this tile's steps of an item
       auto do_s = [&](const Step& s) {
+        // (Both warps see every slot filled and free it, whether they use it or not: a wait tells phases apart by their
+        // parity alone, so no warp may get a whole round ahead of a slot or behind it.)
         mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
-        if (active(s)) {
-          if (s.j == 0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q);
+        if (!active(s)) {
+          if (leader) mbar_arrive(kv_free(slot));
+        } else {
+          if (s.j == j0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q);
           tc_fence_after();
           const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::Q_TILE), b = smem_desc(smem_kv + slot * S::KV_TILE);
 #pragma unroll
@@ -544,15 +561,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
                    IDESC_S, k > 0, leader);
           mma_commit(s_full(t), leader);
           mma_commit(kv_free(slot), leader);
-          if (s.j + 1 == s.it.tiles) mma_commit(q_free(t), leader);       // the query tile's last S
-        } else if (leader) {
-          mbar_arrive(kv_free(slot));
+          if (s.j + jd >= s.it.tiles) mma_commit(q_free(t), leader);       // the query tile's last S
         }
         advance();
       };
       auto do_o = [&](const Step& s) {
         mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
-        if (active(s)) {
+        if (!active(s)) {
+          if (leader) mbar_arrive(kv_free(slot));
+        } else {
           mbar_spin(p_part(t), p_use & 1, &abort_flag, p.status, W_P);
           tc_fence_after();
           const uint64_t b = smem_desc_mn(smem_kv + slot * S::KV_TILE, S::KV_ATOM, 1024);
@@ -562,12 +579,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
               mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P);
               tc_fence_after();
             }
-            mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > 0 || k > 0, leader);
+            mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > j0 || k > 0, leader);
           }
-          if (s.j + 1 == s.it.tiles) mma_commit(o_done(t), leader);
+          if (s.j + jd >= s.it.tiles) mma_commit(o_done(t), leader);
           mma_commit(kv_free(slot), leader);
-        } else if (leader) {
-          mbar_arrive(kv_free(slot));
         }
         advance();
       };
@@ -589,7 +604,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// Joins the splits of a row: weights 2^(lse_i - max) over their sum.  One warp per (token, head).
+// Joins the parts of a row: weights 2^(lse_i - max) over their sum.  One warp per (token, head).
 template <int D>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ Params p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -599,7 +614,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   const long long rows = (long long)p.heads * p.total_q;
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
-  const float mine = lane < p.splits ? p.part_lse[lane * rows + row] : -INFINITY;
+  const float mine = lane < p.parts ? p.part_lse[lane * rows + row] : -INFINITY;
   float top = mine;
 #pragma unroll
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
@@ -610,7 +625,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   float o[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] = 0.f;
-  for (int s = 0; s < p.splits; ++s) {
+  for (int s = 0; s < p.parts; ++s) {
     const float ws = __shfl_sync(~0u, w, s);
     if (ws == 0.f) continue;                       // an empty split, or one whose share is below 2^-126
     const float* src = p.part_o + (s * rows + row) * D + lane * N;
@@ -631,28 +646,35 @@ int sm_count() {
   return sms;
 }
 
-// How many parts the keys of a block of queries are cut into.  Blocks of 256 queries times heads are the items; when
-// they do not fill the SMs, or fill them unevenly, each is cut along its keys.  The time of a cut is estimated as
-// (rounds of items over the SMs) x (key tiles of an item + 3, what an item costs besides its tiles).
-int choose_splits(long long total_q, long long total_k, int n_seqs, int heads, int left, int right, int sinks, int sms) {
-  const long long blocks = (total_q + 2LL * BM * n_seqs - 1) / (2 * BM) ;      // between all full and one more per sequence
-  const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
+// dual where the sequences have at most 128 queries on average, and keys enough for both chains.
+// Items (blocks of queries times heads) that do not fill the SMs, or fill them unevenly, are cut along their keys.  The
+// time of a cut is estimated as (rounds of items over the SMs) x (steps of an item + what it costs besides, in steps); a
+// step of a dual item is half as long as one of two query tiles.  (One query against 32760 keys of 40 heads: 3 runs
+// each, one round, 114 us; 5, two rounds, 145 us; 7 121 us; 11 128 us.  The floor is 104 us.)
+struct Plan {
+  int splits, dual, parts;
+};
+Plan make_plan(long long total_q, long long total_k, int n_seqs, int heads, int left, int right, int sinks, int sms) {
+  if (total_q == 0 || total_k == 0) return Plan{1, 0, 1};
   long long keys = total_k / n_seqs;
   if (left >= 0 && right >= 0) {
     const long long window = (long long)left + right + 2 * BM + sinks;
     if (window < keys) keys = window;
   }
-  const long long tiles = (keys + 99) / 100;            // (80 or 128 keys each)
-  if (items >= 2LL * sms) return 1;
-  int best = 1;
+  const long long tiles = (keys + 127) / 128;
+  Plan best{1, total_q <= (long long)BM * n_seqs && tiles >= 4, 1};
+  const long long rows = best.dual ? BM : 2 * BM, blocks = (total_q + rows / 2 * n_seqs + rows / 2 - 1) / rows;
+  const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
   double best_cost = 1e30;
-  for (int n = 1; n <= MAX_SPLITS && (n == 1 || n * 2 <= tiles); ++n) {
-    const double cost = (double)((items * n + sms - 1) / sms) * (double)((tiles + n - 1) / n + 3) + (n > 1 ? 4.0 : 0.0);
+  for (int n = 1; n <= MAX_PARTS / (best.dual ? 2 : 1) && (n == 1 || n * 4 <= tiles) && (n == 1 || items < 2LL * sms); ++n) {
+    const double steps = (double)((tiles + n - 1) / n) * (best.dual ? 0.5 : 1.0);
+    const double cost = (double)((items * n + sms - 1) / sms) * (steps + (best.dual ? 6.0 : 3.0)) + (n > 1 ? 3.0 : 0.0);
     if (cost < best_cost * 0.97) {
       best_cost = cost;
-      best = n;
+      best.splits = n;
     }
   }
+  best.parts = best.splits * (best.dual ? 2 : 1);
   return best;
 }
 
@@ -661,9 +683,10 @@ cudaError_t launch(const Params& p, const CUtensorMap& mq, const CUtensorMap& mk
   // (the attribute belongs to the device that is current, so it is set every time)
   cudaError_t e = cudaFuncSetAttribute(attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D>::SMEM);
   if (e != cudaSuccess) return e;
-  const long long most = ((long long)(p.total_q + 2 * BM - 1) / (2 * BM) + p.n_seqs) * p.heads * p.splits;
+  const int rows = p.dual ? BM : 2 * BM;
+  const long long most = ((long long)(p.total_q + rows - 1) / rows + p.n_seqs) * p.heads * p.splits;
   e = launch_dependent(attention_kernel<D>, (int)(most < sms ? most : sms), THREADS, Shape<D>::SMEM, st, mq, mk, mv, p);
-  if (e != cudaSuccess || p.splits == 1) return e;
+  if (e != cudaSuccess || p.parts == 1) return e;
   return launch_dependent(attention_join_kernel<D>, (int)(((long long)p.heads * p.total_q + 7) / 8), 256, 0, st, p);
 }
 
@@ -688,9 +711,8 @@ static int attention_check(const oq_attention_args* a) {
   return OQ_OK;
 }
 
-static int attention_splits(const oq_attention_args* a) {
-  if (a->total_q == 0 || a->total_k == 0) return 1;
-  return attn::choose_splits(a->total_q, a->total_k, a->n_seqs, a->n_heads, a->left, a->right, a->sinks, attn::sm_count());
+static attn::Plan attention_plan(const oq_attention_args* a) {
+  return attn::make_plan(a->total_q, a->total_k, a->n_seqs, a->n_heads, a->left, a->right, a->sinks, attn::sm_count());
 }
 
 extern "C" {
@@ -700,7 +722,7 @@ int oq_attention_workspace_bytes(const oq_attention_args* a, size_t* bytes) {
   *bytes = 0;
   const int rc = attention_check(a);
   if (rc != OQ_OK) return rc;
-  const int n = attention_splits(a);
+  const int n = attention_plan(a).parts;
   if (n > 1) *bytes = (size_t)n * a->n_heads * (size_t)a->total_q * (size_t)(a->head_dim + 4) * sizeof(float);
   return OQ_OK;
 }
@@ -716,7 +738,10 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   if (a->ldq_token < 0 || a->ldq_head < 0 || a->ldk_token < 0 || a->ldk_head < 0 || a->ldv_token < 0 || a->ldv_head < 0)
     return fail(OQ_ERR_INVALID_ARG, "oq_attention: strides must not be negative");
   attn::Params p = {};
-  p.splits = attention_splits(a);
+  const attn::Plan plan = attention_plan(a);
+  p.splits = plan.splits;
+  p.dual = plan.dual;
+  p.parts = plan.parts;
   size_t need = 0;
   rc = oq_attention_workspace_bytes(a, &need);
   if (rc != OQ_OK) return rc;
@@ -732,7 +757,7 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.ldo = a->ldo_token; p.hdo = a->ldo_head;
   p.lse = a->lse;
   p.part_o = reinterpret_cast<float*>(workspace);
-  p.part_lse = p.part_o + (size_t)p.splits * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim;
+  p.part_lse = p.part_o + (size_t)p.parts * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim;
   p.q_start = a->q_start; p.k_start = a->k_start;
   p.total_q = a->total_q; p.total_k = a->total_k;
   p.n_seqs = a->n_seqs; p.heads = a->n_heads; p.group = a->n_heads / a->n_kv_heads;
