@@ -92,12 +92,6 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _raw_stream(device_index):
-    """The current stream's handle without a stream object: 0.2 us instead of 3.5, which counts in calls of a few us."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device_index)
-
-
 class Codebook:
     """Owns an oq_codebook handle."""
 
@@ -398,29 +392,44 @@ def _dtype_code(dtype, what):
     raise OqError(1, f"{what}: bf16 or fp32 expected, got {dtype}")
 
 
+# The calls below are short on the GPU at small sizes (3 to 7 us), so their marshalling looks at every property of a tensor
+# once, and outputs that are allocated here are not looked at again.
 _QK_SIDE = struct.Struct("@PqqiPPqq")               # oq_qk_side
 NORMS = {"none": 0, "head": 1, "row": 2}
 
 
-def _qk_side(X, w, Y, norm, n, head_dim, dtype):
-    """Checks one side of oq_qk_norm_rope and packs its oq_qk_side."""
-    import torch
+def _qk_side(torch, X, w, Y, norm, n, head_dim, dtype, out_dtype):
+    """Checks one side of oq_qk_norm_rope, allocates its output if there is none, and packs its oq_qk_side."""
     shape = X.shape
     if len(shape) != 3 or shape[0] != n or shape[2] != head_dim or X.dtype != dtype:
         raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim] of one T, head_dim and type")
-    if Y.shape != shape:
-        raise OqError(1, "oq_qk_norm_rope: outputs must have the inputs' shape")
-    (lt, lh, lc), (yt, yh, yc) = X.stride(), Y.stride()
-    if (lc != 1 or yc != 1) and n and shape[1]:
-        raise OqError(3, "oq_qk_norm_rope: the coordinates of a head must be adjacent")
     heads = shape[1]
-    if w is not None and (w.dtype != torch.bfloat16 or w.numel() != (head_dim if norm == "head" else heads * head_dim) or not w.is_contiguous()):
-        raise OqError(1, "oq_qk_norm_rope: weights must be contiguous bf16, one for each normed coordinate")
-    if n == 1:                                       # torch leaves the stride of a single row or head free
-        lt = yt = 0
+    lt, lh, lc = X.stride()
+    if Y is None:
+        Y = X.new_empty(shape) if out_dtype is None else X.new_empty(shape, dtype=out_dtype)
+        yt, yh = heads * head_dim, head_dim
+    else:
+        if Y.shape != shape:
+            raise OqError(1, "oq_qk_norm_rope: outputs must have the inputs' shape")
+        yt, yh, yc = Y.stride()
+        if yc != 1 and n:
+            lc = yc
+        if n == 1:                                   # torch leaves the stride of a single row or head free
+            yt = 0
+        if heads == 1:
+            yh = 0
+    if lc != 1 and n:
+        raise OqError(3, "oq_qk_norm_rope: the coordinates of a head must be adjacent")
+    if n == 1:
+        lt = 0
     if heads == 1:
-        lh = yh = 0
-    return _QK_SIDE.pack(X.data_ptr(), lt, lh, heads, w.data_ptr() if w is not None else 0, Y.data_ptr(), yt, yh)
+        lh = 0
+    at = 0
+    if w is not None:
+        if w.dtype != torch.bfloat16 or w.numel() != (head_dim if norm == "head" else heads * head_dim) or not w.is_contiguous():
+            raise OqError(1, "oq_qk_norm_rope: weights must be contiguous bf16, one for each normed coordinate")
+        at = w.data_ptr()
+    return Y, _QK_SIDE.pack(X.data_ptr(), lt, lh, heads, at, Y.data_ptr(), yt, yh)
 
 
 def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", eps=1e-6, out_q=None, out_k=None, out_dtype=None):
@@ -431,20 +440,21 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
     shape, dtype = Q.shape, Q.dtype
     if len(shape) != 3:
         raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim]")
-    n, head_dim = shape[0], shape[2]
-    if norm not in NORMS:
+    n, _, head_dim = shape
+    norm_code = NORMS.get(norm)
+    if norm_code is None:
         raise OqError(1, f"oq_qk_norm_rope: norm must be one of {sorted(NORMS)}")
-    x_code = _dtype_code(dtype, "oq_qk_norm_rope")
-    if out_q is None:
-        out_q = Q.new_empty(shape) if out_dtype is None else Q.new_empty(shape, dtype=out_dtype)
-    y_code = _dtype_code(out_q.dtype, "oq_qk_norm_rope")
-    q_side, k_side = _qk_side(Q, wq, out_q, norm, n, head_dim, dtype), None
+    x_code = y_code = _dtype_code(dtype, "oq_qk_norm_rope")
+    out_q, q_side = _qk_side(torch, Q, wq, out_q, norm, n, head_dim, dtype, out_dtype)
+    if out_q.dtype != dtype:
+        y_code = _dtype_code(out_q.dtype, "oq_qk_norm_rope")
+    k_side = None
     if K is not None:
-        if out_k is None:
-            out_k = K.new_empty(K.shape) if out_dtype is None else K.new_empty(K.shape, dtype=out_dtype)
+        out_k, k_side = _qk_side(torch, K, wk, out_k, norm, n, head_dim, dtype, out_dtype)
         if out_k.dtype != out_q.dtype:
             raise OqError(1, "oq_qk_norm_rope: outputs must have one type")
-        k_side = _qk_side(K, wk, out_k, norm, n, head_dim, dtype)
+    else:
+        out_k = None
     ldpos, table, at = 0, None, None
     if rope is not None:
         axes = len(rope.axis_dims)
@@ -456,9 +466,11 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
         if n <= 1:
             ldpos = axes
         table, at = rope.handle, pos.data_ptr()
-    _check(lib().oq_qk_norm_rope(q_side, k_side, n, head_dim, table, at, ldpos, NORMS[norm], eps, x_code, y_code,
-                                 _raw_stream(Q.get_device())))
-    return out_q, out_k if K is not None else None
+    code = (_lib or lib()).oq_qk_norm_rope(q_side, k_side, n, head_dim, table, at, ldpos, norm_code, eps, x_code, y_code,
+                                           torch._C._cuda_getCurrentRawStream(Q.get_device()))
+    if code:
+        _check(code)
+    return out_q, out_k
 
 
 _ATTENTION_ARGS = struct.Struct("@PPPqqqqqqPqqPPPiiiiiiiiif")      # oq_attention_args
@@ -478,21 +490,27 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     if Q.dtype != bf16 or K.dtype != bf16 or V.dtype != bf16:
         raise OqError(1, "oq_attention: bf16 expected")
     tq, heads, head_dim = qs
-    tk, kv_heads = ks[0], ks[1]
-    n_seqs, starts = 1, [0, 0]
+    tk, kv_heads, _ = ks
+    n_seqs, q_at, k_at = 1, 0, 0
     if q_start is not None or k_start is not None:
-        for i, t in enumerate((q_start, k_start)):
+        for t in (q_start, k_start):
             if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
                 raise OqError(1, "oq_attention: q_start and k_start must both be contiguous CUDA int32 [sequences + 1]")
-            n_seqs, starts[i] = t.shape[0] - 1, t.data_ptr()
-        if q_start.shape[0] != k_start.shape[0]:
+        n_seqs = len(q_start) - 1
+        if len(k_start) != n_seqs + 1:
             raise OqError(1, "oq_attention: q_start and k_start must have one length")
+        q_at, k_at = q_start.data_ptr(), k_start.data_ptr()
+    (qt, qh, qc), (kt, kh, kc), (vt, vh, vc) = Q.stride(), K.stride(), V.stride()
     if out is None:
         out = Q.new_empty(qs)
-    elif out.shape != qs or out.dtype != bf16:
-        raise OqError(1, "oq_attention: out must be bf16, shaped like Q")
-    (qt, qh, qc), (kt, kh, kc), (vt, vh, vc), (ot, oh, oc) = Q.stride(), K.stride(), V.stride(), out.stride()
-    if (qc != 1 or oc != 1) and Q.numel() or (kc != 1 or vc != 1) and K.numel():
+        ot, oh = heads * head_dim, head_dim
+    else:
+        if out.shape != qs or out.dtype != bf16:
+            raise OqError(1, "oq_attention: out must be bf16, shaped like Q")
+        ot, oh, oc = out.stride()
+        if oc != 1 and tq:
+            qc = oc
+    if qc != 1 and tq or (kc != 1 or vc != 1) and tk:
         raise OqError(3, "oq_attention: the coordinates of a head must be adjacent")
     if tq <= 1:                                      # torch leaves the stride of a single row or head free
         qt = ot = 0
@@ -502,20 +520,28 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
         kt = vt = 0
     if kv_heads == 1:
         kh = vh = 0
-    lse = torch.empty((heads, tq), dtype=torch.float32, device=Q.device) if want_lse else None
-    args = _ATTENTION_ARGS.pack(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qt, qh, kt, kh, vt, vh, out.data_ptr(), ot, oh,
-                                lse.data_ptr() if want_lse else 0, starts[0], starts[1], n_seqs, tq, tk, heads, kv_heads, head_dim,
-                                left, right, sinks, scale)
+    lse, lse_at = None, 0
+    if want_lse:
+        lse = Q.new_empty((heads, tq), dtype=torch.float32)
+        lse_at = lse.data_ptr()
+    args = _ATTENTION_ARGS.pack(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qt, qh, kt, kh, vt, vh, out.data_ptr(), ot, oh, lse_at,
+                                q_at, k_at, n_seqs, tq, tk, heads, kv_heads, head_dim, left, right, sinks, scale)
+    L = _lib or lib()
     space = size = 0
     if workspace is not None:
         space, size = workspace.data_ptr(), workspace.numel()
     else:
         need = C.c_size_t()
-        _check(lib().oq_attention_workspace_bytes(args, C.byref(need)))
-        if need.value:
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=Q.device)
-            space, size = workspace.data_ptr(), need.value
-    _check(lib().oq_attention(args, space, size, _raw_stream(Q.get_device())))
+        code = L.oq_attention_workspace_bytes(args, C.byref(need))
+        if code:
+            _check(code)
+        size = need.value
+        if size:
+            workspace = Q.new_empty(size, dtype=torch.uint8)
+            space = workspace.data_ptr()
+    code = L.oq_attention(args, space, size, torch._C._cuda_getCurrentRawStream(Q.get_device()))
+    if code:
+        _check(code)
     return (out, lse) if want_lse else out
 
 
@@ -559,7 +585,7 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
         space, size = workspace.data_ptr(), workspace.numel()
     _check(lib().oq_adapter_add(X.data_ptr(), n, ldx, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(), seg_start.data_ptr(),
                                 seg_adapter.data_ptr(), segs, base.data_ptr(), ldb, out.data_ptr(), ldy, m,
-                                _dtype_code(base.dtype, "oq_adapter_add"), space, size, _raw_stream(X.get_device())))
+                                _dtype_code(base.dtype, "oq_adapter_add"), space, size, torch._C._cuda_getCurrentRawStream(X.get_device())))
     return out
 
 

@@ -392,12 +392,19 @@ cudaError_t launch(const Params& p, int mode, bool halves, long long most_ctas, 
   } else {
     kernel = halves ? qk_norm_rope_kernel<In, Out, WIDE_ROW, true, 0> : qk_norm_rope_kernel<In, Out, WIDE_ROW, false, 0>;
   }
-  int dev = 0, sms = 0, per_sm = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0);
-  if (e != cudaSuccess) return e;
-  const long long slots = ((long long)sms * (per_sm < 1 ? 1 : per_sm)) & ~1ll;      // (even: a CTA of a row norm keeps its side)
+  // what fits beside each other is asked only where there are more CTAs than one an SM
+  long long slots = 2;
+  if (most_ctas > slots) {
+    int dev = 0, sms = 0, per_sm = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    slots = sms & ~1;
+    if (e == cudaSuccess && most_ctas > slots) {
+      e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0);
+      slots = ((long long)sms * (per_sm < 1 ? 1 : per_sm)) & ~1ll;      // (even: a CTA of a row norm keeps its side)
+    }
+    if (e != cudaSuccess) return e;
+  }
   return launch_dependent(kernel, (int)(most_ctas < slots ? most_ctas : slots), threads, 0, st, p);
 }
 
