@@ -368,13 +368,33 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         for (int q = 0; q < BN / 32; ++q) tmem_use32(sr + 32 * q);
         if (BN % 32) tmem_use16(sr + BN - 16);
         if (!(k0 + BN - 1 <= full_hi && (k0 >= full_lo || k0 + BN <= p.sinks))) {
+          uint32_t some = 0;
 #pragma unroll
-          for (int q = 0; q < BN / 16; ++q) {
-            const int b = k0 + 16 * q;
+          for (int q = 0; q < BN / 32; ++q) {
+            const int b = k0 + 32 * q;
             const uint32_t keep = ones_below(hi + 1 - b) & (~ones_below(lo - b) | ones_below(p.sinks - b));
+            some |= keep;
+            if (__all_sync(~0u, keep == ~0u)) continue;          // (an edge of the mask crosses one or two of the four)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (!((keep >> e) & 1u)) sr[16 * q + e] = 0xFF800000u;
+            for (int e = 0; e < 32; ++e)
+              if (!((keep >> e) & 1u)) sr[32 * q + e] = 0xFF800000u;
+          }
+          if (!__any_sync(~0u, some)) {         // the warp's rows see nothing of this tile: weights of zero, m and l stay
+            uint32_t zero[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) zero[e] = 0u;
+#pragma unroll
+            for (int q = 0; q < BN / 32; ++q) tmem_store16(col_p + 16u * q, zero);
+            tmem_wait_st();
+            if (turns && (t == 1 || j > 0)) turn_wait();
+            if (turns && (t == 0 || j + 1 < it.tiles)) turn_pass();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(p_part(t));
+              mbar_arrive(p_full(t));
+            }
+            continue;
           }
         }
         float mx[4];
