@@ -35,8 +35,8 @@ namespace oq {
 namespace attn {
 
 constexpr int THREADS = 384;              // 8 softmax warps; the load warp, two mma warps and one that only fills their group
-// Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S and grow to 208; the last
-// group shrinks to 80: 256 * 208 + 128 * 80 = 63488.
+// Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S and grow to 216; the last
+// group shrinks to 72: 256 * 216 + 128 * 72 = 64512.
 constexpr int LOAD_WARP = 8, MMA_WARP = 9;
 constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
@@ -60,6 +60,7 @@ struct Params {
   long long ldq, hdq, ldk, hdk, ldv, hdv;
   __nv_bfloat16* out;
   long long ldo, hdo;
+  int wide_out;                           // rows of out begin on 32 bytes
   float* lse;                             // [heads][total_q] or NULL
   float* part_o;                          // [parts][heads][total_q][D]: sums scaled to weights that add up to one
   float* part_lse;                        // [parts][heads][total_q], base 2
@@ -107,8 +108,11 @@ __device__ __forceinline__ bool takes(const Params& p, int t, int j) { return !p
 template <int BN>
 __device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix, int index) {
   Item<BN> it;
-  it.split = index % p.splits;
-  index /= p.splits;
+  it.split = 0;
+  if (p.splits > 1) {
+    it.split = index % p.splits;
+    index /= p.splits;
+  }
   const int blocks = prefix[p.n_seqs];
   it.head = index / blocks;
   int b = blocks - 1 - index % blocks;         // the last queries see the most keys under a causal mask: first
@@ -139,8 +143,11 @@ __device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix
     it.n_sink = min((min(p.sinks, hi + 1) + BN - 1) / BN, it.win0);
     it.tiles = it.n_sink + hi / BN - it.win0 + 1;
   }
-  it.first = (int)((long long)it.tiles * it.split / p.splits);
-  it.tiles = (int)((long long)it.tiles * (it.split + 1) / p.splits) - it.first;
+  it.first = 0;
+  if (p.splits > 1) {
+    it.first = (int)((long long)it.tiles * it.split / p.splits);
+    it.tiles = (int)((long long)it.tiles * (it.split + 1) / p.splits) - it.first;
+  }
   return it;
 }
 
@@ -321,7 +328,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   };
 
   if (warp < LOAD_WARP) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ------------------------------------------------ softmax ------------------------------------------------
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t columns = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256u * (uint32_t)t;
@@ -339,18 +346,30 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     auto turn_wait = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + 2 * quarter + t) : "memory"); };
     auto turn_pass = [&]() { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 2 * quarter - t) : "memory"); };
     for (int i = blockIdx.x; i < n_items; i += gridDim.x) {
-      const Item<BN> it = make_item<BN>(p, prefix, i);
-      const int rows = t ? it.rows1 : it.rows0;
+      // (What only the item's beginning and end need is not kept through the loop, whose registers hold a row of scores: the
+      // end works the item out again.)
+      int rows, first, hi, lo, full_hi, full_lo, tiles, n_sink, skipped;
+      bool turns;
+      {
+        const Item<BN> it = make_item<BN>(p, prefix, i);
+        rows = t ? it.rows1 : it.rows0;
+        const int r0 = it.q0 + (p.dual ? 0 : t * BM);
+        hi = row_hi(p, it, r0 + row);
+        lo = row_lo(p, it, r0 + row);
+        full_hi = row_hi(p, it, r0);                     // what every row of the tile sees
+        full_lo = row_lo(p, it, r0 + rows - 1);
+        tiles = it.tiles;
+        n_sink = it.n_sink - it.first;                   // step j: key tile first + j, with a gap after the sinks
+        skipped = it.win0 - it.n_sink;
+        turns = !p.dual && it.rows1 > quarter * 32;      // both warps have rows (tile 0 is full where tile 1 has any)
+        first = it.first;
+      }
       if (rows == 0) continue;
-      const int r0 = it.q0 + (p.dual ? 0 : t * BM), qi = r0 + row;
-      const bool mine = row < rows, idle = (warp & 3) * 32 >= rows;      // idle: none of the warp's rows exists
-      const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
-      const int full_hi = row_hi(p, it, r0), full_lo = row_lo(p, it, r0 + rows - 1);     // what every row of the tile sees
+      const bool idle = quarter * 32 >= rows;            // none of the warp's rows exists
       float m = -INFINITY, l = 0.f;
-      const bool turns = !p.dual && it.rows1 > quarter * 32;       // both warps have rows (tile 0 is full where tile 1 has any)
       const int j0 = p.dual ? t : 0, jd = p.dual ? 2 : 1;
-      for (int j = j0; j < it.tiles; j += jd, ++steps) {
-        const int k0 = it.key0(j);
+      for (int j = j0; j < tiles; j += jd, ++steps) {
+        const int k0 = BN * (first + j + (j < n_sink ? 0 : skipped));
         warp_wait(s_full(t), steps & 1, W_S);
         if (idle) {                             // (O's rows are never read: whatever P holds there may stay)
           if (lane == 0) {
@@ -387,7 +406,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
             for (int q = 0; q < BN / 32; ++q) tmem_store16(col_p + 16u * q, zero);
             tmem_wait_st();
             if (turns && (t == 1 || j > 0)) turn_wait();
-            if (turns && (t == 0 || j + 1 < it.tiles)) turn_pass();
+            if (turns && (t == 0 || j + 1 < tiles)) turn_pass();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -438,7 +457,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
             add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], x, y);
             pk[e] = pack_bf16(x, y);
           }
-          if (q == 3 && turns && (t == 0 || j + 1 < it.tiles)) turn_pass();
+          if (q == 3 && turns && (t == 0 || j + 1 < tiles)) turn_pass();
           tmem_store16(col_p + 16u * q, pk);
           if (q >= 2) {                                   // the first 96 keys, then the rest
             tmem_wait_st();
@@ -450,63 +469,71 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       // ------------------------------------------- the item's result -------------------------------------------
-      const bool any = it.tiles > j0;
+      int again_i = i;
+      asm volatile("" : "+r"(again_i));
+      const Item<BN> it = make_item<BN>(p, prefix, again_i);
+      const int qi = it.q0 + (p.dual ? 0 : t * BM) + row;
+      const bool any = tiles > j0, mine = row < rows;
       if (any) warp_wait(o_done(t), items++ & 1, W_O);
       if (idle) continue;
-      uint32_t o[D];
-      if (any) {
-        tc_fence_after();
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) tmem_load32_nowait(col_o + 32u * q, o + 32 * q);
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) tmem_use32(o + 32 * q);
-        tc_fence_before();                      // (the next item's first P, which lets O be overwritten, comes after this)
-      } else {
-#pragma unroll
-        for (int e = 0; e < D; ++e) o[e] = 0u;
-      }
+      // (32 columns at a time in a loop that is not unrolled: straight-line code for all of them ran once an item and came from
+      // far away each time, 6000 cycles for a block where this takes 2000.)
+      tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      float nan_probe = 0.f;
-#pragma unroll
-      for (int e = 0; e < D; ++e) {
-        const float v = __uint_as_float(o[e]) * inv;
-        nan_probe = fmaf(v, 0.f, nan_probe);
-        o[e] = __float_as_uint(v);
-      }
-      const bool bad = mine && !(nan_probe == 0.f);
+      float probe[4] = {0.f, 0.f, 0.f, 0.f};
       const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c, log2f(l));
       const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
-      if (mine && !bad) {
+      const long long part_row = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + out_row;
+      __nv_bfloat16* const dst = p.out + (long long)(it.q_base + qi) * p.ldo + it.head * p.hdo;
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (any) {
+          tmem_load32_nowait(col_o + 32u * q, o);
+          tmem_use32(o);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float v = any ? __uint_as_float(o[e]) * inv : 0.f;
+          probe[e & 3] = fmaf(v, 0.f, probe[e & 3]);               // stays zero while everything is finite
+          o[e] = __float_as_uint(v);
+        }
+        if (!mine) continue;
         if (p.parts > 1) {
-          const long long at = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + out_row;
-          float4* dst = reinterpret_cast<float4*>(p.part_o + at * D);
+          uint4* const to = reinterpret_cast<uint4*>(p.part_o + part_row * D + 32 * q);
 #pragma unroll
-          for (int e = 0; e < D / 4; ++e)
-            dst[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
-          p.part_lse[at] = lse2;
+          for (int e = 0; e < 8; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + (long long)(it.q_base + qi) * p.ldo + it.head * p.hdo);
+          uint32_t v[16];
 #pragma unroll
-          for (int e = 0; e < D / 8; ++e) {
-            uint4 v;
-            v.x = pack_bf16(__uint_as_float(o[8 * e]), __uint_as_float(o[8 * e + 1]));
-            v.y = pack_bf16(__uint_as_float(o[8 * e + 2]), __uint_as_float(o[8 * e + 3]));
-            v.z = pack_bf16(__uint_as_float(o[8 * e + 4]), __uint_as_float(o[8 * e + 5]));
-            v.w = pack_bf16(__uint_as_float(o[8 * e + 6]), __uint_as_float(o[8 * e + 7]));
-            dst[e] = v;
+          for (int e = 0; e < 16; ++e) v[e] = pack_bf16(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+          if (p.wide_out) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst + 32 * q + 16 * e), "r"(v[8 * e]), "r"(v[8 * e + 1]),
+                           "r"(v[8 * e + 2]), "r"(v[8 * e + 3]), "r"(v[8 * e + 4]), "r"(v[8 * e + 5]), "r"(v[8 * e + 6]), "r"(v[8 * e + 7])
+                           : "memory");
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst + 32 * q)[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
           }
-          if (p.lse) p.lse[out_row] = lse2 * 0.69314718055994531f;
         }
       }
-      uint32_t again = __ballot_sync(~0u, bad);
+      if (mine) {
+        if (p.parts > 1) p.part_lse[part_row] = lse2;
+        else if (p.lse) p.lse[out_row] = lse2 * 0.69314718055994531f;
+      }
+      tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
+      // what is not finite is written again, by the whole warp
+      uint32_t again = __ballot_sync(~0u, mine && !((probe[0] + probe[1]) + (probe[2] + probe[3]) == 0.f));
       while (again) {
         const int r = __ffs(again) - 1;
         again &= again - 1;
-        exact_row<D>(p, it, r0 + (warp & 3) * 32 + r, t);
+        exact_row<D>(p, it, qi - lane + r, t);
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     uint32_t slot = 0, round = 0;               // position in the ring, the same sequence in all three warps
     auto advance = [&]() {
       if (++slot == SLOTS) {
@@ -775,6 +802,7 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.ldv = a->ldv_token; p.hdv = a->ldv_head;
   p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
   p.ldo = a->ldo_token; p.hdo = a->ldo_head;
+  p.wide_out = reinterpret_cast<uintptr_t>(a->out) % 32 == 0 && a->ldo_token % 16 == 0 && a->ldo_head % 16 == 0;
   p.lse = a->lse;
   p.part_o = reinterpret_cast<float*>(workspace);
   p.part_lse = p.part_o + (size_t)p.parts * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim;
