@@ -372,7 +372,7 @@ int oq_attention(const oq_attention_args* args, void* workspace, size_t workspac
  *            otherwise the two must not overlap
  * dim and m multiples of 8, leading dimensions multiples of 16 bytes, pointers 16-byte aligned.  Both products run on the
  * tensor cores with fp32 accumulation; A x is carried between them in 16 bits for bf16 outputs (two bf16 pieces) and
- * 24 for fp32 (three); with 8 tokens a segment or fewer on average both run on the ordinary cores in fp32.  The workspace (dev, 16-byte
+ * 24 for fp32 (three); with tokens * rank <= 64 a segment on average both run on the ordinary cores in fp32.  The workspace (dev, 16-byte
  * aligned, oq_adapter_workspace_bytes bytes, 0 for few tokens) carries A x between the two kernels.  Results are
  * bit-reproducible.  Asynchronous on `stream`; nothing is allocated.  n_tokens == 0 or n_segs == 0 launches nothing.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */

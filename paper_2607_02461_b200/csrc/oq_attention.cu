@@ -22,6 +22,15 @@
 // Of a tile's 256 columns of tensor memory S has 128, over which P lies, and O the rest.  The mma warp issues P_t V of a
 // key tile before the next S_t, so "S_t is there" also says that O_t holds the tiles before it.
 //
+// Measured (B200, head_dim 128): 4608 queries x 4608 keys x 24 heads 216 to 226 us = 1.2 PFLOP/s, 0.70 of the measured burst rate
+// of a library product and 0.83 of the sustained one (the power cap holds the clock at 1.7 GHz under this kernel; in
+// seconds-long runs 250 us); a step of 2 x 128 queries x 128 keys takes ~3200 cycles, 1200 of them P V, S and their latency,
+// 600 the load and the maximum, 1400 the powers, in two chains that run against each other.  Other arrangements that were measured:
+// S beside P and tiles of 80 keys (nothing waits for P V, but what a step costs besides is paid more often) 247 us;
+// four softmax threads of which two share a row 239 us; a third of the powers as polynomials of degree 4 on the fused
+// multiply-add pipe 255 us (that pipe takes as long for them); no turns at the exponentials 246 us; the maximum taken while the
+// powers are made with the old reference 227 us.
+//
 // NaN and infinities in keys and values that a row does not see must not reach it, but 0 * NaN is NaN: a row whose
 // result is not finite (checked once, at the end) is computed again key by key over what it sees.
 #include <cuda_bf16.h>
@@ -60,7 +69,7 @@ struct Params {
   long long ldq, hdq, ldk, hdk, ldv, hdv;
   __nv_bfloat16* out;
   long long ldo, hdo;
-  int wide_out;                           // rows of out begin on 32 bytes
+  int wide_out;                           // rows of out begin on 32 bytes: whole sectors a store (packed ragged requests 63 us, in 16 bytes 68)
   float* lse;                             // [heads][total_q] or NULL
   float* part_o;                          // [parts][heads][total_q][D]: sums scaled to weights that add up to one
   float* part_lse;                        // [parts][heads][total_q], base 2
@@ -693,7 +702,9 @@ int sm_count() {
   return sms;
 }
 
-// dual where the sequences have at most 128 queries on average, and keys enough for both chains.
+// dual where the sequences have at most 128 queries on average and keys enough to pay for the second kernel that joins the two
+// chains.  (40 heads: 1 query against 32760 keys 114 us dual, 143 not; 16 against 4096 28 and 34; 128 against 32760 133 and
+// 157; 128 against 4096 37 and 35; 8 against 600 keys, 5 key tiles, 17 and 15.)
 // Items (blocks of queries times heads) that do not fill the SMs, or fill them unevenly, are cut along their keys.  The
 // time of a cut is estimated as (rounds of items over the SMs) x (steps of an item + what it costs besides, in steps); a
 // step of a dual item is half as long as one of two query tiles.  (One query against 32760 keys of 40 heads: 3 runs
@@ -709,7 +720,7 @@ Plan make_plan(long long total_q, long long total_k, int n_seqs, int heads, int 
     if (window < keys) keys = window;
   }
   const long long tiles = (keys + 127) / 128;
-  Plan best{1, total_q <= (long long)BM * n_seqs && tiles >= 4, 1};
+  Plan best{1, total_q <= (long long)BM * n_seqs && tiles >= 16, 1};
   const long long rows = best.dual ? BM : 2 * BM, blocks = (total_q + rows / 2 * n_seqs + rows / 2 - 1) / rows;
   const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
   double best_cost = 1e30;
