@@ -294,8 +294,10 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // (the second kernel may start once every CTA of this one has passed its wait: what was written before this kernel is then
+  // complete, and the second kernel reads its base tiles without waiting for this kernel's end)
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -434,7 +436,6 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -508,6 +509,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
       }
     }
   } else {
+    asm volatile("griddepcontrol.wait;" ::: "memory");           // u's parts are complete; and nothing of Y is written before
     const int group = warp >> 2, row = (warp & 3) * 32 + lane;
     uint32_t held = 0;                                           // the stage whose tile is still being stored, + 1
     while (next_run()) {                    // (the groups meet at barriers: no warp leaves early, not even when a wait has given up)
