@@ -53,6 +53,7 @@ struct Params {
   float* part;                             // [tiles][parts][128][rank16]
   int parts;                               // places for them, the most stretches a tile can meet
   int ctas;                                // stretches of the shrink line, at most
+  int chunk;                               // k-blocks added up in tensor memory at a time
   int* status;
 };
 
@@ -308,14 +309,16 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
   const int c = (int)blockIdx.x;
   long long pos = c * len;
   const long long end = min(pos + len, total);
-  // runs: the k-blocks k .. k + count - 1 of one token tile
+  // runs: the k-blocks k .. k + count - 1 of one token tile, at most p.chunk; first: of the tile in this stretch
   Tile t;
   int tile = 0, k = 0, count = 0;
+  bool first = true;
   auto next_run = [&]() {
     while (pos < end) {
       tile = (int)(pos / kbs);
       k = (int)(pos % kbs);
-      count = (int)min((long long)(kbs - k), end - pos);
+      count = min((int)min((long long)(kbs - k), end - pos), p.chunk);
+      first = k == 0 || pos == c * len;
       pos += count;
       t = find_tile(p, tile);
       if (t.id >= 0) return true;
@@ -377,7 +380,15 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
         tmem_use16(r);
         if (row < t.rows)
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(dst + q + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+          for (int i = 0; i < 16; i += 4) {
+            float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+            float4* const at = reinterpret_cast<float4*>(dst + q + i);
+            if (!first) {                                        // (this thread wrote it, one run ago)
+              const float4 o = *at;
+              v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+            }
+            *at = v;
+          }
       }
       tc_fence_before();
       __syncwarp();
@@ -496,11 +507,11 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
         tc_fence_after();
         if (t.id >= 0) {
           const uint32_t bt = smem_st + st * S::STAGE + ATOM;
-          for (int q = 0; q < S::PIECES; ++q)
+          for (int q = S::PIECES - 1; q >= 0; --q)                // (the small pieces first)
             for (int s = 0; s < steps; ++s) {
               const uint64_t da = smem_desc(smem_u + (uint32_t)(q * RB + (s >> 2)) * ATOM) + 2u * (uint32_t)(s & 3);
               const uint64_t db = smem_desc(bt + (uint32_t)(s >> 2) * S::B_ATOM) + 2u * (uint32_t)(s & 3);
-              mma_ss(tmem + 64u * a, da, db, IDESC, q > 0 || s > 0, leader);
+              mma_ss(tmem + 64u * a, da, db, IDESC, q < S::PIECES - 1 || s > 0, leader);
             }
         }
         mma_commit(acc_full(a), leader);
@@ -754,6 +765,9 @@ int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const voi
   const int sms = adapter::sm_count();
   p.part = reinterpret_cast<float*>(workspace);
   p.ctas = sms;
+  // The tensor cores do not round their running sums to nearest, so an error of the sum's last bits grows with its length: for
+  // fp32 outputs 256 columns are added up at a time (relative error of the result at d = 8192: 1.7e-6 without this).
+  p.chunk = dtype == OQ_F32 ? 4 : 1 << 30;
   p.parts = adapter::most_parts(n_tokens, (dim + adapter::KB - 1) / adapter::KB, sms);
   CUtensorMap mx, ma, mb, mbase, my;
   const uint64_t size = dtype == OQ_F32 ? 4 : 2;
