@@ -52,6 +52,8 @@ class AttentionLayer:
         starts: int32 [requests + 1] or None (one request); left, right, sinks: the attention window of oq_attention.
         adapters: None or (Adapters of the QKV projection or None, Adapters of the output projection or None, seg_adapter
         int32 [requests]), which needs starts.  keep: a dict that receives what passes between the steps."""
+        if adapters is not None and starts is None:
+            raise B.OqError(1, "AttentionLayer: adapters go by request, so they need starts")
         t, (h, hk, d) = x.shape[0], (self.heads, self.kv_heads, self.head_dim)
         if keep is not None:
             keep["x"] = x

@@ -19,8 +19,8 @@
 //
 // Segments of a few tokens (serving one token each) run in a third kernel on the ordinary cores, see few_tokens.
 //
-// Measured (B200): 32760 tokens, 5120 -> 15360, rank 64, bf16: 430 us for 2.35 GB = 5.5 TB/s, 0.85 of the copy rate (shrink 62 us,
-// expand 361); 4608 tokens, 3072 -> 9216, rank 32: 48 us where 200 MB take 31 (the two launches and their first loads are 10 of
+// Measured (B200): 32760 tokens, 5120 -> 15360, rank 64, bf16: 427 us for 2.35 GB = 5.5 TB/s, 0.85 of the copy rate (shrink 62 us,
+// expand 361); 4608 tokens, 3072 -> 9216, rank 32: 47 us where 200 MB take 31 (the two launches and their first loads are 10 of
 // it); eight single tokens, 3072 -> 18432, rank 16, fp32: 7.2 us.
 #include <cuda_bf16.h>
 
@@ -367,29 +367,27 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
       mma_commit(u_full(a), leader);
     }
   } else {
+    float sum[64 * RB];                                          // of the tile's runs so far
     for (; next_run(); ++runs) {
       const uint32_t a = runs & 1u;
       mbar_spin(u_full(a), (runs >> 1) & 1u, &abort_flag, p.status, W_U);
       __syncwarp();
       tc_fence_after();
       const int row = warp * 32 + lane, place = c - (int)((long long)tile * kbs / len);
-      float* dst = p.part + (((long long)tile * p.parts + place) * BM + row) * p.rank16;
-      for (int q = 0; q < p.rank16; q += 16) {
-        uint32_t r[16];
-        tmem_load16_at(tmem + ((uint32_t)(warp * 32) << 16) + 128u * a + (uint32_t)q, r);
-        tmem_use16(r);
-        if (row < t.rows)
+      float4* const dst = reinterpret_cast<float4*>(p.part + (((long long)tile * p.parts + place) * BM + row) * p.rank16);
+      const bool last = k + count == kbs || pos == end;          // of the tile in this stretch
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-            float4* const at = reinterpret_cast<float4*>(dst + q + i);
-            if (!first) {                                        // (this thread wrote it, one run ago)
-              const float4 o = *at;
-              v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-            }
-            *at = v;
-          }
-      }
+      for (int q = 0; q < 4 * RB; ++q)
+        if (16 * q < p.rank16) {
+          uint32_t r[16];
+          tmem_load16_at(tmem + ((uint32_t)(warp * 32) << 16) + 128u * a + 16u * (uint32_t)q, r);
+          tmem_use16(r);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[16 * q + i] = first ? __uint_as_float(r[i]) : sum[16 * q + i] + __uint_as_float(r[i]);
+          if (last && row < t.rows)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[4 * q + i] = make_float4(sum[16 * q + 4 * i], sum[16 * q + 4 * i + 1], sum[16 * q + 4 * i + 2], sum[16 * q + 4 * i + 3]);
+        }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(u_free(a));

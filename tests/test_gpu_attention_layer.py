@@ -69,6 +69,8 @@ def test_every_step_matches_fp64(mask):
     ref = oat.adapter_add(_f(keep["o"]), _f(a.a), _f(a.b), _f(a.scale), lens, ids, _f(keep["y_shared"]))
     assert _rel(y, ref) <= STEP
     assert torch.equal(layer(x, pos, starts, adapters=adapters, **mask), y)
+    with pytest.raises(B.OqError):
+        layer(x, pos, adapters=adapters, **mask)             # adapters go by request
     plain = layer(x, pos, starts, **mask)
     assert not torch.equal(plain, y)
 
