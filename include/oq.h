@@ -334,8 +334,7 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
  *   out      dev bf16, laid out by ldo_*; must not overlap the inputs.   lse  dev fp32 [n_heads][total_q], or NULL
  *   q_start, k_start  dev int32 [n_seqs + 1]: sequence s owns the queries q_start[s] .. q_start[s + 1] - 1 and the keys
  *            k_start[s] .. k_start[s + 1] - 1 (either may be empty).  NULL, both: one sequence.  Values are cut to
- *            0 .. total_q / total_k; queries that no sequence owns are not written when the call does not split (see
- *            below) and are undefined when it does.
+ *            0 .. total_q / total_k; queries before the first sequence or after the last are not written.
  *   n_heads  a multiple of n_kv_heads; query head h reads the key and value head h / (n_heads / n_kv_heads)
  *   scale    0: 1 / sqrt(head_dim).   head_dim 64 or 128.  n_seqs <= 256.
  * The products run on the tensor cores with fp32 accumulation; the softmax weights are rounded to bf16 for the product

@@ -670,6 +670,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   const long long rows = (long long)p.heads * p.total_q;
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
+  const int head = (int)(row / p.total_q), tok = (int)(row % p.total_q);
+  if (p.q_start && (tok < __ldg(p.q_start) || tok >= __ldg(p.q_start + p.n_seqs))) return;      // no sequence owns it: no part was written
   const float mine = lane < p.parts ? p.part_lse[lane * rows + row] : -INFINITY;
   float top = mine;
 #pragma unroll
@@ -689,7 +691,6 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
     for (int i = 0; i < N; ++i) o[i] = fmaf(ws, src[i], o[i]);
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  const int head = (int)(row / p.total_q), tok = (int)(row % p.total_q);
   __nv_bfloat16* dst = p.out + (long long)tok * p.ldo + head * p.hdo + lane * N;
 #pragma unroll
   for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16(o[i] * inv, o[i + 1] * inv);
@@ -765,7 +766,7 @@ static int attention_check(const oq_attention_args* a) {
   if (a->n_seqs > 1 && !a->q_start) return fail(OQ_ERR_INVALID_ARG, "oq_attention: several sequences need q_start and k_start");
   if (a->sinks < 0) return fail(OQ_ERR_INVALID_ARG, "oq_attention: sinks must not be negative");
   if (!(a->scale >= 0.f) || !(a->scale < 1e30f)) return fail(OQ_ERR_INVALID_ARG, "oq_attention: scale must be positive, or 0 for 1 / sqrt(head_dim)");
-  if ((long long)a->total_q * a->n_heads > (1ll << 31) * 8) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: too many rows for one launch");
+  if ((long long)a->total_q * a->n_heads > (1ll << 33)) return fail(OQ_ERR_UNSUPPORTED, "oq_attention: too many rows for one launch");
   return OQ_OK;
 }
 

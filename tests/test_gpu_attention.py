@@ -170,6 +170,18 @@ def test_strides_heads_first_and_streams():
     assert torch.equal(wide[:, :, :d], want) and torch.equal(lse, want_lse) and torch.all(wide[:, :, d:] == 7.0)
 
 
+@pytest.mark.parametrize("ql,kl", [([3, 2], [5000, 4000]), ([300, 200], [300, 200])])
+def test_queries_outside_the_sequences_are_left_alone(ql, kl):
+    import torch
+    q, k, v = _inputs(sum(ql) + 9, sum(kl), 2, 2, 128, 61)
+    out = torch.full_like(q, 7.0)
+    starts = (_starts(ql) + 4).to(torch.int32)
+    B.oq_attention(q, k, v, starts, _starts(kl), right=0, out=out)
+    want = B.oq_attention(q[4:4 + sum(ql)], k, v, _starts(ql), _starts(kl), right=0)
+    assert torch.equal(out[4:4 + sum(ql)], want)
+    assert torch.all(out[:4] == 7.0) and torch.all(out[4 + sum(ql):] == 7.0)
+
+
 def test_repeated_calls_are_bit_identical():
     import torch
     for ql, kl in [([700], [700]), ([2], [9000])]:
