@@ -330,8 +330,9 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
  * sees no key gets out = 0 and lse = -inf.  Keys and values that a query does not see do not reach it, whatever they
  * hold (NaN and infinities included).  causal: right = 0; joint attention: left = right = -1.
  *   Q, K, V  dev bf16, element (token, head, c) at X[token * ld_token + head * ld_head + c]; strides in elements,
- *            multiples of 8, at least head_dim where there is more than one token or head; 16-byte aligned
- *   out      dev bf16, laid out by ldo_*; must not overlap the inputs.   lse  dev fp32 [n_heads][total_q], or NULL
+ *            multiples of 8, at least head_dim where there is more than one token or head, or for heads 0: one head serves
+ *            all of them; 16-byte aligned
+ *   out      dev bf16, laid out by ldo_* (at least head_dim where used); must not overlap the inputs.   lse  dev fp32 [n_heads][total_q], or NULL
  *   q_start, k_start  dev int32 [n_seqs + 1]: sequence s owns the queries q_start[s] .. q_start[s + 1] - 1 and the keys
  *            k_start[s] .. k_start[s + 1] - 1 (either may be empty).  NULL, both: one sequence.  Values are cut to
  *            0 .. total_q / total_k; queries before the first sequence or after the last are not written.

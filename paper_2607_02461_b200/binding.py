@@ -478,8 +478,8 @@ _ATTENTION_ARGS = struct.Struct("@PPPqqqqqqPqqPPPiiiiiiiiif")      # oq_attentio
 
 def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0, scale=0.0, out=None, want_lse=False,
                  workspace=None):
-    """Q: CUDA bf16 [Tq, heads, head_dim], K, V: [Tk, kv_heads, head_dim] (any token and head strides, unit stride inside
-    a head); q_start, k_start: CUDA int32 [sequences + 1], or None for one sequence.  left, right, sinks: see oq.h.
+    """Q: CUDA bf16 [Tq, heads, head_dim], K, V: [Tk, kv_heads, head_dim] (token and head strides of at least head_dim, or a
+    head stride of 0: a head expanded over all; unit stride inside a head); q_start, k_start: CUDA int32 [sequences + 1], or None for one sequence.  left, right, sinks: see oq.h.
     Returns out [Tq, heads, head_dim], or (out, lse fp32 [heads, Tq]) with want_lse.  workspace: CUDA uint8 tensor, by
     default one is taken from torch's allocator when the call needs it."""
     import torch

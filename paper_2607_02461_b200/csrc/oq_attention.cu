@@ -75,6 +75,7 @@ struct Params {
   float* part_lse;                        // [parts][heads][total_q], base 2
   const int *q_start, *k_start;           // n_seqs + 1, or NULL: one sequence
   int total_q, total_k, n_seqs, heads, group;
+  int q_step, k_step, v_step;             // of the head coordinate in the tensor maps: 1, or 0 where one head serves all (stride 0)
   int splits;                             // runs that an item's key tiles are cut into
   int dual;                               // see below
   int parts;                              // results of a row to be joined: splits, twice as many when dual
@@ -553,11 +554,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     if (warp == LOAD_WARP) {
       if (lane == 0) {
         uint32_t q_use[2] = {0, 0};
-        auto load_kv = [&](const Step& s, const CUtensorMap* map) {
+        auto load_kv = [&](const Step& s, const CUtensorMap* map, int head_step) {
           if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
           mbar_expect_tx(kv_full(slot), S::KV_TILE);
           for (uint32_t a = 0; a < S::ATOMS; ++a)
-            tma_load_3d(smem_kv + slot * S::KV_TILE + a * S::KV_ATOM, map, 64 * (int)a, s.it.head / p.group, s.it.k_base + s.it.key0(s.j), kv_full(slot));
+            tma_load_3d(smem_kv + slot * S::KV_TILE + a * S::KV_ATOM, map, 64 * (int)a, s.it.head / p.group * head_step, s.it.k_base + s.it.key0(s.j), kv_full(slot));
           advance();
         };
         auto load_k = [&](const Step& s) {
@@ -568,10 +569,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
               ++q_use[t];
               mbar_expect_tx(q_full(t), S::Q_TILE);
               for (uint32_t a = 0; a < S::ATOMS; ++a)
-                tma_load_3d(smem_q + (uint32_t)t * S::Q_TILE + a * S::Q_ATOM, &map_q, 64 * (int)a, s.it.head, s.it.q_base + s.it.q0 + (p.dual ? 0 : t * BM), q_full(t));
+                tma_load_3d(smem_q + (uint32_t)t * S::Q_TILE + a * S::Q_ATOM, &map_q, 64 * (int)a, s.it.head * p.q_step, s.it.q_base + s.it.q0 + (p.dual ? 0 : t * BM), q_full(t));
             }
           }
-          load_kv(s, &map_k);
+          load_kv(s, &map_k, p.k_step);
         };
         Step now, ahead;
         bool have = first_from(now, blockIdx.x);
@@ -579,7 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         while (have && !abort_flag) {
           ahead = now;
           have = next_step(ahead);
-          load_kv(now, &map_v);
+          load_kv(now, &map_v, p.v_step);
           if (have) load_k(ahead);
           now = ahead;
         }
@@ -770,6 +771,13 @@ static int attention_check(const oq_attention_args* a) {
   return OQ_OK;
 }
 
+// A stride is used where there is more than one token or head.  Inputs may have a head stride of 0 (one head serves all); any other stride
+// that is used must reach past a head's coordinates: the tensor maps have no rows that lie over each other, and rows of the
+// output that do would overwrite each other.
+static bool strides_ok(long long ld, long long hd, int tokens, int heads, int head_dim, bool input) {
+  return ld >= 0 && hd >= 0 && (tokens <= 1 || ld >= head_dim) && (heads <= 1 || hd >= head_dim || (input && hd == 0));
+}
+
 static attn::Plan attention_plan(const oq_attention_args* a) {
   return attn::make_plan(a->total_q, a->total_k, a->n_seqs, a->n_heads, a->left, a->right, a->sinks, attn::sm_count());
 }
@@ -794,8 +802,11 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   if (!aligned16(a->Q) || !aligned16(a->K) || !aligned16(a->V) || !aligned16(a->out) || a->ldq_token % 8 || a->ldq_head % 8 ||
       a->ldk_token % 8 || a->ldk_head % 8 || a->ldv_token % 8 || a->ldv_head % 8 || a->ldo_token % 8 || a->ldo_head % 8)
     return fail(OQ_ERR_ALIGNMENT, "oq_attention: pointers must be 16-byte aligned and strides multiples of 8");
-  if (a->ldq_token < 0 || a->ldq_head < 0 || a->ldk_token < 0 || a->ldk_head < 0 || a->ldv_token < 0 || a->ldv_head < 0)
-    return fail(OQ_ERR_INVALID_ARG, "oq_attention: strides must not be negative");
+  if (!strides_ok(a->ldq_token, a->ldq_head, a->total_q, a->n_heads, a->head_dim, true) ||
+      !strides_ok(a->ldk_token, a->ldk_head, a->total_k, a->n_kv_heads, a->head_dim, true) ||
+      !strides_ok(a->ldv_token, a->ldv_head, a->total_k, a->n_kv_heads, a->head_dim, true) ||
+      !strides_ok(a->ldo_token, a->ldo_head, a->total_q, a->n_heads, a->head_dim, false))
+    return fail(OQ_ERR_INVALID_ARG, "oq_attention: strides must be at least head_dim (head strides of the inputs: or 0, one head for all)");
   attn::Params p = {};
   const attn::Plan plan = attention_plan(a);
   p.splits = plan.splits;
@@ -830,10 +841,14 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.status = device_status_word();
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_attention: cannot allocate the device status word");
   CUtensorMap mq, mk, mv;
+  p.q_step = a->ldq_head > 0;
+  p.k_step = a->ldk_head > 0;
+  p.v_step = a->ldv_head > 0;
   auto make_map = [&](CUtensorMap* map, const void* base, int heads, long long tokens, long long ld, long long hd, int rows) {
+    if (hd == 0) heads = 1;                        // (one head, or one for all: the coordinate stays 0)
     const uint64_t dims[3] = {(uint64_t)a->head_dim, (uint64_t)heads, (uint64_t)tokens};
-    // a stride that is never used (one head, one token) still has to be one that the encoder takes
-    const uint64_t strides[2] = {(uint64_t)(heads > 1 && hd > 0 ? hd : a->head_dim) * 2, (uint64_t)(tokens > 1 && ld > 0 ? ld : (long long)a->head_dim * heads) * 2};
+    // a stride that is not used (one head, one token) still has to be one that the encoder takes
+    const uint64_t strides[2] = {(uint64_t)(heads > 1 ? hd : a->head_dim) * 2, (uint64_t)(tokens > 1 ? ld : (long long)a->head_dim * heads) * 2};
     const uint32_t box[3] = {64, 1, (uint32_t)rows};
     return encode_tensor_map_sw128(map, base, false, 3, dims, strides, box);
   };

@@ -230,3 +230,39 @@ def test_empty_and_refusals():
     small = torch.zeros(16, dtype=torch.uint8, device="cuda")
     long = _inputs(1, 9000, 2, 2, 128, 2)
     assert code(*long, workspace=small) == 6
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "kv", "qkv"])
+@pytest.mark.parametrize("nq,nk,d", [(130, 270, 128), (2, 3000, 128), (40, 77, 64)])
+def test_one_head_expanded_over_all(which, nq, nk, d):
+    """A head stride of 0 reads the one head that is there, on every path: single part, joined parts, rows made again."""
+    import torch
+    h = 8
+    mask = dict(left=nk // 2, right=0, sinks=2)
+    full = dict(zip("qkv", _inputs(nq, nk, h, h, d, 71)))
+    for name in which:
+        full[name] = full[name][:, :1].expand(-1, h, -1)
+    full["v"] = full["v"].clone() if "v" not in which else full["v"][:, :1].clone().expand(-1, h, -1)
+    full["v"][nk - 1, 0] = float("nan")                    # seen by the last query alone
+    out, lse = B.oq_attention(*full.values(), want_lse=True, **mask)
+    copies = [t.contiguous() for t in full.values()]
+    want, want_lse = B.oq_attention(*copies, want_lse=True, **mask)
+    torch.cuda.synchronize()
+    assert B.oq_device_status() == 0
+    assert torch.equal(lse, want_lse) and torch.equal(torch.isnan(out), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+    _verify(*[t[:nq - 1] for t in copies[:1]], copies[1][:nk - 1], copies[2][:nk - 1], [nq - 1], [nk - 1], out[:nq - 1], lse[:, :nq - 1], **mask)
+
+
+def test_strides_that_cannot_be_served_are_refused():
+    import torch
+    q, k, v = _inputs(4, 6, 2, 2, 128, 1)
+    for args in ((q[:1].expand(4, -1, -1), k, v), (q, k[:1].expand(6, -1, -1), v), (q, k, v[:1].expand(6, -1, -1)),
+                 (q, k.as_strided((6, 2, 128), (64, 768, 1)), v), (q, k, v.as_strided((6, 2, 128), (256, 64, 1)))):
+        with pytest.raises(B.OqError) as e:
+            B.oq_attention(*args)
+        assert e.value.code == 1
+    for out in (q[:, :1].clone().expand(-1, 2, -1), q[:1].clone().expand(4, -1, -1)):
+        with pytest.raises(B.OqError) as e:
+            B.oq_attention(q, k, v, out=out)
+        assert e.value.code == 1

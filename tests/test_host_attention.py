@@ -31,3 +31,31 @@ def test_rope_constructor():
     assert _code(B.oq_make_rope, [64], [4], 0.0) == 1
     assert _code(B.oq_make_rope, [64], [4], float("nan")) == 1
     assert _code(B.oq_make_rope, [64], [4], 10000.0, "thirds") == 1
+
+
+def _attention_code(**fields):
+    """Status of oq_attention for 4 queries and 6 keys, 4 heads on 2 of 64, contiguous but for `fields`.  (The buffers are not
+    memory: a call that is not refused for its arguments ends at the device's status word, as there is no device.)"""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("made-up buffers are for hosts without a device")
+    at = dict(ldq_token=256, ldq_head=64, ldk_token=128, ldk_head=64, ldv_token=128, ldv_head=64, ldo_token=256, ldo_head=64,
+              total_q=4, total_k=6, n_heads=4, n_kv_heads=2)
+    at.update(fields)
+    args = B._ATTENTION_ARGS.pack(4096, 8192, 12288, at["ldq_token"], at["ldq_head"], at["ldk_token"], at["ldk_head"], at["ldv_token"],
+                                  at["ldv_head"], 16384, at["ldo_token"], at["ldo_head"], 0, 0, 0, 1, at["total_q"], at["total_k"],
+                                  at["n_heads"], at["n_kv_heads"], 64, -1, -1, 0, 0.0)
+    return B.lib().oq_attention(args, None, 0, None)
+
+
+@pytest.mark.parametrize("field", ["ldq_token", "ldk_token", "ldv_token", "ldo_token", "ldo_head"])
+@pytest.mark.parametrize("stride", [0, 8, 56, -64])
+def test_rows_that_lie_over_each_other_are_refused(field, stride):
+    """A token stride of 0, rows that overlap, outputs that overwrite each other: code 1, before anything touches a device."""
+    assert _attention_code(**{field: stride}) == 1
+
+
+@pytest.mark.parametrize("field", ["ldq_head", "ldk_head", "ldv_head"])
+@pytest.mark.parametrize("stride", [8, 56, -64])
+def test_heads_that_overlap_in_part_are_refused(field, stride):
+    assert _attention_code(**{field: stride}) == 1
