@@ -367,7 +367,8 @@ int oq_attention(const oq_attention_args* args, void* workspace, size_t workspac
  *   A_bf16   dev [n_adapters][rank][dim], B_bf16 dev [n_adapters][m][rank], both dense; scale dev fp32 [n_adapters].
  *            Adapters of smaller rank are filled up with zeros.  rank: a multiple of 8, at most 128
  *   seg_start dev int32 [n_segs + 1], seg_adapter dev int32 [n_segs].  Values are cut to 0 .. n_tokens; a segment may be
- *            empty, tokens in no segment are left alone, none may be in two
+ *            empty, tokens in no segment are left alone, none may be in two (where a table is not ascending, the tokens
+ *            that it names more than once get unspecified values; nothing else is touched)
  *   base, Y  dev [n_tokens][ldb] / [n_tokens][ldy] of dtype (OQ_BF16 or OQ_F32).  Y may be base (in place, ldy == ldb);
  *            otherwise the two must not overlap
  * dim and m multiples of 8, leading dimensions multiples of 16 bytes, pointers 16-byte aligned.  Both products run on the

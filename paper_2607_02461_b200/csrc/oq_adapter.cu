@@ -51,6 +51,7 @@ struct Params {
   long long ldy;
   int copy;                                // Y is not base: rows without an adapter are copied
   float* part;                             // [tiles][parts][128][rank16]
+  int max_tiles;                           // places for tiles: as many as segments that share no token can make
   int parts;                               // places for them, the most stretches a tile can meet
   int ctas;                                // stretches of the shrink line, at most
   int chunk;                               // k-blocks added up in tensor memory at a time
@@ -132,10 +133,13 @@ __device__ __forceinline__ Tile find_tile(const Params& p, int want) {
       t.id = __shfl_sync(~0u, id, l);
       return t;
     }
-    before += __shfl_sync(~0u, sum, 31);
+    before = min(before + __shfl_sync(~0u, sum, 31), 1 << 30);     // (more than any call has, even of a table that is not ascending)
   }
   return Tile{before, 0, -1};
 }
+// Tiles that the two kernels work on.  A table that is not ascending names tokens more than once and makes more tiles than the
+// workspace has places for: those are left out.
+__device__ __forceinline__ int count_tiles(const Params& p) { return min(find_tile(p, 0x7FFFFFFF).tok0, p.max_tiles); }
 // Steps of a stretch of the shrink line: an equal share, but so many that the kbs steps of a tile never meet more than
 // p.parts stretches, however few tiles the segments turn out to make: ceil((kbs - 1) / len) + 1 <= parts.
 __device__ __forceinline__ long long shrink_stretch(const Params& p, long long total, int kbs) {
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int kbs = (p.d + KB - 1) / KB;
-  const long long total = (long long)find_tile(p, 0x7FFFFFFF).tok0 * kbs;
+  const long long total = (long long)count_tiles(p) * kbs;
   const long long len = shrink_stretch(p, total, kbs);
   const int c = (int)blockIdx.x;
   long long pos = c * len;
@@ -450,7 +454,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int nbs = (p.m + BN - 1) / BN, kbs = (p.d + KB - 1) / KB, steps = p.rank16 / 16;
-  const int tiles = find_tile(p, 0x7FFFFFFF).tok0;
+  const int tiles = count_tiles(p);
   const long long total = (long long)tiles * nbs, len = shrink_stretch(p, (long long)tiles * kbs, kbs);
   long long pos = total * blockIdx.x / gridDim.x;
   const long long end = total * (blockIdx.x + 1) / gridDim.x;
@@ -763,6 +767,7 @@ int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const voi
   const int sms = adapter::sm_count();
   p.part = reinterpret_cast<float*>(workspace);
   p.ctas = sms;
+  p.max_tiles = adapter::most_tiles(n_tokens, n_segs);
   // The tensor cores do not round their running sums to nearest, so an error of the sum's last bits grows with its length: for
   // fp32 outputs 256 columns are added up at a time (relative error of the result at d = 8192: 1.7e-6 without this).
   p.chunk = dtype == OQ_F32 ? 4 : 1 << 30;

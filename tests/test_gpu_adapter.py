@@ -158,3 +158,26 @@ def test_empty_and_refusals():
     assert code(*many[:4], *_tables([300], [0]), many[4], workspace=small) == 6
     odd = torch.zeros(4, 68, dtype=torch.bfloat16, device="cuda")
     assert code(x, a, b, scale, start, seg, odd[:, :64]) == 3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,segs,rank", [(1024, 64, 32), (5000, 300, 128), (24, 64, 16)])
+def test_a_table_that_is_not_ascending_stays_inside_the_buffers(n, segs, rank, dtype):
+    """Segments that name the same tokens again and again make more tiles than the workspace has places for."""
+    import ctypes
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    d, m = 192, 136
+    x, a, b, scale, base = _inputs(n + 70, d, m, rank, 2, t, 8)
+    start = torch.tensor([0, n] * (segs // 2) + [0], dtype=torch.int32, device="cuda")
+    seg = torch.arange(segs, dtype=torch.int32, device="cuda") % 2
+    need = ctypes.c_size_t()
+    assert B.lib().oq_adapter_workspace_bytes(n + 70, segs, d, rank, ctypes.byref(need)) == 0
+    space = torch.full((need.value + (1 << 24),), 77, dtype=torch.uint8, device="cuda")
+    out = torch.full((n + 70, m), 7.0, dtype=t, device="cuda")
+    B.oq_adapter_add(x, a, b, scale, start, seg, base, out=out, workspace=space[:max(need.value, 16)])
+    torch.cuda.synchronize()
+    assert B.oq_device_status() == 0
+    assert torch.all(space[max(need.value, 16):] == 77) and torch.all(out[n:] == 7.0)
+    lens = [n]                                             # a sound call right after it
+    _verify(B.oq_adapter_add(x[:n], a, b, scale, *_tables(lens, [1]), base[:n]), x[:n], a, b, scale, base[:n], lens, [1])
