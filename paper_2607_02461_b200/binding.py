@@ -392,6 +392,22 @@ def _dtype_code(dtype, what):
     raise OqError(1, f"{what}: bf16 or fp32 expected, got {dtype}")
 
 
+def _on_one_device(what, first, *rest):
+    """All of these tensors (or None) on one CUDA device: the kernels would follow a host pointer."""
+    device = first.get_device()                      # -1: host memory
+    if device < 0:
+        raise OqError(1, f"{what}: CUDA tensors expected")
+    for t in rest:
+        if t is not None and t.get_device() != device:
+            raise OqError(1, f"{what}: all tensors must be on one CUDA device")
+    return device
+
+
+def _check_workspace(what, t, torch):
+    if t.dtype != torch.uint8 or not t.is_contiguous():
+        raise OqError(1, f"{what}: the workspace must be a contiguous uint8 tensor")
+
+
 # The calls below are short on the GPU at small sizes (3 to 7 us), so their marshalling looks at every property of a tensor
 # once, and outputs that are allocated here are not looked at again.
 _QK_SIDE = struct.Struct("@PqqiPPqq")               # oq_qk_side
@@ -441,6 +457,7 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
     if len(shape) != 3:
         raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim]")
     n, _, head_dim = shape
+    device = _on_one_device("oq_qk_norm_rope", Q, K, pos if rope is not None else None, wq, wk, out_q, out_k)
     norm_code = NORMS.get(norm)
     if norm_code is None:
         raise OqError(1, f"oq_qk_norm_rope: norm must be one of {sorted(NORMS)}")
@@ -467,7 +484,7 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
             ldpos = axes
         table, at = rope.handle, pos.data_ptr()
     code = (_lib or lib()).oq_qk_norm_rope(q_side, k_side, n, head_dim, table, at, ldpos, norm_code, eps, x_code, y_code,
-                                           torch._C._cuda_getCurrentRawStream(Q.get_device()))
+                                           torch._C._cuda_getCurrentRawStream(device))
     if code:
         _check(code)
     return out_q, out_k
@@ -489,13 +506,14 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
         raise OqError(1, "oq_attention: Q must be [Tq, heads, head_dim], K and V [Tk, kv_heads, head_dim]")
     if Q.dtype != bf16 or K.dtype != bf16 or V.dtype != bf16:
         raise OqError(1, "oq_attention: bf16 expected")
+    device = _on_one_device("oq_attention", Q, K, V, q_start, k_start, out, workspace)
     tq, heads, head_dim = qs
     tk, kv_heads, _ = ks
     n_seqs, q_at, k_at = 1, 0, 0
     if q_start is not None or k_start is not None:
         for t in (q_start, k_start):
-            if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
-                raise OqError(1, "oq_attention: q_start and k_start must both be contiguous CUDA int32 [sequences + 1]")
+            if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+                raise OqError(1, "oq_attention: q_start and k_start must both be contiguous int32 [sequences + 1]")
         n_seqs = len(q_start) - 1
         if len(k_start) != n_seqs + 1:
             raise OqError(1, "oq_attention: q_start and k_start must have one length")
@@ -529,6 +547,7 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     L = _lib or lib()
     space = size = 0
     if workspace is not None:
+        _check_workspace("oq_attention", workspace, torch)
         space, size = workspace.data_ptr(), workspace.numel()
     else:
         need = C.c_size_t()
@@ -539,7 +558,7 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
         if size:
             workspace = Q.new_empty(size, dtype=torch.uint8)
             space = workspace.data_ptr()
-    code = L.oq_attention(args, space, size, torch._C._cuda_getCurrentRawStream(Q.get_device()))
+    code = L.oq_attention(args, space, size, torch._C._cuda_getCurrentRawStream(device))
     if code:
         _check(code)
     return (out, lse) if want_lse else out
@@ -555,14 +574,15 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
     xs, sa, sb, shape = X.shape, A.shape, Bm.shape, base.shape
     if len(xs) != 2 or len(sa) != 3 or len(sb) != 3 or len(shape) != 2:
         raise OqError(1, "oq_adapter_add: X [T, d], A [adapters, rank, d], B [adapters, m, rank], base [T, m] expected")
+    device = _on_one_device("oq_adapter_add", X, A, Bm, scale, seg_start, seg_adapter, base, out, workspace)
     n, d = xs
     na, rank, m = sa[0], sa[1], sb[1]
-    segs = seg_adapter.shape[0]
+    segs = seg_adapter.numel()
     if sa[2] != d or sb[0] != na or sb[2] != rank or shape[0] != n or shape[1] != m or scale.shape != (na,):
         raise OqError(1, "oq_adapter_add: sizes do not match")
     if X.dtype != bf16 or A.dtype != bf16 or Bm.dtype != bf16 or scale.dtype != torch.float32:
         raise OqError(1, "oq_adapter_add: X, A, B must be bf16 and scale fp32")
-    if seg_start.dtype != i32 or seg_adapter.dtype != i32 or seg_start.shape != (segs + 1,):
+    if seg_start.dtype != i32 or seg_adapter.dtype != i32 or seg_adapter.dim() != 1 or seg_start.shape != (segs + 1,):
         raise OqError(1, "oq_adapter_add: seg_start int32 [segments + 1], seg_adapter int32 [segments] expected")
     if not (A.is_contiguous() and Bm.is_contiguous() and scale.is_contiguous() and seg_start.is_contiguous() and seg_adapter.is_contiguous()):
         raise OqError(1, "oq_adapter_add: adapters, scales and segment tables must be contiguous")
@@ -576,7 +596,9 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
     if n <= 1:
         ldx, ldb, ldy = d, m, m
     space = size = 0
-    if workspace is None:
+    if workspace is not None:
+        _check_workspace("oq_adapter_add", workspace, torch)
+    else:
         need = C.c_size_t()
         _check(lib().oq_adapter_workspace_bytes(n, segs, d, rank, C.byref(need)))
         if need.value:
@@ -585,7 +607,7 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
         space, size = workspace.data_ptr(), workspace.numel()
     _check(lib().oq_adapter_add(X.data_ptr(), n, ldx, d, A.data_ptr(), Bm.data_ptr(), na, rank, scale.data_ptr(), seg_start.data_ptr(),
                                 seg_adapter.data_ptr(), segs, base.data_ptr(), ldb, out.data_ptr(), ldy, m,
-                                _dtype_code(base.dtype, "oq_adapter_add"), space, size, torch._C._cuda_getCurrentRawStream(X.get_device())))
+                                _dtype_code(base.dtype, "oq_adapter_add"), space, size, torch._C._cuda_getCurrentRawStream(device)))
     return out
 
 

@@ -181,3 +181,19 @@ def test_a_table_that_is_not_ascending_stays_inside_the_buffers(n, segs, rank, d
     assert torch.all(space[max(need.value, 16):] == 77) and torch.all(out[n:] == 7.0)
     lens = [n]                                             # a sound call right after it
     _verify(B.oq_adapter_add(x[:n], a, b, scale, *_tables(lens, [1]), base[:n]), x[:n], a, b, scale, base[:n], lens, [1])
+
+
+def test_tensors_off_the_device_and_odd_tables_are_refused():
+    import torch
+    x, a, b, scale, base = _inputs(300, 64, 64, 16, 2, torch.bfloat16, 1)
+    start, seg = _tables([300], [0])
+    args = dict(X=x, A=a, Bm=b, scale=scale, seg_start=start, seg_adapter=seg, base=base, out=torch.empty_like(base),
+                workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
+    B.oq_adapter_add(**args)
+    bad = [{name: t.cpu()} for name, t in args.items()]
+    bad += [dict(workspace=torch.empty(1 << 22, device="cuda")), dict(workspace=args["workspace"][:1].expand(1 << 24)),
+            dict(seg_adapter=torch.zeros(1, 0, dtype=torch.int32, device="cuda"))]
+    for change in bad:
+        with pytest.raises(B.OqError) as e:
+            B.oq_adapter_add(**{**args, **change})
+        assert e.value.code == 1, change.keys()

@@ -266,3 +266,17 @@ def test_strides_that_cannot_be_served_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_attention(q, k, v, out=out)
         assert e.value.code == 1
+
+
+def test_tensors_off_the_device_and_odd_workspaces_are_refused():
+    import torch
+    q, k, v = _inputs(4, 6, 2, 2, 128, 1)
+    args = dict(Q=q, K=k, V=v, q_start=_starts([4]), k_start=_starts([6]), out=torch.empty_like(q),
+                workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    B.oq_attention(**args)
+    bad = [{name: t.cpu()} for name, t in args.items()]
+    bad += [dict(workspace=torch.empty(1 << 18, device="cuda")), dict(workspace=args["workspace"][:1].expand(1 << 20))]
+    for change in bad:
+        with pytest.raises(B.OqError) as e:
+            B.oq_attention(**{**args, **change})
+        assert e.value.code == 1, change.keys()

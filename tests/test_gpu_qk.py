@@ -153,3 +153,16 @@ def test_refusals():
     assert code(x.half(), None, rope, pos) == 1
     assert code(x, x.float(), rope, pos) == 1
     assert code(x, None, rope, pos, eps=-1.0) == 1
+
+
+def test_tensors_off_the_device_are_refused():
+    import torch
+    x = torch.zeros(3, 2, 128, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(128, dtype=torch.bfloat16, device="cuda")
+    args = dict(Q=x, K=x.clone(), rope=B.oq_make_rope([16, 56, 56], [4, 4, 4], 10000.0), pos=torch.zeros(3, 3, dtype=torch.int32, device="cuda"),
+                wq=w, wk=w.clone(), out_q=x.clone(), out_k=x.clone())
+    B.oq_qk_norm_rope(**args)
+    for name in ("Q", "K", "pos", "wq", "wk", "out_q", "out_k"):
+        with pytest.raises(B.OqError) as e:
+            B.oq_qk_norm_rope(**{**args, name: args[name].cpu()})
+        assert e.value.code == 1, name

@@ -59,3 +59,14 @@ def test_rows_that_lie_over_each_other_are_refused(field, stride):
 @pytest.mark.parametrize("stride", [8, 56, -64])
 def test_heads_that_overlap_in_part_are_refused(field, stride):
     assert _attention_code(**{field: stride}) == 1
+
+
+def test_host_tensors_are_refused():
+    """A pointer to host memory never reaches a kernel."""
+    import torch
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    assert _code(B.oq_attention, x, x, x) == 1
+    assert _code(B.oq_qk_norm_rope, x, x) == 1
+    a, b = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 16, 8, dtype=torch.bfloat16)
+    start, seg = torch.tensor([0, 3], dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    assert _code(B.oq_adapter_add, x[:, 0], a, b, torch.ones(1), start, seg, torch.zeros(3, 16, dtype=torch.bfloat16)) == 1
