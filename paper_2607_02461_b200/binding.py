@@ -14,6 +14,7 @@ _LIB_PATH = os.path.join(_HERE, "liboq.so")
 _lib = None
 
 OQ_BF16, OQ_F32 = 0, 1
+_INT_MAX = 2 ** 31 - 1
 STATUS_NAMES = {0: "OQ_OK", 1: "OQ_ERR_INVALID_ARG", 2: "OQ_ERR_UNSUPPORTED", 3: "OQ_ERR_ALIGNMENT",
                 4: "OQ_ERR_CUDA", 5: "OQ_ERR_DEVICE_TIMEOUT", 6: "OQ_ERR_NOMEM"}
 
@@ -482,6 +483,8 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
             raise OqError(3, "oq_qk_norm_rope: the positions of a token must be adjacent")
         if n <= 1:
             ldpos = axes
+        if ldpos > _INT_MAX:                         # (ctypes would cut it to 32 bits)
+            raise OqError(2, "oq_qk_norm_rope: a stride of positions above 2^31 - 1")
         table, at = rope.handle, pos.data_ptr()
     code = (_lib or lib()).oq_qk_norm_rope(q_side, k_side, n, head_dim, table, at, ldpos, norm_code, eps, x_code, y_code,
                                            torch._C._cuda_getCurrentRawStream(device))
@@ -542,8 +545,11 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     if want_lse:
         lse = Q.new_empty((heads, tq), dtype=torch.float32)
         lse_at = lse.data_ptr()
-    args = _ATTENTION_ARGS.pack(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qt, qh, kt, kh, vt, vh, out.data_ptr(), ot, oh, lse_at,
-                                q_at, k_at, n_seqs, tq, tk, heads, kv_heads, head_dim, left, right, sinks, scale)
+    try:
+        args = _ATTENTION_ARGS.pack(Q.data_ptr(), K.data_ptr(), V.data_ptr(), qt, qh, kt, kh, vt, vh, out.data_ptr(), ot, oh, lse_at,
+                                    q_at, k_at, n_seqs, tq, tk, heads, kv_heads, head_dim, left, right, sinks, scale)
+    except (struct.error, OverflowError):
+        raise OqError(1, "oq_attention: sizes and the window must be whole numbers of 32 bits, scale a number in fp32") from None
     L = _lib or lib()
     space = size = 0
     if workspace is not None:
@@ -595,6 +601,8 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
         raise OqError(3, "oq_adapter_add: the elements of a row must be adjacent")
     if n <= 1:
         ldx, ldb, ldy = d, m, m
+    if max(ldx, ldb, ldy) > _INT_MAX:                # (ctypes would cut it to 32 bits)
+        raise OqError(2, "oq_adapter_add: a leading dimension above 2^31 - 1")
     space = size = 0
     if workspace is not None:
         _check_workspace("oq_adapter_add", workspace, torch)

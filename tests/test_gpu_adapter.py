@@ -197,3 +197,15 @@ def test_tensors_off_the_device_and_odd_tables_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_adapter_add(**{**args, **change})
         assert e.value.code == 1, change.keys()
+
+
+def test_rows_too_far_apart_are_refused():
+    """A leading dimension that 32 bits cannot hold is an error and not another leading dimension."""
+    import torch
+    x, a, b, scale, base = _inputs(2, 64, 64, 16, 2, torch.bfloat16, 1)
+    far = torch.empty(2 ** 32 + 256, dtype=torch.bfloat16, device="cuda").as_strided((2, 64), (2 ** 32 + 64, 1))
+    far.copy_(x)
+    for args in ((far, base, None), (x, far, None), (x, base, far)):
+        with pytest.raises(B.OqError) as e:
+            B.oq_adapter_add(args[0], a, b, scale, *_tables([2], [0]), args[1], out=args[2])
+        assert e.value.code == 2

@@ -280,3 +280,11 @@ def test_tensors_off_the_device_and_odd_workspaces_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_attention(**{**args, **change})
         assert e.value.code == 1, change.keys()
+
+
+def test_window_numbers_that_do_not_fit_are_refused():
+    q, k, v = _inputs(4, 6, 2, 2, 128, 1)
+    for kw in (dict(left=2 ** 40), dict(right=-2 ** 40), dict(sinks=2 ** 31), dict(scale=1e60)):
+        with pytest.raises(B.OqError) as e:
+            B.oq_attention(q, k, v, **kw)
+        assert e.value.code == 1

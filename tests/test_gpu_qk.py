@@ -166,3 +166,13 @@ def test_tensors_off_the_device_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_qk_norm_rope(**{**args, name: args[name].cpu()})
         assert e.value.code == 1, name
+
+
+def test_positions_too_far_apart_are_refused():
+    import torch
+    x = torch.zeros(2, 2, 128, dtype=torch.bfloat16, device="cuda")
+    far = torch.empty(2 ** 32 + 16, dtype=torch.int32, device="cuda").as_strided((2, 3), (2 ** 32 + 3, 1))
+    far.zero_()
+    with pytest.raises(B.OqError) as e:
+        B.oq_qk_norm_rope(x, None, B.oq_make_rope([16, 56, 56], [4, 4, 4], 10000.0), far)
+    assert e.value.code == 2
