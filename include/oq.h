@@ -15,7 +15,9 @@
  *   - "dev" pointers are CUDA device pointers on the current device, owned by the caller (for example a
  *     PyTorch tensor's data_ptr()).  "host" pointers are ordinary host memory.  The library allocates
  *     only the small tables that belong to an oq_rpbh handle (permutation and signs, < 128 KB, uploaded on
- *     first use on the device that is current at that moment and freed by oq_rpbh_destroy).
+ *     first use on the device that is current at that moment and freed by oq_rpbh_destroy) or an oq_rope handle.
+ *     A first use may be on any stream, also on one that is being captured: what it uploads is complete before the
+ *     kernel is launched and does not become part of the graph.
  *   - `stream` is a cudaStream_t passed as void* (NULL = default stream).  Kernel launches are
  *     asynchronous on that stream; argument validation happens on the host before any launch.
  *   - Matrices are row-major.  X is [n_tokens][ldx] bf16, W is [m][ldw] bf16 (the layout of a linear

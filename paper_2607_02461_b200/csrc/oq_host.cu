@@ -226,6 +226,19 @@ cudaError_t encode_tensor_map_sw128(CUtensorMap* map, const void* base, bool f32
                            rank, dims, strides_bytes, box);
 }
 
+// Fills device memory from the host (src NULL: with zeros) and returns when the bytes are there.  cudaMemcpy from pageable memory
+// and cudaMemset may return before that, and a kernel on a stream that does not wait for the legacy stream would read ahead
+// of them: so the copy has a stream of its own, which is waited for.
+cudaError_t upload(void* dst, const void* src, size_t bytes) {
+  cudaStream_t st;
+  cudaError_t e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+  if (e != cudaSuccess) return e;
+  e = src ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaMemsetAsync(dst, 0, bytes, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  cudaStreamDestroy(st);
+  return e;
+}
+
 // First-use state (status words, device tables of the handles) is created under one mutex, so that threads making their
 // first call on a device at the same time do not allocate twice or see half-published tables.
 static std::mutex g_first_use_mutex;
@@ -236,9 +249,10 @@ int* device_status_word() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
   std::lock_guard<std::mutex> lock(g_first_use_mutex);
   if (!g_status_word[dev]) {
+    FirstUse first;
     int* p = nullptr;
     if (cudaMalloc(&p, sizeof(int)) != cudaSuccess) return nullptr;
-    if (cudaMemset(p, 0, sizeof(int)) != cudaSuccess) {
+    if (upload(p, nullptr, sizeof(int)) != cudaSuccess) {
       cudaFree(p);
       return nullptr;
     }
@@ -255,10 +269,11 @@ int ensure_wide_tables(const oq_codebook* cb) {
   std::lock_guard<std::mutex> lock(g_first_use_mutex);
   if (cb->d_wide && cb->wide_device == dev) return OQ_OK;
   if (cb->d_wide) return fail(OQ_ERR_INVALID_ARG, "codebook handle was first used on another device");
+  FirstUse first;
   WideTables* d = nullptr;
   e = cudaMalloc(&d, sizeof(WideTables));
   if (e != cudaSuccess) return cuda_fail(e, "cudaMalloc(codebook tables)");
-  e = cudaMemcpy(d, &cb->wide, sizeof(WideTables), cudaMemcpyHostToDevice);
+  e = upload(d, &cb->wide, sizeof(WideTables));
   if (e != cudaSuccess) {
     cudaFree(d);
     return cuda_fail(e, "cudaMemcpy(codebook tables)");
@@ -302,6 +317,7 @@ int ensure_device_tables(const oq_rpbh* rc) {
   }
   const int ntab = 5;
   const std::vector<uint32_t>* host[ntab] = {&g, &off, &mask, &pmask, &mm};
+  FirstUse first;
   uint32_t* dev_tab[ntab] = {nullptr, nullptr, nullptr, nullptr, nullptr};
   const char* what = "cudaMalloc(rpbh tables)";
   for (int i = 0; i < ntab && e == cudaSuccess; ++i) {
@@ -309,7 +325,7 @@ int ensure_device_tables(const oq_rpbh* rc) {
     e = cudaMalloc(&dev_tab[i], sizeof(uint32_t) * host[i]->size());
     if (e != cudaSuccess) break;
     what = "cudaMemcpy(rpbh tables)";
-    e = cudaMemcpy(dev_tab[i], host[i]->data(), sizeof(uint32_t) * host[i]->size(), cudaMemcpyHostToDevice);
+    e = upload(dev_tab[i], host[i]->data(), sizeof(uint32_t) * host[i]->size());
   }
   if (e != cudaSuccess) {
     for (int i = 0; i < ntab; ++i)
@@ -513,8 +529,8 @@ int oq_device_status(int* status) {
     e = cudaMemcpy(&code[i], word[i], sizeof(int), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(e, "cudaMemcpy(status)");
     if (code[i] != 0) {
-      e = cudaMemset(word[i], 0, sizeof(int));
-      if (e != cudaSuccess) return cuda_fail(e, "cudaMemset(status)");
+      e = upload(word[i], nullptr, sizeof(int));       // (a kernel launched after this call must not find the old code)
+      if (e != cudaSuccess) return cuda_fail(e, "clearing the status");
     }
   }
   *status = code[0] != 0 ? code[0] : code[1];

@@ -141,6 +141,15 @@ cudaError_t encode_tensor_map_bf16(CUtensorMap* map, const void* base, int rank,
 cudaError_t encode_tensor_map_sw128(CUtensorMap* map, const void* base, bool f32, int rank, const uint64_t* dims,
                                     const uint64_t* strides_bytes, const uint32_t* box);
 
+// For first-use state (device tables of the handles, status words): while it lives, this thread may allocate and copy also when a
+// stream is being captured, and none of it becomes part of the graph.
+struct FirstUse {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  FirstUse() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~FirstUse() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+cudaError_t upload(void* dst, const void* src, size_t bytes);   // returns when the bytes are on the device; src NULL: zeros
+
 // Device status word (bounded waits report here).
 int* device_status_word();   // device pointer (allocated on first use), or nullptr on failure
 

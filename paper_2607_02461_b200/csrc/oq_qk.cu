@@ -421,10 +421,11 @@ int ensure_table(const oq_rope* r) {
   std::lock_guard<std::mutex> lock(r->mutex);
   if (r->d_table && r->device == dev) return OQ_OK;
   if (r->d_table) return fail(OQ_ERR_INVALID_ARG, "rope handle was first used on another device");
+  FirstUse first;
   float2* d = nullptr;
   e = cudaMalloc(&d, r->table.size() * sizeof(float));
   if (e != cudaSuccess) return cuda_fail(e, "cudaMalloc(rope table)");
-  e = cudaMemcpy(d, r->table.data(), r->table.size() * sizeof(float), cudaMemcpyHostToDevice);
+  e = upload(d, r->table.data(), r->table.size() * sizeof(float));
   if (e != cudaSuccess) {
     cudaFree(d);
     return cuda_fail(e, "cudaMemcpy(rope table)");

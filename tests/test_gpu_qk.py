@@ -176,3 +176,36 @@ def test_positions_too_far_apart_are_refused():
     with pytest.raises(B.OqError) as e:
         B.oq_qk_norm_rope(x, None, B.oq_make_rope([16, 56, 56], [4, 4, 4], 10000.0), far)
     assert e.value.code == 2
+
+
+def test_first_use_of_a_table_on_a_side_stream():
+    """A table of 27 MB whose upload the kernel on a stream of its own must not overtake."""
+    import torch
+    _, q, k = _inputs(300, 4, 2, 128, 11, torch.bfloat16)
+    pos = torch.arange(70000 - 300, 70000, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for theta in (10000.0, 500.0, 77.0):
+        rope = B.oq_make_rope([96], [70000], theta)
+        with torch.cuda.stream(side):
+            y, _ = B.oq_qk_norm_rope(q, None, rope, pos, out_dtype=torch.float32)
+        side.synchronize()
+        _check(y, q, None, "head", pos, rope)
+
+
+def test_first_use_of_a_table_while_a_stream_is_captured():
+    import torch
+    _, q, k = _inputs(50, 4, 2, 128, 12, torch.bfloat16)
+    pos = torch.randint(0, 40, (50, 3), dtype=torch.int32, device="cuda")
+    rope, again = (B.oq_make_rope([44, 42, 42], [40, 40, 40], 10000.0) for _ in range(2))
+    B.oq_qk_norm_rope(q, k)                          # (the kernel itself is loaded)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        yq, yk = B.oq_qk_norm_rope(q, k, rope, pos)
+    for _ in range(2):
+        yq.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        want_q, want_k = B.oq_qk_norm_rope(q, k, again, pos)
+        assert torch.equal(yq, want_q) and torch.equal(yk, want_k)
