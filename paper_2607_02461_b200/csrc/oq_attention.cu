@@ -51,6 +51,7 @@ constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
 constexpr int MAX_PARTS = 32;
 constexpr float SLACK = 8.f;              // powers stay below 2^8
+constexpr float FAR = 4096.f;             // references above this (as exponents) are subtracted before the scaling, see below
 enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46 };
 
 template <int D>
@@ -72,7 +73,7 @@ struct Params {
   int wide_out;                           // rows of out begin on 32 bytes: whole sectors a store (packed ragged requests 63 us, in 16 bytes 68)
   float* lse;                             // [heads][total_q] or NULL
   float* part_o;                          // [parts][heads][total_q][D]: sums scaled to weights that add up to one
-  float* part_lse;                        // [parts][heads][total_q], base 2
+  float2* part_ml;                        // [parts][heads][total_q]: reference m and sum l of a part's powers
   const int *q_start, *k_start;           // n_seqs + 1, or NULL: one sequence
   int total_q, total_k, n_seqs, heads, group;
   int q_step, k_step, v_step;             // of the head coordinate in the tensor maps: 1, or 0 where one head serves all (stride 0)
@@ -190,6 +191,10 @@ __device__ __forceinline__ uint32_t ones_below(int n) {
   return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u);
 }
 
+__device__ __forceinline__ float natural_lse(const Params& p, float m, float l) {
+  return l == 0.f ? -INFINITY : fmaf(m, p.scale_log2, log2f(l)) * 0.69314718055994531f;
+}
+
 // One row again, key by key over the keys it sees, by a whole warp (each lane holds D / 32 coordinates).
 template <int D>
 __device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>& it, int qi, int t) {
@@ -214,8 +219,7 @@ __device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>
       for (int i = 0; i < N; ++i) s = fmaf(q[i], __bfloat162float(p.K[at * p.ldk + hk * p.hdk + lane * N + i]), s);
 #pragma unroll
       for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-      s *= p.scale_log2;
-      const float mn = fmaxf(m, s), a = m == mn ? 1.f : exp2f(m - mn), w = s == -INFINITY ? 0.f : exp2f(s - mn);
+      const float c = p.scale_log2, mn = fmaxf(m, s), a = m == mn ? 1.f : exp2f((m - mn) * c), w = s == -INFINITY ? 0.f : exp2f((s - mn) * c);
       m = mn;
       l = l * a + w;
 #pragma unroll
@@ -225,18 +229,18 @@ __device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>
       }
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   const long long row = (long long)it.head * p.total_q + it.q_base + qi;
   if (p.parts > 1) {
     const long long at = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + row;
 #pragma unroll
     for (int i = 0; i < N; ++i) p.part_o[at * D + lane * N + i] = o[i] * inv;
-    if (lane == 0) p.part_lse[at] = lse2;
+    if (lane == 0) p.part_ml[at] = make_float2(m, l);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       p.out[(long long)(it.q_base + qi) * p.ldo + it.head * p.hdo + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
-    if (lane == 0 && p.lse) p.lse[row] = lse2 * 0.69314718055994531f;
+    if (lane == 0 && p.lse) p.lse[row] = natural_lse(p, m, l);
   }
 }
 
@@ -451,7 +455,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
             tmem_store16(col_o + 16u * x, o);
           }
         }
-        const float shift = m == -INFINITY ? 0.f : -m * c;
+        float shift = m == -INFINITY ? 0.f : -m * c;
+        // s c - m c with m c rounded is off by half a unit of m c: 2^-12 at the limit here, but beyond 2^31 enough to lose the maximum's
+        // own weight, which has to be 2^0.  There s - m comes first, which is exact wherever the power is not zero.
+        if (__any_sync(~0u, fabsf(shift) > FAR)) {
+          const float ref = m == -INFINITY ? 0.f : m;
+          shift = 0.f;
+#pragma unroll
+          for (int e = 0; e < BN; ++e) sr[e] = __float_as_uint(__uint_as_float(sr[e]) - ref);
+        }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         // one warp of the two that share a scheduler exponentiates while the other does all else
         if (turns && (t == 1 || j > 0)) turn_wait();
@@ -491,7 +503,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       float probe[4] = {0.f, 0.f, 0.f, 0.f};
-      const float lse2 = l == 0.f ? -INFINITY : fmaf(m, c, log2f(l));
       const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
       const long long part_row = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + out_row;
       __nv_bfloat16* const dst = p.out + (long long)(it.q_base + qi) * p.ldo + it.head * p.hdo;
@@ -530,8 +541,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         }
       }
       if (mine) {
-        if (p.parts > 1) p.part_lse[part_row] = lse2;
-        else if (p.lse) p.lse[out_row] = lse2 * 0.69314718055994531f;
+        if (p.parts > 1) p.part_ml[part_row] = make_float2(m, l);
+        else if (p.lse) p.lse[out_row] = natural_lse(p, m, l);
       }
       tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
       // what is not finite is written again, by the whole warp
@@ -661,7 +672,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
 }
 
-// Joins the parts of a row: weights 2^(lse_i - max) over their sum.  One warp per (token, head).
+// Joins the parts of a row: weights l_i 2^(c (m_i - max m)) over their sum.  (Not from the parts' log sums: with scores of 1e9 those hold no
+// more than m.)  One warp per (token, head).
 template <int D>
 __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_constant__ Params p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -673,11 +685,11 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   if (row >= rows) return;
   const int head = (int)(row / p.total_q), tok = (int)(row % p.total_q);
   if (p.q_start && (tok < __ldg(p.q_start) || tok >= __ldg(p.q_start + p.n_seqs))) return;      // no sequence owns it: no part was written
-  const float mine = lane < p.parts ? p.part_lse[lane * rows + row] : -INFINITY;
-  float top = mine;
+  const float2 mine = lane < p.parts ? p.part_ml[lane * rows + row] : make_float2(-INFINITY, 0.f);
+  float top = mine.x;
 #pragma unroll
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  const float w = mine == -INFINITY ? 0.f : exp2f(mine - top);
+  const float w = mine.y == 0.f ? 0.f : mine.y * exp2f((mine.x - top) * p.scale_log2);
   float total = w;
 #pragma unroll
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
@@ -695,7 +707,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   __nv_bfloat16* dst = p.out + (long long)tok * p.ldo + head * p.hdo + lane * N;
 #pragma unroll
   for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16(o[i] * inv, o[i + 1] * inv);
-  if (lane == 0 && p.lse) p.lse[row] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+  if (lane == 0 && p.lse) p.lse[row] = natural_lse(p, top, total);
 }
 
 int sm_count() {
@@ -828,7 +840,7 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.wide_out = reinterpret_cast<uintptr_t>(a->out) % 32 == 0 && a->ldo_token % 16 == 0 && a->ldo_head % 16 == 0;
   p.lse = a->lse;
   p.part_o = reinterpret_cast<float*>(workspace);
-  p.part_lse = p.part_o + (size_t)p.parts * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim;
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)p.parts * a->n_heads * (size_t)a->total_q * (size_t)a->head_dim);
   p.q_start = a->q_start; p.k_start = a->k_start;
   p.total_q = a->total_q; p.total_k = a->total_k;
   p.n_seqs = a->n_seqs; p.heads = a->n_heads; p.group = a->n_heads / a->n_kv_heads;

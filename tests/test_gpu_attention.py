@@ -288,3 +288,44 @@ def test_window_numbers_that_do_not_fit_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_attention(q, k, v, **kw)
         assert e.value.code == 1
+
+
+@pytest.mark.parametrize("size", [1e5, 3e7, 1e11, 1e20, 1e30])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("nq,nk", [(5, 1), (150, 300), (2, 5000)])
+def test_scores_of_any_finite_size(nq, nk, sign, size):
+    """The largest score's key gets its weight however large the scores are.  The scores are fp32 sums of exact products, off by at
+    most 2^-17 of sum |q k|: rows whose best two keys lie closer than twice that and 40 exponents are left out, and in
+    the others one key has weight 1, so that out is its value (one rounding of a weight, one of the output)."""
+    d, h, hk = 128, 2, 1
+    q, k, v = _inputs(nq, nk, h, hk, d, 81)
+    q, k = (q.abs() * sign * size ** 0.5).bfloat16(), (k.abs() * size ** 0.5).bfloat16()
+    out, lse = _run(q, k, v, [nq], [nk])
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    z = np.einsum("ihd,jd->hij", f(q), f(k)[:, 0]) / np.sqrt(d)           # (all products have one sign: sum |q k| = |z|)
+    best = z.argmax(2)
+    top = z.max(2)
+    rest = np.where(np.arange(nk) == best[..., None], -np.inf, z).max(2)
+    clear = top - rest > 2 * 2.0 ** -17 * np.abs(z).max(2) + 40
+    assert clear.mean() > 0.5 or size < 1e6
+    want = f(v)[best, 0].transpose(1, 0, 2)
+    err = np.abs(f(out) - want)
+    assert np.all((err <= 2.0 ** -7 * np.abs(want))[clear.T])
+    assert np.all(np.isfinite(f(lse))) and np.all(np.abs(f(lse) - top)[clear] <= 2.0 ** -16 * np.abs(top)[clear])
+
+
+@pytest.mark.parametrize("score", [700.0, -9e4, 6e10, -1.7e11, 2e20])
+@pytest.mark.parametrize("nq,nk", [(130, 257), (1, 5003)])
+def test_equal_scores_share_their_weight_at_any_size(nq, nk, score):
+    """Equal keys have equal scores bit for bit, so out is the mean of the values, also across parts of unequal length.  The weights
+    and l are equal powers and their sum: fp32 sums (2^-20 here) and the one rounding of the output."""
+    import torch
+    _, _, v = _inputs(1, nk, 1, 1, 128, 82)
+    half = abs(score) ** 0.5
+    q = torch.full((nq, 1, 128), half if score > 0 else -half, dtype=torch.bfloat16, device="cuda")
+    k = torch.full((nk, 1, 128), half, dtype=torch.bfloat16, device="cuda")
+    out, lse = _run(q, k, v, [nq], [nk], scale=1 / 128)
+    mean = v.double().mean(0)
+    assert torch.all((out.double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -8 * v.double().abs().mean(0) + 1e-30)
+    z = q[0, 0, 0].double() * k[0, 0, 0].double()
+    assert torch.all((lse.double() - z - np.log(nk)).abs() <= 1e-5 * (1 + z.abs()))
