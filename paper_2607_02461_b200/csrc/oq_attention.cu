@@ -32,7 +32,7 @@
 // powers are made with the old reference 227 us.
 //
 // NaN and infinities in keys and values that a row does not see must not reach it, but 0 * NaN is NaN: a row whose
-// result is not finite (checked once, at the end) is computed again key by key over what it sees.
+// result is not finite (checked once, at the end) is made again over what it sees, unless what it sees explains it (redo_rows).
 #include <cuda_bf16.h>
 
 #include <string>
@@ -51,7 +51,9 @@ constexpr int BM = 128;                   // query rows of a tile
 constexpr int MAX_SEQS = 256;
 constexpr int MAX_PARTS = 32;
 constexpr float SLACK = 8.f;              // powers stay below 2^8
-constexpr float FAR = 4096.f;             // references above this (as exponents) are subtracted before the scaling, see below
+constexpr float FAR = 65536.f;            // rows whose reference passes this (as an exponent) are made again, see below
+// While a warp makes rows again the others wait for it: the limit of the waits has this for each key, five times what 32 rows take.
+constexpr long long REDO_CYCLES = 32768;
 enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46 };
 
 template <int D>
@@ -82,6 +84,7 @@ struct Params {
   int parts;                              // results of a row to be joined: splits, twice as many when dual
   int left, right, sinks;
   float scale, scale_log2;
+  long long max_wait;                     // cycles, see REDO_CYCLES
   int* status;
 };
 
@@ -195,53 +198,190 @@ __device__ __forceinline__ float natural_lse(const Params& p, float m, float l) 
   return l == 0.f ? -INFINITY : fmaf(m, p.scale_log2, log2f(l)) * 0.69314718055994531f;
 }
 
-// One row again, key by key over the keys it sees, by a whole warp (each lane holds D / 32 coordinates).
+// Rows `again` of a warp's 32 (row r: query qi0 + r) once more, over the keys that they see and no others.  Four rows and 8 keys at a
+// time: a quarter of a key per lane for the scores, then D / 32 coordinates per lane for the values.  What bounds it are the latencies of its
+// loads, which the rows share: 190 cycles for a row and a key with all 8 warps at it (two rows at a time 230, one 490).
+// (Kept below the 168 registers that the kernel is launched with, without spills: a form that held 32 keys and the sums of 32 rows wanted
+// twice that, with 1120 bytes of stack, and its first call ended as an illegal instruction.)
 template <int D>
-__device__ __noinline__ void exact_row(const Params& p, const Item<Shape<D>::BN>& it, int qi, int t) {
+__device__ __noinline__ void exact_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t again) {
   constexpr int BN = Shape<D>::BN;
-  constexpr int N = D / 32;
-  const int lane = threadIdx.x & 31, hk = it.head / p.group;
-  const int hi = row_hi(p, it, qi), lo = row_lo(p, it, qi);
-  float q[N], o[N], m = -INFINITY, l = 0.f;
+  constexpr int N = D / 32, ROWS = 4;
+  const int lane = threadIdx.x & 31, hk = it.head / p.group, quarter = lane >> 3;
+  const float c = p.scale_log2;
+  const int nk = it.nk, tiles = it.tiles, sinks = p.sinks;
+  const long long ldk = p.ldk, ldv = p.ldv;
+  const __nv_bfloat16* const Q = p.Q + (long long)(it.q_base + qi0) * p.ldq + it.head * p.hdq + lane * N;
+  const __nv_bfloat16 *const K = p.K + it.k_base * p.ldk + hk * p.hdk + quarter * (D / 4), *const V = p.V + it.k_base * p.ldv + hk * p.hdv + lane * N;
+  while (again) {
+    int row[ROWS], hi[ROWS], lo[ROWS];
+    uint32_t q[ROWS][N / 2];
+    float m[ROWS], l[ROWS], o[ROWS][N];            // o: the mean of the values so far (their sum may leave the range)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = __bfloat162float(p.Q[(long long)(it.q_base + qi) * p.ldq + it.head * p.hdq + lane * N + i]);
-    o[i] = 0.f;
-  }
-  for (int j = 0; j < it.tiles; ++j) {
-    if (!takes(p, t, j)) continue;
-    const int k0 = it.key0(j);
-    for (int key = k0; key < k0 + BN && key <= hi; ++key) {
-      if (key < lo && key >= p.sinks) continue;
-      const long long at = it.k_base + key;
-      float s = 0.f;
+    for (int r = 0; r < ROWS; ++r) {
+      row[r] = again ? __ffs(again) - 1 : -1;
+      again &= again - 1;
+      hi[r] = row[r] < 0 ? -1 : row_hi(p, it, qi0 + row[r]);
+      lo[r] = row_lo(p, it, qi0 + max(row[r], 0));
+      m[r] = -INFINITY;
+      l[r] = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) s = fmaf(q[i], __bfloat162float(p.K[at * p.ldk + hk * p.hdk + lane * N + i]), s);
+      for (int i = 0; i < N / 2; ++i) q[r][i] = __ldg(reinterpret_cast<const uint32_t*>(Q + max(row[r], 0) * p.ldq) + i);
 #pragma unroll
-      for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-      const float c = p.scale_log2, mn = fmaxf(m, s), a = m == mn ? 1.f : exp2f((m - mn) * c), w = s == -INFINITY ? 0.f : exp2f((s - mn) * c);
-      m = mn;
-      l = l * a + w;
+      for (int i = 0; i < N; ++i) o[r][i] = 0.f;
+    }
+    for (int j = 0; j < tiles; ++j) {
+      if (!takes(p, t, j)) continue;
+      for (int k0 = it.key0(j), end = min(k0 + BN, nk); k0 < end; k0 += 8) {
+        const int key = k0 + (lane & 7);
+        uint4 k[D / 32];
+        uint32_t v[8][N / 2];
+        // (keys past the end are seen by no row: the last one stands in for them)
+        const uint4* const kp = reinterpret_cast<const uint4*>(K + min(key, nk - 1) * ldk);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float v = __bfloat162float(p.V[at * p.ldv + hk * p.hdv + lane * N + i]);
-        o[i] = o[i] * a + w * v;
+        for (int x = 0; x < D / 32; ++x) k[x] = __ldg(kp + x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const __nv_bfloat16* const vp = V + min(k0 + e, nk - 1) * ldv;
+          if (N == 4) {
+            const uint2 two = __ldg(reinterpret_cast<const uint2*>(vp));
+            v[e][0] = two.x;
+            v[e][N / 2 - 1] = two.y;
+          } else {
+            v[e][0] = __ldg(reinterpret_cast<const uint32_t*>(vp));
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          const bool see = key <= hi[r] && (key >= lo[r] || key < sinks);
+          const uint32_t seen = __ballot_sync(~0u, see);
+          if (!seen) continue;
+          float s = 0.f;
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x) {
+            const uint32_t w[4] = {k[x].x, k[x].y, k[x].z, k[x].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {          // the quarter's pair 4 x + e of the query is in lane 8 quarter + (4 x + e) / (N / 2)
+              const uint32_t u = __shfl_sync(~0u, q[r][(4 * x + e) % (N / 2)], 8 * quarter + (4 * x + e) / (N / 2));
+              s = fmaf(__uint_as_float(u << 16), __uint_as_float(w[e] << 16), s);
+              s = fmaf(__uint_as_float(u & 0xFFFF0000u), __uint_as_float(w[e] & 0xFFFF0000u), s);
+            }
+          }
+          s += __shfl_xor_sync(~0u, s, 16);
+          s += __shfl_xor_sync(~0u, s, 8);
+          if (!see) s = -INFINITY;
+          float mn = s;
+#pragma unroll
+          for (int d = 4; d; d >>= 1) mn = fmaxf(mn, __shfl_xor_sync(~0u, mn, d));
+          mn = fmaxf(mn, m[r]);
+          float w = s == -INFINITY ? 0.f : exp2f((s - mn) * c), sum = w;
+#pragma unroll
+          for (int d = 4; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+          const float before = l[r] * (m[r] == mn ? 1.f : exp2f((m[r] - mn) * c)), inv = before + sum == 0.f ? 0.f : 1.f / (before + sum);
+          m[r] = mn;
+          l[r] = before + sum;
+          w *= inv;
+#pragma unroll
+          for (int i = 0; i < N; ++i) o[r][i] *= before * inv;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float we = __shfl_sync(~0u, w, e);
+            if ((seen >> e) & 1u)
+#pragma unroll
+              for (int i = 0; i < N; ++i) o[r][i] = fmaf(we, __uint_as_float(i & 1 ? v[e][i / 2] & 0xFFFF0000u : v[e][i / 2] << 16), o[r][i]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (row[r] < 0) continue;
+      const int qi = qi0 + row[r];
+      const long long at = (long long)it.head * p.total_q + it.q_base + qi;
+      if (p.parts > 1) {
+        const long long part = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.part_o[part * D + lane * N + i] = o[r][i];
+        if (lane == 0) p.part_ml[part] = make_float2(m[r], l[r]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.out[(long long)(it.q_base + qi) * p.ldo + it.head * p.hdo + lane * N + i] = __float2bfloat16_rn(o[r][i]);
+        if (lane == 0 && p.lse) p.lse[at] = natural_lse(p, m[r], l[r]);
       }
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const long long row = (long long)it.head * p.total_q + it.q_base + qi;
-  if (p.parts > 1) {
-    const long long at = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + row;
+}
+
+// Rows `odd` of a warp's 32 (row r: query qi0 + r) have finite weights and a result that is not finite.  In most cases that is the result: a
+// value that the row sees is not finite.  It is not where the only such values in a column are ones that the row does not see (0 * NaN), or
+// where the sums left the range on their way.  So the values of the item's tiles are looked through (only until all is
+// explained), and the rows with a column that what they see does not explain are returned: of one NaN in the values those are at most
+// the rows of the blocks at the mask's edges, whatever the number of rows that see it.  (8192 x 8192 x 4 heads, causal: 0.16 ms, with one NaN
+// seen by all but 300 rows 0.90 ms; with every such row made again 144 ms.)
+template <int D>
+__device__ uint32_t unexplained_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t odd) {
+  constexpr int BN = Shape<D>::BN;
+  constexpr int N = D / 32, AHEAD = 8;
+  const int lane = threadIdx.x & 31, hk = it.head / p.group;
+  // bit r of a lane's words: row r, in the lane's N columns
+  uint32_t bad[N], nan_seen[N], inf_seen[N], hidden[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) p.part_o[at * D + lane * N + i] = o[i] * inv;
-    if (lane == 0) p.part_ml[at] = make_float2(m, l);
-  } else {
+  for (int i = 0; i < N; ++i) bad[i] = nan_seen[i] = inf_seen[i] = hidden[i] = 0u;
+  for (uint32_t rest = odd; rest; rest &= rest - 1) {
+    const int r = __ffs(rest) - 1;
+    const long long row = (long long)it.head * p.total_q + it.q_base + qi0 + r;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      p.out[(long long)(it.q_base + qi) * p.ldo + it.head * p.hdo + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
-    if (lane == 0 && p.lse) p.lse[row] = natural_lse(p, m, l);
+    for (int i = 0; i < N; ++i) {
+      const float v = p.parts > 1 ? p.part_o[((long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + row) * D + lane * N + i]
+                                  : __bfloat162float(p.out[(long long)(it.q_base + qi0 + r) * p.ldo + it.head * p.hdo + lane * N + i]);
+      if (!(fabsf(v) < INFINITY)) bad[i] |= 1u << r;
+    }
   }
+  const int hi = row_hi(p, it, qi0 + lane), lo = row_lo(p, it, qi0 + lane);
+  const __nv_bfloat16* const V = p.V + it.k_base * p.ldv + hk * p.hdv + lane * N;
+  for (int j = 0; j < it.tiles; ++j) {
+    if (!takes(p, t, j)) continue;
+    const int k0 = it.key0(j), end = min(k0 + BN, p.total_k - it.k_base);       // (all that the product went over)
+    for (int k = k0; k < end; k += AHEAD) {
+      uint32_t v[AHEAD][N / 2], some = 0;
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v[e][i] = k + e < end ? *reinterpret_cast<const uint32_t*>(V + (k + e) * p.ldv + 2 * i) : 0u;
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) some |= (v[e][i] & 0x7F80u) == 0x7F80u || (v[e][i] & 0x7F800000u) == 0x7F800000u;
+      if (!__any_sync(~0u, some)) continue;
+      bool explained = true;
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) {
+        const uint32_t sees = __ballot_sync(~0u, k + e <= hi && (k + e >= lo || k + e < p.sinks));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t x = (i & 1 ? v[e][i / 2] >> 16 : v[e][i / 2]) & 0x7FFFu;
+          if (x < 0x7F80u) continue;
+          if (x > 0x7F80u) nan_seen[i] |= sees; else inf_seen[i] |= sees;
+          hidden[i] |= ~sees;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) explained &= !(bad[i] & ~nan_seen[i]);
+      if (__all_sync(~0u, explained)) return 0u;
+    }
+  }
+  uint32_t again = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) again |= bad[i] & ~nan_seen[i] & ~(inf_seen[i] & ~hidden[i]);
+  return __reduce_or_sync(~0u, again);
+}
+
+// By a whole warp: rows `odd` where what they see does not explain them, and rows `sure` in any case.
+template <int D>
+__device__ __noinline__ void redo_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t odd, uint32_t sure) {
+  __syncwarp();                                  // (each row was written by a lane of its own)
+  const uint32_t again = sure | (odd ? unexplained_rows<D>(p, it, qi0, t, odd) : 0u);
+  if (again) exact_rows<D>(p, it, qi0, t, again);
 }
 
 template <int D>
@@ -350,13 +490,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     const float c = p.scale_log2;
     uint32_t steps = 0, items = 0;              // of this tile so far
     auto warp_wait = [&](uint32_t bar, uint32_t parity, int code) {
-      mbar_spin(bar, parity, &abort_flag, p.status, code);
+      mbar_spin(bar, parity, &abort_flag, p.status, code, p.max_wait);
       __syncwarp();
     };
     // Warp w of tile 0 and of tile 1 sit on the same scheduler.  They take turns: left alone they run in step, fight for the
     // exponential unit and then leave it idle together.  (The turns are counted, so no warp leaves its loops early, not
     // even when a wait has given up.)
     const int quarter = warp & 3;
+    auto is_far = [&](float m) { return fabsf(m) * c > FAR && fabsf(m) < INFINITY; };
     auto turn_wait = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + 2 * quarter + t) : "memory"); };
     auto turn_pass = [&]() { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 2 * quarter - t) : "memory"); };
     for (int i = blockIdx.x; i < n_items; i += gridDim.x) {
@@ -381,6 +522,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       if (rows == 0) continue;
       const bool idle = quarter * 32 >= rows;            // none of the warp's rows exists
       float m = -INFINITY, l = 0.f;
+      // The powers are 2^(s c - m c) with m c rounded: the maximum's own power, which has to be 1, is off by half a unit of m c in the
+      // exponent.  Up to FAR that is at most 2^-9, as s c itself is; beyond 2^31 it lost the power altogether.  Rows that have passed
+      // FAR are made again with s - m before the scaling.  (Subtracting first here, in a branch that is never taken, cost 2 us an item.)
+      bool far = false;
       const int j0 = p.dual ? t : 0, jd = p.dual ? 2 : 1;
       for (int j = j0; j < tiles; j += jd, ++steps) {
         const int k0 = BN * (first + j + (j < n_sink ? 0 : skipped));
@@ -440,10 +585,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
         if (j == j0) {
           m = mn;
+          far = is_far(m);
         } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
           // (S_t of this key tile is there, so O_t holds the tiles before it and nothing is writing it)
           const float a = m == mn ? 1.f : exp2_fast((m - mn) * c);
           m = mn;
+          far = far || is_far(m);
           l *= a;
 #pragma unroll 1
           for (int x = 0; x < D / 16; ++x) {
@@ -455,15 +602,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
             tmem_store16(col_o + 16u * x, o);
           }
         }
-        float shift = m == -INFINITY ? 0.f : -m * c;
-        // s c - m c with m c rounded is off by half a unit of m c: 2^-12 at the limit here, but beyond 2^31 enough to lose the maximum's
-        // own weight, which has to be 2^0.  There s - m comes first, which is exact wherever the power is not zero.
-        if (__any_sync(~0u, fabsf(shift) > FAR)) {
-          const float ref = m == -INFINITY ? 0.f : m;
-          shift = 0.f;
-#pragma unroll
-          for (int e = 0; e < BN; ++e) sr[e] = __float_as_uint(__uint_as_float(sr[e]) - ref);
-        }
+        const float shift = m == -INFINITY ? 0.f : -m * c;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         // one warp of the two that share a scheduler exponentiates while the other does all else
         if (turns && (t == 1 || j > 0)) turn_wait();
@@ -503,6 +642,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
       float probe[4] = {0.f, 0.f, 0.f, 0.f};
+      const float lse = natural_lse(p, m, l);
       const long long out_row = (long long)it.head * p.total_q + it.q_base + qi;
       const long long part_row = (long long)(p.dual ? 2 * it.split + t : it.split) * p.heads * p.total_q + out_row;
       __nv_bfloat16* const dst = p.out + (long long)(it.q_base + qi) * p.ldo + it.head * p.hdo;
@@ -515,7 +655,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-          const float v = any ? __uint_as_float(o[e]) * inv : 0.f;
+          const float v = l != 0.f ? __uint_as_float(o[e]) * inv : 0.f;
           probe[e & 3] = fmaf(v, 0.f, probe[e & 3]);               // stays zero while everything is finite
           o[e] = __float_as_uint(v);
         }
@@ -542,16 +682,13 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       }
       if (mine) {
         if (p.parts > 1) p.part_ml[part_row] = make_float2(m, l);
-        else if (p.lse) p.lse[out_row] = natural_lse(p, m, l);
+        else if (p.lse) p.lse[out_row] = lse;
       }
       tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
-      // what is not finite is written again, by the whole warp
-      uint32_t again = __ballot_sync(~0u, mine && !((probe[0] + probe[1]) + (probe[2] + probe[3]) == 0.f));
-      while (again) {
-        const int r = __ffs(again) - 1;
-        again &= again - 1;
-        exact_row<D>(p, it, qi - lane + r, t);
-      }
+      // (Where l is not finite, the row sees a score that is not, and has its result.)
+      const uint32_t sure = __ballot_sync(~0u, mine && far);
+      const uint32_t odd = __ballot_sync(~0u, mine && fabsf(l) < INFINITY && !((probe[0] + probe[1]) + (probe[2] + probe[3]) == 0.f));
+      if (sure | odd) redo_rows<D>(p, it, qi - lane, t, odd & ~sure, sure);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -566,7 +703,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       if (lane == 0) {
         uint32_t q_use[2] = {0, 0};
         auto load_kv = [&](const Step& s, const CUtensorMap* map, int head_step) {
-          if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
+          if (round > 0) mbar_wait(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE, p.max_wait);
           mbar_expect_tx(kv_full(slot), S::KV_TILE);
           for (uint32_t a = 0; a < S::ATOMS; ++a)
             tma_load_3d(smem_kv + slot * S::KV_TILE + a * S::KV_ATOM, map, 64 * (int)a, s.it.head / p.group * head_step, s.it.k_base + s.it.key0(s.j), kv_full(slot));
@@ -576,7 +713,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           if (s.j == 0) {
             for (int t = 0; t < 2; ++t) {
               if (t == 1 && (s.it.rows1 == 0 || (p.dual && s.it.tiles == 1))) continue;      // no step of this tile
-              if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE);
+              if (q_use[t] > 0) mbar_wait(q_free(t), (q_use[t] - 1) & 1, &abort_flag, p.status, W_QFREE, p.max_wait);
               ++q_use[t];
               mbar_expect_tx(q_full(t), S::Q_TILE);
               for (uint32_t a = 0; a < S::ATOMS; ++a)
@@ -616,11 +753,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       auto do_s = [&](const Step& s) {
         // (Both warps see every slot filled and free it, whether they use it or not: a wait tells phases apart by their
         // parity alone, so no warp may get a whole round ahead of a slot or behind it.)
-        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
+        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV, p.max_wait);
         if (!active(s)) {
           if (leader) mbar_arrive(kv_free(slot));
         } else {
-          if (s.j == j0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q);
+          if (s.j == j0) mbar_spin(q_full(t), q_use++ & 1, &abort_flag, p.status, W_Q, p.max_wait);
           tc_fence_after();
           const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::Q_TILE), b = smem_desc(smem_kv + slot * S::KV_TILE);
 #pragma unroll
@@ -634,17 +771,17 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         advance();
       };
       auto do_o = [&](const Step& s) {
-        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV);
+        mbar_spin(kv_full(slot), round & 1, &abort_flag, p.status, W_KV, p.max_wait);
         if (!active(s)) {
           if (leader) mbar_arrive(kv_free(slot));
         } else {
-          mbar_spin(p_part(t), p_use & 1, &abort_flag, p.status, W_P);
+          mbar_spin(p_part(t), p_use & 1, &abort_flag, p.status, W_P, p.max_wait);
           tc_fence_after();
           const uint64_t b = smem_desc_mn(smem_kv + slot * S::KV_TILE, S::KV_ATOM, 1024);
 #pragma unroll
           for (uint32_t k = 0; k < BN / 16; ++k) {
             if (k == 6) {
-              mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P);
+              mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P, p.max_wait);
               tc_fence_after();
             }
             mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > j0 || k > 0, leader);
@@ -685,7 +822,16 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   if (row >= rows) return;
   const int head = (int)(row / p.total_q), tok = (int)(row % p.total_q);
   if (p.q_start && (tok < __ldg(p.q_start) || tok >= __ldg(p.q_start + p.n_seqs))) return;      // no sequence owns it: no part was written
+  constexpr int AHEAD = 8;                         // parts requested together (the first ones before their weights are known)
+  float v[AHEAD][N];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[s][i] = s0 + s < p.parts ? p.part_o[((s0 + s) * rows + row) * D + lane * N + i] : 0.f;
+  };
   const float2 mine = lane < p.parts ? p.part_ml[lane * rows + row] : make_float2(-INFINITY, 0.f);
+  load(0);
   float top = mine.x;
 #pragma unroll
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
@@ -693,20 +839,23 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const __grid_consta
   float total = w;
 #pragma unroll
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
+  const float share = total == 0.f ? 0.f : w / total;      // (shares first: a sum of weights times values may leave the range)
   float o[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] = 0.f;
-  for (int s = 0; s < p.parts; ++s) {
-    const float ws = __shfl_sync(~0u, w, s);
-    if (ws == 0.f) continue;                       // an empty split, or one whose share is below 2^-126
-    const float* src = p.part_o + (s * rows + row) * D + lane * N;
+  for (int s0 = 0; s0 < p.parts; s0 += AHEAD) {
+    if (s0 > 0) load(s0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = fmaf(ws, src[i], o[i]);
+    for (int s = 0; s < AHEAD; ++s) {
+      const float ws = __shfl_sync(~0u, share, s0 + s);
+      if (ws == 0.f) continue;                     // an empty split, or one whose share is below 2^-126
+#pragma unroll
+      for (int i = 0; i < N; ++i) o[i] = fmaf(ws, v[s][i], o[i]);
+    }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
   __nv_bfloat16* dst = p.out + (long long)tok * p.ldo + head * p.hdo + lane * N;
 #pragma unroll
-  for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16(o[i] * inv, o[i + 1] * inv);
+  for (int i = 0; i < N; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_bf16(o[i], o[i + 1]);
   if (lane == 0 && p.lse) p.lse[row] = natural_lse(p, top, total);
 }
 
@@ -850,6 +999,7 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
   p.sinks = a->sinks > far ? far : a->sinks;
   p.scale = a->scale > 0.f ? a->scale : (a->head_dim == 128 ? 0.08838834764831845f : 0.125f);
   p.scale_log2 = p.scale * 1.4426950408889634f;
+  p.max_wait = WAIT_CYCLES + attn::REDO_CYCLES * a->total_k;
   p.status = device_status_word();
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_attention: cannot allocate the device status word");
   CUtensorMap mq, mk, mv;

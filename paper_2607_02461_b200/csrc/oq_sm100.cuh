@@ -205,11 +205,12 @@ __device__ __forceinline__ bool mbar_try_for(uint32_t bar, uint32_t parity, uint
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ void mbar_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+__device__ __forceinline__ void mbar_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code,
+                                          long long max_cycles = WAIT_CYCLES) {
   if (mbar_try_for(bar, parity, 20000u)) return;
   const long long t0 = clock64();
   while (!*abort_flag && !mbar_try_for(bar, parity, 20000u)) {
-    if (*reinterpret_cast<volatile int*>(status) != 0 || clock64() - t0 > WAIT_CYCLES) {
+    if (*reinterpret_cast<volatile int*>(status) != 0 || clock64() - t0 > max_cycles) {
       atomicCAS(status, 0, code);
       *abort_flag = 1;
       return;

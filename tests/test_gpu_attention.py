@@ -329,3 +329,73 @@ def test_equal_scores_share_their_weight_at_any_size(nq, nk, score):
     assert torch.all((out.double() - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -8 * v.double().abs().mean(0) + 1e-30)
     z = q[0, 0, 0].double() * k[0, 0, 0].double()
     assert torch.all((lse.double() - z - np.log(nk)).abs() <= 1e-5 * (1 + z.abs()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", [dict(right=0), dict(left=60, right=0, sinks=3), dict(left=30, right=20), dict()], ids=str)
+@pytest.mark.parametrize("nq,nk", [(200, 200), (300, 555), (2, 3000), (129, 2900)])
+def test_values_that_are_not_finite_reach_exactly_the_rows_that_see_them(nq, nk, mask, d):
+    """NaN and both infinities strewn over V (several columns, some of them met twice in a column) and one key: every element is the
+    definition's, finite, infinite or NaN."""
+    import torch
+    h = 2
+    q, k, v = _inputs(nq, nk, h, 1, d, 91)
+    g = np.random.default_rng(nq + nk)
+    for what in (float("nan"), float("inf"), -float("inf"), float("nan"), float("inf")):
+        for at in (int(g.integers(nk)), nk - 1 - int(g.integers(min(nk, 120)))):
+            v[at, 0, int(g.integers(d))] = what
+    v[nk - 7, 0, 5], v[nk - 40, 0, 5], v[nk - 60, 0, 9] = float("inf"), float("nan"), -float("inf")
+    k[nk - 3, 0, 1] = float("nan")
+    out, lse = _run(q, k, v, [nq], [nk], **mask)
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        ref, ref_lse = oat.attention(f(q), f(k), f(v), [nq], [nk], **mask)
+    got, got_lse = f(out), f(lse)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(np.isnan(got_lse), np.isnan(ref_lse))
+    assert np.array_equal(np.isposinf(got), np.isposinf(ref)) and np.array_equal(np.isneginf(got), np.isneginf(ref))
+    ok = np.isfinite(ref)
+    size, _ = oat.attention(f(q), f(torch.nan_to_num(k, 0.0)), np.abs(f(torch.nan_to_num(v, 0.0, 0.0, 0.0))), [nq], [nk], **mask)
+    assert np.all(np.abs(got - ref)[ok] <= (2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 1e-3) * size)[ok] + 1e-30)
+    ok = np.isfinite(ref_lse)
+    assert np.all(np.abs(got_lse - ref_lse)[ok] <= LSE * (1 + np.abs(ref_lse[ok])))
+
+
+@pytest.mark.parametrize("nq,nk", [(200, 300), (1, 4100)])
+def test_sums_that_leave_the_range_on_the_way_do_not_show(nq, nk):
+    """Values near the type's largest: a sum of weights above 1 times such a value is infinite, the weighted mean is not."""
+    import torch
+    q, k, v = _inputs(nq, nk, 1, 1, 128, 92)
+    q[:], k[:] = 0, 0
+    q[..., 0], k[nk - 60, 0, 0] = 1.0, 5.25 * 128 ** 0.5      # the last tile's best key: weight 2^7.6 against the others'
+    k[nk - 55, 0, 0] = 40 * 128 ** 0.5
+    v[:] = 1e37
+    out, lse = _run(q, k, v, [nq], [nk])
+    assert torch.all((out.double() - v[0, 0, 0].double()).abs() <= 2.0 ** -7 * 1e37) and torch.all(torch.isfinite(lse))
+
+
+def test_one_nan_that_many_rows_see_does_not_change_the_pace():
+    """A NaN in a value that thousands of rows see is their result: they are not made again one by one.  (Key by key the rows would take
+    over a hundred times as long.)"""
+    import torch
+    n, h = 8192, 4
+    q, k, v = _inputs(n, n, h, h, 128, 93)
+
+    def pace(values):
+        times = []
+        for _ in range(5):
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record()
+            out = B.oq_attention(q, k, values, right=0)
+            e1.record()
+            torch.cuda.synchronize()
+            times.append(e0.elapsed_time(e1))
+        return min(times), out
+
+    clean, want = pace(v)
+    bad = v.clone()
+    bad[300, :, 3] = float("nan")
+    slow, got = pace(bad)
+    print("clean %.3f ms, one NaN %.3f ms" % (clean, slow))
+    assert torch.all(torch.isnan(got[300:, :, 3])) and torch.equal(got[300:, :, 4:], want[300:, :, 4:])
+    assert torch.equal(got[:256], want[:256]) and torch.all(torch.isfinite(got[256:300]))         # (the latter share the NaN's tile and are made again)
+    assert slow <= 10 * clean
