@@ -341,7 +341,7 @@ __device__ uint32_t unexplained_rows(const Params& p, const Item<Shape<D>::BN>& 
   const __nv_bfloat16* const V = p.V + it.k_base * p.ldv + hk * p.hdv + lane * N;
   for (int j = 0; j < it.tiles; ++j) {
     if (!takes(p, t, j)) continue;
-    const int k0 = it.key0(j), end = min(k0 + BN, p.total_k - it.k_base);       // (all that the product went over)
+    const int k0 = it.key0(j), end = min(k0 + BN, it.nk);
     for (int k = k0; k < end; k += AHEAD) {
       uint32_t v[AHEAD][N / 2], some = 0;
 #pragma unroll
@@ -775,6 +775,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         if (!active(s)) {
           if (leader) mbar_arrive(kv_free(slot));
         } else {
+          // Rows of V past the end of the sequence (another one's, or a buffer's that nothing has been written to) have weights of zero, but
+          // may be NaN: they are cleared, which takes less time than the weights do.  (Both mma warps write the same zeros.)
+          const int valid = s.it.nk - s.it.key0(s.j);
+          if (valid < BN && s.it.k_base + s.it.nk < p.total_k) {
+            for (uint32_t a = 0; a < S::ATOMS; ++a)
+              for (int x = valid * 8 + lane; x < BN * 8; x += 32)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(smem_kv + slot * S::KV_TILE + a * S::KV_ATOM + 16u * (uint32_t)x), "r"(0u) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
           mbar_spin(p_part(t), p_use & 1, &abort_flag, p.status, W_P, p.max_wait);
           tc_fence_after();
           const uint64_t b = smem_desc_mn(smem_kv + slot * S::KV_TILE, S::KV_ATOM, 1024);

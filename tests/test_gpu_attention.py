@@ -399,3 +399,27 @@ def test_one_nan_that_many_rows_see_does_not_change_the_pace():
     assert torch.all(torch.isnan(got[300:, :, 3])) and torch.equal(got[300:, :, 4:], want[300:, :, 4:])
     assert torch.equal(got[:256], want[:256]) and torch.all(torch.isfinite(got[256:300]))         # (the latter share the NaN's tile and are made again)
     assert slow <= 10 * clean
+
+
+def test_a_buffer_that_nothing_was_written_to_does_not_change_the_pace():
+    """Keys and values in a larger buffer whose rest is NaN: nothing is made again, so the call takes what it takes beside zeros."""
+    import torch
+    nq, nk, h = 1000, 4001, 8
+    q, k, v = _inputs(nq, nk, h, h, 128, 94)
+    want, want_lse = _run(q, k, v, [nq], [nk])
+    times = {}
+    for rest in (0.0, float("nan")):
+        big_k, big_v = (torch.full((2 * nk, h, 128), rest, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        big_k[:nk], big_v[:nk] = k, v
+        for _ in range(5):
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record()
+            out, lse = B.oq_attention(q, big_k, big_v, _starts([nq]), _starts([nk]), want_lse=True)
+            e1.record()
+            torch.cuda.synchronize()
+            times[rest != 0] = min(times.get(rest != 0, 1e9), e0.elapsed_time(e1))
+        # (the plan goes by the buffer's length, so the keys may be cut elsewhere: two roundings of the output and of the weights)
+        assert torch.all(torch.isfinite(out)) and (lse - want_lse).abs().max() <= 1e-5 * (1 + want_lse.abs().max())
+        assert (out.double() - want.double()).norm() <= 2 * FRO * want.double().norm()
+    print("beside zeros %.3f ms, beside NaN %.3f ms" % (times[False], times[True]))
+    assert times[True] <= 3 * times[False]
