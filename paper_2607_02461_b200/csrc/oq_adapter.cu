@@ -99,6 +99,12 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return d;
 }
 
+// What a piece leaves of a value; an infinite piece leaves nothing (inf - inf is NaN).
+__device__ __forceinline__ float rest_of(float w, uint32_t piece) {
+  const float rest = w - __uint_as_float(piece);
+  return fabsf(rest) < INFINITY ? rest : 0.f;
+}
+
 // 128 tokens of one segment.  Tiles are counted segment by segment.
 struct Tile {
   int tok0, rows, id;                      // id: the adapter, or -1
@@ -553,16 +559,18 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
           for (int e = 0; e < 4; ++e) {
             const int x = x0 + e * 32 * EPI, r = x / quads, col = 4 * (x % quads);
             if (r >= BM) break;
+            // (the ranks that fill up the last 16 have no adapter, but 0 * inf in A x where X holds an infinity)
             float w[4] = {u[e].x * sc, u[e].y * sc, u[e].z * sc, u[e].w * sc};
+            if (col >= p.rank) w[0] = w[1] = w[2] = w[3] = 0.f;
             unsigned char* dst = smem_p + (col >> 6) * (int)ATOM + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 4) * 2;
 #pragma unroll
             for (int q = 0; q < S::PIECES; ++q) {
               const uint32_t lo = pack2(w[0], w[1]), hi = pack2(w[2], w[3]);
               *reinterpret_cast<uint2*>(dst + q * RB * (int)ATOM) = make_uint2(lo, hi);
-              w[0] -= __uint_as_float(lo << 16);
-              w[1] -= __uint_as_float(lo & 0xFFFF0000u);
-              w[2] -= __uint_as_float(hi << 16);
-              w[3] -= __uint_as_float(hi & 0xFFFF0000u);
+              w[0] = rest_of(w[0], lo << 16);
+              w[1] = rest_of(w[1], lo & 0xFFFF0000u);
+              w[2] = rest_of(w[2], hi << 16);
+              w[3] = rest_of(w[3], hi & 0xFFFF0000u);
             }
           }
         }

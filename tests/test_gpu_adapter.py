@@ -209,3 +209,31 @@ def test_rows_too_far_apart_are_refused():
         with pytest.raises(B.OqError) as e:
             B.oq_adapter_add(args[0], a, b, scale, *_tables([2], [0]), args[1], out=args[2])
         assert e.value.code == 2
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [8, 24, 72, 128])
+def test_infinities_come_out_the_same_on_every_path(rank, dtype):
+    """An infinite token: A x is infinite with A's signs, and so is the output where B's signs agree, NaN where they do not; the other
+    tokens of the tile do not notice.  As one segment (tensor cores) and as segments of one token (ordinary cores)."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n, d, m = 40, 200, 136
+    x, a, b, scale, base = _inputs(n, d, m, rank, 1, t, 77)
+    a, b = a.abs() + 0.01, b.clone()
+    b[:, :100] = b[:, :100].abs() + 0.01
+    b[:, :30] *= -1                                        # columns of minus infinity, plus infinity, and both
+    x = x.clone()
+    x[3, 17], x[21, 199], x[30, 5], x[35, 0] = float("inf"), -float("inf"), float("nan"), float("inf")
+    f = lambda v: v.double().cpu().numpy()  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        ref = oat.adapter_add(f(x), f(a), f(b), f(scale), [n], [0], f(base))
+    whole = B.oq_adapter_add(x, a, b, scale, *_tables([n], [0]), base)
+    singles = B.oq_adapter_add(x, a, b, scale, *_tables([1] * n + [0] * 64 * n, [0] * (65 * n)), base)
+    for got in (f(whole), f(singles)):
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+        assert np.array_equal(np.isposinf(got), np.isposinf(ref)) and np.array_equal(np.isneginf(got), np.isneginf(ref))
+    rows = [i for i in range(n) if i not in (3, 21, 30, 35)]
+    clean = _inputs(n, d, m, rank, 1, t, 77)[0].clone()
+    want = B.oq_adapter_add(clean, a, b, scale, *_tables([n], [0]), base)
+    assert torch.equal(whole[rows], want[rows])
