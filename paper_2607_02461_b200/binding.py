@@ -393,20 +393,15 @@ def _dtype_code(dtype, what):
     raise OqError(1, f"{what}: bf16 or fp32 expected, got {dtype}")
 
 
-def _on_one_device(what, first, *rest):
-    """All of these tensors (or None) on one CUDA device: the kernels would follow a host pointer."""
-    device = first.get_device()                      # -1: host memory
-    if device < 0:
-        raise OqError(1, f"{what}: CUDA tensors expected")
-    for t in rest:
-        if t is not None and t.get_device() != device:
-            raise OqError(1, f"{what}: all tensors must be on one CUDA device")
-    return device
+def _off_device(what):
+    """Raised unless all tensors of a call are on one CUDA device (get_device() is -1 in host memory, whose pointers the kernels would
+    follow).  The calls compare in place: a loop over their tensors takes half a microsecond more."""
+    return OqError(1, f"{what}: all tensors must be on one CUDA device")
 
 
-def _check_workspace(what, t, torch):
-    if t.dtype != torch.uint8 or not t.is_contiguous():
-        raise OqError(1, f"{what}: the workspace must be a contiguous uint8 tensor")
+def _check_workspace(what, t, torch, device):
+    if t.dtype != torch.uint8 or not t.is_contiguous() or t.get_device() != device:
+        raise OqError(1, f"{what}: the workspace must be a contiguous uint8 tensor on the inputs' device")
 
 
 # The calls below are short on the GPU at small sizes (3 to 7 us), so their marshalling looks at every property of a tensor
@@ -458,7 +453,12 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
     if len(shape) != 3:
         raise OqError(1, "oq_qk_norm_rope: queries and keys must be [T, heads, head_dim]")
     n, _, head_dim = shape
-    device = _on_one_device("oq_qk_norm_rope", Q, K, pos if rope is not None else None, wq, wk, out_q, out_k)
+    device = Q.get_device()
+    if device < 0 or (wq is not None and wq.get_device() != device) or (out_q is not None and out_q.get_device() != device):
+        raise _off_device("oq_qk_norm_rope")
+    if K is not None and (K.get_device() != device or (wk is not None and wk.get_device() != device) or
+                          (out_k is not None and out_k.get_device() != device)):
+        raise _off_device("oq_qk_norm_rope")
     norm_code = NORMS.get(norm)
     if norm_code is None:
         raise OqError(1, f"oq_qk_norm_rope: norm must be one of {sorted(NORMS)}")
@@ -478,6 +478,8 @@ def oq_qk_norm_rope(Q, K, rope=None, pos=None, wq=None, wk=None, norm="head", ep
         axes = len(rope.axis_dims)
         if pos is None or pos.dtype != torch.int32 or pos.shape != (n, axes):
             raise OqError(1, "oq_qk_norm_rope: pos must be int32 [T, axes]")
+        if pos.get_device() != device:
+            raise _off_device("oq_qk_norm_rope")
         ldpos, step = pos.stride()
         if step != 1 and axes > 1 and n:
             raise OqError(3, "oq_qk_norm_rope: the positions of a token must be adjacent")
@@ -509,14 +511,16 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
         raise OqError(1, "oq_attention: Q must be [Tq, heads, head_dim], K and V [Tk, kv_heads, head_dim]")
     if Q.dtype != bf16 or K.dtype != bf16 or V.dtype != bf16:
         raise OqError(1, "oq_attention: bf16 expected")
-    device = _on_one_device("oq_attention", Q, K, V, q_start, k_start, out, workspace)
+    device = Q.get_device()
+    if device < 0 or not device == K.get_device() == V.get_device():
+        raise _off_device("oq_attention")
     tq, heads, head_dim = qs
     tk, kv_heads, _ = ks
     n_seqs, q_at, k_at = 1, 0, 0
     if q_start is not None or k_start is not None:
         for t in (q_start, k_start):
-            if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
-                raise OqError(1, "oq_attention: q_start and k_start must both be contiguous int32 [sequences + 1]")
+            if t is None or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != device:
+                raise OqError(1, "oq_attention: q_start and k_start must both be contiguous int32 [sequences + 1] on Q's device")
         n_seqs = len(q_start) - 1
         if len(k_start) != n_seqs + 1:
             raise OqError(1, "oq_attention: q_start and k_start must have one length")
@@ -526,8 +530,8 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
         out = Q.new_empty(qs)
         ot, oh = heads * head_dim, head_dim
     else:
-        if out.shape != qs or out.dtype != bf16:
-            raise OqError(1, "oq_attention: out must be bf16, shaped like Q")
+        if out.shape != qs or out.dtype != bf16 or out.get_device() != device:
+            raise OqError(1, "oq_attention: out must be bf16, shaped like Q and on its device")
         ot, oh, oc = out.stride()
         if oc != 1 and tq:
             qc = oc
@@ -553,7 +557,7 @@ def oq_attention(Q, K, V, q_start=None, k_start=None, left=-1, right=-1, sinks=0
     L = _lib or lib()
     space = size = 0
     if workspace is not None:
-        _check_workspace("oq_attention", workspace, torch)
+        _check_workspace("oq_attention", workspace, torch, device)
         space, size = workspace.data_ptr(), workspace.numel()
     else:
         need = C.c_size_t()
@@ -580,7 +584,10 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
     xs, sa, sb, shape = X.shape, A.shape, Bm.shape, base.shape
     if len(xs) != 2 or len(sa) != 3 or len(sb) != 3 or len(shape) != 2:
         raise OqError(1, "oq_adapter_add: X [T, d], A [adapters, rank, d], B [adapters, m, rank], base [T, m] expected")
-    device = _on_one_device("oq_adapter_add", X, A, Bm, scale, seg_start, seg_adapter, base, out, workspace)
+    device = X.get_device()
+    if device < 0 or not (device == A.get_device() == Bm.get_device() == scale.get_device() == seg_start.get_device() ==
+                          seg_adapter.get_device() == base.get_device()):
+        raise _off_device("oq_adapter_add")
     n, d = xs
     na, rank, m = sa[0], sa[1], sb[1]
     segs = seg_adapter.numel()
@@ -594,8 +601,8 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
         raise OqError(1, "oq_adapter_add: adapters, scales and segment tables must be contiguous")
     if out is None:
         out = base.new_empty(shape)
-    elif out.shape != shape or out.dtype != base.dtype:
-        raise OqError(1, "oq_adapter_add: out must have base's shape and type")
+    elif out.shape != shape or out.dtype != base.dtype or out.get_device() != device:
+        raise OqError(1, "oq_adapter_add: out must have base's shape, type and device")
     (ldx, xc), (ldb, bc), (ldy, yc) = X.stride(), base.stride(), out.stride()
     if n and (xc != 1 or bc != 1 or yc != 1):
         raise OqError(3, "oq_adapter_add: the elements of a row must be adjacent")
@@ -605,7 +612,7 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
         raise OqError(2, "oq_adapter_add: a leading dimension above 2^31 - 1")
     space = size = 0
     if workspace is not None:
-        _check_workspace("oq_adapter_add", workspace, torch)
+        _check_workspace("oq_adapter_add", workspace, torch, device)
     else:
         need = C.c_size_t()
         _check(lib().oq_adapter_workspace_bytes(n, segs, d, rank, C.byref(need)))
