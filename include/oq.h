@@ -302,8 +302,9 @@ void oq_rope_destroy(oq_rope* rope);
  * with the mean over one head (OQ_NORM_HEAD, w has head_dim values) or over all heads of the token (OQ_NORM_ROW, w has
  * n_heads * head_dim values); OQ_NORM_NONE only turns.  Arithmetic in fp32, one rounding when y_dtype is OQ_BF16.
  *   oq_qk_side   X dev, element (token, head, c) at X[token * ld_token + head * ld_head + c], of x_dtype (OQ_BF16 or
- *                OQ_F32); Y dev, laid out by ldy_*, of y_dtype; w_bf16 dev or NULL (no weights).  Y may be X with the
- *                same strides and type; otherwise the two must not overlap.  All strides are in elements.
+ *                OQ_F32); Y dev, laid out by ldy_* (at least head_dim where used), of y_dtype; w_bf16 dev or NULL (no
+ *                weights).  Y may be X with the same strides and type; otherwise the two must not overlap.  All strides are in
+ *                elements; those of X may be 0.
  *   q, k         either may be NULL (cross attention, where queries and keys come from different tokens).
  *   pos          dev int32, pos[token * ldpos + axis]; NULL with rope == NULL.  A token with a position outside the
  *                table gets NaN in the coordinates of that axis.
@@ -366,7 +367,7 @@ int oq_attention(const oq_attention_args* args, void* workspace, size_t workspac
  *     Y[t] = base[t] + scale[a] * B_a (A_a X[t]),   a = seg_adapter[s] for the tokens seg_start[s] .. seg_start[s + 1] - 1
  * and Y[t] = base[t] where a is outside 0 .. n_adapters - 1 (-1: no adapter).
  *   X_bf16   dev [n_tokens][ldx]: the tokens as they enter the projection (not rotated)
- *   A_bf16   dev [n_adapters][rank][dim], B_bf16 dev [n_adapters][m][rank], both dense; scale dev fp32 [n_adapters].
+ *   A_bf16   dev [n_adapters][rank][dim], B_bf16 dev [n_adapters][m][rank] (finite), both dense; scale dev fp32 [n_adapters].
  *            Adapters of smaller rank are filled up with zeros.  rank: a multiple of 8, at most 128
  *   seg_start dev int32 [n_segs + 1], seg_adapter dev int32 [n_segs].  Values are cut to 0 .. n_tokens; a segment may be
  *            empty, tokens in no segment are left alone, none may be in two (where a table is not ascending, the tokens

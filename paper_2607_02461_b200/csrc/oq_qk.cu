@@ -531,6 +531,12 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
     if (!aligned16(in[s]->X) || !aligned16(in[s]->Y) || !aligned16(in[s]->w_bf16) || in[s]->ld_token % xa || in[s]->ld_head % xa ||
         in[s]->ldy_token % ya || in[s]->ldy_head % ya)
       return fail(OQ_ERR_ALIGNMENT, who + "pointers must be 16-byte aligned and strides multiples of 16 bytes");
+    // (rows of the output that lie over each other would overwrite each other; strides of one token or one head are not used)
+    const bool tokens = n_tokens > 1, heads = in[s]->n_heads > 1;
+    if ((tokens && in[s]->ldy_token < head_dim) || (heads && in[s]->ldy_head < head_dim))
+      return fail(OQ_ERR_INVALID_ARG, who + "output strides must be at least head_dim");
+    if (in[s]->Y == in[s]->X && (x_dtype != y_dtype || (tokens && in[s]->ldy_token != in[s]->ld_token) || (heads && in[s]->ldy_head != in[s]->ld_head)))
+      return fail(OQ_ERR_INVALID_ARG, who + "Y is X with other strides or another type");
     qk::Side& d = p.side[s];
     d.X = in[s]->X;
     d.Y = in[s]->Y;

@@ -209,3 +209,18 @@ def test_first_use_of_a_table_while_a_stream_is_captured():
         torch.cuda.synchronize()
         want_q, want_k = B.oq_qk_norm_rope(q, k, again, pos)
         assert torch.equal(yq, want_q) and torch.equal(yk, want_k)
+
+
+def test_expanded_inputs_are_read_and_expanded_outputs_refused():
+    import torch
+    x = torch.randn(70, 1, 128, device="cuda").bfloat16()
+    rope = B.oq_make_rope([16, 56, 56], [9, 9, 9], 10000.0)
+    pos = torch.randint(0, 9, (70, 3), dtype=torch.int32, device="cuda")
+    for norm in ("head", "row"):
+        for view in (x.expand(70, 5, 128), x[:1].expand(70, 5, 128)):
+            got, _ = B.oq_qk_norm_rope(view, None, rope, pos, norm=norm)
+            want, _ = B.oq_qk_norm_rope(view.contiguous(), None, rope, pos, norm=norm)
+            assert torch.equal(got, want)
+            with pytest.raises(B.OqError) as e:
+                B.oq_qk_norm_rope(view.contiguous(), None, rope, pos, norm=norm, out_q=x.clone().expand(70, 5, 128))
+            assert e.value.code == 1

@@ -70,3 +70,21 @@ def test_host_tensors_are_refused():
     a, b = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 16, 8, dtype=torch.bfloat16)
     start, seg = torch.tensor([0, 3], dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     assert _code(B.oq_adapter_add, x[:, 0], a, b, torch.ones(1), start, seg, torch.zeros(3, 16, dtype=torch.bfloat16)) == 1
+
+
+def _qk_code(x=4096, y=8192, ld_token=256, ld_head=64, ldy_token=256, ldy_head=64, tokens=3, heads=4, types=(0, 0)):
+    """Status of oq_qk_norm_rope for queries of 64 on made-up buffers."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("made-up buffers are for hosts without a device")
+    side = B._QK_SIDE.pack(x, ld_token, ld_head, heads, 0, y, ldy_token, ldy_head)
+    return B.lib().oq_qk_norm_rope(side, None, tokens, 64, None, None, 0, 1, 1e-6, types[0], types[1], None)
+
+
+def test_norm_outputs_that_lie_over_each_other_are_refused():
+    for stride in (0, 8, 56, -64):
+        assert _qk_code(ldy_token=stride) == 1 and _qk_code(ldy_head=stride) == 1
+    assert _qk_code(y=4096, ldy_token=512) == 1 and _qk_code(y=4096, ldy_head=128) == 1      # X with other strides
+    assert _qk_code(y=4096, types=(0, 1)) == 1                                               # and another type
+    for sound in (dict(), dict(ldy_token=0, tokens=1), dict(ldy_head=0, heads=1), dict(ld_token=0), dict(ld_head=0), dict(y=4096)):
+        assert _qk_code(**sound) == 4                                                        # as far as the device
