@@ -875,13 +875,15 @@ int sm_count() {
   return sms;
 }
 
-// dual where the sequences have at most 128 queries on average and keys enough to pay for the second kernel that joins the two
-// chains.  (40 heads: 1 query against 32760 keys 114 us dual, 143 not; 16 against 4096 28 and 34; 128 against 32760 133 and
-// 157; 128 against 4096 37 and 35; 8 against 600 keys, 5 key tiles, 17 and 15.)
-// Items (blocks of queries times heads) that do not fill the SMs, or fill them unevenly, are cut along their keys.  The
-// time of a cut is estimated as (rounds of items over the SMs) x (steps of an item + what it costs besides, in steps); a
-// step of a dual item is half as long as one of two query tiles.  (One query against 32760 keys of 40 heads: 3 runs
-// each, one round, 114 us; 5, two rounds, 145 us; 7 121 us; 11 128 us.  The floor is 104 us.)
+// Items (blocks of queries times heads) that do not fill the SMs, or fill them unevenly, are cut along their keys.  The time of a cut is
+// estimated as (rounds of items over the SMs) x (steps of an item + what it costs besides, in steps); a step of a dual item is
+// half as long as one of two query tiles.  (One query against 32760 keys of 40 heads: 3 runs each, one round, 114 us; 5, two rounds,
+// 145 us; 7 121 us; 11 128 us.  The floor is 104 us.)
+// Where the sequences have at most 128 queries on average, the better cut with dual items is set against the better one without, now
+// with what the queries and the parts cost (a part is written and read for every row).  (8, 24 and 40 heads of 128; 3 to 256 key tiles; 1 to
+// 32 sequences of 1 to 128 queries, 192 calls measured both ways: 0.6 % above the better one on average and 9 % at worst; dual from 16 key
+// tiles on 2.7 and 30 %.  One query, 40 heads, 256 tiles: 113 us dual, 140 not; 16 queries, 8 heads, 64 tiles: 26 and 21; 32 sequences of 128
+// queries, 24 heads, 20 tiles: 293 and 226.)
 struct Plan {
   int splits, dual, parts;
 };
@@ -893,19 +895,29 @@ Plan make_plan(long long total_q, long long total_k, int n_seqs, int heads, int 
     if (window < keys) keys = window;
   }
   const long long tiles = (keys + 127) / 128;
-  Plan best{1, total_q <= (long long)BM * n_seqs && tiles >= 16, 1};
-  const long long rows = best.dual ? BM : 2 * BM, blocks = (total_q + rows / 2 * n_seqs + rows / 2 - 1) / rows;
-  const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
-  double best_cost = 1e30;
-  for (int n = 1; n <= MAX_PARTS / (best.dual ? 2 : 1) && (n == 1 || n * 4 <= tiles) && (n == 1 || items < 2LL * sms); ++n) {
-    const double steps = (double)((tiles + n - 1) / n) * (best.dual ? 0.5 : 1.0);
-    const double cost = (double)((items * n + sms - 1) / sms) * (steps + (best.dual ? 6.0 : 3.0)) + (n > 1 ? 3.0 : 0.0);
-    if (cost < best_cost * 0.97) {
-      best_cost = cost;
-      best.splits = n;
+  Plan best{1, 0, 1};
+  double best_total = 1e30;
+  for (int dual = 0; dual < (total_q <= (long long)BM * n_seqs ? 2 : 1); ++dual) {
+    const long long rows = dual ? BM : 2 * BM, blocks = (total_q + rows / 2 * n_seqs + rows / 2 - 1) / rows;
+    const long long items = (blocks < n_seqs ? n_seqs : blocks) * heads;
+    double best_cost = 1e30, total = 0.0;
+    int splits = 1;
+    for (int n = 1; n <= MAX_PARTS / (dual ? 2 : 1) && (n == 1 || n * 4 <= tiles) && (n == 1 || items < 2LL * sms); ++n) {
+      const double rounds = (double)((items * n + sms - 1) / sms), steps = (double)((tiles + n - 1) / n) * (dual ? 0.5 : 1.0);
+      const double cost = rounds * (steps + (dual ? 6.0 : 3.0)) + (n > 1 ? 3.0 : 0.0);
+      if (cost < best_cost * 0.97) {
+        const int parts = dual ? 2 * n : n;
+        best_cost = cost;
+        splits = n;
+        total = rounds * (steps + (dual ? 4.0 + (double)total_q / ((double)n_seqs * BM) : 3.0));
+        if (parts > 1) total += 3.0 + parts * (0.2 + 2.0 * (double)total_q * heads / ((double)sms * BM));
+      }
+    }
+    if (total < best_total) {
+      best_total = total;
+      best = Plan{splits, dual, dual ? 2 * splits : splits};
     }
   }
-  best.parts = best.splits * (best.dual ? 2 : 1);
   return best;
 }
 
