@@ -105,11 +105,12 @@ __device__ __forceinline__ float rest_of(float w, uint32_t piece) {
   return fabsf(rest) < INFINITY ? rest : 0.f;
 }
 
-// 128 tokens of one segment.  Tiles are counted segment by segment.
+// Up to SIZE tokens of one segment.  Tiles are counted segment by segment.
 struct Tile {
   int tok0, rows, id;                      // id: the adapter, or -1
 };
 // By a whole warp: tile `want`; rows = 0 and tok0 = the number of tiles when there are no more than `want`.
+template <int SIZE>
 __device__ __forceinline__ Tile find_tile(const Params& p, int want) {
   const int lane = threadIdx.x & 31;
   int before = 0;
@@ -122,7 +123,7 @@ __device__ __forceinline__ Tile find_tile(const Params& p, int want) {
       id = __ldg(p.seg_adapter + s);
       if (id < 0 || id >= p.n_adapters) id = -1;
     }
-    const int tiles = (n + BM - 1) / BM;
+    const int tiles = (n + SIZE - 1) / SIZE;
     int sum = tiles;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -134,8 +135,8 @@ __device__ __forceinline__ Tile find_tile(const Params& p, int want) {
     if (mine) {
       const int l = __ffs(mine) - 1;
       Tile t;
-      t.tok0 = __shfl_sync(~0u, b + at * BM, l);
-      t.rows = __shfl_sync(~0u, min(BM, n - at * BM), l);
+      t.tok0 = __shfl_sync(~0u, b + at * SIZE, l);
+      t.rows = __shfl_sync(~0u, min(SIZE, n - at * SIZE), l);
       t.id = __shfl_sync(~0u, id, l);
       return t;
     }
@@ -145,7 +146,7 @@ __device__ __forceinline__ Tile find_tile(const Params& p, int want) {
 }
 // Tiles that the two kernels work on.  A table that is not ascending names tokens more than once and makes more tiles than the
 // workspace has places for: those are left out.
-__device__ __forceinline__ int count_tiles(const Params& p) { return min(find_tile(p, 0x7FFFFFFF).tok0, p.max_tiles); }
+__device__ __forceinline__ int count_tiles(const Params& p) { return min(find_tile<BM>(p, 0x7FFFFFFF).tok0, p.max_tiles); }
 // Steps of a stretch of the shrink line: an equal share, but so many that the kbs steps of a tile never meet more than
 // p.parts stretches, however few tiles the segments turn out to make: ceil((kbs - 1) / len) + 1 <= parts.
 __device__ __forceinline__ long long shrink_stretch(const Params& p, long long total, int kbs) {
@@ -253,17 +254,13 @@ __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant_
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t rank = cluster_rank();
-  const Tile t = find_tile(p, (int)blockIdx.x / FEW_RANKS);        // (the same in every CTA of the cluster)
+  const Tile t = find_tile<FEW>(p, (int)blockIdx.x / FEW_RANKS);   // (the same in every CTA of the cluster)
   if (t.rows == 0 || (t.id < 0 && !p.copy)) return;
   const int kb = (p.d + 63) / 64, nb = (p.m + 63) / 64;
   const int d0 = 64 * (kb * (int)rank / FEW_RANKS), d1 = min(64 * (kb * ((int)rank + 1) / FEW_RANKS), p.d);
   const int m0 = 64 * (nb * (int)rank / FEW_RANKS), m1 = min(64 * (nb * ((int)rank + 1) / FEW_RANKS), p.m);
-  if (t.rows == 1) {
-    few_rows<F32, 1>(p, smem, t.tok0, 1, t.id, d0, d1, m0, m1);
-    return;
-  }
-  for (int r = 0; r < t.rows; r += FEW)                          // (a segment that is not short after all: the weights come again)
-    few_rows<F32, FEW>(p, smem, t.tok0 + r, min(FEW, t.rows - r), t.id, d0, d1, m0, m1);
+  if (t.rows == 1) few_rows<F32, 1>(p, smem, t.tok0, 1, t.id, d0, d1, m0, m1);
+  else few_rows<F32, FEW>(p, smem, t.tok0, t.rows, t.id, d0, d1, m0, m1);
 }
 
 // ------------------------------------------------- shrink -------------------------------------------------
@@ -330,7 +327,7 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
       count = min((int)min((long long)(kbs - k), end - pos), p.chunk);
       first = k == 0 || pos == c * len;
       pos += count;
-      t = find_tile(p, tile);
+      t = find_tile<BM>(p, tile);
       if (t.id >= 0) return true;
     }
     return false;
@@ -473,7 +470,7 @@ __global__ void __launch_bounds__(EXPAND_THREADS, 1) expand_kernel(const __grid_
       k = (int)(pos % nbs);
       count = (int)min((long long)(nbs - k), end - pos);
       pos += count;
-      t = find_tile(p, tile);
+      t = find_tile<BM>(p, tile);
       if (t.id >= 0 || p.copy) return true;
     }
     return false;
@@ -665,10 +662,11 @@ int sm_count() {
 }
 // The few-token kernel's time grows with tokens and rank, that of the other two hardly does.  (8 segments of a 3072 x 9216 layer,
 // bf16, rank 16: 1 token each 6.5 us against 19, 4 tokens 15 against 18, 8 tokens 20 against 18; rank 64: 1 token 16 against
-// 23, 2 tokens 30 against 23.)
+// 23, 2 tokens 30 against 23.)  The segments' lengths are on the device, so the rule goes by their average; where one has nearly all tokens,
+// each 8 of them have a cluster: 256 tokens in one of 64 places 28 us (in one cluster of 8 tokens after the other 281).
 bool few_tokens(int n_tokens, int n_segs, int rank) { return (long long)n_tokens * rank <= 64ll * n_segs; }
-int most_tiles(int n_tokens, int n_segs) {
-  const long long most = (n_tokens + BM - 1) / BM + (long long)n_segs;
+int most_tiles(int n_tokens, int n_segs, int size) {
+  const long long most = (n_tokens + size - 1) / size + (long long)n_segs;
   return (int)(most < n_tokens ? most : n_tokens);
 }
 // Stretches that a tile's k-blocks meet when the segments cover all tokens without gaps (shrink_stretch keeps the stretches
@@ -718,7 +716,7 @@ int oq_adapter_workspace_bytes(int n_tokens, int n_segs, int dim, int rank, size
   if (n_tokens < 0 || n_segs < 0 || dim <= 0 || rank <= 0) return fail(OQ_ERR_INVALID_ARG, "oq_adapter_workspace_bytes: bad sizes");
   if (n_tokens == 0 || n_segs == 0 || adapter::few_tokens(n_tokens, n_segs, rank)) return OQ_OK;
   const int kbs = (dim + adapter::KB - 1) / adapter::KB;
-  *bytes = (size_t)adapter::most_tiles(n_tokens, n_segs) * adapter::most_parts(n_tokens, kbs, adapter::sm_count()) * adapter::BM *
+  *bytes = (size_t)adapter::most_tiles(n_tokens, n_segs, adapter::BM) * adapter::most_parts(n_tokens, kbs, adapter::sm_count()) * adapter::BM *
            (size_t)((rank + 15) / 16 * 16) * sizeof(float);
   return OQ_OK;
 }
@@ -762,7 +760,7 @@ int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const voi
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (adapter::few_tokens(n_tokens, n_segs, rank)) {
-    const int tiles = adapter::most_tiles(n_tokens, n_segs);
+    const int tiles = adapter::most_tiles(n_tokens, n_segs, adapter::FEW);
     e = dtype == OQ_F32 ? adapter::launch_few<true>(p, tiles, st) : adapter::launch_few<false>(p, tiles, st);
     if (e != cudaSuccess) return cuda_fail(e, "oq_adapter_add");
     return OQ_OK;
@@ -775,7 +773,7 @@ int oq_adapter_add(const void* X_bf16, int n_tokens, int ldx, int dim, const voi
   const int sms = adapter::sm_count();
   p.part = reinterpret_cast<float*>(workspace);
   p.ctas = sms;
-  p.max_tiles = adapter::most_tiles(n_tokens, n_segs);
+  p.max_tiles = adapter::most_tiles(n_tokens, n_segs, adapter::BM);
   // The tensor cores do not round their running sums to nearest, so an error of the sum's last bits grows with its length: for
   // fp32 outputs 256 columns are added up at a time (relative error of the result at d = 8192: 1.7e-6 without this).
   p.chunk = dtype == OQ_F32 ? 4 : 1 << 30;

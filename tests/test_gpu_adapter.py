@@ -237,3 +237,22 @@ def test_infinities_come_out_the_same_on_every_path(rank, dtype):
     clean = _inputs(n, d, m, rank, 1, t, 77)[0].clone()
     want = B.oq_adapter_add(clean, a, b, scale, *_tables([n], [0]), base)
     assert torch.equal(whole[rows], want[rows])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[250] + [0] * 63, [0] * 40 + [1, 9, 8, 17, 0, 100, 2] + [0] * 20, [3] * 60 + [0] * 9])
+def test_long_segments_among_empty_ones(lens, dtype):
+    """Few tokens a segment on average, all of them in a few: tiles of 8 tokens in clusters of their own."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n, ids = sum(lens), [i % 4 - 1 for i in range(len(lens))]
+    ids[0] = 2
+    x, a, b, scale, base = _inputs(n, 520, 1096, 16, 3, t, 19, pad=16)
+    start, seg = _tables(lens, ids)
+    out = B.oq_adapter_add(x, a, b, scale, start, seg, base)
+    torch.cuda.synchronize()
+    assert B.oq_device_status() == 0
+    _verify(out, x, a, b, scale, base, lens, ids)
+    held = base.clone()
+    B.oq_adapter_add(x, a, b, scale, start, seg, held, out=held)
+    assert torch.equal(held, out)
