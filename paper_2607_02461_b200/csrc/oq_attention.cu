@@ -47,9 +47,10 @@ constexpr int THREADS = 384;              // 8 softmax warps; the load warp, two
 // Registers: 384 threads start with 168 each (64512).  The softmax threads hold a row of S and grow to 216; the last
 // group shrinks to 72: 256 * 216 + 128 * 72 = 64512.
 constexpr int LOAD_WARP = 8, MMA_WARP = 9;
-constexpr int BM = 128;                   // query rows of a tile
+constexpr int BM = 128, BN = 128;         // query rows and keys of a tile
 constexpr int MAX_SEQS = 256;
 constexpr int MAX_PARTS = 32;
+constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;           // columns of a query tile's 256: P lies over S
 constexpr float SLACK = 8.f;              // powers stay below 2^8
 constexpr float FAR = 65536.f;            // rows whose reference passes this (as an exponent) are made again, see below
 // While a warp makes rows again the others wait for it: the limit of the waits has this for each key, five times what 32 rows take.
@@ -58,13 +59,11 @@ enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O
 
 template <int D>
 struct Shape {
-  static constexpr int BN = 128;                                  // keys of a tile
   static constexpr uint32_t ATOMS = D / 64;
   static constexpr uint32_t Q_ATOM = BM * 128, KV_ATOM = BN * 128;      // 64 coordinates of all rows, 128 bytes each
   static constexpr uint32_t Q_TILE = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
   static constexpr int SLOTS = D == 128 ? 5 : 8;
   static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE;
-  static constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;           // columns of a query tile's 256: P lies over S
 };
 
 struct Params {
@@ -91,7 +90,6 @@ struct Params {
 // What one CTA works on at a time: a block of queries of one head and a run of their key tiles.  A block is 256 queries, one
 // tile of 128 after the other.  With few queries (dual) it is 128, both query tiles hold the same ones, and each takes
 // every other key tile: two chains S -> softmax -> P V run where one would leave everything waiting for the other stages.
-template <int BN>
 struct Item {
   int q_base, k_base;      // first query and key of the sequence
   int nq, nk;
@@ -106,12 +104,10 @@ struct Item {
   }
 };
 
-template <int BN>
-__device__ __forceinline__ int row_hi(const Params& p, const Item<BN>& it, int qi) {       // last visible key
+__device__ __forceinline__ int row_hi(const Params& p, const Item& it, int qi) {       // last visible key
   return p.right < 0 ? it.nk - 1 : min(it.nk - 1, qi + it.nk - it.nq + p.right);
 }
-template <int BN>
-__device__ __forceinline__ int row_lo(const Params& p, const Item<BN>& it, int qi) {       // first key of the window
+__device__ __forceinline__ int row_lo(const Params& p, const Item& it, int qi) {       // first key of the window
   return p.left < 0 ? 0 : max(0, qi + it.nk - it.nq - p.left);
 }
 
@@ -119,9 +115,8 @@ __device__ __forceinline__ int block_rows(const Params& p) { return p.dual ? BM 
 // whether query tile t takes step j of an item that it has rows of
 __device__ __forceinline__ bool takes(const Params& p, int t, int j) { return !p.dual || (j & 1) == t; }
 // prefix[s]: blocks of queries before sequence s
-template <int BN>
-__device__ __forceinline__ Item<BN> make_item(const Params& p, const int* prefix, int index) {
-  Item<BN> it;
+__device__ __forceinline__ Item make_item(const Params& p, const int* prefix, int index) {
+  Item it;
   it.split = 0;
   if (p.splits > 1) {
     it.split = index % p.splits;
@@ -204,8 +199,7 @@ __device__ __forceinline__ float natural_lse(const Params& p, float m, float l) 
 // (Kept below the 168 registers that the kernel is launched with, without spills: a form that held 32 keys and the sums of 32 rows wanted
 // twice that, with 1120 bytes of stack, and its first call ended as an illegal instruction.)
 template <int D>
-__device__ __noinline__ void exact_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t again) {
-  constexpr int BN = Shape<D>::BN;
+__device__ __noinline__ void exact_rows(const Params& p, const Item& it, int qi0, int t, uint32_t again) {
   constexpr int N = D / 32, ROWS = 4;
   const int lane = threadIdx.x & 31, hk = it.head / p.group, quarter = lane >> 3;
   const float c = p.scale_log2;
@@ -319,8 +313,7 @@ __device__ __noinline__ void exact_rows(const Params& p, const Item<Shape<D>::BN
 // the rows of the blocks at the mask's edges, whatever the number of rows that see it.  (8192 x 8192 x 4 heads, causal: 0.16 ms, with one NaN
 // seen by all but 300 rows 0.90 ms; with every such row made again 144 ms.)
 template <int D>
-__device__ uint32_t unexplained_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t odd) {
-  constexpr int BN = Shape<D>::BN;
+__device__ uint32_t unexplained_rows(const Params& p, const Item& it, int qi0, int t, uint32_t odd) {
   constexpr int N = D / 32, AHEAD = 8;
   const int lane = threadIdx.x & 31, hk = it.head / p.group;
   // bit r of a lane's words: row r, in the lane's N columns
@@ -378,7 +371,7 @@ __device__ uint32_t unexplained_rows(const Params& p, const Item<Shape<D>::BN>& 
 
 // By a whole warp: rows `odd` where what they see does not explain them, and rows `sure` in any case.
 template <int D>
-__device__ __noinline__ void redo_rows(const Params& p, const Item<Shape<D>::BN>& it, int qi0, int t, uint32_t odd, uint32_t sure) {
+__device__ __noinline__ void redo_rows(const Params& p, const Item& it, int qi0, int t, uint32_t odd, uint32_t sure) {
   __syncwarp();                                  // (each row was written by a lane of its own)
   const uint32_t again = sure | (odd ? unexplained_rows<D>(p, it, qi0, t, odd) : 0u);
   if (again) exact_rows<D>(p, it, qi0, t, again);
@@ -388,7 +381,7 @@ template <int D>
 __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                                                                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ Params p) {
   using S = Shape<D>;
-  constexpr int SLOTS = S::SLOTS, BN = S::BN;
+  constexpr int SLOTS = S::SLOTS;
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[12 + 2 * SLOTS];
   __shared__ int prefix[MAX_SEQS + 1];
@@ -431,7 +424,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (warp == 0) {
-    // blocks of 256 queries before each sequence
+    // blocks of queries before each sequence
     int before = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
       const int s = s0 + lane;
@@ -462,12 +455,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
   const int n_items = prefix[p.n_seqs] * p.heads * p.splits;
   // All roles walk over the same steps: the key tiles of this CTA's items, one after the other.
   struct Step {
-    Item<BN> it;
+    Item it;
     int index, j;          // the item's number; the key tile inside it
   };
   auto first_from = [&](Step& s, int index) {        // the first step of the first item from `index` on that has a key tile
     for (; index < n_items; index += gridDim.x) {
-      s.it = make_item<BN>(p, prefix, index);
+      s.it = make_item(p, prefix, index);
       if (s.it.tiles > 0) {
         s.index = index;
         s.j = 0;
@@ -486,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
     // ------------------------------------------------ softmax ------------------------------------------------
     const int t = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t columns = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256u * (uint32_t)t;
-    const uint32_t col_s = columns + S::COL_S, col_p = columns + S::COL_P, col_o = columns + S::COL_O;
+    const uint32_t col_s = columns + COL_S, col_p = columns + COL_P, col_o = columns + COL_O;
     const float c = p.scale_log2;
     uint32_t steps = 0, items = 0;              // of this tile so far
     auto warp_wait = [&](uint32_t bar, uint32_t parity, int code) {
@@ -506,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       int rows, first, hi, lo, full_hi, full_lo, tiles, n_sink, skipped;
       bool turns;
       {
-        const Item<BN> it = make_item<BN>(p, prefix, i);
+        const Item it = make_item(p, prefix, i);
         rows = t ? it.rows1 : it.rows0;
         const int r0 = it.q0 + (p.dual ? 0 : t * BM);
         hi = row_hi(p, it, r0 + row);
@@ -541,10 +534,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
         uint32_t sr[BN];
 #pragma unroll
         for (int q = 0; q < BN / 32; ++q) tmem_load32_nowait(col_s + 32u * q, sr + 32 * q);
-        if (BN % 32) tmem_load16_at(col_s + BN - 16u, sr + BN - 16);
 #pragma unroll
         for (int q = 0; q < BN / 32; ++q) tmem_use32(sr + 32 * q);
-        if (BN % 32) tmem_use16(sr + BN - 16);
         if (!(k0 + BN - 1 <= full_hi && (k0 >= full_lo || k0 + BN <= p.sinks))) {
           uint32_t some = 0;
 #pragma unroll
@@ -632,7 +623,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
       // ------------------------------------------- the item's result -------------------------------------------
       int again_i = i;
       asm volatile("" : "+r"(again_i));
-      const Item<BN> it = make_item<BN>(p, prefix, again_i);
+      const Item it = make_item(p, prefix, again_i);
       const int qi = it.q0 + (p.dual ? 0 : t * BM) + row;
       const bool any = tiles > j0, mine = row < rows;
       if (any) warp_wait(o_done(t), items++ & 1, W_O);
@@ -762,7 +753,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
           const uint64_t a = smem_desc(smem_q + (uint32_t)t * S::Q_TILE), b = smem_desc(smem_kv + slot * S::KV_TILE);
 #pragma unroll
           for (uint32_t k = 0; k < D / 16; ++k)
-            mma_ss(columns + S::COL_S, a + (uint64_t)((k >> 2) * (S::Q_ATOM >> 4) + 2 * (k & 3)), b + (uint64_t)((k >> 2) * (S::KV_ATOM >> 4) + 2 * (k & 3)),
+            mma_ss(columns + COL_S, a + (uint64_t)((k >> 2) * (S::Q_ATOM >> 4) + 2 * (k & 3)), b + (uint64_t)((k >> 2) * (S::KV_ATOM >> 4) + 2 * (k & 3)),
                    IDESC_S, k > 0, leader);
           mma_commit(s_full(t), leader);
           mma_commit(kv_free(slot), leader);
@@ -794,7 +785,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kernel(const __grid_cons
               mbar_spin(p_full(t), p_use++ & 1, &abort_flag, p.status, W_P, p.max_wait);
               tc_fence_after();
             }
-            mma_ts(columns + S::COL_O, columns + S::COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > j0 || k > 0, leader);
+            mma_ts(columns + COL_O, columns + COL_P + 8 * k, b + (uint64_t)(k * (2048 >> 4)), IDESC_O, s.j > j0 || k > 0, leader);
           }
           if (s.j + jd >= s.it.tiles) mma_commit(o_done(t), leader);
           mma_commit(kv_free(slot), leader);
@@ -1036,10 +1027,9 @@ int oq_attention(const oq_attention_args* a, void* workspace, size_t workspace_b
     const uint32_t box[3] = {64, 1, (uint32_t)rows};
     return encode_tensor_map_sw128(map, base, false, 3, dims, strides, box);
   };
-  const int keys = a->head_dim == 128 ? attn::Shape<128>::BN : attn::Shape<64>::BN;
   cudaError_t e = make_map(&mq, a->Q, a->n_heads, a->total_q, a->ldq_token, a->ldq_head, attn::BM);
-  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head, keys);
-  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mv, a->V, a->n_kv_heads, a->total_k, a->ldv_token, a->ldv_head, keys);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mk, a->K, a->n_kv_heads, a->total_k, a->ldk_token, a->ldk_head, attn::BN);
+  if (e == cudaSuccess && a->total_k > 0) e = make_map(&mv, a->V, a->n_kv_heads, a->total_k, a->ldv_token, a->ldv_head, attn::BN);
   if (e != cudaSuccess) return cuda_fail(e, "oq_attention (tensor map)");
   if (a->total_k == 0) mk = mv = mq;               // no key tile is ever loaded
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
