@@ -11,7 +11,7 @@
 //   expand   Y = base + u B^T, the column tiles of all token tiles again one line in equal stretches.  At a token tile's
 //            start the parts of u are added in the order of the stretches (bit-reproducible), scaled and cut into pieces of bf16
 //            as an MMA operand: 2 pieces (16 bits) for bf16 outputs, 3 (24 bits) for fp32, each a product of its own, so that
-//            the update is as exact as the output's type can show.  base tiles come by TMA, are added to in shared memory and
+//            the update is as exact as the output's type can show (from 64 bits: bf16 1.66e-3, the output's own rounding; fp32 6e-8 to 1e-7).  base tiles come by TMA, are added to in shared memory and
 //            leave by TMA
 //
 // (One kernel for both, a cluster of CTAs per token tile that exchanges u through distributed shared memory, needs no
@@ -303,7 +303,8 @@ __global__ void __launch_bounds__(SHRINK_THREADS, 1) shrink_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // (the second kernel may start once every CTA of this one has passed its wait: what was written before this kernel is then
-  // complete, and the second kernel reads its base tiles without waiting for this kernel's end)
+  // complete, and the second kernel reads its base tiles without waiting for this kernel's end: on SMs whose CTA of this one
+  // is done, as the two do not fit beside each other, 217 and 225 KB of shared memory)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   tc_fence_before();

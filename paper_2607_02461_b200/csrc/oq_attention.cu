@@ -8,8 +8,10 @@
 //   l = sum_j 2^(c (s_j - m)),   O = sum_j 2^(c (s_j - m)) v_j
 // for ANY m that keeps the powers in range, so m follows the running maximum only when that has moved by more than
 // 2^SLACK; then O and l are multiplied by 2^(c (m - m')).  The sums are fp32; the powers are rounded once, to bf16, as
-// the tensor cores' operand for the product with V (l sums the unrounded ones), which costs about as much as the one rounding of the
-// output.
+// the tensor cores' operand for the product with V (l sums the unrounded ones): an MMA takes both operands in one type, and V is
+// bf16.  That is a choice: the result is 2.3e-3 from 64 bits (relative, over a tensor of normal values) where the output's own
+// rounding is 1.66e-3; with the powers in two bf16 pieces, each multiplied with V, it was 1.66e-3, and the calls below took 377 us for 256
+// (joint), 789 for 542 (streamed frame), 89 for 65 (packed requests) and 162 for 132 (one query).
 //
 // Bound: the tensor cores and the exponentials alike.  128 queries x 128 keys take 128^3 multiply-adds for each of the
 // two products at head_dim 128 and 16384 exponentials: both about 1000 cycles of an SM.  So a CTA carries two query
@@ -22,10 +24,10 @@
 // Of a tile's 256 columns of tensor memory S has 128, over which P lies, and O the rest.  The mma warp issues P_t V of a
 // key tile before the next S_t, so "S_t is there" also says that O_t holds the tiles before it.
 //
-// Measured (B200, head_dim 128): 4608 queries x 4608 keys x 24 heads 216 to 226 us = 1.2 PFLOP/s, 0.70 of the measured burst rate
-// of a library product and 0.83 of the sustained one (the power cap holds the clock at 1.7 GHz under this kernel; in
-// seconds-long runs 250 us); a step of 2 x 128 queries x 128 keys takes ~3200 cycles, 1200 of them P V, S and their latency,
-// 600 the load and the maximum, 1400 the powers, in two chains that run against each other.  Other arrangements that were measured:
+// Measured (B200, head_dim 128), 4608 queries x 4608 keys x 24 heads: 222 us in bursts of 10 ms = 1.18 PFLOP/s, 0.70 of the measured
+// burst rate of a library product; the power cap then holds the clock at 1.7 GHz: 239 us in 0.15 s, 252 in 2 s, 255 a call through the Python
+// entry point.  A step of 2 x 128 queries x 128 keys takes ~3200 cycles, 1200 of them P V, S and their latency,
+// 600 the load and the maximum, 1400 the powers, in two chains that run against each other.  Other arrangements that were measured (beside 216 us):
 // S beside P and tiles of 80 keys (nothing waits for P V, but what a step costs besides is paid more often) 247 us;
 // four softmax threads of which two share a row 239 us; a third of the powers as polynomials of degree 4 on the fused
 // multiply-add pipe 255 us (that pipe takes as long for them); no turns at the exponentials 246 us; the maximum taken while the

@@ -12,9 +12,14 @@
 // The table (fp64 on the host, rounded once) replaces the sine and cosine of an angle that fp32 could not hold: at
 // position 32760 half a unit in the last place is already 1e-3.
 //
-// Measured (B200, head_dim 128, bf16): 4608 tokens x (24 + 24) heads, norm per head, 3 axes: 21.3 us for 113 MB = 5.3 TB/s, 0.82
-// of the copy rate; 32760 tokens x (40 + 40) heads, norm over all heads: 243 us for 1.34 GB = 5.5 TB/s, 0.85.  What is left is
-// instruction issue: about 140 instructions for 256 values, of which the pairwise arithmetic is half.
+// Measured (B200, head_dim 128, two sides, 3 axes; device time and share of the copy rate of 6.46 TB/s):
+//   norm per head, 4608 tokens x (24 + 24) heads: bf16 pairs 21.4 us, 5.3 TB/s, 0.82; bf16 halves 31.2, 0.56; fp32 pairs 42.6, 0.82;
+//     fp32 halves 55.8, 0.63; head_dim 64, (48 + 48) heads: bf16 pairs 25.9, 0.68; halves 34.2, 0.51
+//   norm over the row, (40 + 40) heads: 32760 tokens bf16 pairs 243 us, 5.5 TB/s, 0.85; halves 440, 0.47; 16380 tokens fp32 pairs 273, 0.76;
+//     halves 322, 0.65; (80 + 80) heads (WIDE_ROW): 16380 tokens bf16 pairs 372, 0.56; 8192 tokens fp32 pairs 521, 0.40; halves 734, 0.28
+// bf16 pairs is what the two models here use and what was tuned: what is left there is instruction issue, about 140 instructions for
+// 256 values, of which the pairwise arithmetic is half.  The other forms hold twice the table entries (halves) or rows (fp32) and
+// spill: 8 to 24 bytes a thread for bf16 halves per head, 188 over the row, 52 to 336 for fp32, 450 to 940 for WIDE_ROW.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -149,7 +154,7 @@ enum { HEAD = 0, ROW = 1, WIDE_ROW = 2 };      // WIDE_ROW: more than ROW_WARPS 
 // HEAD: a warp is one (token, side, chunk of heads) and the norm closes inside the lanes of a head.
 // HALVES: the partner of a coordinate lies d_a / 2 further on (in another lane), otherwise right beside it.
 // LANES: lanes of a head, 0: read from the parameters (head_dim 128, the one of the image and video models, with a norm per head has
-// its own: 21.3 us where the general form takes 27.0).
+// its own: 21.3 us where the general form takes 27.0; the other head_dims share the general form).
 // A turned coordinate is y = x * A + partner * B; where the weights are the same for every head (HEAD) they are part of
 // A and B, which are made once for a token and serve all of the warp's heads.  That, and reductions of fixed length,
 // keep the kernel at ~140 instructions for 256 values; at 270 (weights and side read again for every head, loops of run-time
