@@ -509,6 +509,7 @@ void oq_rope_destroy(oq_rope* rope) {
 int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int head_dim, const oq_rope* rope, const int* pos,
                     int ldpos, int norm, float eps, int x_dtype, int y_dtype, void* stream) {
   if (n_tokens < 0) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: n_tokens is negative");
+  if (n_tokens >= 0x7FFFFFFF - (1 << 16)) return fail(OQ_ERR_UNSUPPORTED, "oq_qk_norm_rope: too many tokens for one launch");   // (the walk looks two strides ahead)
   if (!q && !k) return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: neither queries nor keys");
   if ((x_dtype != OQ_BF16 && x_dtype != OQ_F32) || (y_dtype != OQ_BF16 && y_dtype != OQ_F32))
     return fail(OQ_ERR_INVALID_ARG, "oq_qk_norm_rope: unknown element type");

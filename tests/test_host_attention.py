@@ -88,3 +88,8 @@ def test_norm_outputs_that_lie_over_each_other_are_refused():
     assert _qk_code(y=4096, types=(0, 1)) == 1                                               # and another type
     for sound in (dict(), dict(ldy_token=0, tokens=1), dict(ldy_head=0, heads=1), dict(ld_token=0), dict(ld_head=0), dict(y=4096)):
         assert _qk_code(**sound) == 4                                                        # as far as the device
+
+
+def test_more_tokens_than_a_launch_can_walk_over_are_refused():
+    assert _qk_code(tokens=2 ** 31 - 1) == 2 and _qk_code(tokens=2 ** 31 - 2 ** 16) == 2
+    assert _qk_code(tokens=2 ** 30) == 4                                                     # as far as the device
