@@ -330,7 +330,7 @@ int oq_qk_norm_rope(const oq_qk_side* q, const oq_qk_side* k, int n_tokens, int 
  * keys before them) and sees key j iff
  *     j <= p + right   (right < 0: no limit)   and   (j >= p - left  (left < 0: no limit)  or  j < sinks)
  * out = sum_j softmax_j(scale * q . k_j) v_j over the keys seen, lse = log sum_j exp(scale * q . k_j).  A query that
- * sees no key gets out = 0 and lse = -inf.  Keys and values that a query does not see do not reach it, whatever they
+ * sees no key, or no score above minus infinity, gets out = 0 and lse = -inf.  Keys and values that a query does not see do not reach it, whatever they
  * hold (NaN and infinities included).  causal: right = 0; joint attention: left = right = -1.
  *   Q, K, V  dev bf16, element (token, head, c) at X[token * ld_token + head * ld_head + c]; strides in elements,
  *            multiples of 8, at least head_dim where there is more than one token or head, or for heads 0: one head serves

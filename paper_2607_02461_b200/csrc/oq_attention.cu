@@ -55,8 +55,8 @@ constexpr int MAX_PARTS = 32;
 constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;           // columns of a query tile's 256: P lies over S
 constexpr float SLACK = 8.f;              // powers stay below 2^8
 constexpr float FAR = 65536.f;            // rows whose reference passes this (as an exponent) are made again, see below
-// While a warp makes rows again the others wait for it: the limit of the waits has this for each key, five times what 32 rows take.
-constexpr long long REDO_CYCLES = 32768;
+// While a warp makes rows again the others wait for it: the limit of the waits has this for each key, nearly three times what 32 rows take.
+constexpr long long REDO_CYCLES = 16384;
 enum { W_Q = 40, W_QFREE = 41, W_KV = 42, W_KVFREE = 43, W_S = 44, W_P = 45, W_O = 46 };
 
 template <int D>
