@@ -360,6 +360,81 @@ typedef struct {
 int oq_attention_workspace_bytes(const oq_attention_args* args, size_t* bytes);
 int oq_attention(const oq_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- paged cache of quantized keys and values ---------------------------------------------------------------- */
+
+/* Keys and values of the tokens of several sequences, quantized as they are written, in pages of one pool.  The new tokens of a
+ * sequence are its last ones: a call is given where they lie among the packed tokens of all sequences (start), how long
+ * each sequence is with them (lens), and each sequence's pages (table).
+ *
+ *   page      page_size tokens (a power of two, 16 .. 256) of all heads: [n_kv_heads] blocks of oq_cache_block_bytes bytes
+ *   block     keys [page_size][head_dim * bits / 8], values (the same), scales of the keys [page_size][head_dim / 32], of the values
+ *   element   OQ_CACHE_FP8: e4m3;  OQ_CACHE_FP4: e2m1, the even coordinate in the low half of a byte
+ *   scale     one for 32 adjacent coordinates, a byte s for 2^(s - 127): the smallest power of two, from 2^-14 to 2^7 (FP8) or
+ *             2^13 (FP4), with which the group's largest magnitude stays within the format (448; 6); elements are rounded to
+ *             nearest even, and larger magnitudes than 57344 (49152) become that.  Where a key or a value of a token and head is NaN or
+ *             infinite, all its scales (of keys and values) are 255 and its elements 0: it reads back as NaN, and queries that see it get NaN
+ *   place     position p of sequence s is token p % page_size of page table[s * ld_table + p / page_size]; lens are cut to
+ *             0 .. max_pages * page_size.  A page outside 0 .. n_pages - 1 (-1: none yet, or given back) holds nothing: a write passes its
+ *             tokens over, a read gives zeros, attention does not see them
+ *
+ * pages dev, 16-byte aligned; table dev int32 [n_seqs][ld_table], max_pages columns in use; lens dev int32 [n_seqs].  head_dim 64 or 128,
+ * n_seqs <= 256.  Pages may be shared by sequences (a common beginning); of tokens written to one place in one call any is kept, in
+ * each of its values. */
+enum { OQ_CACHE_FP8 = 8, OQ_CACHE_FP4 = 4 };
+typedef struct {
+  void* pages;
+  const int* table;
+  const int* lens;
+  long long ld_table;
+  int n_pages, page_size, n_kv_heads, head_dim, kind, n_seqs, max_pages;
+} oq_cache;
+typedef struct {
+  void* X; /* element (token, head, c) at X[token * ld_token + head * ld_head + c] */
+  long long ld_token, ld_head;
+} oq_cache_rows;
+int oq_cache_block_bytes(int kind, int page_size, int head_dim, size_t* bytes);
+
+/* Writes the keys and values of new tokens (dev, of x_dtype OQ_BF16 or OQ_F32; 16-byte aligned, strides multiples of 16 bytes, 0
+ * allowed) into the pages, one pass.  start dev int32 [n_seqs + 1]: sequence s owns the tokens start[s] .. start[s + 1] - 1 (values are cut to
+ * 0 .. total), which are its positions lens[s] - n .. lens[s] - 1; those before position 0 and tokens of no sequence are passed over.  NULL: one
+ * sequence of all tokens.  Nothing else in the pages changes.  Asynchronous on `stream`; nothing is allocated.  total == 0 launches nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int oq_cache_write(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_rows* V, int x_dtype, const int* start, int total, void* stream);
+
+/* The reverse: reads the last start[s + 1] - start[s] tokens of each sequence into K and V (either may be NULL), of y_dtype.  Every
+ * cached value is an exact bf16.  Tokens of no sequence are left as they are, those before position 0 become 0.  Strides at least head_dim. */
+int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_rows* V, int y_dtype, const int* start, int total, void* stream);
+
+/* Softmax attention of the new tokens over all that is cached, themselves included (they have been written).  Masks as for oq_attention:
+ * query i of a sequence with nq new and nk cached tokens stands at place p = i + nk - nq and sees key j iff
+ *     j <= p + right (right < 0: no limit)   and   (j >= p - left (left < 0: no limit)  or  j < sinks)   and its page is there
+ * out = sum_j softmax_j(scale * q . k_j) v_j, lse = log sum_j exp(scale * q . k_j); a query that sees nothing gets 0 and -inf.  A query that holds
+ * NaN or an infinity gets NaN where it sees something.
+ *   Q        dev bf16, strides in elements, multiples of 8, not negative; 16-byte aligned
+ *   out      dev bf16, strides at least head_dim; must not overlap Q or the pages.   lse dev fp32 [n_heads][total_q], or NULL
+ *   q_start  dev int32 [n_seqs + 1] (see start above), NULL: one sequence.  Queries of no sequence are not written
+ *   n_heads  a multiple of the cache's heads; query head h reads head h / (n_heads / n_kv_heads)
+ *   max_q    a hint: no sequence has more new tokens (1 in a step of single tokens).  0: not known.  Results do not depend on its being true
+ *   scale    0: 1 / sqrt(head_dim)
+ * What is cached is decoded exactly, and queries lose nothing that matters (the parts of a head more than 2^29 below its largest); the products run on the tensor cores in fp16 with fp32 accumulation, the softmax weights are
+ * rounded to fp16 for the second one, everything else is fp32.  Items of work are cut along the keys so that all SMs get the same share, whatever
+ * the lengths; the workspace (dev, 16-byte aligned, oq_cache_attention_workspace_bytes bytes) holds the parts.  Results are bit-reproducible.
+ * Asynchronous on `stream`.  total_q == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */
+typedef struct {
+  oq_cache cache;
+  const void* Q;
+  long long ldq_token, ldq_head;
+  void* out;
+  long long ldo_token, ldo_head;
+  float* lse;
+  const int* q_start;
+  int total_q, n_heads, max_q;
+  int left, right, sinks;
+  float scale;
+} oq_cache_attention_args;
+int oq_cache_attention_workspace_bytes(const oq_cache_attention_args* args, size_t* bytes);
+int oq_cache_attention(const oq_cache_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- low-rank adapters beside a shared projection ------------------------------------------------------------ */
 
 /* Adds the low-rank updates of several requests to a projection's output.  A quantized weight cannot take an update

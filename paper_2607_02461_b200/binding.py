@@ -69,6 +69,11 @@ def lib():
             "oq_attention": (i, [vp, vp, sz, vp]),
             "oq_adapter_workspace_bytes": (i, [i, i, i, i, C.POINTER(sz)]),
             "oq_adapter_add": (i, [vp, i, i, i, vp, vp, i, i, vp, vp, vp, i, vp, i, vp, i, i, i, vp, sz, vp]),
+            "oq_cache_block_bytes": (i, [i, i, i, C.POINTER(sz)]),
+            "oq_cache_write": (i, [vp, vp, vp, i, vp, i, vp]),
+            "oq_cache_read": (i, [vp, vp, vp, i, vp, i, vp]),
+            "oq_cache_attention_workspace_bytes": (i, [vp, C.POINTER(sz)]),
+            "oq_cache_attention": (i, [vp, vp, sz, vp]),
             "oq_last_error": (C.c_char_p, []), "oq_version": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -624,6 +629,185 @@ def oq_adapter_add(X, A, Bm, scale, seg_start, seg_adapter, base, out=None, work
                                 seg_adapter.data_ptr(), segs, base.data_ptr(), ldb, out.data_ptr(), ldy, m,
                                 _dtype_code(base.dtype, "oq_adapter_add"), space, size, torch._C._cuda_getCurrentRawStream(device)))
     return out
+
+
+_CACHE = struct.Struct("@PPPqiiiiiii4x")             # oq_cache
+_CACHE_ROWS = struct.Struct("@Pqq")                  # oq_cache_rows
+_CACHE_ATTENTION = struct.Struct("@PPPqiiiiiii4xPqqPqqPPiiiiiif")      # oq_cache_attention_args
+CACHE_KINDS = {"fp8": 8, "fp4": 4}
+
+
+def oq_cache_block_bytes(page_size, head_dim, kind="fp8"):
+    """Bytes of one head's block in a page of page_size tokens."""
+    n = C.c_size_t()
+    _check(lib().oq_cache_block_bytes(CACHE_KINDS.get(kind, 0), page_size, head_dim, C.byref(n)))
+    return n.value
+
+
+def oq_cache_alloc(n_pages, page_size, kv_heads, head_dim, kind="fp8", device="cuda"):
+    """A pool of pages: uint8 [n_pages, kv_heads, bytes of a block], cleared."""
+    import torch
+    return torch.zeros((n_pages, kv_heads, oq_cache_block_bytes(page_size, head_dim, kind)), dtype=torch.uint8, device=device)
+
+
+def _cache_fields(what, torch, pages, head_dim, kind, table, lens, start, device):
+    """Checks what the calls on a cache have in common.  Returns the fields of oq_cache and the address of start."""
+    i32 = torch.int32
+    bits = CACHE_KINDS.get(kind)
+    if bits is None:
+        raise OqError(1, f"{what}: kind must be one of {sorted(CACHE_KINDS)}")
+    if device < 0 or not device == pages.get_device() == table.get_device() == lens.get_device() or \
+            (start is not None and start.get_device() != device):
+        raise _off_device(what)
+    if device != torch._C._cuda_getDevice():
+        raise OqError(1, f"{what}: the tensors' device must be the current one")
+    shape, tshape = pages.shape, table.shape
+    if pages.dtype != torch.uint8 or len(shape) != 3 or not pages.is_contiguous():
+        raise OqError(1, f"{what}: pages must be contiguous uint8 [pages, kv_heads, bytes of a block]")
+    if head_dim != 64 and head_dim != 128:
+        raise OqError(2, f"{what}: head_dim must be 64 or 128")
+    size, odd = divmod(shape[2], head_dim * bits // 4 + head_dim // 16)        # bytes of a token's keys, values and scales
+    if odd:
+        raise OqError(1, f"{what}: no number of tokens of this kind and head_dim fills a block of these pages")
+    seqs = lens.numel()
+    if table.dtype != i32 or len(tshape) != 2 or tshape[0] != seqs or lens.dtype != i32 or lens.dim() != 1 or not lens.is_contiguous():
+        raise OqError(1, f"{what}: table must be int32 [sequences, pages], lens contiguous int32 [sequences]")
+    ld, step = table.stride()
+    if step != 1 and tshape[1] > 1:
+        raise OqError(3, f"{what}: the entries of a row of the table must be adjacent")
+    at = 0
+    if start is not None:
+        if start.dtype != i32 or start.shape != (seqs + 1,) or not start.is_contiguous():
+            raise OqError(1, f"{what}: start must be contiguous int32 [sequences + 1]")
+        at = start.data_ptr()
+    elif seqs != 1:
+        raise OqError(1, f"{what}: several sequences need start")
+    if max(shape[0], shape[1], tshape[1]) > _INT_MAX:
+        raise OqError(2, f"{what}: sizes above 2^31 - 1")
+    return (pages.data_ptr(), table.data_ptr(), lens.data_ptr(), ld, shape[0], size, shape[1], head_dim, bits, seqs, tshape[1]), at
+
+
+def _cache_rows(what, X, heads, head_dim):
+    """oq_cache_rows of keys or values [T, kv_heads, head_dim]."""
+    n, h, d = X.shape
+    lt, lh, lc = X.stride()
+    if h != heads or d != head_dim:
+        raise OqError(1, f"{what}: keys and values must be [T, {heads}, {head_dim}]")
+    if lc != 1 and n:
+        raise OqError(3, f"{what}: the coordinates of a head must be adjacent")
+    return _CACHE_ROWS.pack(X.data_ptr(), lt if n > 1 else head_dim * heads, lh if h > 1 else head_dim)
+
+
+def oq_cache_write(pages, K, V, table, lens, start=None, kind="fp8"):
+    """Quantizes keys and values of new tokens into the pages of their sequences.  pages: CUDA uint8 [pages, kv_heads, bytes of a
+    block] (oq_cache_alloc); K, V: CUDA bf16 or fp32 [T, kv_heads, head_dim], any strides of multiples of 16 bytes, unit stride
+    inside a head; table: int32 [sequences, pages]; lens: int32 [sequences], the new tokens included; start: int32 [sequences + 1]
+    or None for one sequence."""
+    import torch
+    if K.dim() != 3 or K.shape != V.shape or K.dtype != V.dtype:
+        raise OqError(1, "oq_cache_write: K and V must be [T, kv_heads, head_dim] of one type")
+    device = K.get_device()
+    if V.get_device() != device:
+        raise _off_device("oq_cache_write")
+    code = _dtype_code(K.dtype, "oq_cache_write")
+    n, heads, head_dim = K.shape
+    fields, at = _cache_fields("oq_cache_write", torch, pages, head_dim, kind, table, lens, start, device)
+    if heads != fields[6]:
+        raise OqError(1, "oq_cache_write: the pages are of another number of heads")
+    if n > _INT_MAX:
+        raise OqError(2, "oq_cache_write: too many tokens")
+    rc = (_lib or lib()).oq_cache_write(_CACHE.pack(*fields), _cache_rows("oq_cache_write", K, heads, head_dim),
+                                        _cache_rows("oq_cache_write", V, heads, head_dim), code, at, n,
+                                        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc)
+
+
+def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp8", out_k=None, out_v=None, out_dtype=None):
+    """Reads the last start[s + 1] - start[s] tokens of each sequence back.  total: tokens of all sequences together (the tensors'
+    first size where out_k or out_v is given).  Returns (K, V) [total, kv_heads, head_dim] of out_dtype (bf16 or fp32, bf16 by default).
+    With out_k or out_v given, only what is given is read."""
+    import torch
+    device, heads = pages.get_device(), pages.shape[1] if pages.dim() == 3 else 0
+    fields, at = _cache_fields("oq_cache_read", torch, pages, head_dim, kind, table, lens, start, device)
+    given = [x for x in (out_k, out_v) if x is not None]
+    if not given:
+        if total is None or not 0 <= total <= _INT_MAX:
+            raise OqError(1, "oq_cache_read: total, or out_k or out_v, is needed")
+        out_k = torch.empty((total, heads, head_dim), dtype=out_dtype or torch.bfloat16, device=pages.device)
+        out_v = torch.empty_like(out_k)
+        given = [out_k]
+    for x in given:
+        if x.dim() != 3 or x.shape != given[0].shape or x.dtype != given[0].dtype or (total is not None and x.shape[0] != total) or \
+                (out_dtype is not None and x.dtype != out_dtype):
+            raise OqError(1, "oq_cache_read: out_k and out_v must be [total, kv_heads, head_dim] of one type")
+        if x.get_device() != device:
+            raise _off_device("oq_cache_read")
+    code = _dtype_code(given[0].dtype, "oq_cache_read")
+    rows = [None if x is None else _cache_rows("oq_cache_read", x, heads, head_dim) for x in (out_k, out_v)]
+    rc = (_lib or lib()).oq_cache_read(_CACHE.pack(*fields), rows[0], rows[1], code, at, given[0].shape[0],
+                                       torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        _check(rc)
+    return out_k, out_v
+
+
+def oq_cache_attention(Q, pages, table, lens, q_start=None, kind="fp8", left=-1, right=0, sinks=0, scale=0.0, max_q=0, out=None,
+                       want_lse=False, workspace=None):
+    """Attention of new tokens over the pages of their sequences, which hold the new tokens' keys and values already.  Q: CUDA bf16
+    [T, heads, head_dim] (any strides of multiples of 8, unit stride inside a head); pages, table, lens, q_start: see oq_cache_write.  left, right,
+    sinks, max_q: see oq.h.  Returns out [T, heads, head_dim], or (out, lse fp32 [heads, T]) with want_lse.  workspace: CUDA uint8
+    tensor, by default one is taken from torch's allocator when the call needs it."""
+    import torch
+    qs, bf16 = Q.shape, torch.bfloat16
+    if len(qs) != 3 or Q.dtype != bf16:
+        raise OqError(1, "oq_cache_attention: Q must be bf16 [T, heads, head_dim]")
+    device = Q.get_device()
+    n, heads, head_dim = qs
+    fields, at = _cache_fields("oq_cache_attention", torch, pages, head_dim, kind, table, lens, q_start, device)
+    qt, qh, qc = Q.stride()
+    if out is None:
+        out = Q.new_empty(qs)
+        ot, oh = heads * head_dim, head_dim
+    else:
+        if out.shape != qs or out.dtype != bf16 or out.get_device() != device:
+            raise OqError(1, "oq_cache_attention: out must be bf16, shaped like Q and on its device")
+        ot, oh, oc = out.stride()
+        if oc != 1 and n:
+            qc = oc
+    if qc != 1 and n:
+        raise OqError(3, "oq_cache_attention: the coordinates of a head must be adjacent")
+    if n <= 1:                                       # torch leaves the stride of a single row or head free
+        qt = ot = 0
+    if heads == 1:
+        qh = oh = 0
+    lse, lse_at = None, 0
+    if want_lse:
+        lse = Q.new_empty((heads, n), dtype=torch.float32)
+        lse_at = lse.data_ptr()
+    try:
+        args = _CACHE_ATTENTION.pack(*fields, Q.data_ptr(), qt, qh, out.data_ptr(), ot, oh, lse_at, at, n, heads, max_q, left, right, sinks,
+                                     scale)
+    except (struct.error, OverflowError):
+        raise OqError(1, "oq_cache_attention: sizes and the window must be whole numbers of 32 bits, scale a number in fp32") from None
+    L = _lib or lib()
+    space = size = 0
+    if workspace is not None:
+        _check_workspace("oq_cache_attention", workspace, torch, device)
+        space, size = workspace.data_ptr(), workspace.numel()
+    else:
+        need = C.c_size_t()
+        code = L.oq_cache_attention_workspace_bytes(args, C.byref(need))
+        if code:
+            _check(code)
+        size = need.value
+        if size:
+            workspace = Q.new_empty(size, dtype=torch.uint8)
+            space = workspace.data_ptr()
+    code = L.oq_cache_attention(args, space, size, torch._C._cuda_getCurrentRawStream(device))
+    if code:
+        _check(code)
+    return (out, lse) if want_lse else out
 
 
 def oq_version():

@@ -1,0 +1,222 @@
+// Attention of new tokens over a paged cache: the entry point, the choice of kernels, and the kernel that joins the parts of items which
+// were cut along their keys.
+#include <string>
+
+#include "oq_cache_attention.cuh"
+
+namespace oq {
+namespace cache {
+
+constexpr int JOIN_WARPS = 16, JOIN_THREADS = 32 * JOIN_WARPS, JOIN_ROWS = JOIN_WARPS;
+
+// CTA (c - 1, y): the item that stretch c begins inside of, where c is the first such stretch; its rows 16 y .. 16 y + 15.  Parts of a row are
+// weighed by l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each.
+template <int BM, int D>
+__global__ void __launch_bounds__(JOIN_THREADS) cache_join_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int N = D / 32;
+  __shared__ PlanMemory pm;
+  __shared__ float sums[JOIN_WARPS][D];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long per_head = measure_line<BM, JOIN_THREADS>(p, pm), all = per_head * p.c.kv_heads;
+  const int c = blockIdx.x + 1;
+  const long long at = stretch_begin(p, all, c);
+  if (at >= all) return;
+  int head, block, off;
+  find_place<BM, JOIN_THREADS>(p, pm, per_head, at, head, block, off);
+  const long long begin = at - off;
+  if (off == 0 || stretch_begin(p, all, c - 1) > begin) return;
+  const Item it = make_item<BM>(p, pm.prefix, head, block);
+  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, it.rows - row0);
+  if (rows <= 0) return;
+  // the last stretch that has tiles of the item
+  int last = c;
+  while (last + 1 < p.ctas && stretch_begin(p, all, last + 1) < begin + it.tiles) ++last;
+  int per_row = JOIN_WARPS;
+  while (per_row > 1 && per_row * rows > JOIN_WARPS) per_row >>= 1;
+  const int r = warp / per_row, share = warp % per_row;
+  const bool mine = r < rows;
+  const int row = row0 + (mine ? r : 0), parts = last - c + 2;
+  // part 0: stretch c - 1, which the item begins in; part i: stretch c - 1 + i, which begins inside of it
+  auto slot = [&](int i) { return (2ll * (c - 1 + i) + (i == 0 ? 1 : 0)) * BM + row; };
+  auto empty = [&](int i) { return i > 0 && stretch_begin(p, all, c - 1 + i) == stretch_begin(p, all, c + i); };
+  float top = -INFINITY, factor = 0.f;
+  for (int i = lane; i < parts; i += 32) {
+    if (empty(i)) continue;
+    const float4 ml = p.part_ml[slot(i)];
+    top = fmaxf(top, ml.x);
+    factor = ml.z;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  factor = __shfl_sync(~0u, factor, 0);
+  const float ct = tame(factor, top);
+  float total = 0.f;
+  for (int i = lane; i < parts; i += 32) {
+    if (empty(i)) continue;
+    const float4 ml = p.part_ml[slot(i)];
+    if (ml.y != 0.f) total += ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct));
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  if (mine)
+#pragma unroll 4
+    for (int i = share; i < parts; i += per_row) {
+      if (empty(i)) continue;
+      const float4 ml = p.part_ml[slot(i)];
+      const float* src = p.part_o + slot(i) * D + N * lane;
+      float v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = src[e];
+      const float w = ml.y == 0.f ? 0.f : ml.y * inv * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct));
+      if (w == 0.f) continue;
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+    }
+#pragma unroll
+  for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[e];
+  __syncthreads();
+  if (!mine || share) return;
+  for (int w = 1; w < per_row; ++w)
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] += sums[warp + w][N * lane + e];
+  const int q = it.r0 + row, i = it.s.q_base + q / p.group, qh = it.head * p.group + q % p.group;
+  __nv_bfloat16* dst = p.out + (long long)i * p.ldo + qh * p.hdo + N * lane;
+#pragma unroll
+  for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);
+  if (lane == 0 && p.lse) p.lse[(long long)qh * p.total_q + i] = natural_lse(top, total, factor);
+}
+
+template <int BM>
+static cudaError_t launch_join(const AttnParams& p, int head_dim, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.ctas - 1), (unsigned)(BM / JOIN_ROWS));
+  cfg.blockDim = dim3(JOIN_THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return head_dim == 128 ? cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 128>, p) : cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 64>, p);
+}
+
+static int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  return sms;
+}
+
+// Which kernels run, with how many CTAs, and what their parts take.  Nothing is known here of the sequences but their number, the tokens of all
+// together and what a row of the table can hold: these bound the items and their tiles.
+struct Choice {
+  bool few, chunk;
+  int few_ctas, chunk_ctas;
+  int row_cut;                   // sequences of at most so many rows go to the kernel for few
+  size_t few_bytes, bytes;
+};
+static Choice choose(const oq_cache_attention_args* a, const View& v) {
+  Choice c = {};
+  const int sms = sm_count(), group = a->n_heads / v.kv_heads;
+  c.few = true;
+  c.row_cut = 1 << 30;
+  const long long tiles = (v.max_len + BN - 1) / BN > 0 ? (v.max_len + BN - 1) / BN : 1;
+  auto ctas = [&](int bm, int most) {
+    const long long rows = (long long)a->total_q * group, items = ((rows + bm - 1) / bm + v.n_seqs) * v.kv_heads;
+    const long long line = items * tiles;
+    return (int)(line < most ? line : most);
+  };
+  auto part_bytes = [&](int bm, int n) { return tiles > 1 && n > 1 ? (size_t)2 * n * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4)) : (size_t)0; };
+  if (c.few) {
+    c.few_ctas = ctas(FEW_ROWS, FEW_CTAS * sms);
+    c.few_bytes = part_bytes(FEW_ROWS, c.few_ctas);
+  }
+  c.bytes = c.few_bytes;
+  return c;
+}
+
+static int check(const oq_cache_attention_args* a, View* v) {
+  if (!a) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: NULL arguments");
+  const int rc = make_view(&a->cache, "oq_cache_attention", v);
+  if (rc != OQ_OK) return rc;
+  if (a->total_q < 0 || a->max_q < 0) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: bad sizes");
+  if (a->n_heads <= 0 || a->n_heads % a->cache.n_kv_heads)
+    return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: n_heads must be a positive multiple of the cache's heads");
+  if ((long long)a->total_q * (a->n_heads / a->cache.n_kv_heads) > (1 << 30)) return fail(OQ_ERR_UNSUPPORTED, "oq_cache_attention: more than 2^30 rows");
+  if (a->cache.n_seqs > 1 && !a->q_start) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: several sequences need q_start");
+  if (a->sinks < 0) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: sinks must not be negative");
+  if (!(a->scale >= 0.f) || !(a->scale < 1e30f)) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: scale must be positive, or 0 for 1 / sqrt(head_dim)");
+  return OQ_OK;
+}
+
+}  // namespace cache
+}  // namespace oq
+
+using namespace oq;
+
+extern "C" {
+
+int oq_cache_attention_workspace_bytes(const oq_cache_attention_args* a, size_t* bytes) {
+  if (!bytes) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention_workspace_bytes: bytes is NULL");
+  *bytes = 0;
+  cache::View v;
+  const int rc = cache::check(a, &v);
+  if (rc != OQ_OK) return rc;
+  if (a->total_q > 0) *bytes = cache::choose(a, v).bytes;
+  return OQ_OK;
+}
+
+int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace cache;
+  AttnParams p = {};
+  const int rc = check(a, &p.c);
+  if (rc != OQ_OK) return rc;
+  if (a->total_q == 0) return OQ_OK;
+  const int d = a->cache.head_dim;
+  if (!a->Q || !a->out) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: NULL buffer");
+  if (!aligned16(a->Q) || !aligned16(a->out) || a->ldq_token % 8 || a->ldq_head % 8 || a->ldo_token % 8 || a->ldo_head % 8)
+    return fail(OQ_ERR_ALIGNMENT, "oq_cache_attention: pointers must be 16-byte aligned and strides multiples of 8");
+  if (a->ldq_token < 0 || a->ldq_head < 0 || (a->total_q > 1 && a->ldo_token < d) || (a->n_heads > 1 && a->ldo_head < d))
+    return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: strides of Q must not be negative, those of out at least head_dim");
+  const Choice ch = choose(a, p.c);
+  if (ch.bytes > workspace_bytes || (ch.bytes && (!workspace || !aligned16(workspace))))
+    return fail(OQ_ERR_NOMEM, "oq_cache_attention: workspace of " + std::to_string(ch.bytes) + " bytes (16-byte aligned) needed");
+  p.Q = reinterpret_cast<const __nv_bfloat16*>(a->Q);
+  p.ldq = a->total_q > 1 ? a->ldq_token : 0;
+  p.hdq = a->n_heads > 1 ? a->ldq_head : 0;
+  p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
+  p.ldo = a->total_q > 1 ? a->ldo_token : 0;
+  p.hdo = a->n_heads > 1 ? a->ldo_head : 0;
+  p.lse = a->lse;
+  p.q_start = a->q_start;
+  p.total_q = a->total_q;
+  p.group = a->n_heads / a->cache.n_kv_heads;
+  const int far = 1 << 30;                         // no sequence is longer
+  p.left = a->left < 0 ? -1 : (a->left > far ? far : a->left);
+  p.right = a->right < 0 ? -1 : (a->right > far ? far : a->right);
+  p.sinks = a->sinks > far ? far : a->sinks;
+  p.scale = a->scale > 0.f ? a->scale : (d == 128 ? 0.08838834764831845f : 0.125f);
+  p.scale_log2 = p.scale * 1.4426950408889634f;
+  p.status = device_status_word();
+  if (!p.status) return fail(OQ_ERR_CUDA, "oq_cache_attention: cannot allocate the device status word");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (ch.few) {
+    p.ctas = ch.few_ctas;
+    p.row_min = 0;
+    p.row_max = ch.row_cut;
+    p.part_ml = reinterpret_cast<float4*>(workspace);
+    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * p.ctas * FEW_ROWS);
+    e = launch_few(p, a->cache.kind, d, st);
+    if (e == cudaSuccess && ch.few_bytes) e = launch_join<FEW_ROWS>(p, d, st);
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "oq_cache_attention");
+  return OQ_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,403 @@
+// Attention of a few rows (new tokens times the heads of a group) over a paged cache.
+//
+// With up to 16 rows for a key and value head the cache is read once and every byte is used a few times, so the memory is the bound: 346 MB for one
+// token over 32760 tokens of 40 heads in 8 bits, 53 us at the copy rate.  Decoding is what the SM does most of: 24 elements a cycle for the
+// bytes that arrive, an instruction a pair each for conversion and scale.  So nothing passes through shared memory: a lane reads the cache in 16
+// bytes a time, decodes them in registers, and what it has is its fragment of the operand,
+//   S^T [16 keys x 8 rows] = K [16 x D] Q^T,      O^T [D x 8 rows] += V^T [D x 16 keys] P^T,
+// with the keys (the coordinates) as the 16 rows of an instruction and the queries as its 8 columns.  Which coordinate goes where in the
+// contraction over D is free as long as Q goes the same way, and so is the order of V's coordinates in the result.  S^T has the queries in the columns and
+// so has O^T: a query's maximum and factors stay in the lanes that need them, and P^T comes from S^T by one transposition of 8 x 8 numbers.
+// The tensor cores' older instruction serves here: they are idle most of the time.
+//
+// 8 warps each take 16 keys of a tile of 128 and keep their own maximum, sum and O; they are put together at the end of an item.  A warp's
+// next keys are requested as soon as the present ones are decoded, its next values likewise.
+#include <string>
+
+#include "oq_cache_attention.cuh"
+
+namespace oq {
+namespace cache {
+
+namespace few {
+
+constexpr int WARPS = 8, THREADS = 32 * WARPS;
+constexpr float SLACK = 8.f;                       // powers stay below 2^8
+
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
+  if (N == 1) {
+    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+  } else if (N == 2) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[N > 1 ? 1 : 0]) : "l"(p));
+  } else {
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[N > 1 ? 1 : 0]), "=r"(w[N > 2 ? 2 : 0]), "=r"(w[N > 3 ? 3 : 0]) : "l"(p));
+  }
+}
+
+template <int KIND, int D>
+struct Lane {
+  using F = Format<KIND, D>;
+  static constexpr int LOADS = F::ROW >= 128 ? 2 : 1;          // of a key row by one of its 4 lanes
+  static constexpr int KW = F::ROW / 16 / LOADS;               // words of each
+  static constexpr int VW = F::ROW / 32;                       // words of a value row by one of its 8 lanes
+  // first coordinate of load x by lane t of a row: e4m3 in pieces of 16, e2m1 in one of D / 4
+  __device__ static __forceinline__ int coord(int x, int t) { return KIND == 8 ? 64 * x + 16 * t : D / 4 * t; }
+  static constexpr int PER_WORD = 32 / KIND;                   // coordinates of a word
+};
+
+// The loads of one step (16 keys) by a lane: rows g and g + 8 of the keys, keys 2t, 2t+1, 2t+8, 2t+9 of the values.
+template <int KIND, int D>
+struct Keys {
+  using L = Lane<KIND, D>;
+  uint32_t w[2][L::LOADS][L::KW];
+  uint32_t scale[2];
+};
+template <int KIND, int D>
+struct Values {
+  uint32_t w[4][Lane<KIND, D>::VW];
+  uint32_t scale[4];
+};
+
+template <int KIND, int D, int NT>
+__global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_constant__ AttnParams p) {
+  using F = Format<KIND, D>;
+  using L = Lane<KIND, D>;
+  constexpr int BM = 8 * NT, QP = D + 8;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* const part = reinterpret_cast<float*>(smem);                     // [WARPS][BM][D]
+  __shared__ __align__(16) uint16_t q_s[BM * QP];
+  __shared__ float c_s[BM], m_s[WARPS][BM], l_s[WARPS][BM];
+  __shared__ PlanMemory pm;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  Stretch st = plan<BM, THREADS>(p, pm);
+
+  while (st.count > 0) {
+    const Item it = make_item<BM>(p, pm.prefix, st.head, st.block);
+    const int first = st.off, end = (int)min((long long)it.tiles, st.off + st.count);
+    // ------------------------------------------------ queries ------------------------------------------------
+    for (int r = warp; r < BM; r += WARPS) {
+      constexpr int N = D / 32;
+      float x[N];
+      uint32_t largest = 0;
+      const int row = it.r0 + r;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = 0.f;
+      if (r < it.rows) {
+        const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + row / p.group) * p.ldq + (long long)(it.head * p.group + row % p.group) * p.hdq + N * lane;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(src + e));
+          x[e] = __uint_as_float(u << 16);
+          x[e + 1] = __uint_as_float(u & 0xFFFF0000u);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) largest = max(largest, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+      largest = __reduce_max_sync(~0u, largest);
+      const RowScale rs = row_scale(largest, p.scale_log2);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(q_s + r * QP + N * lane + e) = pack_f16(x[e] * rs.mul, x[e + 1] * rs.mul);
+      if (lane == 0) c_s[r] = rs.c;
+    }
+    __syncthreads();
+    // B fragments of Q^T: coordinates in the order in which the lanes hold the keys'
+    uint32_t qf[D / 16][NT][2];
+#pragma unroll
+    for (int x = 0; x < L::LOADS; ++x)
+#pragma unroll
+      for (int w = 0; w < L::KW; ++w)
+#pragma unroll
+        for (int h = 0; h < L::PER_WORD / 4; ++h)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint16_t* q = q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h;
+            const int s = (x * L::KW + w) * (L::PER_WORD / 4) + h;
+            qf[s][n][0] = *reinterpret_cast<const uint32_t*>(q);
+            qf[s][n][1] = *reinterpret_cast<const uint32_t*>(q + 2);
+          }
+    // columns of this lane: queries 8 n + 2 t and the next
+    float c[NT][2], m[NT][2], l[NT][2];
+    int hi[NT][2], lo[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * n + 2 * t + e, i = (it.r0 + r) / p.group;
+        c[n][e] = c_s[r];
+        m[n][e] = -INFINITY;
+        l[n][e] = 0.f;
+        hi[n][e] = r < it.rows ? row_hi(p, it.s, i) : -1;
+        lo[n][e] = row_lo(p, it.s, i);
+      }
+    const int full_hi = row_hi(p, it.s, it.r0 / p.group), full_lo = row_lo(p, it.s, (it.r0 + it.rows - 1) / p.group);     // what every row sees
+    float o[D / 16][NT][4];
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][n][e] = 0.f;
+
+    // The warp's steps: 16 keys of each tile, where some row may see one of them.
+    int j = first;
+    auto next_pos = [&]() {
+      while (j < end) {
+        const int pos = it.key0(j++) + 16 * warp;
+        if (pos <= it.hi && (pos + 15 >= it.lo || pos < p.sinks)) return pos;
+      }
+      return -1;
+    };
+    auto block_at = [&](int pos) -> const uint8_t* {
+      const int page = pos < 0 ? -1 : page_of(p.c, it.seq, pos);
+      return page < 0 ? nullptr : block_of(p.c, page, it.head);
+    };
+    const int in_page = (1 << p.c.shift) - 1;
+    Keys<KIND, D> k;
+    Values<KIND, D> v;
+    auto load_keys = [&](const uint8_t* block, int pos) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int key = pos + g + 8 * r;
+        k.scale[r] = 0x7F7F7F7Fu;
+#pragma unroll
+        for (int x = 0; x < L::LOADS; ++x)
+#pragma unroll
+          for (int w = 0; w < L::KW; ++w) k.w[r][x][w] = 0u;
+        if (block && key < it.s.nk) {
+          const int at = key & in_page;
+#pragma unroll
+          for (int x = 0; x < L::LOADS; ++x) load_words(block + at * F::ROW + L::coord(x, t) * KIND / 8, k.w[r][x]);
+          k.scale[r] = F::GROUPS == 4 ? *reinterpret_cast<const uint32_t*>(block + p.c.off_ks + 4 * at)
+                                      : (uint32_t)*reinterpret_cast<const uint16_t*>(block + p.c.off_ks + 2 * at);
+        }
+      }
+    };
+    auto load_values = [&](const uint8_t* block, int pos) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = pos + 2 * t + (e & 1) + 8 * (e >> 1);
+        v.scale[e] = 127u;
+#pragma unroll
+        for (int w = 0; w < L::VW; ++w) v.w[e][w] = 0u;
+        if (block && key < it.s.nk) {
+          const int at = key & in_page;
+          load_words(block + p.c.off_v + at * F::ROW + g * (F::ROW / 8), v.w[e]);
+          v.scale[e] = block[p.c.off_vs + at * F::GROUPS + g * F::GROUPS / 8];
+        }
+      }
+    };
+    int pos = next_pos();
+    const uint8_t* block = block_at(pos);
+    if (pos >= 0) {
+      load_keys(block, pos);
+      load_values(block, pos);
+    }
+    int pos_n = next_pos();
+    const uint8_t* block_n = block_at(pos_n);
+    while (pos >= 0) {
+      // ---------------------------------------------- S^T = K Q^T ----------------------------------------------
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+      for (int x = 0; x < L::LOADS; ++x) {
+        uint32_t f[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t b = (k.scale[r] >> (8 * (L::coord(x, t) / 32))) & 255u;
+          f[r] = b == BROKEN ? 0x7FFF7FFFu : scale_pair(b, b);
+        }
+#pragma unroll
+        for (int w = 0; w < L::KW; ++w) {
+          uint32_t a[2][L::PER_WORD / 2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if constexpr (KIND == 8) e4m3_to_f16(k.w[r][x][w], a[r][0], a[r][1]);
+            else e2m1_to_f16(k.w[r][x][w], a[r][0], a[r][1], a[r][2], a[r][3]);
+#pragma unroll
+            for (int e = 0; e < L::PER_WORD / 2; ++e) a[r][e] = mul_f16x2(a[r][e], f[r]);
+          }
+#pragma unroll
+          for (int h = 0; h < L::PER_WORD / 4; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint32_t(&b)[2] = qf[(x * L::KW + w) * (L::PER_WORD / 4) + h][n];
+              mma(s[n], a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b[0], b[1]);
+            }
+        }
+      }
+      if (pos_n >= 0) load_keys(block_n, pos_n);
+      // ------------------------------------------------ softmax ------------------------------------------------
+      if (block == nullptr || !(pos + 15 <= full_hi && (pos >= full_lo || pos + 16 <= p.sinks))) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = pos + g + 8 * (e >> 1);
+            if (block == nullptr || key > hi[n][e & 1] || (key < lo[n][e & 1] && key >= p.sinks)) s[n][e] = -INFINITY;
+          }
+      }
+      bool over = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) over |= (fmaxf(s[n][e], s[n][e + 2]) - m[n][e]) * c[n][e] > SLACK;
+      if (__any_sync(~0u, over)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float x = fmaxf(m[n][e], fmaxf(s[n][e], s[n][e + 2]));
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+            c[n][e] = tame(c[n][e], x);
+            const float a = x == m[n][e] ? 1.f : exp2_fast((m[n][e] - x) * c[n][e]);
+            m[n][e] = x;
+            l[n][e] *= a;
+#pragma unroll
+            for (int y = 0; y < D / 16; ++y) {
+              o[y][n][e] *= a;
+              o[y][n][e + 2] *= a;
+            }
+          }
+      }
+      uint32_t b[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float ref = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1];
+          w[e] = exp2_fast((s[n][e] - ref) * c[n][e & 1]);
+          l[n][e & 1] += w[e];
+        }
+        b[n][0] = transpose8(pack_f16(w[0], w[1]));
+        b[n][1] = transpose8(pack_f16(w[2], w[3]));
+      }
+      // --------------------------------------------- O^T += V^T P^T ---------------------------------------------
+      const uint32_t f0 = scale_pair(v.scale[0], v.scale[1]), f1 = scale_pair(v.scale[2], v.scale[3]);
+#pragma unroll
+      for (int w = 0; w < L::VW; ++w) {
+        // pairs of keys for each coordinate of the word: keys 2t, 2t+1 and 2t+8, 2t+9
+        uint32_t a[2][L::PER_WORD];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x = v.w[2 * h][w], y = v.w[2 * h + 1][w];
+          if constexpr (KIND == 8) {
+            uint32_t p01, p23;
+            asm("prmt.b32 %0, %1, %2, 0x5140;" : "=r"(p01) : "r"(x), "r"(y));
+            asm("prmt.b32 %0, %1, %2, 0x7362;" : "=r"(p23) : "r"(x), "r"(y));
+            e4m3_to_f16(p01, a[h][0], a[h][1]);
+            e4m3_to_f16(p23, a[h][2], a[h][3]);
+          } else {
+            const uint32_t even = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), odd = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+            e2m1_to_f16(even, a[h][0], a[h][2], a[h][4], a[h][6]);
+            e2m1_to_f16(odd, a[h][1], a[h][3], a[h][5], a[h][7]);
+          }
+#pragma unroll
+          for (int e = 0; e < L::PER_WORD; ++e) a[h][e] = mul_f16x2(a[h][e], h ? f1 : f0);
+        }
+#pragma unroll
+        for (int e = 0; e < L::PER_WORD / 2; ++e)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            mma(o[w * (L::PER_WORD / 2) + e][n], a[0][2 * e], a[0][2 * e + 1], a[1][2 * e], a[1][2 * e + 1], b[n][0], b[n][1]);
+      }
+      if (pos_n >= 0) load_values(block_n, pos_n);
+      pos = pos_n;
+      block = block_n;
+      pos_n = next_pos();
+      block_n = block_at(pos_n);
+    }
+    // ----------------------------------------------- the item's result -----------------------------------------------
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(~0u, l[n][e], d);
+        const int r = 8 * n + 2 * t + e;
+        if (g == 0) {
+          m_s[warp][r] = m[n][e];
+          l_s[warp][r] = l[n][e];
+        }
+        float* to = part + (warp * BM + r) * D + g * (D / 8);
+#pragma unroll
+        for (int y = 0; y < D / 16; ++y) *reinterpret_cast<float2*>(to + 2 * y) = make_float2(o[y][n][e], o[y][n][e + 2]);
+      }
+    __syncthreads();
+    const bool whole = first == 0 && end == it.tiles;
+    const long long slot = 2 * (long long)blockIdx.x + (first == 0 ? 1 : 0);
+    constexpr int N = D / 32;
+    for (int r = warp; r < it.rows; r += WARPS) {
+      float top = -INFINITY, total = 0.f, acc[N];
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, m_s[w][r]);
+      const float cr = tame(c_s[r], top);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float lw = l_s[w][r], a = m_s[w][r] == top ? 1.f : exp2_fast((m_s[w][r] - top) * cr);
+        if (lw == 0.f) continue;                        // (saw nothing; NaN goes on)
+        total = fmaf(lw, a, total);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = fmaf(part[(w * BM + r) * D + N * lane + e], a, acc[e]);
+      }
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      const int row = it.r0 + r, i = it.s.q_base + row / p.group, head = it.head * p.group + row % p.group;
+      if (whole) {
+        __nv_bfloat16* dst = p.out + (long long)i * p.ldo + head * p.hdo + N * lane;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+        if (lane == 0 && p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(top, total, c_s[r]);
+      } else {
+        float* dst = p.part_o + (slot * BM + r) * D + N * lane;
+#pragma unroll
+        for (int e = 0; e < N; ++e) dst[e] = acc[e] * inv;
+        if (lane == 0) p.part_ml[slot * BM + r] = make_float4(top, total, c_s[r], 0.f);
+      }
+    }
+    __syncthreads();
+    st.count -= end - first;
+    st.off = 0;
+    if (++st.block == st.blocks) {
+      st.block = 0;
+      ++st.head;
+    }
+  }
+}
+
+template <int KIND, int D, int NT>
+cudaError_t go(const AttnParams& p, cudaStream_t st) {
+  const size_t smem = (size_t)WARPS * 8 * NT * D * sizeof(float);
+  // (the attribute belongs to the device that is current, so it is set every time)
+  const cudaError_t e = cudaFuncSetAttribute(few_kernel<KIND, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(few_kernel<KIND, D, NT>, p.ctas, THREADS, smem, st, p);
+}
+
+}  // namespace few
+
+cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, cudaStream_t st) {
+  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 2>(p, st) : few::go<8, 64, 2>(p, st);
+  return head_dim == 128 ? few::go<4, 128, 2>(p, st) : few::go<4, 64, 2>(p, st);
+}
+
+}  // namespace cache
+}  // namespace oq
