@@ -123,13 +123,14 @@ struct Choice {
 static Choice choose(const oq_cache_attention_args* a, const View& v) {
   Choice c = {};
   const int sms = sm_count(), group = a->n_heads / v.kv_heads;
-  c.few = true;
-  c.row_cut = 1 << 30;
-  const long long tiles = (v.max_len + BN - 1) / BN > 0 ? (v.max_len + BN - 1) / BN : 1;
-  auto ctas = [&](int bm, int most) {
-    const long long rows = (long long)a->total_q * group, items = ((rows + bm - 1) / bm + v.n_seqs) * v.kv_heads;
-    const long long line = items * tiles;
-    return (int)(line < most ? line : most);
+  const long long most = (long long)(a->max_q > 0 && a->max_q < a->total_q ? a->max_q : a->total_q) * group;
+  c.few = most <= FEW_LIMIT || v.n_seqs > 1;
+  c.chunk = most > FEW_LIMIT;
+  c.row_cut = FEW_LIMIT;
+  const long long tiles = v.max_len > 0 ? (v.max_len + BN - 1) / BN : 1;
+  auto ctas = [&](int bm, int all) {
+    const long long items = (((long long)a->total_q * group + bm - 1) / bm + v.n_seqs) * v.kv_heads;
+    return (int)(items >= all || items * tiles >= all ? all : items * tiles);
   };
   auto part_bytes = [&](int bm, int n) { return tiles > 1 && n > 1 ? (size_t)2 * n * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4)) : (size_t)0; };
   if (c.few) {
@@ -137,6 +138,10 @@ static Choice choose(const oq_cache_attention_args* a, const View& v) {
     c.few_bytes = part_bytes(FEW_ROWS, c.few_ctas);
   }
   c.bytes = c.few_bytes;
+  if (c.chunk) {
+    c.chunk_ctas = ctas(CHUNK_ROWS, sms);
+    c.bytes += part_bytes(CHUNK_ROWS, c.chunk_ctas);
+  }
   return c;
 }
 
@@ -206,14 +211,23 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_cache_attention: cannot allocate the device status word");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (ch.few) {
-    p.ctas = ch.few_ctas;
+  auto run = [&](auto launch, int ctas, int rows, size_t at, size_t bytes) {
+    p.ctas = ctas;
+    p.part_ml = reinterpret_cast<float4*>(reinterpret_cast<char*>(workspace) + at);
+    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * rows);
+    cudaError_t err = launch(p, a->cache.kind, d, st);
+    if (err == cudaSuccess && bytes) err = rows == FEW_ROWS ? launch_join<FEW_ROWS>(p, d, st) : launch_join<CHUNK_ROWS>(p, d, st);
+    return err;
+  };
+  if (ch.chunk) {
+    p.row_min = ch.few ? ch.row_cut : 0;
+    p.row_max = 1 << 30;
+    e = run(launch_chunk, ch.chunk_ctas, CHUNK_ROWS, ch.few_bytes, ch.bytes - ch.few_bytes);
+  }
+  if (ch.few && e == cudaSuccess) {
     p.row_min = 0;
-    p.row_max = ch.row_cut;
-    p.part_ml = reinterpret_cast<float4*>(workspace);
-    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * p.ctas * FEW_ROWS);
-    e = launch_few(p, a->cache.kind, d, st);
-    if (e == cudaSuccess && ch.few_bytes) e = launch_join<FEW_ROWS>(p, d, st);
+    p.row_max = ch.chunk ? ch.row_cut : 1 << 30;
+    e = run(launch_few, ch.few_ctas, FEW_ROWS, 0, ch.few_bytes);
   }
   if (e != cudaSuccess) return cuda_fail(e, "oq_cache_attention");
   return OQ_OK;

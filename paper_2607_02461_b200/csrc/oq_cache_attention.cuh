@@ -236,6 +236,7 @@ cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, cudaStream_t
 cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, cudaStream_t st);
 constexpr int FEW_ROWS = 16, CHUNK_ROWS = 256;      // rows of their items
 constexpr int FEW_CTAS = 2;                         // of an SM
+constexpr int FEW_LIMIT = 32;                       // rows up to which a sequence goes to the kernel for few
 
 }  // namespace cache
 }  // namespace oq
