@@ -7,43 +7,40 @@
 namespace oq {
 namespace cache {
 
-constexpr int JOIN_WARPS = 16, JOIN_THREADS = 32 * JOIN_WARPS, JOIN_ROWS = JOIN_WARPS;
+constexpr int JOIN_WARPS = 8, JOIN_ROWS = JOIN_WARPS;
 
-// CTA (c - 1, y): the item that stretch c begins inside of, where c is the first such stretch; its rows 16 y .. 16 y + 15.  Parts of a row are
-// weighed by l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each.
+// CTA (c, y): rows 8 y .. 8 y + 7 of the item that CTA c of the kernel before began and did not finish, if there is one.  Parts of a row are weighed by
+// l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each.
 template <int BM, int D>
-__global__ void __launch_bounds__(JOIN_THREADS) cache_join_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(32 * JOIN_WARPS) cache_join_kernel(const __grid_constant__ AttnParams p) {
   constexpr int N = D / 32;
-  __shared__ PlanMemory pm;
   __shared__ float sums[JOIN_WARPS][D];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long per_head = measure_line<BM, JOIN_THREADS>(p, pm), all = per_head * p.c.kv_heads;
-  const int c = blockIdx.x + 1;
-  const long long at = stretch_begin(p, all, c);
-  if (at >= all) return;
-  int head, block, off;
-  find_place<BM, JOIN_THREADS>(p, pm, per_head, at, head, block, off);
-  const long long begin = at - off;
-  if (off == 0 || stretch_begin(p, all, c - 1) > begin) return;
-  const Item it = make_item<BM>(p, pm.prefix, head, block);
-  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, it.rows - row0);
+  const Cut cut = p.cuts[blockIdx.x];
+  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, cut.rows - row0), parts = cut.parts;
   if (rows <= 0) return;
-  // the last stretch that has tiles of the item
-  int last = c;
-  while (last + 1 < p.ctas && stretch_begin(p, all, last + 1) < begin + it.tiles) ++last;
   int per_row = JOIN_WARPS;
   while (per_row > 1 && per_row * rows > JOIN_WARPS) per_row >>= 1;
   const int r = warp / per_row, share = warp % per_row;
   const bool mine = r < rows;
-  const int row = row0 + (mine ? r : 0), parts = last - c + 2;
-  // part 0: stretch c - 1, which the item begins in; part i: stretch c - 1 + i, which begins inside of it
-  auto slot = [&](int i) { return (2ll * (c - 1 + i) + (i == 0 ? 1 : 0)) * BM + row; };
-  auto empty = [&](int i) { return i > 0 && stretch_begin(p, all, c - 1 + i) == stretch_begin(p, all, c + i); };
-  float top = -INFINITY, factor = 0.f;
+  const int row = row0 + (mine ? r : 0);
+  auto slot = [&](int i) { return (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * BM + row; };
+  // (parts of the first round are requested before their weights are known)
+  constexpr int AHEAD = 4;
+  float v[AHEAD][N];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * per_row;
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[s][e] = i < parts ? p.part_o[slot(i) * D + N * lane + e] : 0.f;
+    }
+  };
+  load(share);
+  float top = -INFINITY, factor = 0.f, total = 0.f;
   for (int i = lane; i < parts; i += 32) {
-    if (empty(i)) continue;
     const float4 ml = p.part_ml[slot(i)];
     top = fmaxf(top, ml.x);
     factor = ml.z;
@@ -52,40 +49,36 @@ __global__ void __launch_bounds__(JOIN_THREADS) cache_join_kernel(const __grid_c
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
   factor = __shfl_sync(~0u, factor, 0);
   const float ct = tame(factor, top);
-  float total = 0.f;
-  for (int i = lane; i < parts; i += 32) {
-    if (empty(i)) continue;
-    const float4 ml = p.part_ml[slot(i)];
-    if (ml.y != 0.f) total += ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct));
-  }
+  auto weight = [&](const float4& ml) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct)); };
+  for (int i = lane; i < parts; i += 32) total += weight(p.part_ml[slot(i)]);
 #pragma unroll
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
   const float inv = total == 0.f ? 0.f : 1.f / total;
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  if (mine)
-#pragma unroll 4
-    for (int i = share; i < parts; i += per_row) {
-      if (empty(i)) continue;
-      const float4 ml = p.part_ml[slot(i)];
-      const float* src = p.part_o + slot(i) * D + N * lane;
-      float v[N];
+  for (int i0 = share; i0 < parts; i0 += AHEAD * per_row) {
+    if (i0 != share) load(i0);
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = src[e];
-      const float w = ml.y == 0.f ? 0.f : ml.y * inv * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct));
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * per_row;
+      if (i >= parts) continue;
+      const float w = weight(p.part_ml[slot(i)]) * inv;
       if (w == 0.f) continue;
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[s][e], acc[e]);
     }
+  }
+  if (per_row > 1) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[e];
-  __syncthreads();
+    for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[e];
+    __syncthreads();
+  }
   if (!mine || share) return;
   for (int w = 1; w < per_row; ++w)
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] += sums[warp + w][N * lane + e];
-  const int q = it.r0 + row, i = it.s.q_base + q / p.group, qh = it.head * p.group + q % p.group;
+  const int q = cut.r0 + row, i = cut.q_base + q / p.group, qh = cut.head * p.group + q % p.group;
   __nv_bfloat16* dst = p.out + (long long)i * p.ldo + qh * p.hdo + N * lane;
 #pragma unroll
   for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);
@@ -93,10 +86,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) cache_join_kernel(const __grid_c
 }
 
 template <int BM>
-static cudaError_t launch_join(const AttnParams& p, int head_dim, cudaStream_t st) {
+static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.ctas - 1), (unsigned)(BM / JOIN_ROWS));
-  cfg.blockDim = dim3(JOIN_THREADS);
+  cfg.gridDim = dim3((unsigned)ctas, (unsigned)(BM / JOIN_ROWS));
+  cfg.blockDim = dim3(32 * JOIN_WARPS);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -118,7 +111,7 @@ struct Choice {
   bool few, chunk;
   int few_ctas, chunk_ctas;
   int row_cut;                   // sequences of at most so many rows go to the kernel for few
-  size_t few_bytes, bytes;
+  size_t few_bytes, chunk_bytes, bytes;
 };
 static Choice choose(const oq_cache_attention_args* a, const View& v) {
   Choice c = {};
@@ -132,7 +125,7 @@ static Choice choose(const oq_cache_attention_args* a, const View& v) {
     const long long items = (((long long)a->total_q * group + bm - 1) / bm + v.n_seqs) * v.kv_heads;
     return (int)(items >= all || items * tiles >= all ? all : items * tiles);
   };
-  auto part_bytes = [&](int bm, int n) { return tiles > 1 && n > 1 ? (size_t)2 * n * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4)) : (size_t)0; };
+  auto part_bytes = [&](int bm, int n) { return tiles > 1 && n > 1 ? n * (sizeof(Cut) + (size_t)2 * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4))) : (size_t)0; };
   if (c.few) {
     c.few_ctas = ctas(FEW_ROWS, FEW_CTAS * sms);
     c.few_bytes = part_bytes(FEW_ROWS, c.few_ctas);
@@ -140,8 +133,10 @@ static Choice choose(const oq_cache_attention_args* a, const View& v) {
   c.bytes = c.few_bytes;
   if (c.chunk) {
     c.chunk_ctas = ctas(CHUNK_ROWS, sms);
-    c.bytes += part_bytes(CHUNK_ROWS, c.chunk_ctas);
+    c.chunk_bytes = part_bytes(CHUNK_ROWS, c.chunk_ctas);
+    c.bytes += c.chunk_bytes;
   }
+  if (c.bytes) c.bytes += 32;                          // the parts begin on 32 bytes, the workspace on 16
   return c;
 }
 
@@ -197,6 +192,7 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
   p.ldo = a->total_q > 1 ? a->ldo_token : 0;
   p.hdo = a->n_heads > 1 ? a->ldo_head : 0;
+  p.wide_out = reinterpret_cast<uintptr_t>(a->out) % 32 == 0 && p.ldo % 16 == 0 && p.hdo % 16 == 0;
   p.lse = a->lse;
   p.q_start = a->q_start;
   p.total_q = a->total_q;
@@ -212,17 +208,21 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   auto run = [&](auto launch, int ctas, int rows, size_t at, size_t bytes) {
-    p.ctas = ctas;
-    p.part_ml = reinterpret_cast<float4*>(reinterpret_cast<char*>(workspace) + at);
-    p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * rows);
-    cudaError_t err = launch(p, a->cache.kind, d, st);
-    if (err == cudaSuccess && bytes) err = rows == FEW_ROWS ? launch_join<FEW_ROWS>(p, d, st) : launch_join<CHUNK_ROWS>(p, d, st);
+    if (bytes) {
+      p.cuts = reinterpret_cast<Cut*>(((reinterpret_cast<uintptr_t>(workspace) + 31) & ~(uintptr_t)31) + at);
+      p.part_ml = reinterpret_cast<float4*>(p.cuts + ctas);
+      p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * rows);
+    } else {
+      p.cuts = nullptr;                              // one tile an item, or one CTA: nothing is cut
+    }
+    cudaError_t err = launch(p, a->cache.kind, d, ctas, st);
+    if (err == cudaSuccess && bytes) err = rows == FEW_ROWS ? launch_join<FEW_ROWS>(p, d, ctas, st) : launch_join<CHUNK_ROWS>(p, d, ctas, st);
     return err;
   };
   if (ch.chunk) {
     p.row_min = ch.few ? ch.row_cut : 0;
     p.row_max = 1 << 30;
-    e = run(launch_chunk, ch.chunk_ctas, CHUNK_ROWS, ch.few_bytes, ch.bytes - ch.few_bytes);
+    e = run(launch_chunk, ch.chunk_ctas, CHUNK_ROWS, ch.few_bytes, ch.chunk_bytes);
   }
   if (ch.few && e == cudaSuccess) {
     p.row_min = 0;

@@ -8,8 +8,8 @@
 // An item is a block of BM rows of one sequence and key and value head, with the tiles of 128 keys that some row of it sees (one, if
 // there are none).  All items' tiles, one after the other, are a line that is cut into as many equal stretches as there are CTAs, so the lengths may
 // be of any kind: they are on the device only, and every CTA finds its own stretch from them.  An item that lies in one stretch is
-// finished there; of others each CTA writes its part, and a second kernel joins them.  A CTA has at most two such parts: of the item that its stretch begins
-// inside of, and of the one that it ends inside of.
+// finished there; of others each CTA writes its part, and a second kernel joins them.  A CTA has at most two such parts: part 0 of the item that its
+// stretch begins inside of, and part 1 of the one that begins in it and goes on behind it.
 #pragma once
 #include "oq_cache.cuh"
 
@@ -24,15 +24,22 @@ struct AttnParams {
   long long ldq, hdq;
   __nv_bfloat16* out;
   long long ldo, hdo;
+  int wide_out;                            // rows of out begin on 32 bytes
   float* lse;                              // [heads][total_q] or NULL
-  float* part_o;                           // [2 * CTAs][BM][D]: weights that add up to one
+  struct Cut* cuts;                        // [CTAs]: the item that the CTA's stretch ends inside of and begins at or before
   float4* part_ml;                         // [2 * CTAs][BM]: reference m, sum l of the powers 2^(c (s - m)), c
+  float* part_o;                           // [2 * CTAs][BM][D]: weights that add up to one
   const int* q_start;                      // n_seqs + 1, or NULL: one sequence
-  int total_q, group, ctas;
+  int total_q, group;
   int row_min, row_max;                    // this kernel takes the sequences with row_min < rows <= row_max
   int left, right, sinks;
   float scale, scale_log2;
   int* status;
+};
+
+// An item in parts: the first is part 1 of this CTA, the others part 0 of the CTAs after it.  rows == 0: none.
+struct __align__(16) Cut {
+  int q_base, r0, rows, head, parts, unused[3];
 };
 
 struct Seq {
@@ -63,19 +70,26 @@ __device__ __forceinline__ int row_hi(const AttnParams& p, const Seq& s, int i) 
 }
 __device__ __forceinline__ int row_lo(const AttnParams& p, const Seq& s, int i) { return p.left < 0 ? 0 : max(0, i + s.nk - s.nq - p.left); }
 
-// prefix[s]: blocks before sequence s
+// What a CTA finds out first: the sequences, the blocks before each of them, and where its stretch begins.
+struct Plan {
+  int prefix[MAX_SEQS + 1];
+  Seq seq[MAX_SEQS];
+  long long sums[32];
+  int block, off;
+};
+
 template <int BM>
-__device__ __forceinline__ Item make_item(const AttnParams& p, const int* prefix, int head, int block) {
+__device__ __forceinline__ Item make_item(const AttnParams& p, const Plan& m, int head, int block) {
   Item it;
   it.head = head;
   int s = 0, e = p.c.n_seqs;
   while (e - s > 1) {
-    const int m = (s + e) >> 1;
-    if (prefix[m] <= block) s = m; else e = m;
+    const int mid = (s + e) >> 1;
+    if (m.prefix[mid] <= block) s = mid; else e = mid;
   }
   it.seq = s;
-  it.s = get_seq(p, s);
-  it.r0 = BM * (block - prefix[s]);
+  it.s = m.seq[s];
+  it.r0 = BM * (block - m.prefix[s]);
   it.rows = min(BM, it.s.nq * p.group - it.r0);
   it.hi = row_hi(p, it.s, (it.r0 + it.rows - 1) / p.group);
   it.lo = row_lo(p, it.s, it.r0 / p.group);
@@ -89,17 +103,17 @@ __device__ __forceinline__ Item make_item(const AttnParams& p, const int* prefix
   return it;
 }
 
-struct PlanMemory {
-  int prefix[MAX_SEQS + 1];
-  long long sums[32];
-  int block, off;
-};
-// A position on the line of all tiles (heads, then sequences, then blocks, then tiles) and the tiles from there to the stretch's end.
+// A place on the line of all tiles (heads, then sequences, then blocks, then tiles) and the tiles from there to the stretch's end.
 struct Stretch {
   int head, block, off;
-  long long count;
   int blocks;                              // of one head
+  long long at, count;                     // the place's number, the tiles left
+  long long all;                           // tiles of the line
+  int ctas;                                // that share it: no more than there are tiles
 };
+__device__ __forceinline__ long long divide(long long a, long long b) {       // (the short form where it serves)
+  return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
 
 // Sum over the CTA; `before`: the sum over the threads before this one.
 template <int THREADS>
@@ -124,73 +138,83 @@ __device__ __forceinline__ long long block_scan(long long v, long long* sums, lo
   return total;
 }
 
-// Position `at` of the line (its tiles numbered through) as head, block and tile; by the whole CTA.
+// By the whole CTA.
 template <int BM, int THREADS>
-__device__ __forceinline__ void find_place(const AttnParams& p, PlanMemory& m, long long per_head, long long at, int& head, int& block, int& off) {
-  const int blocks = m.prefix[p.c.n_seqs];
-  head = (int)(at / per_head);
-  const long long r = at - head * per_head;
-  long long done = 0;
-  for (int b0 = 0; b0 < blocks && done <= r; b0 += THREADS) {
+__device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
+  static_assert(THREADS >= MAX_SEQS, "a thread for each sequence");
+  Stretch st;
+  long long before, n = 0;
+  if ((int)threadIdx.x < p.c.n_seqs) {
+    const Seq s = get_seq(p, threadIdx.x);
+    m.seq[threadIdx.x] = s;
+    const int rows = s.nq * p.group;
+    if (rows > p.row_min && rows <= p.row_max) n = (rows + BM - 1) / BM;
+  }
+  if (p.c.n_seqs > 1) {
+    st.blocks = (int)block_scan<THREADS>(n, m.sums, before);
+    if ((int)threadIdx.x < p.c.n_seqs) m.prefix[threadIdx.x] = (int)before;
+  } else if (threadIdx.x == 0) {
+    m.prefix[0] = 0;
+    m.prefix[1] = (int)n;
+  }
+  if (p.c.n_seqs > 1 && threadIdx.x == 0) m.prefix[p.c.n_seqs] = st.blocks;
+  __syncthreads();
+  st.blocks = m.prefix[p.c.n_seqs];
+  // tiles of one head; the first round's sums are kept, as there is one round mostly
+  n = (int)threadIdx.x < st.blocks ? make_item<BM>(p, m, 0, threadIdx.x).tiles : 0;
+  const long long first = block_scan<THREADS>(n, m.sums, before);
+  long long per_head = first, unused;
+  for (int b0 = THREADS; b0 < st.blocks; b0 += THREADS) {
     const int b = b0 + threadIdx.x;
-    const long long n = b < blocks ? make_item<BM>(p, m.prefix, 0, b).tiles : 0;
-    long long before;
-    const long long total = block_scan<THREADS>(n, m.sums, before);
+    per_head += block_scan<THREADS>(b < st.blocks ? make_item<BM>(p, m, 0, b).tiles : 0, m.sums, unused);
+  }
+  st.all = per_head * p.c.kv_heads;
+  st.ctas = (int)min((long long)gridDim.x, st.all);
+  st.head = st.block = st.off = 0;
+  st.at = st.count = 0;
+  if ((int)blockIdx.x >= st.ctas) return st;
+  st.at = divide(st.all * blockIdx.x, st.ctas);
+  st.count = divide(st.all * (blockIdx.x + 1), st.ctas) - st.at;
+  st.head = (int)divide(st.at, per_head);
+  const long long r = st.at - st.head * per_head;
+  long long done = 0, total = first;
+  for (int b0 = 0;;) {
     before += done;
     if (n > 0 && before <= r && r < before + n) {
-      m.block = b;
+      m.block = b0 + threadIdx.x;
       m.off = (int)(r - before);
     }
     done += total;
+    b0 += THREADS;
+    if (done > r || b0 >= st.blocks) break;
+    n = b0 + (int)threadIdx.x < st.blocks ? make_item<BM>(p, m, 0, b0 + threadIdx.x).tiles : 0;
+    total = block_scan<THREADS>(n, m.sums, before);
   }
   __syncthreads();
-  block = m.block;
-  off = m.off;
-}
-
-// Blocks before each sequence, and the tiles of one head; by the whole CTA.
-template <int BM, int THREADS>
-__device__ __forceinline__ long long measure_line(const AttnParams& p, PlanMemory& m) {
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x;
-    int before = 0;
-    for (int s0 = 0; s0 < p.c.n_seqs; s0 += 32) {
-      const int s = s0 + lane;
-      int n = 0;
-      if (s < p.c.n_seqs) {
-        const int rows = get_seq(p, s).nq * p.group;
-        if (rows > p.row_min && rows <= p.row_max) n = (rows + BM - 1) / BM;
-      }
-      int sum = n;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, sum, d);
-        if (lane >= d) sum += o;
-      }
-      if (s < p.c.n_seqs) m.prefix[s] = before + sum - n;
-      before += __shfl_sync(~0u, sum, 31);
-    }
-    if (lane == 0) m.prefix[p.c.n_seqs] = before;
-  }
-  __syncthreads();
-  const int blocks = m.prefix[p.c.n_seqs];
-  long long n = 0, unused;
-  for (int b = threadIdx.x; b < blocks; b += THREADS) n += make_item<BM>(p, m.prefix, 0, b).tiles;
-  return block_scan<THREADS>(n, m.sums, unused);
-}
-
-__device__ __forceinline__ long long stretch_begin(const AttnParams& p, long long all, int cta) { return all * cta / p.ctas; }
-
-template <int BM, int THREADS>
-__device__ __forceinline__ Stretch plan(const AttnParams& p, PlanMemory& m) {
-  Stretch st;
-  const long long per_head = measure_line<BM, THREADS>(p, m), all = per_head * p.c.kv_heads;
-  st.blocks = m.prefix[p.c.n_seqs];
-  const long long at = stretch_begin(p, all, blockIdx.x);
-  st.count = stretch_begin(p, all, blockIdx.x + 1) - at;
-  st.head = st.block = st.off = 0;
-  if (st.count > 0) find_place<BM, THREADS>(p, m, per_head, at, st.head, st.block, st.off);
+  st.block = m.block;
+  st.off = m.off;
   return st;
+}
+
+// The item that the stretch stands at begins here and goes on behind the stretch: its parts.  (Stretch c begins at all * c / ctas rounded down, so
+// tile x is in stretch ((x + 1) * ctas - 1) / all rounded down.)
+__device__ __forceinline__ Cut cut_here(const Stretch& st, const Item& it) {
+  Cut c = {};
+  c.q_base = it.s.q_base;
+  c.r0 = it.r0;
+  c.rows = it.rows;
+  c.head = it.head;
+  c.parts = (int)divide((st.at + it.tiles) * st.ctas - 1, st.all) - (int)blockIdx.x + 1;
+  return c;
+}
+__device__ __forceinline__ void next_item(Stretch& st, int n) {
+  st.at += n;
+  st.count -= n;
+  st.off = 0;
+  if (++st.block == st.blocks) {
+    st.block = 0;
+    ++st.head;
+  }
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -232,8 +256,8 @@ __device__ __forceinline__ float natural_lse(float m, float l, float c) {
 }
 
 // kernels (a file each)
-cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, cudaStream_t st);
-cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, cudaStream_t st);
+cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
+cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
 constexpr int FEW_ROWS = 16, CHUNK_ROWS = 256;      // rows of their items
 constexpr int FEW_CTAS = 2;                         // of an SM
 constexpr int FEW_LIMIT = 32;                       // rows up to which a sequence goes to the kernel for few

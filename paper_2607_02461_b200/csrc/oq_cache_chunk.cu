@@ -13,7 +13,8 @@
 //
 //   2 x 4 warps              softmax, one thread per row: the item's queries to shared memory in fp16; then S from tensor memory, mask, maximum,
 //                            powers, P (fp16) over S
-//   4 warps                  convert: K and V tiles of 128 keys from the pages to a ring of shared-memory slots, loads one tile ahead
+//   load warp                finds the pages and requests their parts of a tile as they are, by bulk copies into a ring of stages
+//   4 warps                  convert: from a stage, 128 keys of K or V, to a slot of a second ring, fp16 in the tensor cores' order
 //   2 mma warps              one per 128 rows: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t from tensor memory
 //
 // Of a tile's 256 columns of tensor memory S has 128, over which P lies, and O the rest.  The mma warp issues P_t V of a key tile before the next
@@ -28,21 +29,26 @@ namespace cache {
 namespace chunk {
 
 constexpr int THREADS = 512;
-// Registers: 512 threads start with 128 each.  A group of four warps each: softmax 200, 200, convert 72, mma 40.
-constexpr int CONVERT_WARP = 8, MMA_WARP = 12;
+// Registers: 512 threads start with 128 each.  What a group of four warps takes more than that, others have to give up first: the shares' sum is bounded.
+constexpr int SOFTMAX_REGS = 200, CONVERT_REGS = 72, MMA_REGS = 40;
+static_assert(2 * SOFTMAX_REGS + CONVERT_REGS + MMA_REGS <= 4 * 128, "setmaxnreg.inc would wait for ever");
+constexpr int CONVERT_WARP = 8, MMA_WARP = 12, LOAD_WARP = 14;
 constexpr int BM = 128;                            // rows of a query tile, of which a CTA has two
-constexpr int SLOTS = 4;
+constexpr int SLOTS = 3, STAGES = 3;
+constexpr int PIECE = 16, PIECES = BN / PIECE;     // keys that lie in one page whatever its size
 constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;
 constexpr float SLACK = 8.f;
-enum { W_Q = 50, W_KV = 51, W_KVFREE = 52, W_S = 53, W_P = 54, W_O = 55 };
+enum { W_Q = 50, W_KV = 51, W_KVFREE = 52, W_S = 53, W_P = 54, W_O = 55, W_RAW = 56, W_RAWFREE = 57 };
 static_assert(CHUNK_ROWS == 2 * BM, "two query tiles an item");
 
-template <int D>
+template <int KIND, int D>
 struct Shape {
+  using F = Format<KIND, D>;
   static constexpr uint32_t ATOMS = D / 64;
   static constexpr uint32_t Q_ATOM = BM * 128, KV_ATOM = BN * 128;      // 64 coordinates of all rows, 128 bytes each
   static constexpr uint32_t Q_TILE = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
-  static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE;
+  static constexpr uint32_t RAW_SCALES = BN * F::ROW, RAW = RAW_SCALES + BN * F::GROUPS;      // a stage: rows, then their scales
+  static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE + STAGES * RAW;
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -51,9 +57,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 // two fp32 lanes in one instruction
-__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
-  asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n mov.b64 c, {%5, %5};\n fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}"
-      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+__device__ __forceinline__ uint64_t twice(float x) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(x));
+  return d;
+}
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, uint64_t b, uint64_t c) {
+  asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n fma.rn.f32x2 d, a, %4, %5;\n mov.b64 {%0, %1}, d;\n}" : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "l"(b), "l"(c));
 }
 __device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
   asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n mov.b64 d, {%0, %1};\n add.rn.f32x2 d, d, a;\n mov.b64 {%0, %1}, d;\n}"
@@ -66,35 +76,58 @@ __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uin
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// A convert warp's share of a tile: 32 keys, 16 bytes of a row a lane.  The lanes are dealt so that the 8 of them whose stores go together hit 8
-// different 16-byte units of the 128-byte swizzle (unit ^ row % 8): pieces of 2 units (e4m3) of two rows, of 4 units (e2m1) of four.
+__device__ __forceinline__ uint4 load_row16(const __nv_bfloat16* p) {        // (volatile: requested together)
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {         // 32 bytes: a whole sector
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void load_shared16(uint32_t at, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t load_shared1(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// A convert warp's share of a tile: 32 keys, 16 bytes of a row a lane.  The lanes are dealt so that 8 of them, whose accesses go together, read 128
+// bytes that lie in different banks and hit 8 different 16-byte units of the 128-byte swizzle (unit ^ row % 8) when they store: pieces of 2 units
+// (e4m3) of two rows, of 4 units (e2m1) of four.
 template <int KIND, int D>
 struct Share {
   using F = Format<KIND, D>;
   static constexpr int LPR = F::ROW / 16, RPI = 32 / LPR, ITERS = LPR;         // lanes a row, rows at a time, times
   static constexpr int UNITS = 16 / KIND;                                     // 16-byte units of fp16 that a lane's 16 bytes become
   __device__ static __forceinline__ int piece(int lane) {
-    if (KIND == 8) return D == 128 ? (lane & 3) + 4 * ((lane >> 3) & 1) : lane & 3;
-    return D == 128 ? (lane & 1) + 2 * ((lane >> 3) & 1) : lane & 1;
+    if (KIND == 8) return D == 128 ? lane & 7 : lane & 3;                      // (rows of 128 bytes: the halves of two rows, see row)
+    return D == 128 ? (lane & 1) + 2 * ((lane >> 2) & 1) : lane & 1;           // (rows of 64: halves of four)
   }
   __device__ static __forceinline__ int row(int lane) {
-    if (KIND == 8) return D == 128 ? ((lane >> 2) & 1) + 2 * (lane >> 4) : lane >> 2;
-    return D == 128 ? ((lane >> 1) & 3) + 4 * (lane >> 4) : lane >> 1;
+    if (KIND == 8) return D == 128 ? 2 * (lane >> 4) + (((lane >> 2) ^ (lane >> 3)) & 1) : lane >> 2;
+    return D == 128 ? 4 * (lane >> 4) + (((lane >> 1) & 1) | (((lane >> 2) ^ (lane >> 3)) & 1) << 1) : lane >> 1;
   }
 };
 
 template <int KIND, int D>
 __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant__ AttnParams p) {
-  using S = Shape<D>;
+  using S = Shape<KIND, D>;
   using F = Format<KIND, D>;
   extern __shared__ unsigned char smem_dyn[];
-  __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS];
-  __shared__ PlanMemory pm;
+  __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS + 2 * STAGES];
+  __shared__ Plan pm;
+  __shared__ int raw_keys[STAGES];        // what a stage holds: number of keys that exist, and the pieces of 16 whose page is missing in bits 8 .. 15
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-  const uint32_t smem_q = smem, smem_kv = smem + 2 * S::Q_TILE;
+  const uint32_t smem_q = smem, smem_kv = smem + 2 * S::Q_TILE, smem_raw = smem_kv + SLOTS * S::KV_TILE;
   const uint32_t b0 = smem_u32(bars);
   auto q_full = [&](int t) { return b0 + 8u * (uint32_t)t; };
   auto s_full = [&](int t) { return b0 + 8u * (uint32_t)(2 + t); };
@@ -103,6 +136,8 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   auto o_done = [&](int t) { return b0 + 8u * (uint32_t)(8 + t); };     // the item's last P V has been added: O may be read
   auto kv_full = [&](int s) { return b0 + 8u * (uint32_t)(10 + s); };
   auto kv_free = [&](int s) { return b0 + 8u * (uint32_t)(10 + SLOTS + s); };
+  auto raw_full = [&](int s) { return b0 + 8u * (uint32_t)(10 + 2 * SLOTS + s); };
+  auto raw_free = [&](int s) { return b0 + 8u * (uint32_t)(10 + 2 * SLOTS + STAGES + s); };
 
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
@@ -115,6 +150,10 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(kv_full(s), 4);
       mbar_init(kv_free(s), 2);           // both mma warps, also when one of them does not use the slot
+    }
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(raw_full(s), 1);
+      mbar_init(raw_free(s), 4);
     }
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -133,17 +172,8 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   const uint32_t tmem = tmem_slot;
   // All roles walk over the same steps: the key tiles of this CTA's items (of the parts of them in its stretch), one after the other.
   auto run_of = [&](const Item& it) { return (int)min((long long)(it.tiles - st.off), st.count); };
-  auto next_item = [&](int n) {
-    st.count -= n;
-    st.off = 0;
-    if (++st.block == st.blocks) {
-      st.block = 0;
-      ++st.head;
-    }
-  };
-
   if (warp < CONVERT_WARP) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     // ------------------------------------------------ softmax ------------------------------------------------
     const int t = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t columns = tmem + ((uint32_t)(quarter * 32) << 16) + 256u * (uint32_t)t;
@@ -162,7 +192,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       bool turns;
       float c;
       {
-        const Item it = make_item<CHUNK_ROWS>(p, pm.prefix, st.head, st.block);
+        const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         rows = min(max(it.rows - t * BM, 0), BM);
         const int r0 = it.r0 + t * BM, last = r0 + max(rows, 1) - 1;
         const int mine = min(r0 + row, last);             // (rows that do not exist stand in for the last one)
@@ -180,21 +210,22 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         if (rows > 0) {
           // the row's queries to fp16 (the products with the last item's are done: its last S has been waited for)
           const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + mine / p.group) * p.ldq + (long long)(it.head * p.group + mine % p.group) * p.hdq;
+          uint4 v[D / 8];
+#pragma unroll
+          for (int x = 0; x < D / 8; ++x) v[x] = load_row16(src + 8 * x);
           uint32_t largest = 0;
 #pragma unroll
           for (int x = 0; x < D / 8; ++x) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(src) + x);
-            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) largest = max(largest, max((u[e] << 16) & 0x7FFFFFFFu, u[e] & 0x7FFF0000u));
           }
           const RowScale rs = row_scale(largest, p.scale_log2);
           c = rs.c;
           const uint32_t to = smem_q + (uint32_t)t * S::Q_TILE + 128u * (uint32_t)row;
-#pragma unroll 4
+#pragma unroll
           for (int x = 0; x < D / 8; ++x) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(src) + x);
-            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
             uint32_t h[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * rs.mul, __uint_as_float(u[e] & 0xFFFF0000u) * rs.mul);
@@ -206,7 +237,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         }
       }
       if (rows == 0) {
-        next_item(tiles);
+        next_item(st, tiles);
         continue;
       }
       const bool idle = quarter * 32 >= rows;              // none of the warp's rows exists
@@ -297,6 +328,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           }
         }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t c2 = twice(c), shift2 = twice(shift);
         // one warp of the two that share a scheduler exponentiates while the other does all else
         if (turns && (t == 1 || j > 0)) turn_wait();
 #pragma unroll
@@ -305,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float x, y;
-            fma2(x, y, __uint_as_float(sr[32 * q + 2 * e]), __uint_as_float(sr[32 * q + 2 * e + 1]), c, shift);
+            fma2(x, y, __uint_as_float(sr[32 * q + 2 * e]), __uint_as_float(sr[32 * q + 2 * e + 1]), c2, shift2);
             x = exp2_fast(x);
             y = exp2_fast(y);
             add2(sum[2 * (e & 1)], sum[2 * (e & 1) + 1], x, y);
@@ -325,7 +357,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       // ------------------------------------------- the item's result -------------------------------------------
       warp_wait(o_done(t), items++ & 1, W_O);
       if (!idle) {
-        const Item it = make_item<CHUNK_ROWS>(p, pm.prefix, st.head, st.block);
+        const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         tc_fence_after();
         const bool mine = row < rows, whole = first == 0 && tiles == it.tiles;
         const int r = it.r0 + t * BM + row, i = it.s.q_base + r / p.group, head = it.head * p.group + r % p.group;
@@ -341,15 +373,19 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(l != 0.f ? __uint_as_float(o[e]) * inv : 0.f);
           if (!mine) continue;
           if (!whole) {
-            uint4* const to = reinterpret_cast<uint4*>(p.part_o + slot_row * D + 32 * q);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 4; ++e) store32(p.part_o + slot_row * D + 32 * q + 8 * e, o + 8 * e);
           } else {
             uint32_t v[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] = pack_bf16(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1]));
+            if (p.wide_out) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst + 32 * q)[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+              for (int e = 0; e < 2; ++e) store32(dst + 32 * q + 16 * e, v + 8 * e);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst + 32 * q)[e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            }
           }
         }
         if (mine) {
@@ -360,114 +396,79 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         }
         tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
       }
-      next_item(tiles);
+      next_item(st, tiles);
     }
   } else if (warp < MMA_WARP) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
     // ------------------------------------------------ convert ------------------------------------------------
     using H = Share<KIND, D>;
-    const int part = warp - CONVERT_WARP, piece = H::piece(lane), my_row = H::row(lane);
-    const int group = piece * (128 / KIND) / 32;
-    uint32_t slot = 0, round = 0;
-    uint32_t raw[H::ITERS][4];
-    uint32_t scale[H::ITERS];
-    // addresses of the present tile's two pieces of 16 keys, and how many keys of this warp's 32 exist
-    const uint8_t *at0 = nullptr, *at1 = nullptr;
-    int exist = 0;
-    const int in_page = (1 << p.c.shift) - 1;
-    auto look_up = [&](int seq, int head, int pos, int nk) {
-      exist = min(max(nk - pos, 0), 32);
-      const int a = exist > 0 ? page_of(p.c, seq, pos) : -1, b = exist > 16 ? page_of(p.c, seq, pos + 16) : -1;
-      at0 = a < 0 ? nullptr : block_of(p.c, a, head);
-      at1 = b < 0 ? nullptr : block_of(p.c, b, head);
-    };
-    auto load = [&](int i, int pos, bool values) {
-      const int r = i * H::RPI + my_row;
-      const uint8_t* const block = r < 16 ? at0 : at1;
-      raw[i][0] = raw[i][1] = raw[i][2] = raw[i][3] = 0u;
-      scale[i] = 127u;
-      if (block && r < exist) {
-        const int at = (pos + r) & in_page;
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(block + (values ? p.c.off_v : 0u) + at * F::ROW + 16 * piece));
-        raw[i][0] = v.x; raw[i][1] = v.y; raw[i][2] = v.z; raw[i][3] = v.w;
-        scale[i] = __ldg(block + (values ? p.c.off_vs : p.c.off_ks) + at * F::GROUPS + group);
-      }
-    };
-    auto convert = [&](int i, bool values) {
-      const int r = i * H::RPI + my_row, e0 = piece * (128 / KIND);
-      const uint32_t f = !values && scale[i] == BROKEN ? 0x7FFF7FFFu : scale_pair(scale[i], scale[i]);
-      const uint32_t to = smem_kv + slot * S::KV_TILE + (uint32_t)(e0 / 64) * S::KV_ATOM + 128u * (uint32_t)(32 * part + r);
-#pragma unroll
-      for (int u = 0; u < H::UNITS; ++u) {
-        uint32_t h[4];
-        if constexpr (KIND == 8) {
-          e4m3_to_f16(raw[i][2 * u], h[0], h[1]);
-          e4m3_to_f16(raw[i][2 * u + 1], h[2], h[3]);
-        } else {
-          e2m1_to_f16(raw[i][u], h[0], h[1], h[2], h[3]);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = mul_f16x2(h[e], f);
-        store16(to + (uint32_t)(((e0 / 8 + u) ^ r) & 7) * 16u, h[0], h[1], h[2], h[3]);
-      }
-    };
-    auto take_slot = [&]() {
+    const int part = warp - CONVERT_WARP, piece = H::piece(lane), my_row = 32 * part + H::row(lane);
+    const int e0 = piece * (128 / KIND);                       // first coordinate
+    const uint32_t from = smem_raw + (uint32_t)(my_row * F::ROW + 16 * piece), from_scale = smem_raw + S::RAW_SCALES + (uint32_t)(my_row * F::GROUPS + e0 / 32);
+    const uint32_t to = smem_kv + (uint32_t)(e0 / 64) * S::KV_ATOM + 128u * (uint32_t)my_row;
+    uint32_t slot = 0, round = 0, stage = 0, raw_round = 0;
+    auto convert = [&](bool values) {
       if (round > 0) mbar_spin(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
+      mbar_spin(raw_full(stage), raw_round & 1, &abort_flag, p.status, W_RAW);
       __syncwarp();
-    };
-    auto give_slot = [&]() {
+      // (all of a tile's loads first: one after the other with the stores, each would be waited for)
+      uint32_t raws[H::ITERS][4], scales[H::ITERS];
+#pragma unroll
+      for (int i = 0; i < H::ITERS; ++i) {
+        load_shared16(from + stage * S::RAW + (uint32_t)(i * H::RPI * F::ROW), raws[i]);
+        scales[i] = load_shared1(from_scale + stage * S::RAW + (uint32_t)(i * H::RPI * F::GROUPS));
+      }
+      const int keys = raw_keys[stage];
+      if (keys != BN) {                              // some keys do not exist: zeros, whatever lies in their places
+#pragma unroll
+        for (int i = 0; i < H::ITERS; ++i) {
+          const int r = my_row + i * H::RPI;
+          if (r >= (keys & 255) || ((keys >> (8 + r / PIECE)) & 1)) {
+            raws[i][0] = raws[i][1] = raws[i][2] = raws[i][3] = 0u;
+            scales[i] = 127u;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < H::ITERS; ++i) {
+        const uint32_t(&raw)[4] = raws[i];
+        const uint32_t scale = scales[i];
+        const uint32_t f = !values && scale == BROKEN ? 0x7FFF7FFFu : scale_pair(scale, scale);
+#pragma unroll
+        for (int u = 0; u < H::UNITS; ++u) {
+          uint32_t h[4];
+          if constexpr (KIND == 8) {
+            e4m3_to_f16(raw[2 * u], h[0], h[1]);
+            e4m3_to_f16(raw[2 * u + 1], h[2], h[3]);
+          } else {
+            e2m1_to_f16(raw[u], h[0], h[1], h[2], h[3]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = mul_f16x2(h[e], f);
+          store16(to + slot * S::KV_TILE + (uint32_t)(i * H::RPI * 128) + (uint32_t)(((e0 / 8 + u) ^ (my_row + i * H::RPI)) & 7) * 16u, h[0], h[1], h[2], h[3]);
+        }
+      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(kv_full(slot));
+      if (lane == 0) {
+        mbar_arrive(raw_free(stage));
+        mbar_arrive(kv_full(slot));
+      }
       if (++slot == SLOTS) {
         slot = 0;
         ++round;
       }
+      if (++stage == STAGES) {
+        stage = 0;
+        ++raw_round;
+      }
     };
-    bool begun = false;
-    Item it;
-    int n = 0, j = 0, pos = 0;
-    auto enter = [&]() {
-      it = make_item<CHUNK_ROWS>(p, pm.prefix, st.head, st.block);
-      n = run_of(it);
-      j = 0;
-    };
-    if (st.count > 0) {
-      enter();
-      begun = true;
-      pos = it.key0(st.off) + 32 * part;
-      look_up(it.seq, it.head, pos, it.s.nk);
-#pragma unroll
-      for (int i = 0; i < H::ITERS; ++i) load(i, pos, false);
-    }
-    while (begun) {
-      take_slot();
-#pragma unroll
-      for (int i = 0; i < H::ITERS; ++i) {
-        convert(i, false);
-        load(i, pos, true);
-      }
-      give_slot();
-      // the next step
-      if (++j == n) {
-        next_item(n);
-        if (st.count > 0) enter(); else begun = false;
-      }
-      if (begun) {
-        pos = it.key0(st.off + j) + 32 * part;
-        look_up(it.seq, it.head, pos, it.s.nk);
-      }
-      take_slot();
-#pragma unroll
-      for (int i = 0; i < H::ITERS; ++i) {
-        convert(i, true);
-        if (begun) load(i, pos, false);
-      }
-      give_slot();
-      if (abort_flag) break;
+    for (long long n = st.count; n > 0 && !abort_flag; --n) {
+      convert(false);
+      convert(true);
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
     if (warp < MMA_WARP + 2) {
       const int t = warp - MMA_WARP;
       const uint32_t leader = elect_leader();       // (the whole warp runs this, one lane issues)
@@ -525,7 +526,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       int n = 0, j = 0;
       bool active = false, have = st.count > 0;
       auto enter = [&]() {
-        const Item it = make_item<CHUNK_ROWS>(p, pm.prefix, st.head, st.block);
+        const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         n = run_of(it);
         j = 0;
         active = it.rows > t * BM;
@@ -537,11 +538,75 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       while (have && !abort_flag) {
         do_o(active, j == 0, j + 1 == n);
         if (++j == n) {
-          next_item(n);
+          next_item(st, n);
           have = st.count > 0;
           if (have) enter();
         }
         if (have) do_s(active, j == 0);
+      }
+    } else if (warp == LOAD_WARP) {
+      // lanes 0 .. 7: a piece of 16 keys each; the first piece of a page's part of the tile requests all of it
+      const int run = min(PIECES, 1 << (p.c.shift - 4));       // pieces of the tile that lie in one page
+      uint32_t stage = 0, round = 0;
+      Item it;
+      int n = 0, j = 0, pos = 0, page = -1;
+      auto look_up = [&]() {
+        pos = it.key0(st.off + j) + PIECE * lane;
+        page = lane < PIECES && pos < it.s.nk ? page_of(p.c, it.seq, pos) : -1;
+      };
+      if (lane == 0 && p.cuts) p.cuts[blockIdx.x] = Cut{};
+      auto enter = [&]() {
+        it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
+        n = run_of(it);
+        j = 0;
+        if (lane == 0 && st.off == 0 && n < it.tiles) p.cuts[blockIdx.x] = cut_here(st, it);
+      };
+      bool have = st.count > 0;
+      if (have) {
+        enter();
+        look_up();
+      }
+      while (have && !abort_flag) {
+        const uint32_t there = __ballot_sync(~0u, page >= 0);
+        const int exist = min(it.s.nk - it.key0(st.off + j), BN), at = pos & ((1 << p.c.shift) - 1);
+        const bool mine = page >= 0 && lane % run == 0;
+        const uint32_t keys = (uint32_t)(min(PIECES - lane, run) * PIECE);
+        const uint8_t* const block = mine ? block_of(p.c, page, it.head) : nullptr;
+        // pieces of a page that lie behind the sequence's end come along: the page has room for them
+        const uint32_t pieces = (uint32_t)__reduce_add_sync(~0u, mine ? keys : 0u);
+        const int first_piece = lane;
+        // the next step's pages, while the copies are waited for
+        if (++j == n) {
+          next_item(st, n);
+          have = st.count > 0;
+          if (have) enter();
+        }
+        if (have) look_up();
+#pragma unroll 1
+        for (int v = 0; v < 2; ++v) {
+          if (round > 0) mbar_wait(raw_free(stage), (round - 1) & 1, &abort_flag, p.status, W_RAWFREE);
+          __syncwarp();
+          if (lane == 0) {
+            raw_keys[stage] = exist | (int)((~there & 255u) << 8);
+            mbar_expect_tx(raw_full(stage), pieces * (F::ROW + F::GROUPS));
+          }
+          __syncwarp();
+          if (mine) {
+            const uint32_t dst = smem_raw + stage * S::RAW;
+            bulk_load(dst + (uint32_t)(first_piece * PIECE * F::ROW), block + (v ? p.c.off_v : 0u) + at * F::ROW, keys * F::ROW, raw_full(stage));
+            bulk_load(dst + S::RAW_SCALES + (uint32_t)(first_piece * PIECE * F::GROUPS), block + (v ? p.c.off_vs : p.c.off_ks) + at * F::GROUPS, keys * F::GROUPS,
+                      raw_full(stage));
+          }
+          if (++stage == STAGES) {
+            stage = 0;
+            ++round;
+          }
+        }
+      }
+      // copies still in flight end before the CTA does (after an abort nobody else waits for them)
+      for (uint32_t s = 0; s < STAGES; ++s) {
+        const uint32_t fills = round + (s < stage ? 1u : 0u);
+        for (int k = 0; fills > 0 && k < (1 << 20) && !mbar_try(raw_full((int)s), (fills - 1) & 1); ++k) {}
       }
     }
   }
@@ -552,18 +617,18 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
 }
 
 template <int KIND, int D>
-cudaError_t go(const AttnParams& p, cudaStream_t st) {
+cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
   // (the attribute belongs to the device that is current, so it is set every time)
-  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<KIND, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D>::SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<KIND, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<KIND, D>::SMEM);
   if (e != cudaSuccess) return e;
-  return launch_dependent(chunk_kernel<KIND, D>, p.ctas, THREADS, Shape<D>::SMEM, st, p);
+  return launch_dependent(chunk_kernel<KIND, D>, ctas, THREADS, Shape<KIND, D>::SMEM, st, p);
 }
 
 }  // namespace chunk
 
-cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, cudaStream_t st) {
-  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? chunk::go<8, 128>(p, st) : chunk::go<8, 64>(p, st);
-  return head_dim == 128 ? chunk::go<4, 128>(p, st) : chunk::go<4, 64>(p, st);
+cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st) {
+  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? chunk::go<8, 128>(p, ctas, st) : chunk::go<8, 64>(p, ctas, st);
+  return head_dim == 128 ? chunk::go<4, 128>(p, ctas, st) : chunk::go<4, 64>(p, ctas, st);
 }
 
 }  // namespace cache

@@ -78,14 +78,15 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
   float* const part = reinterpret_cast<float*>(smem);                     // [WARPS][BM][D]
   __shared__ __align__(16) uint16_t q_s[BM * QP];
   __shared__ float c_s[BM], m_s[WARPS][BM], l_s[WARPS][BM];
-  __shared__ PlanMemory pm;
+  __shared__ Plan pm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   Stretch st = plan<BM, THREADS>(p, pm);
+  if (threadIdx.x == 0 && p.cuts) p.cuts[blockIdx.x] = Cut{};
 
   while (st.count > 0) {
-    const Item it = make_item<BM>(p, pm.prefix, st.head, st.block);
+    const Item it = make_item<BM>(p, pm, st.head, st.block);
     const int first = st.off, end = (int)min((long long)it.tiles, st.off + st.count);
     // ------------------------------------------------ queries ------------------------------------------------
     for (int r = warp; r < BM; r += WARPS) {
@@ -373,30 +374,26 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         if (lane == 0) p.part_ml[slot * BM + r] = make_float4(top, total, c_s[r], 0.f);
       }
     }
+    if (threadIdx.x == 0 && first == 0 && !whole) p.cuts[blockIdx.x] = cut_here(st, it);
     __syncthreads();
-    st.count -= end - first;
-    st.off = 0;
-    if (++st.block == st.blocks) {
-      st.block = 0;
-      ++st.head;
-    }
+    next_item(st, end - first);
   }
 }
 
 template <int KIND, int D, int NT>
-cudaError_t go(const AttnParams& p, cudaStream_t st) {
+cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
   const size_t smem = (size_t)WARPS * 8 * NT * D * sizeof(float);
   // (the attribute belongs to the device that is current, so it is set every time)
   const cudaError_t e = cudaFuncSetAttribute(few_kernel<KIND, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(few_kernel<KIND, D, NT>, p.ctas, THREADS, smem, st, p);
+  return launch_dependent(few_kernel<KIND, D, NT>, ctas, THREADS, smem, st, p);
 }
 
 }  // namespace few
 
-cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, cudaStream_t st) {
-  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 2>(p, st) : few::go<8, 64, 2>(p, st);
-  return head_dim == 128 ? few::go<4, 128, 2>(p, st) : few::go<4, 64, 2>(p, st);
+cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st) {
+  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 2>(p, ctas, st) : few::go<8, 64, 2>(p, ctas, st);
+  return head_dim == 128 ? few::go<4, 128, 2>(p, ctas, st) : few::go<4, 64, 2>(p, ctas, st);
 }
 
 }  // namespace cache
