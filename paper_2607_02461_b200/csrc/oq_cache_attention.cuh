@@ -31,6 +31,7 @@ struct AttnParams {
   float* part_o;                           // [2 * CTAs][BM][D]: weights that add up to one
   const int* q_start;                      // n_seqs + 1, or NULL: one sequence
   int total_q, group;
+  uint32_t group_mul, group_shift;         // row / group = (mulhi(row, group_mul) + row) >> group_shift, for rows below 2^31
   int row_min, row_max;                    // this kernel takes the sequences with row_min < rows <= row_max
   int left, right, sinks;
   float scale, scale_log2;
@@ -56,6 +57,8 @@ __device__ __forceinline__ Seq get_seq(const AttnParams& p, int s) {
   q.nk = seq_len(p.c, s);
   return q;
 }
+
+__device__ __forceinline__ int token_of(const AttnParams& p, int row) { return (int)((__umulhi((uint32_t)row, p.group_mul) + (uint32_t)row) >> p.group_shift); }
 
 struct Item {
   Seq s;
@@ -91,8 +94,8 @@ __device__ __forceinline__ Item make_item(const AttnParams& p, const Plan& m, in
   it.s = m.seq[s];
   it.r0 = BM * (block - m.prefix[s]);
   it.rows = min(BM, it.s.nq * p.group - it.r0);
-  it.hi = row_hi(p, it.s, (it.r0 + it.rows - 1) / p.group);
-  it.lo = row_lo(p, it.s, it.r0 / p.group);
+  it.hi = row_hi(p, it.s, token_of(p, it.r0 + it.rows - 1));
+  it.lo = row_lo(p, it.s, token_of(p, it.r0));
   it.n_sink = it.win0 = 0;
   it.tiles = 1;
   if (it.hi >= 0) {

@@ -34,7 +34,6 @@ constexpr int SOFTMAX_REGS = 200, CONVERT_REGS = 72, MMA_REGS = 40;
 static_assert(2 * SOFTMAX_REGS + CONVERT_REGS + MMA_REGS <= 4 * 128, "setmaxnreg.inc would wait for ever");
 constexpr int CONVERT_WARP = 8, MMA_WARP = 12, LOAD_WARP = 14;
 constexpr int BM = 128;                            // rows of a query tile, of which a CTA has two
-constexpr int SLOTS = 3, STAGES = 3;
 constexpr int PIECE = 16, PIECES = BN / PIECE;     // keys that lie in one page whatever its size
 constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;
 constexpr float SLACK = 8.f;
@@ -47,6 +46,7 @@ struct Shape {
   static constexpr uint32_t ATOMS = D / 64;
   static constexpr uint32_t Q_ATOM = BM * 128, KV_ATOM = BN * 128;      // 64 coordinates of all rows, 128 bytes each
   static constexpr uint32_t Q_TILE = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
+  static constexpr int STAGES = 3, SLOTS = F::ROW == 128 ? 3 : 4;        // (a fourth slot where it fits)
   static constexpr uint32_t RAW_SCALES = BN * F::ROW, RAW = RAW_SCALES + BN * F::GROUPS;      // a stage: rows, then their scales
   static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE + STAGES * RAW;
 };
@@ -115,10 +115,42 @@ struct Share {
   }
 };
 
+// A thread's row of the item's query tile t to shared memory in fp16; returns its factor c.  (A function, as two places want it: straight-line
+// code that runs once an item comes from far away each time.)
+template <int D>
+__device__ __noinline__ float prepare_row(const AttnParams& p, const Item& it, int t, int row, uint32_t to, uint32_t atom) {
+  const int r = min(it.r0 + t * BM + row, it.r0 + it.rows - 1), i = token_of(p, r);      // (rows that do not exist stand in for the last one)
+  const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + i) * p.ldq + (long long)(it.head * p.group + r - i * p.group) * p.hdq;
+  uint4 v[D / 8];
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) v[x] = load_row16(src + 8 * x);
+  uint32_t largest = 0;
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) largest = max(largest, max((u[e] << 16) & 0x7FFFFFFFu, u[e] & 0x7FFF0000u));
+  }
+  const RowScale rs = row_scale(largest, p.scale_log2);
+  to += 128u * (uint32_t)row;
+#pragma unroll
+  for (int x = 0; x < D / 8; ++x) {
+    const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+    uint32_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * rs.mul, __uint_as_float(u[e] & 0xFFFF0000u) * rs.mul);
+    store16(to + (uint32_t)(x >> 3) * atom + (uint32_t)((x ^ row) & 7) * 16u, h[0], h[1], h[2], h[3]);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  return rs.c;
+}
+
 template <int KIND, int D>
 __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant__ AttnParams p) {
   using S = Shape<KIND, D>;
   using F = Format<KIND, D>;
+  constexpr int SLOTS = S::SLOTS, STAGES = S::STAGES;
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS + 2 * STAGES];
   __shared__ Plan pm;
@@ -187,19 +219,29 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
     // its loops early, not even when a wait has given up.)
     auto turn_wait = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + 2 * quarter + t) : "memory"); };
     auto turn_pass = [&]() { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 2 * quarter - t) : "memory"); };
+    // The queries of an item are prepared while the tensor cores are at the end of the one before it: its products with Q are done once its
+    // last S has been waited for.
+    auto prepare = [&](const Stretch& at) {
+      const Item it = make_item<CHUNK_ROWS>(p, pm, at.head, at.block);
+      if (it.rows <= t * BM) return 0.f;
+      const float c = prepare_row<D>(p, it, t, row, smem_q + (uint32_t)t * S::Q_TILE, S::Q_ATOM);
+      if (lane == 0) mbar_arrive(q_full(t));
+      return c;
+    };
+    float c_next = st.count > 0 ? prepare(st) : 0.f;
     while (st.count > 0) {
       int rows, first, hi, lo, full_hi, full_lo, tiles, n_sink, skipped, seq, nk;
       bool turns;
-      float c;
+      float c = c_next;
       {
         const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         rows = min(max(it.rows - t * BM, 0), BM);
         const int r0 = it.r0 + t * BM, last = r0 + max(rows, 1) - 1;
         const int mine = min(r0 + row, last);             // (rows that do not exist stand in for the last one)
-        hi = row_hi(p, it.s, mine / p.group);
-        lo = row_lo(p, it.s, mine / p.group);
-        full_hi = row_hi(p, it.s, r0 / p.group);          // what every row of the tile sees
-        full_lo = row_lo(p, it.s, last / p.group);
+        hi = row_hi(p, it.s, token_of(p, mine));
+        lo = row_lo(p, it.s, token_of(p, mine));
+        full_hi = row_hi(p, it.s, token_of(p, r0));       // what every row of the tile sees
+        full_lo = row_lo(p, it.s, token_of(p, last));
         first = st.off;
         tiles = run_of(it);
         n_sink = it.n_sink - first;                       // step j: key tile first + j, with a gap after the sinks
@@ -207,37 +249,12 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         turns = it.rows - BM > quarter * 32;              // both warps have rows (tile 0 is full where tile 1 has any)
         seq = it.seq;
         nk = it.s.nk;
-        if (rows > 0) {
-          // the row's queries to fp16 (the products with the last item's are done: its last S has been waited for)
-          const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + mine / p.group) * p.ldq + (long long)(it.head * p.group + mine % p.group) * p.hdq;
-          uint4 v[D / 8];
-#pragma unroll
-          for (int x = 0; x < D / 8; ++x) v[x] = load_row16(src + 8 * x);
-          uint32_t largest = 0;
-#pragma unroll
-          for (int x = 0; x < D / 8; ++x) {
-            const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) largest = max(largest, max((u[e] << 16) & 0x7FFFFFFFu, u[e] & 0x7FFF0000u));
-          }
-          const RowScale rs = row_scale(largest, p.scale_log2);
-          c = rs.c;
-          const uint32_t to = smem_q + (uint32_t)t * S::Q_TILE + 128u * (uint32_t)row;
-#pragma unroll
-          for (int x = 0; x < D / 8; ++x) {
-            const uint32_t u[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * rs.mul, __uint_as_float(u[e] & 0xFFFF0000u) * rs.mul);
-            store16(to + (uint32_t)(x >> 3) * S::Q_ATOM + (uint32_t)((x ^ row) & 7) * 16u, h[0], h[1], h[2], h[3]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(q_full(t));
-        }
       }
+      Stretch next = st;
+      next_item(next, tiles);
       if (rows == 0) {
-        next_item(st, tiles);
+        if (next.count > 0) c_next = prepare(next);
+        st = next;
         continue;
       }
       const bool idle = quarter * 32 >= rows;              // none of the warp's rows exists
@@ -354,13 +371,14 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
+      if (next.count > 0) c_next = prepare(next);
       // ------------------------------------------- the item's result -------------------------------------------
       warp_wait(o_done(t), items++ & 1, W_O);
       if (!idle) {
         const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         tc_fence_after();
         const bool mine = row < rows, whole = first == 0 && tiles == it.tiles;
-        const int r = it.r0 + t * BM + row, i = it.s.q_base + r / p.group, head = it.head * p.group + r % p.group;
+        const int r = it.r0 + t * BM + row, tok = token_of(p, r), i = it.s.q_base + tok, head = it.head * p.group + r - tok * p.group;
         const long long slot_row = (2 * (long long)blockIdx.x + (first == 0 ? 1 : 0)) * CHUNK_ROWS + t * BM + row;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         __nv_bfloat16* const dst = p.out + (long long)i * p.ldo + head * p.hdo;
@@ -396,7 +414,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         }
         tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
       }
-      next_item(st, tiles);
+      st = next;
     }
   } else if (warp < MMA_WARP) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));

@@ -97,7 +97,8 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
 #pragma unroll
       for (int e = 0; e < N; ++e) x[e] = 0.f;
       if (r < it.rows) {
-        const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + row / p.group) * p.ldq + (long long)(it.head * p.group + row % p.group) * p.hdq + N * lane;
+        const int i = token_of(p, row);
+        const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + i) * p.ldq + (long long)(it.head * p.group + row - i * p.group) * p.hdq + N * lane;
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
           const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(src + e));
@@ -136,14 +137,14 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int r = 8 * n + 2 * t + e, i = (it.r0 + r) / p.group;
+        const int r = 8 * n + 2 * t + e, i = token_of(p, it.r0 + r);
         c[n][e] = c_s[r];
         m[n][e] = -INFINITY;
         l[n][e] = 0.f;
         hi[n][e] = r < it.rows ? row_hi(p, it.s, i) : -1;
         lo[n][e] = row_lo(p, it.s, i);
       }
-    const int full_hi = row_hi(p, it.s, it.r0 / p.group), full_lo = row_lo(p, it.s, (it.r0 + it.rows - 1) / p.group);     // what every row sees
+    const int full_hi = row_hi(p, it.s, token_of(p, it.r0)), full_lo = row_lo(p, it.s, token_of(p, it.r0 + it.rows - 1));     // what every row sees
     float o[D / 16][NT][4];
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         for (int e = 0; e < N; ++e) acc[e] = fmaf(part[(w * BM + r) * D + N * lane + e], a, acc[e]);
       }
       const float inv = total == 0.f ? 0.f : 1.f / total;
-      const int row = it.r0 + r, i = it.s.q_base + row / p.group, head = it.head * p.group + row % p.group;
+      const int row = it.r0 + r, tok = token_of(p, row), i = it.s.q_base + tok, head = it.head * p.group + row - tok * p.group;
       if (whole) {
         __nv_bfloat16* dst = p.out + (long long)i * p.ldo + head * p.hdo + N * lane;
 #pragma unroll
