@@ -261,7 +261,7 @@ __device__ __forceinline__ float natural_lse(float m, float l, float c) {
 // kernels (a file each)
 cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
 cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
-constexpr int FEW_ROWS = 16, CHUNK_ROWS = 256;      // rows of their items
+constexpr int FEW_ROWS = 8, CHUNK_ROWS = 256;      // rows of their items
 constexpr int FEW_CTAS = 2;                         // of an SM
 constexpr int FEW_LIMIT = 32;                       // rows up to which a sequence goes to the kernel for few
 

@@ -45,6 +45,15 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
   }
 }
 
+template <int N>
+__device__ __forceinline__ uint32_t load_scales(const uint8_t* p) {      // (volatile, as all these: left to itself the compiler moves loads to their use)
+  uint32_t x;
+  if (N == 4) asm volatile("ld.global.u32 %0, [%1];" : "=r"(x) : "l"(p));
+  else if (N == 2) asm volatile("ld.global.u16 %0, [%1];" : "=r"(x) : "l"(p));
+  else asm volatile("ld.global.u8 %0, [%1];" : "=r"(x) : "l"(p));
+  return x;
+}
+
 template <int KIND, int D>
 struct Lane {
   using F = Format<KIND, D>;
@@ -182,8 +191,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
           const int at = key & in_page;
 #pragma unroll
           for (int x = 0; x < L::LOADS; ++x) load_words(block + at * F::ROW + L::coord(x, t) * KIND / 8, k.w[r][x]);
-          k.scale[r] = F::GROUPS == 4 ? *reinterpret_cast<const uint32_t*>(block + p.c.off_ks + 4 * at)
-                                      : (uint32_t)*reinterpret_cast<const uint16_t*>(block + p.c.off_ks + 2 * at);
+          k.scale[r] = load_scales<F::GROUPS>(block + p.c.off_ks + F::GROUPS * at);
         }
       }
     };
@@ -197,7 +205,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         if (block && key < it.s.nk) {
           const int at = key & in_page;
           load_words(block + p.c.off_v + at * F::ROW + g * (F::ROW / 8), v.w[e]);
-          v.scale[e] = block[p.c.off_vs + at * F::GROUPS + g * F::GROUPS / 8];
+          v.scale[e] = load_scales<1>(block + p.c.off_vs + at * F::GROUPS + g * F::GROUPS / 8);
         }
       }
     };
@@ -393,8 +401,8 @@ cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
 }  // namespace few
 
 cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st) {
-  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 2>(p, ctas, st) : few::go<8, 64, 2>(p, ctas, st);
-  return head_dim == 128 ? few::go<4, 128, 2>(p, ctas, st) : few::go<4, 64, 2>(p, ctas, st);
+  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 1>(p, ctas, st) : few::go<8, 64, 1>(p, ctas, st);
+  return head_dim == 128 ? few::go<4, 128, 1>(p, ctas, st) : few::go<4, 64, 1>(p, ctas, st);
 }
 
 }  // namespace cache
