@@ -54,6 +54,12 @@ __device__ __forceinline__ uint32_t load_scales(const uint8_t* p) {      // (vol
   return x;
 }
 
+__device__ __forceinline__ int load_entry(const int* p) {
+  int x;
+  asm volatile("ld.global.b32 %0, [%1];" : "=r"(x) : "l"(p));
+  return x;
+}
+
 template <int KIND, int D>
 struct Lane {
   using F = Format<KIND, D>;
@@ -162,8 +168,12 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[x][n][e] = 0.f;
 
-    // The warp's steps: 16 keys of each tile, where some row may see one of them.
+    // The warp's steps: 16 keys of each tile, where some row may see one of them and their page is there.  The 16 lie in one page, so all of
+    // a step's loads have one address and constants beside it; keys behind the sequence's end are in the page too, and are read (K's scores are
+    // replaced and V's rows cleared).
+    const int in_page = (1 << p.c.shift) - 1;
     int j = first;
+    const int* const table = p.c.table + it.seq * p.c.ld_table;
     auto next_pos = [&]() {
       while (j < end) {
         const int pos = it.key0(j++) + 16 * warp;
@@ -171,52 +181,44 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       }
       return -1;
     };
-    auto block_at = [&](int pos) -> const uint8_t* {
-      const int page = pos < 0 ? -1 : page_of(p.c, it.seq, pos);
-      return page < 0 ? nullptr : block_of(p.c, page, it.head);
-    };
-    const int in_page = (1 << p.c.shift) - 1;
+    auto look_up = [&](int pos) { return pos < 0 ? 0 : load_entry(table + (pos >> p.c.shift)); };
     Keys<KIND, D> k;
     Values<KIND, D> v;
-    auto load_keys = [&](const uint8_t* block, int pos) {
+    const uint32_t k_lane = (uint32_t)(g * F::ROW + L::coord(0, t) * KIND / 8), v_lane = p.c.off_v + (uint32_t)(2 * t * F::ROW + g * (F::ROW / 8));
+    const uint32_t ks_lane = p.c.off_ks + (uint32_t)(g * F::GROUPS), vs_lane = p.c.off_vs + (uint32_t)(2 * t * F::GROUPS + g * F::GROUPS / 8);
+    auto load_keys = [&](const uint8_t* block, int at) {
+      const uint8_t *rows = block + (k_lane + (uint32_t)(at * F::ROW)), *scales = block + (ks_lane + (uint32_t)(at * F::GROUPS));
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int key = pos + g + 8 * r;
-        k.scale[r] = 0x7F7F7F7Fu;
 #pragma unroll
-        for (int x = 0; x < L::LOADS; ++x)
-#pragma unroll
-          for (int w = 0; w < L::KW; ++w) k.w[r][x][w] = 0u;
-        if (block && key < it.s.nk) {
-          const int at = key & in_page;
-#pragma unroll
-          for (int x = 0; x < L::LOADS; ++x) load_words(block + at * F::ROW + L::coord(x, t) * KIND / 8, k.w[r][x]);
-          k.scale[r] = load_scales<F::GROUPS>(block + p.c.off_ks + F::GROUPS * at);
-        }
+        for (int x = 0; x < L::LOADS; ++x) load_words(rows + 8 * r * F::ROW + (L::coord(x, 0) - L::coord(0, 0)) * KIND / 8, k.w[r][x]);
+        k.scale[r] = load_scales<F::GROUPS>(scales + 8 * r * F::GROUPS);
       }
     };
-    auto load_values = [&](const uint8_t* block, int pos) {
+    auto load_values = [&](const uint8_t* block, int at) {
+      const uint8_t *rows = block + (v_lane + (uint32_t)(at * F::ROW)), *scales = block + (vs_lane + (uint32_t)(at * F::GROUPS));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int key = pos + 2 * t + (e & 1) + 8 * (e >> 1);
-        v.scale[e] = 127u;
-#pragma unroll
-        for (int w = 0; w < L::VW; ++w) v.w[e][w] = 0u;
-        if (block && key < it.s.nk) {
-          const int at = key & in_page;
-          load_words(block + p.c.off_v + at * F::ROW + g * (F::ROW / 8), v.w[e]);
-          v.scale[e] = load_scales<1>(block + p.c.off_vs + at * F::GROUPS + g * F::GROUPS / 8);
-        }
+        const int key = (e & 1) + 8 * (e >> 1);
+        load_words(rows + key * F::ROW, v.w[e]);
+        v.scale[e] = load_scales<1>(scales + key * F::GROUPS);
       }
     };
+    // the next step whose page is there, looked up a step before its loads (again where it is not)
+    auto settle = [&](int& pos, int page) -> const uint8_t* {
+      while (pos >= 0 && (unsigned)page >= (unsigned)p.c.n_pages) {
+        pos = next_pos();
+        page = look_up(pos);
+      }
+      return pos < 0 ? nullptr : block_of(p.c, page, it.head);
+    };
     int pos = next_pos();
-    const uint8_t* block = block_at(pos);
+    const uint8_t* block = settle(pos, look_up(pos));
     if (pos >= 0) {
-      load_keys(block, pos);
-      load_values(block, pos);
+      load_keys(block, pos & in_page);
+      load_values(block, pos & in_page);
     }
-    int pos_n = next_pos();
-    const uint8_t* block_n = block_at(pos_n);
+    int pos_n = next_pos(), page_n = look_up(pos_n);
     while (pos >= 0) {
       // ---------------------------------------------- S^T = K Q^T ----------------------------------------------
       float s[NT][4];
@@ -251,15 +253,16 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
             }
         }
       }
-      if (pos_n >= 0) load_keys(block_n, pos_n);
+      const uint8_t* const block_n = settle(pos_n, page_n);
+      if (pos_n >= 0) load_keys(block_n, pos_n & in_page);
       // ------------------------------------------------ softmax ------------------------------------------------
-      if (block == nullptr || !(pos + 15 <= full_hi && (pos >= full_lo || pos + 16 <= p.sinks))) {
+      if (!(pos + 15 <= full_hi && (pos >= full_lo || pos + 16 <= p.sinks))) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = pos + g + 8 * (e >> 1);
-            if (block == nullptr || key > hi[n][e & 1] || (key < lo[n][e & 1] && key >= p.sinks)) s[n][e] = -INFINITY;
+            if (key > hi[n][e & 1] || (key < lo[n][e & 1] && key >= p.sinks)) s[n][e] = -INFINITY;
           }
       }
       bool over = false;
@@ -300,6 +303,15 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         b[n][1] = transpose8(pack_f16(w[2], w[3]));
       }
       // --------------------------------------------- O^T += V^T P^T ---------------------------------------------
+      if (pos + 16 > it.s.nk) {                          // what lies behind the end may be anything
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (pos + 2 * t + (e & 1) + 8 * (e >> 1) >= it.s.nk) {
+            v.scale[e] = 127u;
+#pragma unroll
+            for (int w = 0; w < L::VW; ++w) v.w[e][w] = 0u;
+          }
+      }
       const uint32_t f0 = scale_pair(v.scale[0], v.scale[1]), f1 = scale_pair(v.scale[2], v.scale[3]);
 #pragma unroll
       for (int w = 0; w < L::VW; ++w) {
@@ -328,11 +340,10 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
           for (int n = 0; n < NT; ++n)
             mma(o[w * (L::PER_WORD / 2) + e][n], a[0][2 * e], a[0][2 * e + 1], a[1][2 * e], a[1][2 * e + 1], b[n][0], b[n][1]);
       }
-      if (pos_n >= 0) load_values(block_n, pos_n);
+      if (pos_n >= 0) load_values(block_n, pos_n & in_page);
       pos = pos_n;
-      block = block_n;
       pos_n = next_pos();
-      block_n = block_at(pos_n);
+      page_n = look_up(pos_n);
     }
     // ----------------------------------------------- the item's result -----------------------------------------------
 #pragma unroll
