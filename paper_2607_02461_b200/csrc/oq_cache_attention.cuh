@@ -118,16 +118,21 @@ __device__ __forceinline__ long long divide(long long a, long long b) {       //
   return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
 
+template <typename T>
+__device__ __forceinline__ T warp_scan(T v) {      // inclusive
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const T o = __shfl_up_sync(~0u, v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
 // Sum over the CTA; `before`: the sum over the threads before this one.
 template <int THREADS>
 __device__ __forceinline__ long long block_scan(long long v, long long* sums, long long& before) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(~0u, x, d);
-    if (lane >= d) x += o;
-  }
+  const long long x = warp_scan(v);
   __syncthreads();
   if (lane == 31) sums[warp] = x;
   __syncthreads();
@@ -141,28 +146,65 @@ __device__ __forceinline__ long long block_scan(long long v, long long* sums, lo
   return total;
 }
 
-// By the whole CTA.
+__device__ __forceinline__ void set_stretch(Stretch& st, long long per_head, int kv_heads) {
+  st.all = per_head * kv_heads;
+  st.ctas = (int)min((long long)gridDim.x, st.all);
+  st.head = st.block = st.off = 0;
+  st.at = st.count = 0;
+  if ((int)blockIdx.x >= st.ctas) return;
+  st.at = divide(st.all * blockIdx.x, st.ctas);
+  st.count = divide(st.all * (blockIdx.x + 1), st.ctas) - st.at;
+  st.head = (int)divide(st.at, per_head);
+}
+
+// By the whole CTA.  Up to 32 sequences and 32 blocks (a step of single tokens, one long chunk) every warp works out for itself: what is waited
+// for is the length of a call's shortest part.
 template <int BM, int THREADS>
 __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   static_assert(THREADS >= MAX_SEQS, "a thread for each sequence");
   Stretch st;
   long long before, n = 0;
-  if ((int)threadIdx.x < p.c.n_seqs) {
-    const Seq s = get_seq(p, threadIdx.x);
-    m.seq[threadIdx.x] = s;
+  const int lane = threadIdx.x & 31;
+  auto blocks_of = [&](const Seq& s) {
     const int rows = s.nq * p.group;
-    if (rows > p.row_min && rows <= p.row_max) n = (rows + BM - 1) / BM;
-  }
-  if (p.c.n_seqs > 1) {
+    return rows > p.row_min && rows <= p.row_max ? (rows + BM - 1) / BM : 0;
+  };
+  if (p.c.n_seqs <= 32) {
+    int mine = 0;
+    if (lane < p.c.n_seqs) {
+      const Seq s = get_seq(p, lane);
+      mine = blocks_of(s);
+      if (threadIdx.x < 32) m.seq[lane] = s;
+    }
+    const int sum = warp_scan(mine);
+    st.blocks = __shfl_sync(~0u, sum, 31);
+    if (threadIdx.x < 32) {
+      m.prefix[lane] = sum - mine;
+      if (lane == 0) m.prefix[32] = st.blocks;
+      if (lane == 0 && p.c.n_seqs < 32) m.prefix[p.c.n_seqs] = st.blocks;
+    }
+    __syncthreads();
+    if (st.blocks <= 32) {
+      const int tiles = lane < st.blocks ? make_item<BM>(p, m, 0, lane).tiles : 0, upto = warp_scan(tiles);
+      const int per_head = __shfl_sync(~0u, upto, 31);
+      set_stretch(st, per_head, p.c.kv_heads);
+      if (st.count == 0) return st;
+      const int r = (int)(st.at - (long long)st.head * per_head);
+      st.block = __popc(__ballot_sync(~0u, upto <= r && lane < st.blocks));
+      st.off = r - __shfl_sync(~0u, upto - tiles, st.block);
+      return st;
+    }
+  } else {
+    if ((int)threadIdx.x < p.c.n_seqs) {
+      const Seq s = get_seq(p, threadIdx.x);
+      m.seq[threadIdx.x] = s;
+      n = blocks_of(s);
+    }
     st.blocks = (int)block_scan<THREADS>(n, m.sums, before);
     if ((int)threadIdx.x < p.c.n_seqs) m.prefix[threadIdx.x] = (int)before;
-  } else if (threadIdx.x == 0) {
-    m.prefix[0] = 0;
-    m.prefix[1] = (int)n;
+    if (threadIdx.x == 0) m.prefix[p.c.n_seqs] = st.blocks;
+    __syncthreads();
   }
-  if (p.c.n_seqs > 1 && threadIdx.x == 0) m.prefix[p.c.n_seqs] = st.blocks;
-  __syncthreads();
-  st.blocks = m.prefix[p.c.n_seqs];
   // tiles of one head; the first round's sums are kept, as there is one round mostly
   n = (int)threadIdx.x < st.blocks ? make_item<BM>(p, m, 0, threadIdx.x).tiles : 0;
   const long long first = block_scan<THREADS>(n, m.sums, before);
@@ -171,14 +213,8 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
     const int b = b0 + threadIdx.x;
     per_head += block_scan<THREADS>(b < st.blocks ? make_item<BM>(p, m, 0, b).tiles : 0, m.sums, unused);
   }
-  st.all = per_head * p.c.kv_heads;
-  st.ctas = (int)min((long long)gridDim.x, st.all);
-  st.head = st.block = st.off = 0;
-  st.at = st.count = 0;
-  if ((int)blockIdx.x >= st.ctas) return st;
-  st.at = divide(st.all * blockIdx.x, st.ctas);
-  st.count = divide(st.all * (blockIdx.x + 1), st.ctas) - st.at;
-  st.head = (int)divide(st.at, per_head);
+  set_stretch(st, per_head, p.c.kv_heads);
+  if (st.count == 0) return st;
   const long long r = st.at - st.head * per_head;
   long long done = 0, total = first;
   for (int b0 = 0;;) {

@@ -103,71 +103,6 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
   while (st.count > 0) {
     const Item it = make_item<BM>(p, pm, st.head, st.block);
     const int first = st.off, end = (int)min((long long)it.tiles, st.off + st.count);
-    // ------------------------------------------------ queries ------------------------------------------------
-    for (int r = warp; r < BM; r += WARPS) {
-      constexpr int N = D / 32;
-      float x[N];
-      uint32_t largest = 0;
-      const int row = it.r0 + r;
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = 0.f;
-      if (r < it.rows) {
-        const int i = token_of(p, row);
-        const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + i) * p.ldq + (long long)(it.head * p.group + row - i * p.group) * p.hdq + N * lane;
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(src + e));
-          x[e] = __uint_as_float(u << 16);
-          x[e + 1] = __uint_as_float(u & 0xFFFF0000u);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < N; ++e) largest = max(largest, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-      largest = __reduce_max_sync(~0u, largest);
-      const RowScale rs = row_scale(largest, p.scale_log2);
-#pragma unroll
-      for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(q_s + r * QP + N * lane + e) = pack_f16(x[e] * rs.mul, x[e + 1] * rs.mul);
-      if (lane == 0) c_s[r] = rs.c;
-    }
-    __syncthreads();
-    // B fragments of Q^T: coordinates in the order in which the lanes hold the keys'
-    uint32_t qf[D / 16][NT][2];
-#pragma unroll
-    for (int x = 0; x < L::LOADS; ++x)
-#pragma unroll
-      for (int w = 0; w < L::KW; ++w)
-#pragma unroll
-        for (int h = 0; h < L::PER_WORD / 4; ++h)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const uint16_t* q = q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h;
-            const int s = (x * L::KW + w) * (L::PER_WORD / 4) + h;
-            qf[s][n][0] = *reinterpret_cast<const uint32_t*>(q);
-            qf[s][n][1] = *reinterpret_cast<const uint32_t*>(q + 2);
-          }
-    // columns of this lane: queries 8 n + 2 t and the next
-    float c[NT][2], m[NT][2], l[NT][2];
-    int hi[NT][2], lo[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = 8 * n + 2 * t + e, i = token_of(p, it.r0 + r);
-        c[n][e] = c_s[r];
-        m[n][e] = -INFINITY;
-        l[n][e] = 0.f;
-        hi[n][e] = r < it.rows ? row_hi(p, it.s, i) : -1;
-        lo[n][e] = row_lo(p, it.s, i);
-      }
-    const int full_hi = row_hi(p, it.s, token_of(p, it.r0)), full_lo = row_lo(p, it.s, token_of(p, it.r0 + it.rows - 1));     // what every row sees
-    float o[D / 16][NT][4];
-#pragma unroll
-    for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][n][e] = 0.f;
-
     // The warp's steps: 16 keys of each tile, where some row may see one of them and their page is there.  The 16 lie in one page, so all of
     // a step's loads have one address and constants beside it; keys behind the sequence's end are in the page too, and are read (K's scores are
     // replaced and V's rows cleared).
@@ -213,12 +148,78 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       return pos < 0 ? nullptr : block_of(p.c, page, it.head);
     };
     int pos = next_pos();
-    const uint8_t* block = settle(pos, look_up(pos));
+    const int page_0 = look_up(pos);
+    // ------------------------------------------------ queries ------------------------------------------------
+    for (int r = warp; r < BM; r += WARPS) {
+      constexpr int N = D / 32;
+      float x[N];
+      uint32_t largest = 0;
+      const int row = it.r0 + r;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = 0.f;
+      if (r < it.rows) {
+        const int i = token_of(p, row);
+        const __nv_bfloat16* src = p.Q + (long long)(it.s.q_base + i) * p.ldq + (long long)(it.head * p.group + row - i * p.group) * p.hdq + N * lane;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(src + e));
+          x[e] = __uint_as_float(u << 16);
+          x[e + 1] = __uint_as_float(u & 0xFFFF0000u);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) largest = max(largest, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+      largest = __reduce_max_sync(~0u, largest);
+      const RowScale rs = row_scale(largest, p.scale_log2);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(q_s + r * QP + N * lane + e) = pack_f16(x[e] * rs.mul, x[e + 1] * rs.mul);
+      if (lane == 0) c_s[r] = rs.c;
+    }
+    const uint8_t* block = settle(pos, page_0);
     if (pos >= 0) {
       load_keys(block, pos & in_page);
       load_values(block, pos & in_page);
     }
     int pos_n = next_pos(), page_n = look_up(pos_n);
+    __syncthreads();
+    // B fragments of Q^T: coordinates in the order in which the lanes hold the keys'
+    uint32_t qf[D / 16][NT][2];
+#pragma unroll
+    for (int x = 0; x < L::LOADS; ++x)
+#pragma unroll
+      for (int w = 0; w < L::KW; ++w)
+#pragma unroll
+        for (int h = 0; h < L::PER_WORD / 4; ++h)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint16_t* q = q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h;
+            const int s = (x * L::KW + w) * (L::PER_WORD / 4) + h;
+            qf[s][n][0] = *reinterpret_cast<const uint32_t*>(q);
+            qf[s][n][1] = *reinterpret_cast<const uint32_t*>(q + 2);
+          }
+    // columns of this lane: queries 8 n + 2 t and the next
+    float c[NT][2], m[NT][2], l[NT][2];
+    int hi[NT][2], lo[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * n + 2 * t + e, i = token_of(p, it.r0 + r);
+        c[n][e] = c_s[r];
+        m[n][e] = -INFINITY;
+        l[n][e] = 0.f;
+        hi[n][e] = r < it.rows ? row_hi(p, it.s, i) : -1;
+        lo[n][e] = row_lo(p, it.s, i);
+      }
+    const int full_hi = row_hi(p, it.s, token_of(p, it.r0)), full_lo = row_lo(p, it.s, token_of(p, it.r0 + it.rows - 1));     // what every row sees
+    float o[D / 16][NT][4];
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][n][e] = 0.f;
+
     while (pos >= 0) {
       // ---------------------------------------------- S^T = K Q^T ----------------------------------------------
       float s[NT][4];
