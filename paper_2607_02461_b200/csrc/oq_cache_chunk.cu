@@ -30,7 +30,7 @@ namespace chunk {
 
 constexpr int THREADS = 512;
 // Registers: 512 threads start with 128 each.  What a group of four warps takes more than that, others have to give up first: the shares' sum is bounded.
-constexpr int SOFTMAX_REGS = 200, CONVERT_REGS = 72, MMA_REGS = 40;
+constexpr int SOFTMAX_REGS = 208, CONVERT_REGS = 48, MMA_REGS = 48;
 static_assert(2 * SOFTMAX_REGS + CONVERT_REGS + MMA_REGS <= 4 * 128, "setmaxnreg.inc would wait for ever");
 constexpr int CONVERT_WARP = 8, MMA_WARP = 12, LOAD_WARP = 14;
 constexpr int BM = 128;                            // rows of a query tile, of which a CTA has two
@@ -425,46 +425,56 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
     const uint32_t from = smem_raw + (uint32_t)(my_row * F::ROW + 16 * piece), from_scale = smem_raw + S::RAW_SCALES + (uint32_t)(my_row * F::GROUPS + e0 / 32);
     const uint32_t to = smem_kv + (uint32_t)(e0 / 64) * S::KV_ATOM + 128u * (uint32_t)my_row;
     uint32_t slot = 0, round = 0, stage = 0, raw_round = 0;
-    auto convert = [&](bool values) {
+    // One short loop for keys and values: the code of all roles together has to stay near the schedulers (unrolled over a whole tile, and once for
+    // each of the two, it cost XX).
+    constexpr int BATCH = H::ITERS < 2 ? H::ITERS : 2;
+    for (long long n = 2 * st.count; n > 0 && !abort_flag; --n) {
+      const uint32_t broken = n & 1 ? 256u : BROKEN;           // (a broken token's keys become NaN, its values stay zeros)
       if (round > 0) mbar_spin(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
       mbar_spin(raw_full(stage), raw_round & 1, &abort_flag, p.status, W_RAW);
       __syncwarp();
-      // (all of a tile's loads first: one after the other with the stores, each would be waited for)
-      uint32_t raws[H::ITERS][4], scales[H::ITERS];
-#pragma unroll
-      for (int i = 0; i < H::ITERS; ++i) {
-        load_shared16(from + stage * S::RAW + (uint32_t)(i * H::RPI * F::ROW), raws[i]);
-        scales[i] = load_shared1(from_scale + stage * S::RAW + (uint32_t)(i * H::RPI * F::GROUPS));
-      }
       const int keys = raw_keys[stage];
-      if (keys != BN) {                              // some keys do not exist: zeros, whatever lies in their places
+      uint32_t src = from + stage * S::RAW, src_scale = from_scale + stage * S::RAW, dst = to + slot * S::KV_TILE;
+      int r = my_row;
+#pragma unroll 1
+      for (int i0 = 0; i0 < H::ITERS; i0 += BATCH) {
+        uint32_t raws[BATCH][4], scales[BATCH];
 #pragma unroll
-        for (int i = 0; i < H::ITERS; ++i) {
-          const int r = my_row + i * H::RPI;
-          if (r >= (keys & 255) || ((keys >> (8 + r / PIECE)) & 1)) {
-            raws[i][0] = raws[i][1] = raws[i][2] = raws[i][3] = 0u;
-            scales[i] = 127u;
+        for (int i = 0; i < BATCH; ++i) {
+          load_shared16(src + (uint32_t)(i * H::RPI * F::ROW), raws[i]);
+          scales[i] = load_shared1(src_scale + (uint32_t)(i * H::RPI * F::GROUPS));
+        }
+        if (keys != BN) {                            // some keys do not exist: zeros, whatever lies in their places
+#pragma unroll
+          for (int i = 0; i < BATCH; ++i) {
+            const int row = r + i * H::RPI;
+            if (row >= (keys & 255) || ((keys >> (8 + row / PIECE)) & 1)) {
+              raws[i][0] = raws[i][1] = raws[i][2] = raws[i][3] = 0u;
+              scales[i] = 127u;
+            }
           }
         }
-      }
 #pragma unroll
-      for (int i = 0; i < H::ITERS; ++i) {
-        const uint32_t(&raw)[4] = raws[i];
-        const uint32_t scale = scales[i];
-        const uint32_t f = !values && scale == BROKEN ? 0x7FFF7FFFu : scale_pair(scale, scale);
+        for (int i = 0; i < BATCH; ++i) {
+          const uint32_t f = scales[i] == broken ? 0x7FFF7FFFu : scale_pair(scales[i], scales[i]);
 #pragma unroll
-        for (int u = 0; u < H::UNITS; ++u) {
-          uint32_t h[4];
-          if constexpr (KIND == 8) {
-            e4m3_to_f16(raw[2 * u], h[0], h[1]);
-            e4m3_to_f16(raw[2 * u + 1], h[2], h[3]);
-          } else {
-            e2m1_to_f16(raw[u], h[0], h[1], h[2], h[3]);
+          for (int u = 0; u < H::UNITS; ++u) {
+            uint32_t h[4];
+            if constexpr (KIND == 8) {
+              e4m3_to_f16(raws[i][2 * u], h[0], h[1]);
+              e4m3_to_f16(raws[i][2 * u + 1], h[2], h[3]);
+            } else {
+              e2m1_to_f16(raws[i][u], h[0], h[1], h[2], h[3]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = mul_f16x2(h[e], f);
+            store16(dst + (uint32_t)(i * H::RPI * 128) + (uint32_t)(((e0 / 8 + u) ^ (r + i * H::RPI)) & 7) * 16u, h[0], h[1], h[2], h[3]);
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = mul_f16x2(h[e], f);
-          store16(to + slot * S::KV_TILE + (uint32_t)(i * H::RPI * 128) + (uint32_t)(((e0 / 8 + u) ^ (my_row + i * H::RPI)) & 7) * 16u, h[0], h[1], h[2], h[3]);
         }
+        src += BATCH * H::RPI * F::ROW;
+        src_scale += BATCH * H::RPI * F::GROUPS;
+        dst += BATCH * H::RPI * 128;
+        r += BATCH * H::RPI;
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -480,10 +490,6 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         stage = 0;
         ++raw_round;
       }
-    };
-    for (long long n = st.count; n > 0 && !abort_flag; --n) {
-      convert(false);
-      convert(true);
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
