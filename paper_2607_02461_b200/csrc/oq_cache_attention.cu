@@ -7,113 +7,87 @@
 namespace oq {
 namespace cache {
 
-constexpr int JOIN_WARPS = 8;
+constexpr int JOIN_WARPS = 8, JOIN_ROWS = JOIN_WARPS;
 
-// CTA (c, y): some rows of the item that CTA c of the kernel before began and did not finish, if there is one.  Parts of a row are weighed by
-// l 2^(c (m - max m)); the first two (there are seldom more of an item of many rows) are requested before their weights are known.  A warp takes ROWS
-// rows at a time; where the item has few, the warps of a row take every so many of its parts each.
-template <int BM, int D, int ROWS>
+// CTA (c, y): rows 8 y .. 8 y + 7 of the item that CTA c of the kernel before began and did not finish, if there is one.  Parts of a row are weighed by
+// l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each; the first ones are requested before their
+// weights are known.  (Four rows a warp, for more bytes on their way: the same time with two parts a row, 2 to 4 us more with eighteen.)
+template <int BM, int D>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) cache_join_kernel(const __grid_constant__ AttnParams p) {
-  constexpr int N = D / 32, AHEAD = ROWS > 1 ? 2 : 4;
-  __shared__ float sums[ROWS > 1 ? 1 : JOIN_WARPS][D];
+  constexpr int N = D / 32, AHEAD = 4;
+  __shared__ float sums[JOIN_WARPS][D];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Cut cut = p.cuts[blockIdx.x];
-  const int row0 = JOIN_WARPS * ROWS * blockIdx.y, rows = min(JOIN_WARPS * ROWS, cut.rows - row0), parts = cut.parts;
+  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, cut.rows - row0), parts = cut.parts;
   if (rows <= 0) return;
-  int per_row = 1;
-  if (ROWS == 1) {
-    per_row = JOIN_WARPS;
-    while (per_row > 1 && per_row * rows > JOIN_WARPS) per_row >>= 1;
-  }
-  const int share = ROWS > 1 ? 0 : warp % per_row, r0 = ROWS > 1 ? warp * ROWS : warp / per_row;
-  const bool any = r0 < rows;
-  auto slot = [&](int i, int r) { return (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * BM + row0 + min(r0 + r, rows - 1); };
-  float v[ROWS][AHEAD][N];
+  int per_row = JOIN_WARPS;
+  while (per_row > 1 && per_row * rows > JOIN_WARPS) per_row >>= 1;
+  const int r = warp / per_row, share = warp % per_row;
+  const bool mine = r < rows;
+  const int row = row0 + (mine ? r : 0);
+  auto slot = [&](int i) { return (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * BM + row; };
+  float v[AHEAD][N];
   auto load = [&](int i0) {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * per_row;
 #pragma unroll
-      for (int s = 0; s < AHEAD; ++s) {
-        const int i = i0 + s * per_row;
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[r][s][e] = i < parts ? p.part_o[slot(i, r) * D + N * lane + e] : 0.f;
-      }
+      for (int e = 0; e < N; ++e) v[s][e] = i < parts ? p.part_o[slot(i) * D + N * lane + e] : 0.f;
+    }
   };
   load(share);
-  float top[ROWS], factor[ROWS], ct[ROWS], inv[ROWS], total[ROWS], acc[ROWS][N];
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    top[r] = -INFINITY;
-    factor[r] = total[r] = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[r][e] = 0.f;
+  float top = -INFINITY, factor = 0.f, total = 0.f;
+  for (int i = lane; i < parts; i += 32) {
+    const float4 ml = p.part_ml[slot(i)];
+    top = fmaxf(top, ml.x);
+    factor = ml.z;
   }
-  for (int i = lane; i < parts; i += 32)
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const float4 ml = p.part_ml[slot(i, r)];
-      top[r] = fmaxf(top[r], ml.x);
-      factor[r] = ml.z;
-    }
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  factor = __shfl_sync(~0u, factor, 0);
+  const float ct = tame(factor, top);
+  auto weight = [&](const float4& ml) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct)); };
+  for (int i = lane; i < parts; i += 32) total += weight(p.part_ml[slot(i)]);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
+  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  float acc[N];
 #pragma unroll
-    for (int d = 16; d; d >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], d));
-    factor[r] = __shfl_sync(~0u, factor[r], 0);
-    ct[r] = tame(factor[r], top[r]);
-  }
-  auto weight = [&](const float4& ml, int r) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top[r] ? 1.f : exp2_fast((ml.x - top[r]) * ct[r])); };
-  for (int i = lane; i < parts; i += 32)
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) total[r] += weight(p.part_ml[slot(i, r)], r);
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) total[r] += __shfl_xor_sync(~0u, total[r], d);
-    inv[r] = total[r] == 0.f ? 0.f : 1.f / total[r];
-  }
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
   for (int i0 = share; i0 < parts; i0 += AHEAD * per_row) {
     if (i0 != share) load(i0);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * per_row;
+      if (i >= parts) continue;
+      const float w = weight(p.part_ml[slot(i)]) * inv;
+      if (w == 0.f) continue;
 #pragma unroll
-      for (int s = 0; s < AHEAD; ++s) {
-        const int i = i0 + s * per_row;
-        if (i >= parts) continue;
-        const float w = weight(p.part_ml[slot(i, r)], r) * inv[r];
-        if (w == 0.f) continue;
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[r][e] = fmaf(w, v[r][s][e], acc[r][e]);
-      }
+      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[s][e], acc[e]);
+    }
   }
-  if (ROWS == 1 && per_row > 1) {
+  if (per_row > 1) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[0][e];
+    for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[e];
     __syncthreads();
-    if (share == 0 && any)
-      for (int w = 1; w < per_row; ++w)
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[0][e] += sums[warp + w][N * lane + e];
   }
-  if (!any || share) return;
+  if (!mine || share) return;
+  for (int w = 1; w < per_row; ++w)
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (r0 + r >= rows) continue;
-    const int q = cut.r0 + row0 + r0 + r, tok = token_of(p, q), i = cut.q_base + tok, qh = cut.head * p.group + q - tok * p.group;
-    __nv_bfloat16* dst = p.out + (long long)i * p.ldo + qh * p.hdo + N * lane;
+    for (int e = 0; e < N; ++e) acc[e] += sums[warp + w][N * lane + e];
+  const int q = cut.r0 + row, tok = token_of(p, q), i = cut.q_base + tok, qh = cut.head * p.group + q - tok * p.group;
+  __nv_bfloat16* dst = p.out + (long long)i * p.ldo + qh * p.hdo + N * lane;
 #pragma unroll
-    for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[r][e], acc[r][e + 1]);
-    if (lane == 0 && p.lse) p.lse[(long long)qh * p.total_q + i] = natural_lse(top[r], total[r], factor[r]);
-  }
+  for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);
+  if (lane == 0 && p.lse) p.lse[(long long)qh * p.total_q + i] = natural_lse(top, total, factor);
 }
 
 template <int BM>
 static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cudaStream_t st) {
-  constexpr int ROWS = BM > 16 ? 4 : 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas, (unsigned)(BM / (JOIN_WARPS * ROWS)));
+  cfg.gridDim = dim3((unsigned)ctas, (unsigned)(BM / JOIN_ROWS));
   cfg.blockDim = dim3(32 * JOIN_WARPS);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -121,7 +95,7 @@ static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cuda
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return head_dim == 128 ? cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 128, ROWS>, p) : cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 64, ROWS>, p);
+  return head_dim == 128 ? cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 128>, p) : cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 64>, p);
 }
 
 static int sm_count() {

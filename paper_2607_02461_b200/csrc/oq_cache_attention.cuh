@@ -299,7 +299,10 @@ cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cu
 cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
 constexpr int FEW_ROWS = 8, CHUNK_ROWS = 256;      // rows of their items
 constexpr int FEW_CTAS = 2;                         // of an SM
-constexpr int FEW_LIMIT = 32;                       // rows up to which a sequence goes to the kernel for few
+// Rows up to which a sequence goes to the kernel for few, which reads the cache once for 8 of them where the other reads it once for 256 but takes
+// longer to begin.  us, kernel for few / for chunks, e4m3: 16384 keys x 40 heads, 8 rows 42 / 91, 16 rows 70 / 91, 24 rows 93 / 92, 32 rows 123 / 93;
+// 4096 keys x 8 heads, 24 rows 18 / 21, 40 rows 20 / 22, 64 rows 24 / 23; 16384 keys x 8 heads, 24 rows 29 / 34, 40 rows 37 / 35, 64 rows 51 / 38.
+constexpr int FEW_LIMIT = 24;
 
 }  // namespace cache
 }  // namespace oq
