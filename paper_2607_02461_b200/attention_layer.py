@@ -3,9 +3,13 @@
     x -> rotate+quantize -> QKV projection -> + low-rank adapters -> q/k norms and rotation by position (in place)
       -> attention -> rotate+quantize -> output projection -> + low-rank adapters
 
-    python -m paper_2607_02461_b200.attention_layer [--shape flux|wan|small] [--adapters 2] [--window 0]
+Where the tokens come in chunks (streamed video, requests that go on), the keys and values of all chunks are held in a PagedCache in 8 or 4
+bits, and attention of a chunk runs over it.
 
-runs a layer of the named shape on synthetic data and prints one JSON line with the time of each step.
+    python -m paper_2607_02461_b200.attention_layer [--shape flux|wan|small] [--adapters 2] [--window 0] [--cache fp8|fp4 [--chunk 1560]]
+
+runs a layer of the named shape on synthetic data and prints one JSON line with the time of each step (with --cache: of a chunk's steps, once
+the cache holds the shape's other tokens).
 """
 import argparse
 import json
@@ -37,6 +41,52 @@ class _Projection:
         return B.oq_qlinear(xq, xs, self.cb_a, self.wq, self.wr, self.cb_w, self.dim)
 
 
+class PagedCache:
+    """Keys and values of one layer for several requests, in 8 or 4 bits, in pages of one pool (see oq_cache_write).  The book-keeping is the
+    host's: extend() and forget() take pages from the pool and give them back, table and lens on the device follow in the next step()."""
+
+    def __init__(self, n_pages, kv_heads, head_dim, requests, max_tokens, page_size=64, kind="fp8", device="cuda"):
+        self.pages = B.oq_cache_alloc(n_pages, page_size, kv_heads, head_dim, kind, device)
+        self.kind, self.page_size, self.max_tokens = kind, page_size, max_tokens
+        self.free = list(range(n_pages - 1, -1, -1))
+        self._table = torch.full((requests, -(-max_tokens // page_size)), -1, dtype=torch.int32)
+        self._lens = torch.zeros(requests, dtype=torch.int32)
+        self.table, self.lens = self._table.to(device), self._lens.to(device)
+
+    def extend(self, new):
+        """Room for new[r] more tokens of each request r."""
+        if len(new) != len(self._lens) or min(new) < 0:
+            raise B.OqError(1, "PagedCache: one number of new tokens for each request")
+        ends = [int(n) + more for n, more in zip(self._lens, new)]
+        if max(ends) > self.max_tokens:
+            raise B.OqError(1, f"PagedCache: a request would have {max(ends)} tokens, more than {self.max_tokens}")
+        wanted = [(r, p) for r, end in enumerate(ends) for p in range(-(-int(self._lens[r]) // self.page_size), -(-end // self.page_size))]
+        if len(wanted) > len(self.free):
+            raise B.OqError(6, f"PagedCache: {len(wanted)} pages wanted, {len(self.free)} free")
+        for r, p in wanted:
+            self._table[r, p] = self.free.pop()
+        self._lens += torch.tensor(new, dtype=torch.int32)
+
+    def forget(self, request, before, keep=0):
+        """Gives back the pages that hold none but tokens keep .. before - 1 of a request: no later window sees them."""
+        before = min(before, int(self._lens[request]))
+        for p in range(-(-keep // self.page_size), before // self.page_size):
+            if self._table[request, p] >= 0:
+                self.free.append(int(self._table[request, p]))
+                self._table[request, p] = -1
+
+    def drop(self, request):
+        """Gives a request's pages back; its place is free for another one."""
+        self.free += [p for p in self._table[request].tolist() if p >= 0]
+        self._table[request] = -1
+        self._lens[request] = 0
+
+    def step(self):
+        """Brings table and lens to the device (the same tensors, so captured calls see them)."""
+        self.table.copy_(self._table)
+        self.lens.copy_(self._lens)
+
+
 class AttentionLayer:
     """w_qkv: CUDA bf16 [(heads + 2 kv_heads) * head_dim, d], w_proj: [d, heads * head_dim]; both are quantized here.
     rope: Rope handle or None.  wq, wk: bf16 norm weights, norm: "head", "row" or "none" (see oq_qk_norm_rope)."""
@@ -47,11 +97,13 @@ class AttentionLayer:
         self.rope, self.wq, self.wk, self.norm = rope, wq, wk, norm
         self.qkv, self.proj = _Projection(w_qkv, bits_a, bits_w, block, seed), _Projection(w_proj, bits_a, bits_w, block, seed)
 
-    def __call__(self, x, pos=None, starts=None, left=-1, right=-1, sinks=0, adapters=None, keep=None):
+    def __call__(self, x, pos=None, starts=None, left=-1, right=-1, sinks=0, adapters=None, keep=None, cache=None):
         """x: CUDA bf16 [T, d], the tokens of one or several requests one after the other; pos: int32 [T, axes];
         starts: int32 [requests + 1] or None (one request); left, right, sinks: the attention window of oq_attention.
         adapters: None or (Adapters of the QKV projection or None, Adapters of the output projection or None, seg_adapter
-        int32 [requests]), which needs starts.  keep: a dict that receives what passes between the steps."""
+        int32 [requests]), which needs starts.  keep: a dict that receives what passes between the steps.
+        cache: a PagedCache with a request for each of x's, extended by x's tokens: these are new tokens, their keys and values are written into it, and
+        they see what it holds of their request (right = 0: causal; left, right, sinks count from a token's place in the whole request)."""
         if adapters is not None and starts is None:
             raise B.OqError(1, "AttentionLayer: adapters go by request, so they need starts")
         t, (h, hk, d) = x.shape[0], (self.heads, self.kv_heads, self.head_dim)
@@ -66,7 +118,11 @@ class AttentionLayer:
             keep["qkv"] = qkv.clone()
         q, k, v = (qkv[:, a * d:b * d].view(t, -1, d) for a, b in ((0, h), (h, h + hk), (h + hk, h + 2 * hk)))
         B.oq_qk_norm_rope(q, k, self.rope, pos, self.wq, self.wk, norm=self.norm, out_q=q, out_k=k)
-        o = B.oq_attention(q, k, v, q_start=starts, k_start=starts, left=left, right=right, sinks=sinks).flatten(1)
+        if cache is None:
+            o = B.oq_attention(q, k, v, q_start=starts, k_start=starts, left=left, right=right, sinks=sinks).flatten(1)
+        else:
+            B.oq_cache_write(cache.pages, k, v, cache.table, cache.lens, starts, kind=cache.kind)
+            o = B.oq_cache_attention(q, cache.pages, cache.table, cache.lens, starts, kind=cache.kind, left=left, right=right, sinks=sinks).flatten(1)
         y = self.proj(o)
         if keep is not None:
             keep.update(q=q, k=k, v=v, o=o, y_shared=y.clone())
@@ -110,6 +166,8 @@ def main():
     ap.add_argument("--shape", choices=sorted(SHAPES), default="flux")
     ap.add_argument("--adapters", type=int, default=2)
     ap.add_argument("--window", type=int, default=0, help="keys seen to the left of a query (0: all)")
+    ap.add_argument("--cache", choices=sorted(B.CACHE_KINDS), help="hold keys and values in a paged cache of this kind; the last tokens come as a chunk")
+    ap.add_argument("--chunk", type=int, default=1560, help="tokens of a chunk, with --cache")
     ap.add_argument("--iters", type=int, default=10)
     a = ap.parse_args()
     layer, x, pos, starts, adapters = make_layer(a.shape, a.adapters)
@@ -128,6 +186,8 @@ def main():
             ts.append(e0.elapsed_time(e1))
         return sorted(ts)[len(ts) // 2]
 
+    if a.cache:
+        return stream(a, layer, x, pos, left, adapters, timed)
     keep = {}
     layer(x, pos, starts, left, -1, 0, adapters, keep)
     q, k, v, qkv, o = (keep[n] for n in ("q", "k", "v", "qkv", "o"))
@@ -141,6 +201,31 @@ def main():
     if adapters:
         line["ms_adapter_qkv"] = timed(lambda: adapters[0].add(x, qkv, starts, adapters[2]))
         line["ms_adapter_proj"] = timed(lambda: adapters[1].add(o, y, starts, adapters[2]))
+    assert B.oq_device_status() == 0
+    print(json.dumps(line))
+
+
+def stream(a, layer, x, pos, left, adapters, timed):
+    """The shape's tokens as one request that comes in chunks: all but the last fill the cache, the last is timed."""
+    total, n = x.shape[0], min(a.chunk, x.shape[0])
+    cache = PagedCache(-(-total // 64), layer.kv_heads, layer.head_dim, 1, total, kind=a.cache)
+    if adapters:
+        adapters = (adapters[0], adapters[1], adapters[2][:1])
+    keep, right = {}, n - 1                              # the tokens of a chunk see each other
+    for at in range(0, total, n):
+        end = min(at + n, total)
+        cache.extend([end - at])
+        cache.step()
+        start = torch.tensor([0, end - at], device="cuda", dtype=torch.int32)
+        args = (x[at:end], pos[at:end], start, left, right, 0, adapters)
+        layer(*args, keep=keep, cache=cache)
+    q, k, v = (keep[name] for name in ("q", "k", "v"))
+    where = (cache.pages,), (cache.table, cache.lens, start)
+    line = {"layer": a.shape, "tokens": total, "chunk": q.shape[0], "cache": a.cache, "cache_bytes": cache.pages.numel(), "left": left,
+            "ms": timed(lambda: layer(*args, cache=cache)),
+            "ms_cache_write": timed(lambda: B.oq_cache_write(*where[0], k, v, *where[1], kind=a.cache)),
+            "ms_cache_attention": timed(lambda: B.oq_cache_attention(q, *where[0], *where[1], kind=a.cache, left=left, right=right)),
+            "ms_cache_read": timed(lambda: B.oq_cache_read(*where[0], layer.head_dim, *where[1], q.shape[0], kind=a.cache))}
     assert B.oq_device_status() == 0
     print(json.dumps(line))
 

@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS + 2 * STAGES];
   __shared__ Plan pm;
   __shared__ int raw_keys[STAGES];        // what a stage holds: number of keys that exist, and the pieces of 16 whose page is missing in bits 8 .. 15
+  __shared__ float row_c[2 * BM];         // the rows' factors as they were before `tame`: the loop has no register for them
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -233,6 +234,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       int rows, first, hi, lo, full_hi, full_lo, tiles, n_sink, skipped, seq, nk;
       bool turns;
       float c = c_next;
+      row_c[t * BM + row] = c;                   // (read by this thread alone)
       {
         const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         rows = min(max(it.rows - t * BM, 0), BM);
@@ -409,8 +411,9 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         if (mine) {
           // the powers had m c rounded in them, which shows in the sum (not in the weights' ratios)
           if (l != 0.f && m > -INFINITY) l *= exp2_fast(-fmaf(m, c, shift));
-          if (!whole) p.part_ml[slot_row] = make_float4(m, l, c, 0.f);
-          else if (p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(m, l, c);
+          const float factor = row_c[t * BM + row];
+          if (!whole) p.part_ml[slot_row] = make_float4(m, l, factor, 0.f);
+          else if (p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(m, l, factor);
         }
         tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
       }
