@@ -734,8 +734,8 @@ def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp
     if not given:
         if total is None or not 0 <= total <= _INT_MAX:
             raise OqError(1, "oq_cache_read: total, or out_k or out_v, is needed")
-        out_k = torch.empty((total, heads, head_dim), dtype=out_dtype or torch.bfloat16, device=pages.device)
-        out_v = torch.empty_like(out_k)
+        shape, dtype = (total, heads, head_dim), out_dtype or torch.bfloat16
+        out_k, out_v = pages.new_empty(shape, dtype=dtype), pages.new_empty(shape, dtype=dtype)
         given = [out_k]
     for x in given:
         if x.dim() != 3 or x.shape != given[0].shape or x.dtype != given[0].dtype or (total is not None and x.shape[0] != total) or \

@@ -1,5 +1,6 @@
 // Attention of new tokens over a paged cache: the entry point, the choice of kernels, and the kernel that joins the parts of items which
 // were cut along their keys.
+#include <atomic>
 #include <string>
 
 #include "oq_cache_attention.cuh"
@@ -99,8 +100,12 @@ static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cuda
 }
 
 static int sm_count() {
+  static std::atomic<int> known[64];               // of each device (asked twice a call otherwise)
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  if ((sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
 

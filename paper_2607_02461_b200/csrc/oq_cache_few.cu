@@ -404,9 +404,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
 template <int KIND, int D, int NT>
 cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
   const size_t smem = (size_t)WARPS * 8 * NT * D * sizeof(float);
-  // (the attribute belongs to the device that is current, so it is set every time)
-  const cudaError_t e = cudaFuncSetAttribute(few_kernel<KIND, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
+  static_assert(WARPS * 8 * NT * D * sizeof(float) + 8 * NT * (2 * (D + 8) + 4 + 8 * WARPS) + sizeof(Plan) + 256 <= 48 * 1024, "what every launch may have");
   return launch_dependent(few_kernel<KIND, D, NT>, ctas, THREADS, smem, st, p);
 }
 
