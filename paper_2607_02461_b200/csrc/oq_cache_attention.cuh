@@ -6,8 +6,10 @@
 //
 // The queries of all heads that share a key and value head are rows of one matrix: row r of a sequence is query r / group, head r % group of the group.
 // An item is a block of BM rows of one sequence and key and value head, with the tiles of 128 keys that some row of it sees (one, if
-// there are none).  All items' tiles, one after the other, are a line that is cut into as many equal stretches as there are CTAs, so the lengths may
-// be of any kind: they are on the device only, and every CTA finds its own stretch from them.  An item that lies in one stretch is
+// there are none).  All items, one after the other, are a line that is cut into as many equal stretches as there are CTAs, so the lengths may
+// be of any kind: they are on the device only, and every CTA finds its own stretch from them.  The line's units are tiles, and beside an item's tiles
+// as many units, in front of them, as it takes time to begin and end it (requests of a few tiles beside long ones: 113 us without them, 88 with).  Where a cut
+// falls among these the item begins in the stretch behind it.  An item that lies in one stretch is
 // finished there; of others each CTA writes its part, and a second kernel joins them.  A CTA has at most two such parts: part 0 of the item that its
 // stretch begins inside of, and part 1 of the one that begins in it and goes on behind it.
 #pragma once
@@ -73,12 +75,13 @@ __device__ __forceinline__ int row_hi(const AttnParams& p, const Seq& s, int i) 
 }
 __device__ __forceinline__ int row_lo(const AttnParams& p, const Seq& s, int i) { return p.left < 0 ? 0 : max(0, i + s.nk - s.nq - p.left); }
 
-// What a CTA finds out first: the sequences, the blocks before each of them, and where its stretch begins.
+// What a CTA finds out first: the sequences, the blocks before each of them, and where its stretch begins and ends.
 struct Plan {
   int prefix[MAX_SEQS + 1];
   Seq seq[MAX_SEQS];
   long long sums[32];
-  int block, off;
+  long long found[2];        // first unit of the block
+  int block[2];
 };
 
 template <int BM>
@@ -106,13 +109,13 @@ __device__ __forceinline__ Item make_item(const AttnParams& p, const Plan& m, in
   return it;
 }
 
-// A place on the line of all tiles (heads, then sequences, then blocks, then tiles) and the tiles from there to the stretch's end.
+// Where a CTA stands: tile `off` of an item, the first unit of that item on the line, and the tiles from there to the stretch's end.
 struct Stretch {
   int head, block, off;
   int blocks;                              // of one head
-  long long at, count;                     // the place's number, the tiles left
-  long long all;                           // tiles of the line
-  int ctas;                                // that share it: no more than there are tiles
+  long long unit, count;
+  long long all;                           // units of the line
+  int ctas;                                // that share it: no more than there are units
 };
 __device__ __forceinline__ long long divide(long long a, long long b) {       // (the short form where it serves)
   return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
@@ -146,29 +149,19 @@ __device__ __forceinline__ long long block_scan(long long v, long long* sums, lo
   return total;
 }
 
-__device__ __forceinline__ void set_stretch(Stretch& st, long long per_head, int kv_heads) {
-  st.all = per_head * kv_heads;
-  st.ctas = (int)min((long long)gridDim.x, st.all);
-  st.head = st.block = st.off = 0;
-  st.at = st.count = 0;
-  if ((int)blockIdx.x >= st.ctas) return;
-  st.at = divide(st.all * blockIdx.x, st.ctas);
-  st.count = divide(st.all * (blockIdx.x + 1), st.ctas) - st.at;
-  st.head = (int)divide(st.at, per_head);
-}
-
-// By the whole CTA.  Up to 32 sequences and 32 blocks (a step of single tokens, one long chunk) every warp works out for itself: what is waited
-// for is the length of a call's shortest part.
-template <int BM, int THREADS>
+// By the whole CTA.  OVERHEAD: units of an item beside its tiles.  Up to 32 sequences and 32 blocks (a step of single tokens, one long chunk) every warp
+// works out for itself: what is waited for is the length of a call's shortest part.
+template <int BM, int THREADS, int OVERHEAD>
 __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   static_assert(THREADS >= MAX_SEQS, "a thread for each sequence");
-  Stretch st;
+  Stretch st = {};
   long long before, n = 0;
   const int lane = threadIdx.x & 31;
   auto blocks_of = [&](const Seq& s) {
     const int rows = s.nq * p.group;
     return rows > p.row_min && rows <= p.row_max ? (rows + BM - 1) / BM : 0;
   };
+  auto units_of = [&](int b) { return b < st.blocks ? make_item<BM>(p, m, 0, b).tiles + OVERHEAD : 0; };
   if (p.c.n_seqs <= 32) {
     int mine = 0;
     if (lane < p.c.n_seqs) {
@@ -180,19 +173,7 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
     st.blocks = __shfl_sync(~0u, sum, 31);
     if (threadIdx.x < 32) {
       m.prefix[lane] = sum - mine;
-      if (lane == 0) m.prefix[32] = st.blocks;
-      if (lane == 0 && p.c.n_seqs < 32) m.prefix[p.c.n_seqs] = st.blocks;
-    }
-    __syncthreads();
-    if (st.blocks <= 32) {
-      const int tiles = lane < st.blocks ? make_item<BM>(p, m, 0, lane).tiles : 0, upto = warp_scan(tiles);
-      const int per_head = __shfl_sync(~0u, upto, 31);
-      set_stretch(st, per_head, p.c.kv_heads);
-      if (st.count == 0) return st;
-      const int r = (int)(st.at - (long long)st.head * per_head);
-      st.block = __popc(__ballot_sync(~0u, upto <= r && lane < st.blocks));
-      st.off = r - __shfl_sync(~0u, upto - tiles, st.block);
-      return st;
+      if (lane == 0) m.prefix[p.c.n_seqs] = m.prefix[32] = st.blocks;
     }
   } else {
     if ((int)threadIdx.x < p.c.n_seqs) {
@@ -203,57 +184,104 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
     st.blocks = (int)block_scan<THREADS>(n, m.sums, before);
     if ((int)threadIdx.x < p.c.n_seqs) m.prefix[threadIdx.x] = (int)before;
     if (threadIdx.x == 0) m.prefix[p.c.n_seqs] = st.blocks;
-    __syncthreads();
-  }
-  // tiles of one head; the first round's sums are kept, as there is one round mostly
-  n = (int)threadIdx.x < st.blocks ? make_item<BM>(p, m, 0, threadIdx.x).tiles : 0;
-  const long long first = block_scan<THREADS>(n, m.sums, before);
-  long long per_head = first, unused;
-  for (int b0 = THREADS; b0 < st.blocks; b0 += THREADS) {
-    const int b = b0 + threadIdx.x;
-    per_head += block_scan<THREADS>(b < st.blocks ? make_item<BM>(p, m, 0, b).tiles : 0, m.sums, unused);
-  }
-  set_stretch(st, per_head, p.c.kv_heads);
-  if (st.count == 0) return st;
-  const long long r = st.at - st.head * per_head;
-  long long done = 0, total = first;
-  for (int b0 = 0;;) {
-    before += done;
-    if (n > 0 && before <= r && r < before + n) {
-      m.block = b0 + threadIdx.x;
-      m.off = (int)(r - before);
-    }
-    done += total;
-    b0 += THREADS;
-    if (done > r || b0 >= st.blocks) break;
-    n = b0 + (int)threadIdx.x < st.blocks ? make_item<BM>(p, m, 0, b0 + threadIdx.x).tiles : 0;
-    total = block_scan<THREADS>(n, m.sums, before);
   }
   __syncthreads();
-  st.block = m.block;
-  st.off = m.off;
+  if (st.blocks == 0) return st;
+  // units of one head; the first round's sums are kept, as there is one round mostly
+  const bool short_line = st.blocks <= 32;
+  long long first, per_head, unused;
+  if (short_line) {
+    n = units_of(lane);
+    before = warp_scan(n);
+    first = per_head = __shfl_sync(~0u, before, 31);
+    before -= n;
+  } else {
+    n = units_of(threadIdx.x);
+    first = per_head = block_scan<THREADS>(n, m.sums, before);
+    for (int b0 = THREADS; b0 < st.blocks; b0 += THREADS) per_head += block_scan<THREADS>(units_of(b0 + threadIdx.x), m.sums, unused);
+  }
+  st.all = per_head * p.c.kv_heads;
+  st.ctas = (int)min((long long)gridDim.x, st.all);
+  if ((int)blockIdx.x >= st.ctas) return st;
+  long long at[2], head[2], found[2];
+  int block[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {                    // where the stretch begins, and where the next one does
+    at[i] = divide(st.all * (blockIdx.x + i), st.ctas);
+    head[i] = divide(at[i], per_head);
+    at[i] -= head[i] * per_head;
+  }
+  if (short_line) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      block[i] = __popc(__ballot_sync(~0u, before + n <= at[i] && lane < st.blocks));
+      found[i] = __shfl_sync(~0u, before, block[i]);
+    }
+  } else {
+    long long done = 0, total = first;
+    for (int b0 = 0;;) {
+      before += done;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (before <= at[i] && at[i] < before + n) {
+          m.block[i] = b0 + threadIdx.x;
+          m.found[i] = before;
+        }
+      done += total;
+      b0 += THREADS;
+      if (b0 >= st.blocks) break;
+      n = units_of(b0 + threadIdx.x);
+      total = block_scan<THREADS>(n, m.sums, before);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      block[i] = m.block[i];
+      found[i] = m.found[i];
+    }
+  }
+  // tiles before a place: units before its block less what is no tile of them, and what is behind the block's own OVERHEAD
+  const long long tiles = per_head - (long long)OVERHEAD * st.blocks;
+  long long number[2];
+  int off[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    off[i] = max((int)(at[i] - found[i]) - OVERHEAD, 0);
+    number[i] = head[i] * tiles + found[i] - (long long)OVERHEAD * block[i] + off[i];
+  }
+  st.head = (int)head[0];
+  st.block = block[0];
+  st.off = off[0];
+  st.unit = head[0] * per_head + found[0];
+  st.count = number[1] - number[0];
   return st;
 }
 
 // The item that the stretch stands at begins here and goes on behind the stretch: its parts.  (Stretch c begins at all * c / ctas rounded down, so
-// tile x is in stretch ((x + 1) * ctas - 1) / all rounded down.)
+// unit x is in stretch ((x + 1) * ctas - 1) / all rounded down.)
+template <int OVERHEAD>
 __device__ __forceinline__ Cut cut_here(const Stretch& st, const Item& it) {
   Cut c = {};
   c.q_base = it.s.q_base;
   c.r0 = it.r0;
   c.rows = it.rows;
   c.head = it.head;
-  c.parts = (int)divide((st.at + it.tiles) * st.ctas - 1, st.all) - (int)blockIdx.x + 1;
+  c.parts = (int)divide((st.unit + OVERHEAD + it.tiles) * st.ctas - 1, st.all) - (int)blockIdx.x + 1;
   return c;
 }
+// Behind the n tiles of an item that are in the stretch (all that are left of the item, or of the stretch).  Who asks for cuts keeps the unit too.
 __device__ __forceinline__ void next_item(Stretch& st, int n) {
-  st.at += n;
   st.count -= n;
   st.off = 0;
   if (++st.block == st.blocks) {
     st.block = 0;
     ++st.head;
   }
+}
+template <int OVERHEAD>
+__device__ __forceinline__ void next_item(Stretch& st, const Item& it, int n) {
+  st.unit += it.tiles + OVERHEAD;
+  next_item(st, n);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -298,6 +326,7 @@ __device__ __forceinline__ float natural_lse(float m, float l, float c) {
 cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
 cudaError_t launch_chunk(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st);
 constexpr int FEW_ROWS = 8, CHUNK_ROWS = 256;      // rows of their items
+constexpr int FEW_OVERHEAD = 2, CHUNK_OVERHEAD = 4;       // what an item takes beside its tiles, in tiles
 constexpr int FEW_CTAS = 2;                         // of an SM
 // Rows up to which a sequence goes to the kernel for few, which reads the cache once for 8 of them where the other reads it once for 256 but takes
 // longer to begin.  us, kernel for few / for chunks, e4m3: 16384 keys x 40 heads, 8 rows 42 / 91, 16 rows 70 / 91, 24 rows 93 / 92, 32 rows 123 / 93;

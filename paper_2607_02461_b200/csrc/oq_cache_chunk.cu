@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  Stretch st = plan<CHUNK_ROWS, THREADS>(p, pm);
+  Stretch st = plan<CHUNK_ROWS, THREADS, CHUNK_OVERHEAD>(p, pm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -586,7 +586,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         n = run_of(it);
         j = 0;
-        if (lane == 0 && st.off == 0 && n < it.tiles) p.cuts[blockIdx.x] = cut_here(st, it);
+        if (lane == 0 && st.off == 0 && n < it.tiles) p.cuts[blockIdx.x] = cut_here<CHUNK_OVERHEAD>(st, it);
       };
       bool have = st.count > 0;
       if (have) {
@@ -604,7 +604,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         const int first_piece = lane;
         // the next step's pages, while the copies are waited for
         if (++j == n) {
-          next_item(st, n);
+          next_item<CHUNK_OVERHEAD>(st, it, n);
           have = st.count > 0;
           if (have) enter();
         }

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  Stretch st = plan<BM, THREADS>(p, pm);
+  Stretch st = plan<BM, THREADS, FEW_OVERHEAD>(p, pm);
   if (threadIdx.x == 0 && p.cuts) p.cuts[blockIdx.x] = Cut{};
 
   while (st.count > 0) {
@@ -395,9 +395,9 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         if (lane == 0) p.part_ml[slot * BM + r] = make_float4(top, total, c_s[r], 0.f);
       }
     }
-    if (threadIdx.x == 0 && first == 0 && !whole) p.cuts[blockIdx.x] = cut_here(st, it);
+    if (threadIdx.x == 0 && first == 0 && !whole) p.cuts[blockIdx.x] = cut_here<FEW_OVERHEAD>(st, it);
     __syncthreads();
-    next_item(st, end - first);
+    next_item<FEW_OVERHEAD>(st, it, end - first);
   }
 }
 
