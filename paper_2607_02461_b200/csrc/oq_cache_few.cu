@@ -182,21 +182,6 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
     }
     int pos_n = next_pos(), page_n = look_up(pos_n);
     __syncthreads();
-    // B fragments of Q^T: coordinates in the order in which the lanes hold the keys'
-    uint32_t qf[D / 16][NT][2];
-#pragma unroll
-    for (int x = 0; x < L::LOADS; ++x)
-#pragma unroll
-      for (int w = 0; w < L::KW; ++w)
-#pragma unroll
-        for (int h = 0; h < L::PER_WORD / 4; ++h)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const uint16_t* q = q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h;
-            const int s = (x * L::KW + w) * (L::PER_WORD / 4) + h;
-            qf[s][n][0] = *reinterpret_cast<const uint32_t*>(q);
-            qf[s][n][1] = *reinterpret_cast<const uint32_t*>(q + 2);
-          }
     // columns of this lane: queries 8 n + 2 t and the next
     float c[NT][2], m[NT][2], l[NT][2];
     int hi[NT][2], lo[NT][2];
@@ -248,9 +233,9 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
 #pragma unroll
           for (int h = 0; h < L::PER_WORD / 4; ++h)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const uint32_t(&b)[2] = qf[(x * L::KW + w) * (L::PER_WORD / 4) + h][n];
-              mma(s[n], a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b[0], b[1]);
+            for (int n = 0; n < NT; ++n) {                     // (Q^T's fragment in the order in which the lanes hold the keys' coordinates)
+              const uint2 b = *reinterpret_cast<const uint2*>(q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h);
+              mma(s[n], a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b.x, b.y);
             }
         }
       }
