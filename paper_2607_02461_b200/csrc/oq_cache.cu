@@ -11,6 +11,9 @@
 // Bound: memory, or the launch.  A lane owns 8 adjacent coordinates of a head (16 bytes of bf16, 8 or 4 bytes of the cache), a group is 4
 // lanes, and a warp takes keys and values of some heads of one token, all requested before the first is used; the look-up of the token's
 // page runs beside those loads.
+//
+// Measured (B200, device time of captured calls): reading 32760 tokens of 40 heads of 128 back from e4m3 to bf16, 1.0 GB: 166 us = 6.1 TB/s, 0.93 of the copy rate;
+// writing 1560 tokens, 48 MB: 12 us, of which half is the launch and the chain start -> length -> page -> store; one token 3.3 us.
 #include <string>
 
 #include "oq_cache.cuh"

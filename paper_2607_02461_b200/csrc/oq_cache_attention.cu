@@ -1,6 +1,7 @@
 // Attention of new tokens over a paged cache: the entry point, the choice of kernels, and the kernel that joins the parts of items which
 // were cut along their keys.
 #include <atomic>
+#include <chrono>
 #include <string>
 
 #include "oq_cache_attention.cuh"
@@ -109,6 +110,12 @@ static int sm_count() {
   return sms;
 }
 
+// 48 bits that are another call's, or what lies in a workspace by chance, once in 2^48 times.
+static unsigned long long next_tag() {
+  static std::atomic<unsigned long long> calls{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull};
+  return calls.fetch_add(0x9E3779B97F4A7C15ull, std::memory_order_relaxed) >> 16;
+}
+
 // Which kernels run, with how many CTAs, and what their parts take.  Nothing is known here of the sequences but their number, the tokens of all
 // together and what a row of the table can hold: these bound the items and their tiles.
 struct Choice {
@@ -213,16 +220,18 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_cache_attention: cannot allocate the device status word");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
+  p.tag = next_tag();
   auto run = [&](auto launch, int ctas, int rows, size_t at, size_t bytes) {
     if (bytes) {
       p.cuts = reinterpret_cast<Cut*>(((reinterpret_cast<uintptr_t>(workspace) + 31) & ~(uintptr_t)31) + at);
+      p.arrivals = reinterpret_cast<unsigned long long*>(p.cuts);      // (the one or the other)
       p.part_ml = reinterpret_cast<float4*>(p.cuts + ctas);
       p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * rows);
     } else {
       p.cuts = nullptr;                              // one tile an item, or one CTA: nothing is cut
     }
     cudaError_t err = launch(p, a->cache.kind, d, ctas, st);
-    if (err == cudaSuccess && bytes) err = rows == FEW_ROWS ? launch_join<FEW_ROWS>(p, d, ctas, st) : launch_join<CHUNK_ROWS>(p, d, ctas, st);
+    if (err == cudaSuccess && bytes && rows == CHUNK_ROWS) err = launch_join<CHUNK_ROWS>(p, d, ctas, st);
     return err;
   };
   if (ch.chunk) {

@@ -10,8 +10,10 @@
 // be of any kind: they are on the device only, and every CTA finds its own stretch from them.  The line's units are tiles, and beside an item's tiles
 // as many units, in front of them, as it takes time to begin and end it (requests of a few tiles beside long ones: 113 us without them, 88 with).  Where a cut
 // falls among these the item begins in the stretch behind it.  An item that lies in one stretch is
-// finished there; of others each CTA writes its part, and a second kernel joins them.  A CTA has at most two such parts: part 0 of the item that its
-// stretch begins inside of, and part 1 of the one that begins in it and goes on behind it.
+// finished there; of others each CTA writes its part.  A CTA has at most two such parts: part 0 of the item that its stretch begins inside of, and part 1 of
+// the one that begins in it and goes on behind it.  Of an item of few rows who writes the last part joins them (in the order of the keys, whoever it is, so
+// results do not depend on it): that saves a launch, 2 us of the 20 of four requests of five tokens.  The parts of an item of 256 rows are too long to be joined by what wrote
+// one of them (2048 tokens over 16385: 416 us) and have a kernel of their own (380).
 #pragma once
 #include "oq_cache.cuh"
 
@@ -28,7 +30,9 @@ struct AttnParams {
   long long ldo, hdo;
   int wide_out;                            // rows of out begin on 32 bytes
   float* lse;                              // [heads][total_q] or NULL
-  struct Cut* cuts;                        // [CTAs]: the item that the CTA's stretch ends inside of and begins at or before
+  unsigned long long* arrivals;            // few rows: [CTAs], see arrive
+  unsigned long long tag;                  // of this call
+  struct Cut* cuts;                        // many rows: [CTAs]: the item that the CTA's stretch ends inside of and begins at or before
   float4* part_ml;                         // [2 * CTAs][BM]: reference m, sum l of the powers 2^(c (s - m)), c
   float* part_o;                           // [2 * CTAs][BM][D]: weights that add up to one
   const int* q_start;                      // n_seqs + 1, or NULL: one sequence
@@ -257,8 +261,33 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   return st;
 }
 
-// The item that the stretch stands at begins here and goes on behind the stretch: its parts.  (Stretch c begins at all * c / ctas rounded down, so
-// unit x is in stretch ((x + 1) * ctas - 1) / all rounded down.)
+// Which CTAs have parts of the item that the stretch stands at: parts CTAs from `first` on.  (Stretch c begins at all * c / ctas rounded down, so unit x
+// is in stretch ((x + 1) * ctas - 1) / all rounded down.)
+struct Parts {
+  int first, parts;
+};
+template <int OVERHEAD>
+__device__ __forceinline__ Parts parts_of(const Stretch& st, int tiles) {
+  Parts q;
+  q.first = (int)divide((st.unit + OVERHEAD + 1) * st.ctas - 1, st.all);
+  q.parts = (int)divide((st.unit + OVERHEAD + tiles) * st.ctas - 1, st.all) - q.first + 1;
+  return q;
+}
+// By one thread, when what it and those that it has waited for wrote of a part is written: true for the last part.  The counter needs no preparation: it
+// counts only while its upper 48 bits are the call's tag, which no other call has, and anything else is replaced by no arrival.  The last one
+// clears it, so that a captured call, whose tag comes again, finds it so.  (No arrival waits for another: a compare-and-swap a count took 30 us for 37.)
+__device__ __forceinline__ bool arrive(unsigned long long* counter, unsigned long long tag, int parts) {
+  __threadfence();
+  const unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(counter);
+  if (seen >> 16 != tag) atomicCAS(counter, seen, tag << 16);          // (who comes too late finds the tag there)
+  const bool last = (int)(atomicAdd(counter, 1ull) & 0xFFFFu) + 1 == parts;
+  if (last) {
+    *reinterpret_cast<volatile unsigned long long*>(counter) = 0ull;
+    __threadfence();
+  }
+  return last;
+}
+// The item that the stretch stands at begins here and goes on behind the stretch: its parts.
 template <int OVERHEAD>
 __device__ __forceinline__ Cut cut_here(const Stretch& st, const Item& it) {
   Cut c = {};
@@ -320,6 +349,88 @@ __device__ __forceinline__ float tame(float c, float m) { return fabsf(m) * c > 
 
 __device__ __forceinline__ float natural_lse(float m, float l, float c) {
   return l == 0.f ? -INFINITY : fmaf(m, c, log2f(l)) * 0.69314718055994531f;
+}
+
+// Rows row0 .. row0 + ROWS - 1 of an item (those from `rows` on stand in for the last) from the parts of CTAs q.first .. : by a warp, its parts share,
+// share + step, ... of them; lane l has coordinates N l .. of the results, and the rows' references and sums are returned.  Parts are weighed by
+// l 2^(c (m - max m)); the first ones are requested before their weights are known.
+template <int BM, int D, int ROWS>
+__device__ __forceinline__ void join_rows(const AttnParams& p, const Parts& q, int row0, int rows, int share, int step, float (&acc)[ROWS][D / 32], float (&top)[ROWS],
+                                          float (&total)[ROWS], float (&factor)[ROWS]) {
+  constexpr int N = D / 32, AHEAD = ROWS > 1 ? 2 : 4;
+  const int lane = threadIdx.x & 31;
+  auto slot = [&](int i, int r) { return (2ll * (q.first + i) + (i == 0 ? 1 : 0)) * BM + min(row0 + r, rows - 1); };
+  float v[ROWS][AHEAD][N];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int s = 0; s < AHEAD; ++s) {
+        const float* at = p.part_o + slot(min(i0 + s * step, q.parts - 1), r) * D + N * lane;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const float2 x = __ldcg(reinterpret_cast<const float2*>(at + e));
+          v[r][s][e] = x.x;
+          v[r][s][e + 1] = x.y;
+        }
+      }
+  };
+  load(share);
+  float ct[ROWS] = {}, w[ROWS];                      // w: of part `lane`, where there are no more than the lanes
+  float4 ml[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    ml[r] = __ldcg(p.part_ml + slot(min(lane, q.parts - 1), r));
+    top[r] = ml[r].x;
+    factor[r] = ml[r].z;
+    total[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[r][e] = 0.f;
+  }
+  for (int i = lane + 32; i < q.parts; i += 32)
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __ldcg(p.part_ml + slot(i, r)).x);
+  auto weight = [&](const float4& x, int r) { return x.y == 0.f ? 0.f : x.y * (x.x == top[r] ? 1.f : exp2_fast((x.x - top[r]) * ct[r])); };
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], d));
+    ct[r] = tame(factor[r], top[r]);
+    w[r] = total[r] = lane < q.parts ? weight(ml[r], r) : 0.f;
+  }
+  for (int i = lane + 32; i < q.parts; i += 32)
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) total[r] += weight(__ldcg(p.part_ml + slot(i, r)), r);
+  float inv[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total[r] += __shfl_xor_sync(~0u, total[r], d);
+    inv[r] = total[r] == 0.f ? 0.f : 1.f / total[r];
+  }
+  for (int i0 = share; i0 < q.parts; i0 += AHEAD * step) {
+    if (i0 != share) load(i0);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int s = 0; s < AHEAD; ++s) {
+        const int i = i0 + s * step;
+        if (i >= q.parts) continue;
+        const float x = (i < 32 ? __shfl_sync(~0u, w[r], i) : weight(__ldcg(p.part_ml + slot(i, r)), r)) * inv[r];
+        if (x == 0.f) continue;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[r][e] = fmaf(x, v[r][s][e], acc[r][e]);
+      }
+  }
+}
+template <int D>
+__device__ __forceinline__ void write_row(const AttnParams& p, const Item& it, int row, const float (&acc)[D / 32], float top, float total, float factor) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31, r = it.r0 + row, tok = token_of(p, r), i = it.s.q_base + tok, head = it.head * p.group + r - tok * p.group;
+  __nv_bfloat16* dst = p.out + (long long)i * p.ldo + head * p.hdo + N * lane;
+#pragma unroll
+  for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);
+  if (lane == 0 && p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(top, total, factor);
 }
 
 // kernels (a file each)

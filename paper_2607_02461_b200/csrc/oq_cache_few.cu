@@ -1,8 +1,8 @@
 // Attention of a few rows (new tokens times the heads of a group) over a paged cache.
 //
-// With up to 16 rows for a key and value head the cache is read once and every byte is used a few times, so the memory is the bound: 346 MB for one
+// With up to 8 rows for a key and value head the cache is read once and every byte is used a few times, so the memory is the bound: 346 MB for one
 // token over 32760 tokens of 40 heads in 8 bits, 53 us at the copy rate.  Decoding is what the SM does most of: 24 elements a cycle for the
-// bytes that arrive, an instruction a pair each for conversion and scale.  So nothing passes through shared memory: a lane reads the cache in 16
+// bytes that arrive (48 in 4 bits), an instruction a pair each for conversion and scale.  So nothing passes through shared memory: a lane reads the cache in 16
 // bytes a time, decodes them in registers, and what it has is its fragment of the operand,
 //   S^T [16 keys x 8 rows] = K [16 x D] Q^T,      O^T [D x 8 rows] += V^T [D x 16 keys] P^T,
 // with the keys (the coordinates) as the 16 rows of an instruction and the queries as its 8 columns.  Which coordinate goes where in the
@@ -11,7 +11,13 @@
 // The tensor cores' older instruction serves here: they are idle most of the time.
 //
 // 8 warps each take 16 keys of a tile of 128 and keep their own maximum, sum and O; they are put together at the end of an item.  A warp's
-// next keys are requested as soon as the present ones are decoded, its next values likewise.
+// next keys are requested as soon as the present ones are decoded, its next values likewise; two CTAs an SM have 66 KB on their way.
+//
+// Measured (B200, device time of captured calls): one token over 32760 of 40 heads of 128 in e4m3 66 us = 5.2 TB/s, 0.80 of the copy rate (the loop alone runs at 0.95 of it;
+// 5 us go by before the first keys arrive, as much at the end); in e2m1 57 us = 3.1 TB/s, bound by issue and latency: 410 instructions for 16 keys x 128 a warp, 145 of
+// them at half rate; 16 requests of one token, 17 to 16384 cached, 24 heads on 8, e2m1 38 us; four of five tokens 15 us.  With 16 rows a block (twice the sums and fragments,
+// spilled) the first took 270 us; loads that the compiler could move to their use 2 us more; one CTA an SM 87 us; three, with spills, 65 (e2m1); two sums of S in
+// turn, to halve its chain of products, no less.
 #include <string>
 
 #include "oq_cache_attention.cuh"
@@ -84,21 +90,22 @@ struct Values {
   uint32_t scale[4];
 };
 
-template <int KIND, int D, int NT>
+template <int KIND, int D>
 __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_constant__ AttnParams p) {
   using F = Format<KIND, D>;
   using L = Lane<KIND, D>;
-  constexpr int BM = 8 * NT, QP = D + 8;
+  constexpr int BM = FEW_ROWS, QP = D + 8;
+  static_assert(BM == 8, "the columns of an instruction");
   extern __shared__ __align__(16) unsigned char smem[];
   float* const part = reinterpret_cast<float*>(smem);                     // [WARPS][BM][D]
   __shared__ __align__(16) uint16_t q_s[BM * QP];
   __shared__ float c_s[BM], m_s[WARPS][BM], l_s[WARPS][BM];
   __shared__ Plan pm;
+  __shared__ int last_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   Stretch st = plan<BM, THREADS, FEW_OVERHEAD>(p, pm);
-  if (threadIdx.x == 0 && p.cuts) p.cuts[blockIdx.x] = Cut{};
 
   while (st.count > 0) {
     const Item it = make_item<BM>(p, pm, st.head, st.block);
@@ -182,36 +189,30 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
     }
     int pos_n = next_pos(), page_n = look_up(pos_n);
     __syncthreads();
-    // columns of this lane: queries 8 n + 2 t and the next
-    float c[NT][2], m[NT][2], l[NT][2];
-    int hi[NT][2], lo[NT][2];
+    // columns of this lane: queries 2 t and the next
+    float c[2], m[2], l[2];
+    int hi[2], lo[2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = 8 * n + 2 * t + e, i = token_of(p, it.r0 + r);
-        c[n][e] = c_s[r];
-        m[n][e] = -INFINITY;
-        l[n][e] = 0.f;
-        hi[n][e] = r < it.rows ? row_hi(p, it.s, i) : -1;
-        lo[n][e] = row_lo(p, it.s, i);
-      }
+    for (int e = 0; e < 2; ++e) {
+      const int r = 2 * t + e, i = token_of(p, it.r0 + r);
+      c[e] = c_s[r];
+      m[e] = -INFINITY;
+      l[e] = 0.f;
+      hi[e] = r < it.rows ? row_hi(p, it.s, i) : -1;
+      lo[e] = row_lo(p, it.s, i);
+    }
     const int full_hi = row_hi(p, it.s, token_of(p, it.r0)), full_lo = row_lo(p, it.s, token_of(p, it.r0 + it.rows - 1));     // what every row sees
-    float o[D / 16][NT][4];
+    float o[D / 16][4];
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][n][e] = 0.f;
+        for (int e = 0; e < 4; ++e) o[x][e] = 0.f;
 
     while (pos >= 0) {
       // ---------------------------------------------- S^T = K Q^T ----------------------------------------------
-      float s[NT][4];
+      float s[4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[e] = 0.f;
 #pragma unroll
       for (int x = 0; x < L::LOADS; ++x) {
         uint32_t f[2];
@@ -231,12 +232,10 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
             for (int e = 0; e < L::PER_WORD / 2; ++e) a[r][e] = mul_f16x2(a[r][e], f[r]);
           }
 #pragma unroll
-          for (int h = 0; h < L::PER_WORD / 4; ++h)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {                     // (Q^T's fragment in the order in which the lanes hold the keys' coordinates)
-              const uint2 b = *reinterpret_cast<const uint2*>(q_s + (8 * n + g) * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h);
-              mma(s[n], a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b.x, b.y);
-            }
+          for (int h = 0; h < L::PER_WORD / 4; ++h) {            // (Q^T's fragment in the order in which the lanes hold the keys' coordinates)
+            const uint2 b = *reinterpret_cast<const uint2*>(q_s + g * QP + L::coord(x, t) + L::PER_WORD * w + 4 * h);
+            mma(s, a[0][2 * h], a[1][2 * h], a[0][2 * h + 1], a[1][2 * h + 1], b.x, b.y);
+          }
         }
       }
       const uint8_t* const block_n = settle(pos_n, page_n);
@@ -244,50 +243,41 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       // ------------------------------------------------ softmax ------------------------------------------------
       if (!(pos + 15 <= full_hi && (pos >= full_lo || pos + 16 <= p.sinks))) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = pos + g + 8 * (e >> 1);
-            if (key > hi[n][e & 1] || (key < lo[n][e & 1] && key >= p.sinks)) s[n][e] = -INFINITY;
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int key = pos + g + 8 * (e >> 1);
+          if (key > hi[e & 1] || (key < lo[e & 1] && key >= p.sinks)) s[e] = -INFINITY;
+        }
       }
       bool over = false;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) over |= (fmaxf(s[n][e], s[n][e + 2]) - m[n][e]) * c[n][e] > SLACK;
+      for (int e = 0; e < 2; ++e) over |= (fmaxf(s[e], s[e + 2]) - m[e]) * c[e] > SLACK;
       if (__any_sync(~0u, over)) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 2; ++e) {
+          float x = fmaxf(m[e], fmaxf(s[e], s[e + 2]));
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x = fmaxf(m[n][e], fmaxf(s[n][e], s[n][e + 2]));
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+          c[e] = tame(c[e], x);
+          const float a = x == m[e] ? 1.f : exp2_fast((m[e] - x) * c[e]);
+          m[e] = x;
+          l[e] *= a;
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
-            c[n][e] = tame(c[n][e], x);
-            const float a = x == m[n][e] ? 1.f : exp2_fast((m[n][e] - x) * c[n][e]);
-            m[n][e] = x;
-            l[n][e] *= a;
-#pragma unroll
-            for (int y = 0; y < D / 16; ++y) {
-              o[y][n][e] *= a;
-              o[y][n][e + 2] *= a;
-            }
+          for (int y = 0; y < D / 16; ++y) {
+            o[y][e] *= a;
+            o[y][e + 2] *= a;
           }
-      }
-      uint32_t b[NT][2];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float ref = m[n][e & 1] == -INFINITY ? 0.f : m[n][e & 1];
-          w[e] = exp2_fast((s[n][e] - ref) * c[n][e & 1]);
-          l[n][e & 1] += w[e];
         }
-        b[n][0] = transpose8(pack_f16(w[0], w[1]));
-        b[n][1] = transpose8(pack_f16(w[2], w[3]));
       }
+      uint32_t b[2];
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float ref = m[e & 1] == -INFINITY ? 0.f : m[e & 1];
+        w[e] = exp2_fast((s[e] - ref) * c[e & 1]);
+        l[e & 1] += w[e];
+      }
+      b[0] = transpose8(pack_f16(w[0], w[1]));
+      b[1] = transpose8(pack_f16(w[2], w[3]));
       // --------------------------------------------- O^T += V^T P^T ---------------------------------------------
       if (pos + 16 > it.s.nk) {                          // what lies behind the end may be anything
 #pragma unroll
@@ -322,9 +312,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         }
 #pragma unroll
         for (int e = 0; e < L::PER_WORD / 2; ++e)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            mma(o[w * (L::PER_WORD / 2) + e][n], a[0][2 * e], a[0][2 * e + 1], a[1][2 * e], a[1][2 * e + 1], b[n][0], b[n][1]);
+          mma(o[w * (L::PER_WORD / 2) + e], a[0][2 * e], a[0][2 * e + 1], a[1][2 * e], a[1][2 * e + 1], b[0], b[1]);
       }
       if (pos_n >= 0) load_values(block_n, pos_n & in_page);
       pos = pos_n;
@@ -333,19 +321,17 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
     }
     // ----------------------------------------------- the item's result -----------------------------------------------
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(~0u, l[n][e], d);
-        const int r = 8 * n + 2 * t + e;
+        for (int d = 4; d < 32; d <<= 1) l[e] += __shfl_xor_sync(~0u, l[e], d);
+        const int r = 2 * t + e;
         if (g == 0) {
-          m_s[warp][r] = m[n][e];
-          l_s[warp][r] = l[n][e];
+          m_s[warp][r] = m[e];
+          l_s[warp][r] = l[e];
         }
         float* to = part + (warp * BM + r) * D + g * (D / 8);
 #pragma unroll
-        for (int y = 0; y < D / 16; ++y) *reinterpret_cast<float2*>(to + 2 * y) = make_float2(o[y][n][e], o[y][n][e + 2]);
+        for (int y = 0; y < D / 16; ++y) *reinterpret_cast<float2*>(to + 2 * y) = make_float2(o[y][e], o[y][e + 2]);
       }
     __syncthreads();
     const bool whole = first == 0 && end == it.tiles;
@@ -367,12 +353,10 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         for (int e = 0; e < N; ++e) acc[e] = fmaf(part[(w * BM + r) * D + N * lane + e], a, acc[e]);
       }
       const float inv = total == 0.f ? 0.f : 1.f / total;
-      const int row = it.r0 + r, tok = token_of(p, row), i = it.s.q_base + tok, head = it.head * p.group + row - tok * p.group;
       if (whole) {
-        __nv_bfloat16* dst = p.out + (long long)i * p.ldo + head * p.hdo + N * lane;
 #pragma unroll
-        for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-        if (lane == 0 && p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(top, total, c_s[r]);
+        for (int e = 0; e < N; ++e) acc[e] *= inv;
+        write_row<D>(p, it, r, acc, top, total, c_s[r]);
       } else {
         float* dst = p.part_o + (slot * BM + r) * D + N * lane;
 #pragma unroll
@@ -380,24 +364,47 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         if (lane == 0) p.part_ml[slot * BM + r] = make_float4(top, total, c_s[r], 0.f);
       }
     }
-    if (threadIdx.x == 0 && first == 0 && !whole) p.cuts[blockIdx.x] = cut_here<FEW_OVERHEAD>(st, it);
     __syncthreads();
+    if (!whole) {
+      const Parts q = parts_of<FEW_OVERHEAD>(st, it.tiles);
+      if (threadIdx.x == 0) last_s = arrive(p.arrivals + q.first, p.tag, q.parts);
+      __syncthreads();
+      if (last_s) {
+        // as many warps a row as there are, each with every so many of its parts
+        int per_row = WARPS;
+        while (per_row > 1 && per_row * it.rows > WARPS) per_row >>= 1;
+        const int r = warp / per_row, share = warp % per_row;
+        float joined[1][N], top[1], total[1], factor[1];
+        join_rows<BM, D, 1>(p, q, r, it.rows, share, per_row, joined, top, total, factor);
+        float(&acc)[N] = joined[0];
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[warp * D + N * lane + e] = acc[e];
+        __syncthreads();
+        if (r < it.rows && share == 0) {
+          for (int w = 1; w < per_row; ++w)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += part[(warp + w) * D + N * lane + e];
+          write_row<D>(p, it, r, acc, top[0], total[0], factor[0]);
+        }
+        __syncthreads();
+      }
+    }
     next_item<FEW_OVERHEAD>(st, it, end - first);
   }
 }
 
-template <int KIND, int D, int NT>
+template <int KIND, int D>
 cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
-  const size_t smem = (size_t)WARPS * 8 * NT * D * sizeof(float);
-  static_assert(WARPS * 8 * NT * D * sizeof(float) + 8 * NT * (2 * (D + 8) + 4 + 8 * WARPS) + sizeof(Plan) + 256 <= 48 * 1024, "what every launch may have");
-  return launch_dependent(few_kernel<KIND, D, NT>, ctas, THREADS, smem, st, p);
+  const size_t smem = (size_t)WARPS * FEW_ROWS * D * sizeof(float);
+  static_assert(WARPS * FEW_ROWS * D * sizeof(float) + FEW_ROWS * (2 * (D + 8) + 4 + 8 * WARPS) + sizeof(Plan) + 256 <= 48 * 1024, "what every launch may have");
+  return launch_dependent(few_kernel<KIND, D>, ctas, THREADS, smem, st, p);
 }
 
 }  // namespace few
 
 cudaError_t launch_few(const AttnParams& p, int kind, int head_dim, int ctas, cudaStream_t st) {
-  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128, 1>(p, ctas, st) : few::go<8, 64, 1>(p, ctas, st);
-  return head_dim == 128 ? few::go<4, 128, 1>(p, ctas, st) : few::go<4, 64, 1>(p, ctas, st);
+  if (kind == OQ_CACHE_FP8) return head_dim == 128 ? few::go<8, 128>(p, ctas, st) : few::go<8, 64>(p, ctas, st);
+  return head_dim == 128 ? few::go<4, 128>(p, ctas, st) : few::go<4, 64>(p, ctas, st);
 }
 
 }  // namespace cache
