@@ -652,39 +652,40 @@ def oq_cache_alloc(n_pages, page_size, kv_heads, head_dim, kind="fp8", device="c
 
 def _cache_fields(what, torch, pages, head_dim, kind, table, lens, start, device):
     """Checks what the calls on a cache have in common.  Returns the fields of oq_cache and the address of start."""
-    i32 = torch.int32
     bits = CACHE_KINDS.get(kind)
     if bits is None:
         raise OqError(1, f"{what}: kind must be one of {sorted(CACHE_KINDS)}")
-    if device < 0 or not device == pages.get_device() == table.get_device() == lens.get_device() or \
-            (start is not None and start.get_device() != device):
+    if device < 0 or not device == pages.get_device() == table.get_device() == lens.get_device():
         raise _off_device(what)
     if device != torch._C._cuda_getDevice():
         raise OqError(1, f"{what}: the tensors' device must be the current one")
-    shape, tshape = pages.shape, table.shape
-    if pages.dtype != torch.uint8 or len(shape) != 3 or not pages.is_contiguous():
+    shape, tshape, lshape, i32 = pages.shape, table.shape, lens.shape, torch.int32
+    if len(shape) != 3 or pages.dtype != torch.uint8 or not pages.is_contiguous():
         raise OqError(1, f"{what}: pages must be contiguous uint8 [pages, kv_heads, bytes of a block]")
     if head_dim != 64 and head_dim != 128:
         raise OqError(2, f"{what}: head_dim must be 64 or 128")
-    size, odd = divmod(shape[2], head_dim * bits // 4 + head_dim // 16)        # bytes of a token's keys, values and scales
+    n_pages, heads, block = shape
+    size, odd = divmod(block, head_dim * (4 * bits + 1) // 16)        # bytes of a token's keys, values and scales: 2 (d * bits / 8 + d / 32)
     if odd:
         raise OqError(1, f"{what}: no number of tokens of this kind and head_dim fills a block of these pages")
-    seqs = lens.numel()
-    if table.dtype != i32 or len(tshape) != 2 or tshape[0] != seqs or lens.dtype != i32 or lens.dim() != 1 or not lens.is_contiguous():
+    if len(lshape) != 1 or len(tshape) != 2 or tshape[0] != lshape[0] or table.dtype != i32 or lens.dtype != i32 or not lens.is_contiguous():
         raise OqError(1, f"{what}: table must be int32 [sequences, pages], lens contiguous int32 [sequences]")
+    seqs, most = tshape
     ld, step = table.stride()
-    if step != 1 and tshape[1] > 1:
+    if step != 1 and most > 1:
         raise OqError(3, f"{what}: the entries of a row of the table must be adjacent")
     at = 0
     if start is not None:
+        if start.get_device() != device:
+            raise _off_device(what)
         if start.dtype != i32 or start.shape != (seqs + 1,) or not start.is_contiguous():
             raise OqError(1, f"{what}: start must be contiguous int32 [sequences + 1]")
         at = start.data_ptr()
     elif seqs != 1:
         raise OqError(1, f"{what}: several sequences need start")
-    if max(shape[0], shape[1], tshape[1]) > _INT_MAX:
+    if n_pages > _INT_MAX or heads > _INT_MAX or most > _INT_MAX:
         raise OqError(2, f"{what}: sizes above 2^31 - 1")
-    return (pages.data_ptr(), table.data_ptr(), lens.data_ptr(), ld, shape[0], size, shape[1], head_dim, bits, seqs, tshape[1]), at
+    return (pages.data_ptr(), table.data_ptr(), lens.data_ptr(), ld, n_pages, size, heads, head_dim, bits, seqs, most), at
 
 
 def _cache_rows(what, X, heads, head_dim):
@@ -728,25 +729,28 @@ def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp
     first size where out_k or out_v is given).  Returns (K, V) [total, kv_heads, head_dim] of out_dtype (bf16 or fp32, bf16 by default).
     With out_k or out_v given, only what is given is read."""
     import torch
-    device, heads = pages.get_device(), pages.shape[1] if pages.dim() == 3 else 0
+    device = pages.get_device()
     fields, at = _cache_fields("oq_cache_read", torch, pages, head_dim, kind, table, lens, start, device)
-    given = [x for x in (out_k, out_v) if x is not None]
-    if not given:
+    heads = fields[6]
+    if out_k is None and out_v is None:
         if total is None or not 0 <= total <= _INT_MAX:
             raise OqError(1, "oq_cache_read: total, or out_k or out_v, is needed")
         shape, dtype = (total, heads, head_dim), out_dtype or torch.bfloat16
+        code = _dtype_code(dtype, "oq_cache_read")
         out_k, out_v = pages.new_empty(shape, dtype=dtype), pages.new_empty(shape, dtype=dtype)
-        given = [out_k]
-    for x in given:
-        if x.dim() != 3 or x.shape != given[0].shape or x.dtype != given[0].dtype or (total is not None and x.shape[0] != total) or \
-                (out_dtype is not None and x.dtype != out_dtype):
-            raise OqError(1, "oq_cache_read: out_k and out_v must be [total, kv_heads, head_dim] of one type")
-        if x.get_device() != device:
-            raise _off_device("oq_cache_read")
-    code = _dtype_code(given[0].dtype, "oq_cache_read")
-    rows = [None if x is None else _cache_rows("oq_cache_read", x, heads, head_dim) for x in (out_k, out_v)]
-    rc = (_lib or lib()).oq_cache_read(_CACHE.pack(*fields), rows[0], rows[1], code, at, given[0].shape[0],
-                                       torch._C._cuda_getCurrentRawStream(device))
+        k = _CACHE_ROWS.pack(out_k.data_ptr(), heads * head_dim, head_dim)
+        v = _CACHE_ROWS.pack(out_v.data_ptr(), heads * head_dim, head_dim)
+    else:
+        given = [x for x in (out_k, out_v) if x is not None]
+        total = given[0].shape[0] if total is None and given[0].dim() else total
+        for x in given:
+            if x.dim() != 3 or x.shape[0] != total or x.dtype != given[0].dtype or (out_dtype is not None and x.dtype != out_dtype):
+                raise OqError(1, "oq_cache_read: out_k and out_v must be [total, kv_heads, head_dim] of one type")
+            if x.get_device() != device:
+                raise _off_device("oq_cache_read")
+        code = _dtype_code(given[0].dtype, "oq_cache_read")
+        k, v = (None if x is None else _cache_rows("oq_cache_read", x, heads, head_dim) for x in (out_k, out_v))
+    rc = (_lib or lib()).oq_cache_read(_CACHE.pack(*fields), k, v, code, at, total, torch._C._cuda_getCurrentRawStream(device))
     if rc:
         _check(rc)
     return out_k, out_v
