@@ -13,7 +13,7 @@ constexpr int JOIN_WARPS = 8, JOIN_ROWS = JOIN_WARPS;
 
 // CTA (c, y): rows 8 y .. 8 y + 7 of the item that CTA c of the kernel before began and did not finish, if there is one.  Parts of a row are weighed by
 // l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each; the first ones are requested before their
-// weights are known.  (Four rows a warp, for more bytes on their way: the same time with two parts a row, 2 to 4 us more with eighteen.)
+// weights are known.  (Four rows a warp, for more bytes on their way or fewer instructions: the same time with two parts a row, 2 to 8 us more with eighteen.)
 template <int BM, int D>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) cache_join_kernel(const __grid_constant__ AttnParams p) {
   constexpr int N = D / 32, AHEAD = 4;
