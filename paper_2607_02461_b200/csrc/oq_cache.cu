@@ -34,20 +34,36 @@ struct CopyParams {
   int total, chunks;               // chunks of heads, a warp each
 };
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+// 8 values as they were loaded (unpacked they take twice the registers, and a kernel that waits for its loads wants many warps).
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void clear() { a = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(u[i] << 16);
-    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
   }
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
+};
+template <>
+struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
   uint32_t u[4];
 #pragma unroll
@@ -84,17 +100,13 @@ __global__ void __launch_bounds__(32 * WARPS) write_kernel(const __grid_constant
   const long long w = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
   const int tok = (int)(w / p.chunks), head0 = (int)(w % p.chunks) * HEADS * ITERS + lane / LANES;
   if (tok >= p.total) return;
-  float x[2 * ITERS][8];
+  Raw<T> raw[2 * ITERS];
 #pragma unroll
   for (int i = 0; i < 2 * ITERS; ++i) {
     const Rows& r = i & 1 ? p.v : p.k;
     const int head = head0 + HEADS * (i >> 1);
-    if (head < p.c.kv_heads) {
-      load8(reinterpret_cast<const T*>(r.X) + tok * r.ld_token + head * r.ld_head + 8 * sub, x[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    }
+    if (head < p.c.kv_heads) raw[i].load(reinterpret_cast<const T*>(r.X) + tok * r.ld_token + head * r.ld_head + 8 * sub);
+    else raw[i].clear();
   }
   int at;
   const int page = locate(p, tok, at);
@@ -102,12 +114,14 @@ __global__ void __launch_bounds__(32 * WARPS) write_kernel(const __grid_constant
 #pragma unroll
   for (int j = 0; j < ITERS; ++j) {
     uint32_t top[2];
+    float x[2][8];
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      raw[2 * j + i].get(x[i]);
       top[i] = 0u;                                     // magnitudes compare as whole numbers, NaN above all others
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top[i] = max(top[i], __float_as_uint(x[2 * j + i][e]) & 0x7FFFFFFFu);
+      for (int e = 0; e < 8; ++e) top[i] = max(top[i], __float_as_uint(x[i][e]) & 0x7FFFFFFFu);
       top[i] = max(top[i], __shfl_xor_sync(~0u, top[i], 1));
       top[i] = max(top[i], __shfl_xor_sync(~0u, top[i], 2));
       odd |= top[i] >= 0x7F800000u;
@@ -123,7 +137,7 @@ __global__ void __launch_bounds__(32 * WARPS) write_kernel(const __grid_constant
       const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = broken ? 0.f : x[2 * j + i][e] * inv;
+      for (int e = 0; e < 8; ++e) y[e] = broken ? 0.f : x[i][e] * inv;
       uint32_t scale = (broken ? BROKEN : (uint32_t)(k + 127)) << (8 * (sub >> 2));
 #pragma unroll
       for (int d = 4; d < LANES; d <<= 1) scale |= __shfl_xor_sync(~0u, scale, d);      // the row's scales in one word
