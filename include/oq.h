@@ -418,7 +418,8 @@ int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_
  *   scale    0: 1 / sqrt(head_dim)
  * What is cached is decoded exactly, and queries lose nothing that matters (the parts of a head more than 2^29 below its largest); the products run on the tensor cores in fp16 with fp32 accumulation, the softmax weights are
  * rounded to fp16 for the second one, everything else is fp32.  Items of work are cut along the keys so that all SMs get the same share, whatever
- * the lengths; the workspace (dev, 16-byte aligned, oq_cache_attention_workspace_bytes bytes) holds the parts.  Results are bit-reproducible.
+ * the lengths, unless a row of the table holds no more than 512 positions; the workspace (dev, 16-byte aligned, oq_cache_attention_workspace_bytes
+ * bytes, 0 when nothing is cut) holds the parts.  Results are bit-reproducible.
  * Asynchronous on `stream`.  total_q == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */
 typedef struct {
   oq_cache cache;

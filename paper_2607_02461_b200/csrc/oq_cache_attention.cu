@@ -116,10 +116,17 @@ static unsigned long long next_tag() {
   return calls.fetch_add(0x9E3779B97F4A7C15ull, std::memory_order_relaxed) >> 16;
 }
 
+// Items of up to so many tiles are not cut along their keys: joining the parts takes longer than the tiles do.  Measured at 1, 3, 20, 80 and 300 rows, 4 and 24 heads, one
+// sequence and eight: whole items are better in all of 20 at 256 keys and at 384, in 19 at 512, in 8 at 1024.  us, cut / whole: one token, 4 heads, 256 keys 9.1 / 6.8,
+// 512 keys 9.1 / 8.7, 1024 keys 9.1 / 12.5; eight sequences of 20 rows, 24 heads, 512 keys 28.9 / 21.2; 300 rows, 24 heads, 512 keys 30.9 / 24.0; the one that loses at
+// 512 keys, 80 rows, 4 heads: 14.6 / 16.6.  (At 1024 keys whole ones win where there are many items, eight sequences of 300 rows, 24 heads 101 / 87, if their lengths are
+// alike, which is not known here.)
+constexpr long long WHOLE_TILES = 4;
+
 // Which kernels run, with how many CTAs, and what their parts take.  Nothing is known here of the sequences but their number, the tokens of all
 // together and what a row of the table can hold: these bound the items and their tiles.
 struct Choice {
-  bool few, chunk;
+  bool few, chunk, whole;
   int few_ctas, chunk_ctas;
   int row_cut;                   // sequences of at most so many rows go to the kernel for few
   size_t few_bytes, chunk_bytes, bytes;
@@ -132,11 +139,13 @@ static Choice choose(const oq_cache_attention_args* a, const View& v) {
   c.chunk = most > FEW_LIMIT;
   c.row_cut = FEW_LIMIT;
   const long long tiles = v.max_len > 0 ? (v.max_len + BN - 1) / BN : 1;
+  c.whole = tiles <= WHOLE_TILES;
   auto ctas = [&](int bm, int all) {
     const long long items = (((long long)a->total_q * group + bm - 1) / bm + v.n_seqs) * v.kv_heads;
-    return (int)(items >= all || items * tiles >= all ? all : items * tiles);
+    const long long most = c.whole ? items : items * tiles;
+    return (int)(items >= all || most >= all ? all : most);
   };
-  auto part_bytes = [&](int bm, int n) { return tiles > 1 && n > 1 ? n * (sizeof(Cut) + (size_t)2 * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4))) : (size_t)0; };
+  auto part_bytes = [&](int bm, int n) { return !c.whole && n > 1 ? n * (sizeof(Cut) + (size_t)2 * bm * ((size_t)a->cache.head_dim * sizeof(float) + sizeof(float4))) : (size_t)0; };
   if (c.few) {
     c.few_ctas = ctas(FEW_ROWS, FEW_CTAS * sms);
     c.few_bytes = part_bytes(FEW_ROWS, c.few_ctas);
@@ -221,6 +230,7 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   p.tag = next_tag();
+  p.whole = ch.whole;
   auto run = [&](auto launch, int ctas, int rows, size_t at, size_t bytes) {
     if (bytes) {
       p.cuts = reinterpret_cast<Cut*>(((reinterpret_cast<uintptr_t>(workspace) + 31) & ~(uintptr_t)31) + at);
@@ -228,7 +238,7 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
       p.part_ml = reinterpret_cast<float4*>(p.cuts + ctas);
       p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * rows);
     } else {
-      p.cuts = nullptr;                              // one tile an item, or one CTA: nothing is cut
+      p.cuts = nullptr;                              // nothing is cut
     }
     cudaError_t err = launch(p, a->cache.kind, d, ctas, st);
     if (err == cudaSuccess && bytes && rows == CHUNK_ROWS) err = launch_join<CHUNK_ROWS>(p, d, ctas, st);

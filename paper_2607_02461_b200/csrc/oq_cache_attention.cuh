@@ -39,6 +39,7 @@ struct AttnParams {
   int total_q, group;
   uint32_t group_mul, group_shift;         // row / group = (mulhi(row, group_mul) + row) >> group_shift, for rows below 2^31
   int row_min, row_max;                    // this kernel takes the sequences with row_min < rows <= row_max
+  int whole;                               // items are not cut
   int left, right, sinks;
   float scale, scale_log2;
   int* status;
@@ -84,7 +85,7 @@ struct Plan {
   int prefix[MAX_SEQS + 1];
   Seq seq[MAX_SEQS];
   long long sums[32];
-  long long found[2];        // first unit of the block
+  long long found[2], units[2];        // first unit of the block, its units
   int block[2];
 };
 
@@ -153,9 +154,10 @@ __device__ __forceinline__ long long block_scan(long long v, long long* sums, lo
   return total;
 }
 
-// By the whole CTA.  OVERHEAD: units of an item beside its tiles.  Up to 32 sequences and 32 blocks (a step of single tokens, one long chunk) every warp
+// By the whole CTA.  OVERHEAD: units of an item beside its tiles.  WHOLE: items are not cut, a stretch begins with the first item that begins in it (a
+// parameter of the kernels, as its few lines in all of them took 1.6% of 2048 tokens over 16385).  Up to 32 sequences and 32 blocks (a step of single tokens, one long chunk) every warp
 // works out for itself: what is waited for is the length of a call's shortest part.
-template <int BM, int THREADS, int OVERHEAD>
+template <int BM, int THREADS, int OVERHEAD, bool WHOLE>
 __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   static_assert(THREADS >= MAX_SEQS, "a thread for each sequence");
   Stretch st = {};
@@ -207,7 +209,7 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   st.all = per_head * p.c.kv_heads;
   st.ctas = (int)min((long long)gridDim.x, st.all);
   if ((int)blockIdx.x >= st.ctas) return st;
-  long long at[2], head[2], found[2];
+  long long at[2], head[2], found[2], units[2];
   int block[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {                    // where the stretch begins, and where the next one does
@@ -220,6 +222,7 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
     for (int i = 0; i < 2; ++i) {
       block[i] = __popc(__ballot_sync(~0u, before + n <= at[i] && lane < st.blocks));
       found[i] = __shfl_sync(~0u, before, block[i]);
+      if (WHOLE) units[i] = __shfl_sync(~0u, n, block[i]);
     }
   } else {
     long long done = 0, total = first;
@@ -230,6 +233,7 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
         if (before <= at[i] && at[i] < before + n) {
           m.block[i] = b0 + threadIdx.x;
           m.found[i] = before;
+          if (WHOLE) m.units[i] = n;
         }
       done += total;
       b0 += THREADS;
@@ -242,6 +246,7 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
     for (int i = 0; i < 2; ++i) {
       block[i] = m.block[i];
       found[i] = m.found[i];
+      if (WHOLE) units[i] = m.units[i];
     }
   }
   // tiles before a place: units before its block less what is no tile of them, and what is behind the block's own OVERHEAD
@@ -250,6 +255,14 @@ __device__ __forceinline__ Stretch plan(const AttnParams& p, Plan& m) {
   int off[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
+    if (WHOLE && at[i] > found[i]) {                 // the item is the stretch's before
+      at[i] = found[i] += units[i];
+      if (++block[i] == st.blocks) {
+        block[i] = 0;
+        ++head[i];
+        at[i] = found[i] = 0;
+      }
+    }
     off[i] = max((int)(at[i] - found[i]) - OVERHEAD, 0);
     number[i] = head[i] * tiles + found[i] - (long long)OVERHEAD * block[i] + off[i];
   }

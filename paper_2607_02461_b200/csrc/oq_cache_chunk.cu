@@ -155,7 +155,7 @@ __device__ __noinline__ float prepare_row(const AttnParams& p, const Item& it, i
   return rs.c;
 }
 
-template <int KIND, int D>
+template <int KIND, int D, bool WHOLE>
 __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant__ AttnParams p) {
   using S = Shape<KIND, D>;
   using F = Format<KIND, D>;
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  Stretch st = plan<CHUNK_ROWS, THREADS, CHUNK_OVERHEAD>(p, pm);
+  Stretch st = plan<CHUNK_ROWS, THREADS, CHUNK_OVERHEAD, WHOLE>(p, pm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -652,12 +652,16 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
 }
 
+template <int KIND, int D, bool WHOLE>
+cudaError_t go_as(const AttnParams& p, int ctas, cudaStream_t st) {
+  // (the attribute belongs to the device that is current, so it is set every time)
+  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<KIND, D, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<KIND, D>::SMEM);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(chunk_kernel<KIND, D, WHOLE>, ctas, THREADS, Shape<KIND, D>::SMEM, st, p);
+}
 template <int KIND, int D>
 cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
-  // (the attribute belongs to the device that is current, so it is set every time)
-  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<KIND, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<KIND, D>::SMEM);
-  if (e != cudaSuccess) return e;
-  return launch_dependent(chunk_kernel<KIND, D>, ctas, THREADS, Shape<KIND, D>::SMEM, st, p);
+  return p.whole ? go_as<KIND, D, true>(p, ctas, st) : go_as<KIND, D, false>(p, ctas, st);
 }
 
 }  // namespace chunk

@@ -90,7 +90,7 @@ struct Values {
   uint32_t scale[4];
 };
 
-template <int KIND, int D>
+template <int KIND, int D, bool WHOLE>
 __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_constant__ AttnParams p) {
   using F = Format<KIND, D>;
   using L = Lane<KIND, D>;
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  Stretch st = plan<BM, THREADS, FEW_OVERHEAD>(p, pm);
+  Stretch st = plan<BM, THREADS, FEW_OVERHEAD, WHOLE>(p, pm);
 
   while (st.count > 0) {
     const Item it = make_item<BM>(p, pm, st.head, st.block);
@@ -397,7 +397,7 @@ template <int KIND, int D>
 cudaError_t go(const AttnParams& p, int ctas, cudaStream_t st) {
   const size_t smem = (size_t)WARPS * FEW_ROWS * D * sizeof(float);
   static_assert(WARPS * FEW_ROWS * D * sizeof(float) + FEW_ROWS * (2 * (D + 8) + 4 + 8 * WARPS) + sizeof(Plan) + 256 <= 48 * 1024, "what every launch may have");
-  return launch_dependent(few_kernel<KIND, D>, ctas, THREADS, smem, st, p);
+  return p.whole ? launch_dependent(few_kernel<KIND, D, true>, ctas, THREADS, smem, st, p) : launch_dependent(few_kernel<KIND, D, false>, ctas, THREADS, smem, st, p);
 }
 
 }  // namespace few

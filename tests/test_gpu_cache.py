@@ -297,6 +297,18 @@ def test_long_cache_is_cut_and_joined(nq, kind, heads, kv_heads, d):
         _verify(q, pool, [nq], out, lse, **mask)
 
 
+@pytest.mark.parametrize("most", [384, 512, 528])
+def test_tables_at_the_length_from_which_items_are_cut(most):
+    """Up to 512 positions a row of the table, items are whole and no workspace is wanted; more than that, they are cut.  Many items a CTA and few."""
+    for new, kv_heads in (([1, 2, 40], 1), ([1] * 20 + [30] * 12, 12)):
+        lens = [most - 3 * i for i in range(len(new))]
+        pool = Pool(lens, 16, kv_heads, 64, "fp8", nan=True).fill(most)
+        pool.table = np.concatenate([pool.table, np.full((len(new), 40), -1)], 1)[:, :most // 16]
+        q = _bf16((sum(new), 2 * kv_heads, 64), 5, 0.1).cuda()
+        out, lse = _run(q, pool, new)
+        _verify(q, pool, new, out, lse)
+
+
 def test_more_blocks_than_threads_of_a_plan():
     """Blocks of queries that do not fit one round of the division of the work (chunks: 512 blocks of 256 rows; few rows: 256 blocks of 8)."""
     import torch

@@ -128,6 +128,7 @@ def test_bad_attention_arguments_are_refused():
         return B.lib().oq_cache_attention(args, 1 << 20 if size else None, size, None)
     assert code(total=0) == 0
     assert code() == 4                                           # no device; of 64 positions nothing is ever cut, so no workspace is wanted
+    assert code(c=_cache(max_pages=32, ld=32)) == 4              # nor of 512
     long = _cache(max_pages=64, ld=64)
     assert code(c=long) == 6 and code(c=long, size=1 << 30) == 4
     for field in ("Q", "out"):
