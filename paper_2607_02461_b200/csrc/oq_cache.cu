@@ -12,8 +12,8 @@
 // lanes, and a warp takes keys and values of some heads of one token, all requested before the first is used; the look-up of the token's
 // page runs beside those loads.
 //
-// Measured (B200, device time of captured calls): reading 32760 tokens of 40 heads of 128 back from e4m3 to bf16, 1.0 GB: 166 us = 6.1 TB/s, 0.93 of the copy rate;
-// writing 1560 tokens, 48 MB: 12 us, of which half is the launch and the chain start -> length -> page -> store; one token 3.3 us.
+// Measured (B200, device time of captured calls): reading 32760 tokens of 40 heads of 128 back from e4m3 to bf16, 1.0 GB: 166 us = 6.1 TB/s, 0.94 of the copy rate;
+// writing 1560 tokens, 48 MB: 10.8 us, of which half is the launch and the chain start -> length -> page -> store; one token 2.7 us.
 #include <string>
 
 #include "oq_cache.cuh"
