@@ -49,8 +49,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) cache_join_kernel(const __gri
 #pragma unroll
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
   factor = __shfl_sync(~0u, factor, 0);
-  const float ct = tame(factor, top);
-  auto weight = [&](const float4& ml) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * ct)); };
+  auto weight = [&](const float4& ml) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * factor)); };
   for (int i = lane; i < parts; i += 32) total += weight(p.part_ml[slot(i)]);
 #pragma unroll
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);

@@ -355,11 +355,6 @@ __device__ __forceinline__ RowScale row_scale(uint32_t largest, float scale_log2
   r.c = scale_log2 * __uint_as_float((uint32_t)(127 - 14 + min(e, 127)) << 23);
   return r;
 }
-// Scores of 2^26 and more in the exponent: there a product c s of 24 digits is off by more than the powers bear.  With a smaller c the largest
-// score still has all the weight (others differ from it by 2^-24 of it at least, and still fall short by units), and nothing overflows.
-constexpr float FAR = 67108864.f;
-__device__ __forceinline__ float tame(float c, float m) { return fabsf(m) * c > FAR && fabsf(m) < INFINITY ? FAR / fabsf(m) : c; }
-
 __device__ __forceinline__ float natural_lse(float m, float l, float c) {
   return l == 0.f ? -INFINITY : fmaf(m, c, log2f(l)) * 0.69314718055994531f;
 }
@@ -389,7 +384,7 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const Parts& q, i
       }
   };
   load(share);
-  float ct[ROWS] = {}, w[ROWS];                      // w: of part `lane`, where there are no more than the lanes
+  float w[ROWS];                                     // of part `lane`, where there are no more than the lanes
   float4 ml[ROWS];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
@@ -403,12 +398,11 @@ __device__ __forceinline__ void join_rows(const AttnParams& p, const Parts& q, i
   for (int i = lane + 32; i < q.parts; i += 32)
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __ldcg(p.part_ml + slot(i, r)).x);
-  auto weight = [&](const float4& x, int r) { return x.y == 0.f ? 0.f : x.y * (x.x == top[r] ? 1.f : exp2_fast((x.x - top[r]) * ct[r])); };
+  auto weight = [&](const float4& x, int r) { return x.y == 0.f ? 0.f : x.y * (x.x == top[r] ? 1.f : exp2_fast((x.x - top[r]) * factor[r])); };
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], d));
-    ct[r] = tame(factor[r], top[r]);
     w[r] = total[r] = lane < q.parts ? weight(ml[r], r) : 0.f;
   }
   for (int i = lane + 32; i < q.parts; i += 32)

@@ -46,6 +46,9 @@ constexpr int BM = 128;                            // rows of a query tile, of w
 constexpr int PIECE = 16, PIECES = BN / PIECE;     // keys that lie in one page whatever its size
 constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;
 constexpr float SLACK = 8.f;
+// A power is 2^(c s + shift) with shift = -c m rounded, so all of a row's are off by one factor, which cancels, as long as it stays small: it is 2^0.03 at most while
+// |c m| < 2^20.  The warps that have a row beyond that take s - m first.
+constexpr float FAR = 1048576.f;
 enum { W_Q = 50, W_KV = 51, W_KVFREE = 52, W_S = 53, W_P = 54, W_O = 55, W_RAW = 56, W_RAWFREE = 57 };
 static_assert(CHUNK_ROWS == 2 * BM, "two query tiles an item");
 
@@ -164,7 +167,6 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS + 2 * STAGES];
   __shared__ Plan pm;
   __shared__ int raw_keys[STAGES];        // what a stage holds: number of keys that exist, and the pieces of 16 whose page is missing in bits 8 .. 15
-  __shared__ float row_c[2 * BM];         // the rows' factors as they were before `tame`: the loop has no register for them
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -242,8 +244,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
     while (st.count > 0) {
       int rows, first, hi, lo, full_hi, full_lo, tiles, n_sink, skipped, seq, nk;
       bool turns;
-      float c = c_next;
-      row_c[t * BM + row] = c;                   // (read by this thread alone)
+      const float c = c_next;
       {
         const Item it = make_item<CHUNK_ROWS>(p, pm, st.head, st.block);
         rows = min(max(it.rows - t * BM, 0), BM);
@@ -276,6 +277,17 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       };
       int page = piece_page(0);
       float m = -INFINITY, l = 0.f, shift = 0.f;
+      float minus = 0.f;                                   // -m where a row of the warp is far, else 0: the powers are 2^(c (s + minus) + shift)
+      // Brings the reference to mn.  Returns what sums and O have to be multiplied by: the change of the power at the old reference, as the roundings of both references
+      // have it.
+      auto move_to = [&](float mn) {
+        const float old = m, from = fmaf(old + minus, c, shift);
+        m = mn;
+        const bool far = __any_sync(~0u, fabsf(m) * c > FAR && m > -INFINITY);
+        minus = far && m > -INFINITY ? -m : 0.f;
+        shift = far || m == -INFINITY ? 0.f : -m * c;
+        return old > -INFINITY ? exp2_fast(fmaf(old + minus, c, shift) - from) : 1.f;
+      };
       for (int j = 0; j < tiles; ++j, ++steps) {
         const int k0 = BN * (first + j + (j < n_sink ? 0 : skipped));
         const uint32_t there = __ballot_sync(~0u, page >= 0);
@@ -334,25 +346,27 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           for (int e = 2; e < BN / 4; e += 2) mx[q] = max3(mx[q], __uint_as_float(sr[4 * e + q]), __uint_as_float(sr[4 * e + 4 + q]));
         }
         const float mn = max3(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]), m);
-        if (j == 0) {
-          m = mn;
-          c = tame(c, m);
-          shift = m == -INFINITY ? 0.f : -m * c;
-        } else if (__any_sync(~0u, (mn - m) * c > SLACK)) {
-          // (S_t of this key tile is there, so O_t holds the tiles before it and nothing is writing it)
-          c = tame(c, mn);
-          const float a = m == mn ? 1.f : exp2_fast((m - mn) * c);
-          m = mn;
+        if (__any_sync(~0u, (mn - m) * c > SLACK)) {
+          // (S_t of this key tile is there, so O_t holds the tiles before it, none at j == 0, and nothing is writing it)
+          const float a = move_to(mn);
           l *= a;
-          shift = m == -INFINITY ? 0.f : -m * c;
 #pragma unroll 1
-          for (int x = 0; x < D / 16; ++x) {
+          for (int x = j == 0 ? D / 16 : 0; x < D / 16; ++x) {
             uint32_t o[16];
             tmem_load16_at(col_o + 16u * x, o);
             tmem_use16(o);
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
             tmem_store16(col_o + 16u * x, o);
+          }
+        }
+        if (__any_sync(~0u, minus != 0.f)) {
+#pragma unroll
+          for (int e = 0; e < BN; e += 2) {
+            float x = __uint_as_float(sr[e]), y = __uint_as_float(sr[e + 1]);
+            add2(x, y, minus, minus);
+            sr[e] = __float_as_uint(x);
+            sr[e + 1] = __float_as_uint(y);
           }
         }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -419,10 +433,9 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         }
         if (mine) {
           // the powers had m c rounded in them, which shows in the sum (not in the weights' ratios)
-          if (l != 0.f && m > -INFINITY) l *= exp2_fast(-fmaf(m, c, shift));
-          const float factor = row_c[t * BM + row];
-          if (!whole) p.part_ml[slot_row] = make_float4(m, l, factor, 0.f);
-          else if (p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(m, l, factor);
+          if (l != 0.f && m > -INFINITY) l *= exp2_fast(-fmaf(m + minus, c, shift));
+          if (!whole) p.part_ml[slot_row] = make_float4(m, l, c, 0.f);
+          else if (p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(m, l, c);
         }
         tc_fence_before();                        // (the next item's first P, which lets O be overwritten, comes after this)
       }

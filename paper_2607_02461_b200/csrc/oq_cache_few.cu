@@ -257,7 +257,6 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
           float x = fmaxf(m[e], fmaxf(s[e], s[e + 2]));
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
-          c[e] = tame(c[e], x);
           const float a = x == m[e] ? 1.f : exp2_fast((m[e] - x) * c[e]);
           m[e] = x;
           l[e] *= a;
@@ -341,7 +340,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       float top = -INFINITY, total = 0.f, acc[N];
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) top = fmaxf(top, m_s[w][r]);
-      const float cr = tame(c_s[r], top);
+      const float cr = c_s[r];
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] = 0.f;
 #pragma unroll

@@ -1,0 +1,95 @@
+"""Softmax weights of attention over the paged cache where scores lie far from zero.  Against the formula in fp64 over what the cache holds (reading it
+back is exact).
+
+Tolerances, derived.  Weights are rounded to fp16 (half a unit, 2^-11 of the weight), the output once to bf16 (2^-8), and 1e-4 of the weights is left for scores and
+powers (fp32).  Per element: |error| <= 2^-8 |out| + (2^-11 + 1e-4) sum_j w_j |v_j|; lse to 1e-5 (1 + |lse|)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_02461_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TOP = {"fp8": 57344.0, "fp4": 49152.0}
+
+
+class Cache:
+    """One sequence whose keys and values [n, kv_heads, d] are written into pages in falling order; width: positions of the table's row."""
+
+    def __init__(self, k, v, kind, width=0, page=64):
+        n, heads, self.d = k.shape
+        held = -(-n // page)
+        self.kind, self.pages = kind, B.oq_cache_alloc(held, page, heads, self.d, kind)
+        table = list(range(held))[::-1] + [-1] * (max(width // page, held) - held)
+        self.table, self.lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([table], [n]))
+        B.oq_cache_write(self.pages, k, v, self.table, self.lens, kind=kind)
+        self.k, self.v = (x.double() for x in B.oq_cache_read(self.pages, self.d, self.table, self.lens, None, n, kind=kind, out_dtype=torch.float32))
+
+    def attend(self, q, **kw):
+        out = B.oq_cache_attention(q, self.pages, self.table, self.lens, kind=self.kind, want_lse=True, **kw)
+        torch.cuda.synchronize()
+        assert B.oq_device_status() == 0
+        return out
+
+    def plain(self, q, left=-1, right=0, sinks=0, scale=0.0):
+        """(out [T, H, D], lse [H, T], sum of weights times |v|) in fp64."""
+        n, heads, d = q.shape
+        nk, kv_heads = self.k.shape[:2]
+        group = heads // kv_heads
+        k, v = (x.repeat_interleave(group, 1) for x in (self.k, self.v))
+        z = (scale or d ** -0.5) * torch.einsum("ihd,jhd->hij", q.double(), k)
+        at, j = torch.arange(n, device="cuda")[:, None] + nk - n, torch.arange(nk, device="cuda")[None]
+        seen = (j <= at + right) if right >= 0 else torch.ones_like(j <= at)
+        if left >= 0:
+            seen &= (j >= at - left) | (j < sinks)
+        z = z.masked_fill(~seen, -np.inf)
+        lse = torch.logsumexp(z, 2)
+        w = torch.softmax(z, 2)
+        return torch.einsum("hij,jhd->ihd", w, v), lse, torch.einsum("hij,jhd->ihd", w, v.abs())
+
+
+def _verify(got, ref):
+    out, lse, size = ref
+    assert bool(torch.isfinite(got[0]).all())
+    err = (got[0].double() - out).abs()
+    bound = 2.0 ** -8 * out.abs() + (2.0 ** -11 + 1e-4) * size + 1e-30
+    worst = (err / bound).amax((0, 2))
+    assert bool((err <= bound).all()), f"error over bound of each head: {worst.tolist()}"
+    far = (got[1].double() - lse).abs() / (1 + lse.abs())
+    assert bool((far <= 1e-5).all()), f"lse of each head: {far.amax(1).tolist()}"
+
+
+@pytest.mark.parametrize("nk,width", [(450, 512), (450, 40000), (6000, 6016), (40000, 40000)])
+@pytest.mark.parametrize("nq", [1, 3, 60])
+@pytest.mark.parametrize("kind", ["fp8", "fp4"])
+def test_scores_far_from_zero(kind, nq, nk, width):
+    """Scores up to 2^48 whose differences fp32 holds exactly, so the weights are known: the largest among the first keys, in the middle or among the last, hugely
+    negative ones before and behind ordinary ones, and slowly rising ones far from zero (by whole numbers, all of them small beside their common part)."""
+    big, third = TOP[kind], nk // 3
+    steps = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0])
+    j = torch.arange(nk)
+    k = torch.zeros((nk, 1, 64))
+    first, middle, last = j < third, (j >= third) & (j < nk - third), j >= nk - third
+    k[:, 0, 0] = big * (first.float() - last.float())
+    k[:, 0, 33] = -big * (~middle).float()
+    k[middle, 0, 1] = -steps[j[middle] % 6]
+    ramp = torch.zeros((nk, 1, 64))
+    ramp[:, 0, 0] = 2048.0
+    ramp[:, 0, 33] = steps[(j * 6 // nk).long()]               # rising with the place ...
+    ramp[:, 0, 34] = steps[(5 - j * 6 // nk).long()]           # ... and falling
+    v = torch.randn((nk, 2, 64), generator=torch.Generator().manual_seed(nk))
+    cache = Cache(torch.cat((k, ramp), 1).cuda(), v.cuda(), kind, width)
+    # a row: coordinates of the query.  (scale 1/8: a query of 8 makes a key's number the score)
+    rows = [{0: 2.0 ** 20, 1: 8}, {0: -2.0 ** 20, 1: 8}, {33: 2.0 ** 20, 1: 8}, {33: -2.0 ** 20, 1: 8}, {33: 2.0 ** 36, 1: 8}, {33: 2.0 ** 10, 1: 8}, {33: 2.0 ** 14, 1: 24},
+            {0: 2.0 ** 30, 33: 2.0 ** 30}]
+    slow = [{0: 2.0 ** 4, 33: 8}, {0: -2.0 ** 4, 33: 24}, {0: 2.0 ** 10, 33: 8}, {0: 2.0 ** 10, 33: 24}, {0: -2.0 ** 10, 34: 24}, {0: 2.0 ** 14, 33: 8}, {0: -2.0 ** 14, 34: 8},
+            {0: 2.0 ** 20, 33: 128}]
+    q = torch.zeros((nq, 16, 64))
+    for h, row in enumerate(rows + slow):
+        for c, x in row.items():
+            q[:, h, c] = x
+    q = q.bfloat16().cuda()
+    for mask in (dict(right=-1), dict()):
+        got, ref = cache.attend(q, **mask), cache.plain(q, **mask)
+        _verify(got, ref)
