@@ -417,7 +417,7 @@ int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_
  *   max_q    a hint: no sequence has more new tokens (1 in a step of single tokens).  0: not known.  Results do not depend on its being true
  *   scale    0: 1 / sqrt(head_dim)
  * What is cached is decoded exactly, and queries lose nothing that matters (the parts of a head more than 2^29 below its largest); the products run on the tensor cores in fp16 with fp32 accumulation, the softmax weights are
- * rounded to fp16 for the second one, everything else is fp32.  Items of work are cut along the keys so that all SMs get the same share, whatever
+ * rounded to fp16 for the second one (by 2^-11 of a weight at most, or 2^-36 of the row's largest where that is more), everything else is fp32.  Items of work are cut along the keys so that all SMs get the same share, whatever
  * the lengths, unless a row of the table holds no more than 512 positions; the workspace (dev, 16-byte aligned, oq_cache_attention_workspace_bytes
  * bytes, 0 when nothing is cut) holds the parts.  Results are bit-reproducible.
  * Asynchronous on `stream`.  total_q == 0 launches nothing.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, NOMEM (workspace), CUDA. */

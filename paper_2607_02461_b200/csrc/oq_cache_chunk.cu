@@ -3,8 +3,8 @@
 // One pass over the keys with a running reference m and a running sum: with a row's factor c the kernel holds l = sum_j 2^(c (s_j - m)) and
 // O = sum_j 2^(c (s_j - m)) v_j for any m that keeps the powers in range, so m follows the running maximum only when that has moved by more
 // than 2^SLACK; then O and l are multiplied by 2^(c (m - m')).  The sums are fp32; the powers are rounded once, to fp16, as the tensor cores'
-// operand (l sums the unrounded ones).  That is 2^-11 where the output's own rounding to bf16 is 2^-9: results differ from those of unrounded
-// powers by less than a tenth of what that rounding does.
+// operand (l sums the unrounded ones), after a multiplication that keeps them in fp16's range (see HEAD): 2^-11 of a weight, or 2^-36 of the
+// largest where that is more.  The output's own rounding to bf16 is 2^-8 of a value.
 //
 // Bound: the tensor cores and the exponentials alike, as without a cache (256 rows x 128 keys x 128 coordinates: 2048 cycles of products, 2048 of
 // exponentials).  What the cache adds, decoding 2 x 128 x 128 elements for the 256 rows, is done by four warps of their own beside them: 16 bytes
@@ -45,8 +45,7 @@ constexpr int CONVERT_WARP = 8, MMA_WARP = 12, LOAD_WARP = 14;
 constexpr int BM = 128;                            // rows of a query tile, of which a CTA has two
 constexpr int PIECE = 16, PIECES = BN / PIECE;     // keys that lie in one page whatever its size
 constexpr uint32_t COL_S = 0, COL_P = 0, COL_O = BN;
-constexpr float SLACK = 8.f;
-// A power is 2^(c s + shift) with shift = -c m rounded, so all of a row's are off by one factor, which cancels, as long as it stays small: it is 2^0.03 at most while
+// A power is 2^(c s + shift) with shift = HEAD - c m rounded, so all of a row's are off by one factor, which cancels, as long as it stays small: it is 2^0.06 at most while
 // |c m| < 2^20.  The warps that have a row beyond that take s - m first.
 constexpr float FAR = 1048576.f;
 enum { W_Q = 50, W_KV = 51, W_KVFREE = 52, W_S = 53, W_P = 54, W_O = 55, W_RAW = 56, W_RAWFREE = 57 };
@@ -285,7 +284,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
         m = mn;
         const bool far = __any_sync(~0u, fabsf(m) * c > FAR && m > -INFINITY);
         minus = far && m > -INFINITY ? -m : 0.f;
-        shift = far || m == -INFINITY ? 0.f : -m * c;
+        shift = far || m == -INFINITY ? HEAD : fmaf(-m, c, HEAD);
         return old > -INFINITY ? exp2_fast(fmaf(old + minus, c, shift) - from) : 1.f;
       };
       for (int j = 0; j < tiles; ++j, ++steps) {
@@ -432,7 +431,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           }
         }
         if (mine) {
-          // the powers had m c rounded in them, which shows in the sum (not in the weights' ratios)
+          // the powers had HEAD and m c, rounded, in them, which shows in the sum (not in the weights' ratios)
           if (l != 0.f && m > -INFINITY) l *= exp2_fast(-fmaf(m + minus, c, shift));
           if (!whole) p.part_ml[slot_row] = make_float4(m, l, c, 0.f);
           else if (p.lse) p.lse[(long long)head * p.total_q + i] = natural_lse(m, l, c);

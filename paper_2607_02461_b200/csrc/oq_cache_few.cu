@@ -28,7 +28,6 @@ namespace cache {
 namespace few {
 
 constexpr int WARPS = 8, THREADS = 32 * WARPS;
-constexpr float SLACK = 8.f;                       // powers stay below 2^8
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -272,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float ref = m[e & 1] == -INFINITY ? 0.f : m[e & 1];
-        w[e] = exp2_fast((s[e] - ref) * c[e & 1]);
+        w[e] = exp2_fast(fmaf(s[e] - ref, c[e & 1], HEAD));
         l[e & 1] += w[e];
       }
       b[0] = transpose8(pack_f16(w[0], w[1]));
@@ -352,6 +351,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         for (int e = 0; e < N; ++e) acc[e] = fmaf(part[(w * BM + r) * D + N * lane + e], a, acc[e]);
       }
       const float inv = total == 0.f ? 0.f : 1.f / total;
+      total *= UNHEAD;
       if (whole) {
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] *= inv;

@@ -1,8 +1,9 @@
-"""Softmax weights of attention over the paged cache where scores lie far from zero.  Against the formula in fp64 over what the cache holds (reading it
-back is exact).
+"""Softmax weights of attention over the paged cache where they span a wide range: a first key that takes nearly all the weight, scores far from
+zero.  Against the formula in fp64 over what the cache holds (reading it back is exact).
 
-Tolerances, derived.  Weights are rounded to fp16 (half a unit, 2^-11 of the weight), the output once to bf16 (2^-8), and 1e-4 of the weights is left for scores and
-powers (fp32).  Per element: |error| <= 2^-8 |out| + (2^-11 + 1e-4) sum_j w_j |v_j|; lse to 1e-5 (1 + |lse|)."""
+Tolerances, derived.  Weights are rounded to fp16, relative to 2^-11 of the largest one seen so far at the least: half a unit, 2^-11 of the weight, or half
+the smallest fp16, 2^-25 * 2^-11 = 2^-36 of the largest weight, where that is more.  The output is rounded once to bf16 (2^-8), and 1e-4 of the weights is left for scores and
+powers (fp32).  Per element: |error| <= 2^-8 |out| + (2^-11 + 1e-4) sum_j w_j |v_j| + 2^-36 max_j w_j sum_j |v_j|; lse to 1e-5 (1 + |lse|)."""
 import numpy as np
 import pytest
 import torch
@@ -33,7 +34,7 @@ class Cache:
         return out
 
     def plain(self, q, left=-1, right=0, sinks=0, scale=0.0):
-        """(out [T, H, D], lse [H, T], sum of weights times |v|) in fp64."""
+        """(out [T, H, D], lse [H, T], sum of weights times |v|, largest weight times the sum of |v|) in fp64."""
         n, heads, d = q.shape
         nk, kv_heads = self.k.shape[:2]
         group = heads // kv_heads
@@ -46,18 +47,51 @@ class Cache:
         z = z.masked_fill(~seen, -np.inf)
         lse = torch.logsumexp(z, 2)
         w = torch.softmax(z, 2)
-        return torch.einsum("hij,jhd->ihd", w, v), lse, torch.einsum("hij,jhd->ihd", w, v.abs())
+        a = v.abs()
+        ends = torch.einsum("hij,jhd->ihd", w, v), lse, torch.einsum("hij,jhd->ihd", w, a)
+        return *ends, w.amax(2).T[..., None] * torch.einsum("ij,jhd->ihd", seen.double(), a)
 
 
 def _verify(got, ref):
-    out, lse, size = ref
+    out, lse, size, floor = ref
     assert bool(torch.isfinite(got[0]).all())
     err = (got[0].double() - out).abs()
-    bound = 2.0 ** -8 * out.abs() + (2.0 ** -11 + 1e-4) * size + 1e-30
+    bound = 2.0 ** -8 * out.abs() + (2.0 ** -11 + 1e-4) * size + 2.0 ** -36 * floor + 1e-30
     worst = (err / bound).amax((0, 2))
     assert bool((err <= bound).all()), f"error over bound of each head: {worst.tolist()}"
     far = (got[1].double() - lse).abs() / (1 + lse.abs())
     assert bool((far <= 1e-5).all()), f"lse of each head: {far.amax(1).tolist()}"
+
+
+# nk, positions of the table (up to 512 items are whole, beyond that they are cut along the keys)
+LENGTHS = [(300, 320), (500, 40000), (32760, 32768), (131072, 131072)]
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("nq", [1, 40])                       # both kernels
+@pytest.mark.parametrize("kind,d", [("fp8", 64), ("fp4", 128)])
+@pytest.mark.parametrize("nk,width", LENGTHS)
+def test_a_key_that_takes_nearly_all_the_weight(nk, width, kind, d, nq, where):
+    """One key is 2^gap times as heavy as each of the others and has a value of nothing, or a hundredth of theirs: the others make the result."""
+    gaps = [4.0, 12.0, 16.0, 20.0, 22.0, 24.0, 25.0, 26.0, 28.0, 32.0]
+    g = torch.Generator(device="cuda").manual_seed(nk + nq)
+    at = {"first": 0, "middle": nk // 2, "last": nk - nq}[where]
+    k = torch.randn((nk, 2, d), generator=g, device="cuda")
+    k[:, :, 0] = 0.0
+    k[at] = 0.0
+    k[at, :, 0] = 1.0
+    v = 1 + 0.25 * torch.randn((nk, 2, d), generator=g, device="cuda")
+    v[at, 0] = 0.0
+    v[at, 1] *= 0.01
+    cache = Cache(k, v, kind, width)
+    q = 0.3 * d ** -0.5 * torch.randn((nq, 2, len(gaps), d), generator=g, device="cuda")       # the others' scores: 0.3 in standard deviation
+    q[..., 0] = torch.tensor(gaps, device="cuda") * np.log(2.0)
+    q = q.flatten(1, 2).bfloat16()
+    got, ref = cache.attend(q, scale=1.0), cache.plain(q, scale=1.0)
+    _verify(got, ref)
+    near = (torch.tensor(gaps * 2, device="cuda") <= 25).nonzero()[:, 0]
+    diff = (got[0].double() - ref[0])[:, near]
+    assert float(diff.norm() / ref[0][:, near].norm()) <= 2.4e-3
 
 
 @pytest.mark.parametrize("nk,width", [(450, 512), (450, 40000), (6000, 6016), (40000, 40000)])
