@@ -352,7 +352,9 @@ __device__ __forceinline__ RowScale row_scale(uint32_t largest, float scale_log2
   const int e = max((int)(largest >> 23) - 127, -100);
   RowScale r;
   r.mul = largest >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-  r.c = scale_log2 * __uint_as_float((uint32_t)(127 - 14 + min(e, 127)) << 23);
+  // (kept above 0, since minus infinity in a place that is not seen times 0 is NaN, and below infinity, which times a score of 0 is NaN: scores beyond these ends are
+  // alike, or differ by more than the powers bear, with any factor of the kind)
+  r.c = fminf(fmaxf(scale_log2 * __uint_as_float((uint32_t)(127 - 14 + min(e, 127)) << 23), 0x1p-126f), 0x1.fffffep127f);
   return r;
 }
 // The powers of two that become the second product's fp16 operand, 2^(c (s - m)), are held times 2^HEAD: the reference m follows the maximum when that is 2^SLACK above it, so

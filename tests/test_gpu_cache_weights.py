@@ -1,5 +1,5 @@
 """Softmax weights of attention over the paged cache where they span a wide range: a first key that takes nearly all the weight, scores far from
-zero.  Against the formula in fp64 over what the cache holds (reading it back is exact).
+zero, scales at the ends of fp32.  Against the formula in fp64 over what the cache holds (reading it back is exact).
 
 Tolerances, derived.  Weights are rounded to fp16, relative to 2^-11 of the largest one seen so far at the least: half a unit, 2^-11 of the weight, or half
 the smallest fp16, 2^-25 * 2^-11 = 2^-36 of the largest weight, where that is more.  The output is rounded once to bf16 (2^-8), and 1e-4 of the weights is left for scores and
@@ -127,3 +127,24 @@ def test_scores_far_from_zero(kind, nq, nk, width):
     for mask in (dict(right=-1), dict()):
         got, ref = cache.attend(q, **mask), cache.plain(q, **mask)
         _verify(got, ref)
+
+
+@pytest.mark.parametrize("nk,width", [(200, 256), (3000, 3008)])
+@pytest.mark.parametrize("nq", [2, 40])
+def test_scales_at_the_ends_of_fp32(nq, nk, width):
+    """Queries of zero, tiny and huge ones, with scales from 1e-38 to 9e29: uniform weights where the scores are all alike, however small or large the factor is."""
+    g = torch.Generator().manual_seed(nk)
+    k, v = torch.randn((nk, 1, 64), generator=g), torch.randn((nk, 1, 64), generator=g)
+    cache, flat = Cache(k.cuda(), v.cuda(), "fp8", width), Cache(0 * k.cuda(), v.cuda(), "fp8", width)
+    q = torch.randn((nq, 4, 64), generator=g)
+    q[:, 0] = 0.0
+    q[:, 1] *= 1e-36
+    q[:, 2] *= 1e-12
+    mask = dict(left=nk // 2, sinks=3)
+    for scale in (1e-38, 1e-13, 1e-11):
+        x = q.bfloat16().cuda()
+        _verify(cache.attend(x, scale=scale, **mask), cache.plain(x, scale=scale, **mask))
+    q[:, 3] *= 1e30
+    x = q.bfloat16().cuda()
+    for scale in (1.0, 9e29):                                  # keys of zero: all scores are 0
+        _verify(flat.attend(x, scale=scale, **mask), flat.plain(x, scale=scale, **mask))
