@@ -402,7 +402,7 @@ int oq_cache_block_bytes(int kind, int page_size, int head_dim, size_t* bytes);
 int oq_cache_write(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_rows* V, int x_dtype, const int* start, int total, void* stream);
 
 /* The reverse: reads the last start[s + 1] - start[s] tokens of each sequence into K and V (either may be NULL), of y_dtype.  Every
- * cached value is an exact bf16.  Tokens of no sequence are left as they are, those before position 0 become 0.  Strides at least head_dim. */
+ * cached value is an exact bf16.  Tokens of no sequence are left as they are, those before position 0 become 0.  Strides at least head_dim, no row over another. */
 int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_rows* V, int y_dtype, const int* start, int total, void* stream);
 
 /* Softmax attention of the new tokens over all that is cached, themselves included (they have been written).  Masks as for oq_attention:
@@ -411,7 +411,7 @@ int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_
  * out = sum_j softmax_j(scale * q . k_j) v_j, lse = log sum_j exp(scale * q . k_j); a query that sees nothing gets 0 and -inf.  A query that holds
  * NaN or an infinity gets NaN where it sees something.
  *   Q        dev bf16, strides in elements, multiples of 8, not negative; 16-byte aligned
- *   out      dev bf16, strides at least head_dim; must not overlap Q or the pages.   lse dev fp32 [n_heads][total_q], or NULL
+ *   out      dev bf16, strides at least head_dim, no row over another; must not overlap Q or the pages.   lse dev fp32 [n_heads][total_q], or NULL
  *   q_start  dev int32 [n_seqs + 1] (see start above), NULL: one sequence.  Queries of no sequence are not written
  *   n_heads  a multiple of the cache's heads; query head h reads head h / (n_heads / n_kv_heads)
  *   max_q    a hint: no sequence has more new tokens (1 in a step of single tokens).  0: not known.  Results do not depend on its being true

@@ -222,6 +222,29 @@ __global__ void __launch_bounds__(32 * WARPS) read_kernel(const __grid_constant_
   }
 }
 
+bool rows_meet(long long apart, long long tokens, long long heads, long long ld_token, long long ld_head, int width) {
+  using wide = __int128;
+  if (tokens < 2) ld_token = 0;
+  if (heads < 2) ld_head = 0;
+  const wide all_heads = (wide)(heads - 1) * ld_head + width, all_tokens = (wide)(tokens - 1) * ld_token + width;
+  if (apart == 0) {                                  // the two usual orders of one set
+    if (tokens < 2 || heads < 2 || ld_token >= all_heads || ld_head >= all_tokens) return false;
+  } else {                                           // two sets, one behind the other
+    const wide reach = all_heads + all_tokens - width;
+    if (apart >= reach || -(wide)apart >= reach) return false;
+  }
+  // else: rows dh heads and dt tokens from each other are apart + dh ld_head + dt ld_token apart; of the dt only those beside the quotient can be close
+  for (long long dh = 1 - heads; dh < heads; ++dh) {
+    const wide at = (wide)apart + (wide)dh * ld_head;
+    const long long near = ld_token ? (long long)(-at / ld_token) : 0;
+    for (long long dt = near - 1; dt <= near + 1; ++dt) {
+      const wide d = at + (wide)dt * ld_token;
+      if (dt > -tokens && dt < tokens && (apart || dh || dt) && d > -width && d < width) return true;
+    }
+  }
+  return false;
+}
+
 int make_view(const oq_cache* c, const char* what, View* view) {
   const std::string w(what);
   if (!c) return fail(OQ_ERR_INVALID_ARG, w + ": NULL cache");
@@ -276,6 +299,15 @@ static int copy(const char* what, const oq_cache* c, const oq_cache_rows* k, con
     const long long least = WRITE ? 0 : c->head_dim;          // rows that are read may lie over each other
     if ((total > 1 && r.ld_token < least) || (c->n_kv_heads > 1 && r.ld_head < least)) return fail(OQ_ERR_INVALID_ARG, w + ": bad strides");
     (i ? p.v : p.k) = Rows{r.X, total > 1 ? r.ld_token : 0, c->n_kv_heads > 1 ? r.ld_head : 0};
+    if (!WRITE && total > 0 && rows_meet(0, total, c->n_kv_heads, r.ld_token, r.ld_head, c->head_dim))
+      return fail(OQ_ERR_INVALID_ARG, w + ": rows of the output lie over each other");
+  }
+  if (!WRITE && total > 0 && k && v) {
+    // (rows of different strides are only seen to meet where both begin)
+    const long long apart = (reinterpret_cast<intptr_t>(v->X) - reinterpret_cast<intptr_t>(k->X)) / (16 / unit);
+    const bool alike = p.k.ld_token == p.v.ld_token && p.k.ld_head == p.v.ld_head;
+    if (apart == 0 || (alike && rows_meet(apart, total, c->n_kv_heads, p.k.ld_token, p.k.ld_head, c->head_dim)))
+      return fail(OQ_ERR_INVALID_ARG, w + ": keys and values lie over each other");
   }
   if (total == 0) return OQ_OK;
   p.start = start;

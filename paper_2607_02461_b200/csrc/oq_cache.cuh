@@ -86,5 +86,9 @@ __device__ __forceinline__ void e2m1_to_f16(uint32_t w, uint32_t& a, uint32_t& b
 // The part that `what` has in common: checks and fills the view (host).
 int make_view(const oq_cache* c, const char* what, View* view);
 
+// Rows of `width` elements, row (h, t) at h * ld_head + t * ld_token, each stride at least the width where it is used: whether one of them lies over a row of a second such set,
+// which begins `apart` elements behind the first, or (apart == 0) over another one of its own (host).
+bool rows_meet(long long apart, long long tokens, long long heads, long long ld_token, long long ld_head, int width);
+
 }  // namespace cache
 }  // namespace oq

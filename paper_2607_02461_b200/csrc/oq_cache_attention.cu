@@ -211,6 +211,11 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
   p.ldo = a->total_q > 1 ? a->ldo_token : 0;
   p.hdo = a->n_heads > 1 ? a->ldo_head : 0;
+  if (rows_meet(0, a->total_q, a->n_heads, p.ldo, p.hdo, d)) return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: rows of out lie over each other");
+  // (Q and out of different strides are only seen to meet where both begin)
+  const long long apart = (reinterpret_cast<intptr_t>(a->out) - reinterpret_cast<intptr_t>(a->Q)) / 2;
+  if (apart == 0 || (p.ldq == p.ldo && p.hdq == p.hdo && rows_meet(apart, a->total_q, a->n_heads, p.ldo, p.hdo, d)))
+    return fail(OQ_ERR_INVALID_ARG, "oq_cache_attention: out lies over Q");
   p.wide_out = reinterpret_cast<uintptr_t>(a->out) % 32 == 0 && p.ldo % 16 == 0 && p.hdo % 16 == 0;
   p.lse = a->lse;
   p.q_start = a->q_start;

@@ -140,3 +140,46 @@ def test_bad_attention_arguments_are_refused():
     assert code(sinks=-1) == 1 and code(scale=-1.0) == 1 and code(scale=float("nan")) == 1 and code(scale=1e30) == 1
     assert code(total=1 << 30, heads=4) == 2
     assert code(c=_cache(seqs=2), start=0) == 1
+
+
+def _rows(tokens, heads, lt, lh, d):
+    return [h * lh + t * lt + c for t in range(tokens) for h in range(heads) for c in range(d)]
+
+
+def _layouts(d, unit):
+    """(tokens, heads, strides) with strides of at least a row: rows side by side in both orders, padded, dealt out between each other, and over each other."""
+    g = np.random.default_rng(3)
+    out = [(3, 2, 2 * d, d), (3, 2, d, 3 * d), (3, 2, d, d), (3, 2, d, 2 * d), (4, 3, 2 * d, 8 * d), (4, 3, 3 * d, 2 * d), (1, 4, 0, d), (4, 1, d, 0), (2, 2, d, d + unit), (3, 3, 4 * d, 2 * d)]
+    return out + [(int(t), int(h), int(a) * unit, int(b) * unit) for t, h, a, b in zip(*g.integers(1, 5, (2, 40)), *g.integers(d // unit, 5 * d // unit, (2, 40)))]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_read_rows_over_each_other_are_refused(dtype):
+    """Against all addresses: rows of one output, and keys over values."""
+    d, unit, size = 64, (8, 4)[dtype], (2, 4)[dtype]
+    L, pack = B.lib(), B._CACHE_ROWS.pack
+    for tokens, heads, lt, lh in _layouts(d, unit):
+        rows = _rows(tokens, heads, lt, lh, d)
+        clash = len(set(rows)) < len(rows)
+        for other in [None] + [unit * x for x in (-40, -32, -24, -16, -9, -8, -7, 0, 1, 8, 9, 16, 24, 32, 40, 96)]:
+            v = None if other is None else pack((1 << 20) + size * other, lt, lh)
+            meet = other is not None and bool(set(rows) & {x + other for x in rows})
+            assert L.oq_cache_read(_cache(heads=heads), pack(1 << 20, lt, lh), v, dtype, 65536, tokens, None) == (1 if clash or meet else 4), (tokens, heads, lt, lh, other)
+    assert L.oq_cache_read(_cache(), pack(1 << 20, 128, 64), pack(1 << 20, 256, 64), dtype, 65536, 4, None) == 1        # one beginning, other strides
+    assert L.oq_cache_write(_cache(), pack(1 << 20, 0, 64), pack(1 << 20, 0, 64), dtype, 65536, 4, None) == 4           # what is only read may
+
+
+def test_results_over_queries_or_each_other_are_refused():
+    d, L = 64, B.lib()
+    def code(tokens, heads, q, ql, out, ol):
+        return L.oq_cache_attention(_cache(heads=heads) + B.struct.pack("@PqqPqqPPiiiiiif", q, *ql, out, *ol, 0, 65536, tokens, heads, 0, -1, 0, 0, 0.0), None, 0, None)
+    base = 1 << 20
+    for tokens, heads, lt, lh in _layouts(d, 8):
+        rows = _rows(tokens, heads, lt, lh, d)
+        clash = len(set(rows)) < len(rows)
+        assert code(tokens, heads, 2 * base, (0, 0), base, (lt, lh)) == (1 if clash else 4)
+        for other in (-256, -192, -128, -72, -64, -56, 0, 8, 64, 72, 128, 192, 256, 768):
+            meet = bool(set(rows) & {x + other for x in rows})
+            assert code(tokens, heads, base, (lt, lh), base + 2 * other, (lt, lh)) == (1 if clash or meet else 4), (tokens, heads, lt, lh, other)
+    assert code(3, 2, base, (0, 0), base, (128, 64)) == 1        # queries broadcast from where the results begin
+    assert code(1, 1, base, (999 * 8, 8), base + 128, (8, 999 * 8)) == 4      # strides of one token and one head are not used
