@@ -121,8 +121,9 @@ class AttentionLayer:
         if cache is None:
             o = B.oq_attention(q, k, v, q_start=starts, k_start=starts, left=left, right=right, sinks=sinks).flatten(1)
         else:
-            B.oq_cache_write(cache.pages, k, v, cache.table, cache.lens, starts, kind=cache.kind)
-            o = B.oq_cache_attention(q, cache.pages, cache.table, cache.lens, starts, kind=cache.kind, left=left, right=right, sinks=sinks).flatten(1)
+            form = dict(kind=cache.kind, page_size=cache.page_size)
+            B.oq_cache_write(cache.pages, k, v, cache.table, cache.lens, starts, **form)
+            o = B.oq_cache_attention(q, cache.pages, cache.table, cache.lens, starts, left=left, right=right, sinks=sinks, **form).flatten(1)
         y = self.proj(o)
         if keep is not None:
             keep.update(q=q, k=k, v=v, o=o, y_shared=y.clone())

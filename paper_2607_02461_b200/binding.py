@@ -650,7 +650,7 @@ def oq_cache_alloc(n_pages, page_size, kv_heads, head_dim, kind="fp8", device="c
     return torch.zeros((n_pages, kv_heads, oq_cache_block_bytes(page_size, head_dim, kind)), dtype=torch.uint8, device=device)
 
 
-def _cache_fields(what, torch, pages, head_dim, kind, table, lens, start, device):
+def _cache_fields(what, torch, pages, head_dim, kind, table, lens, start, device, page_size):
     """Checks what the calls on a cache have in common.  Returns the fields of oq_cache and the address of start."""
     bits = CACHE_KINDS.get(kind)
     if bits is None:
@@ -668,6 +668,8 @@ def _cache_fields(what, torch, pages, head_dim, kind, table, lens, start, device
     size, odd = divmod(block, head_dim * (4 * bits + 1) // 16)        # bytes of a token's keys, values and scales: 2 (d * bits / 8 + d / 32)
     if odd:
         raise OqError(1, f"{what}: no number of tokens of this kind and head_dim fills a block of these pages")
+    if page_size is not None and page_size != size:
+        raise OqError(1, f"{what}: with this kind and head_dim, blocks of these pages hold {size} tokens, not {page_size}")
     if len(lshape) != 1 or len(tshape) != 2 or tshape[0] != lshape[0] or table.dtype != i32 or lens.dtype != i32 or not lens.is_contiguous():
         raise OqError(1, f"{what}: table must be int32 [sequences, pages], lens contiguous int32 [sequences]")
     seqs, most = tshape
@@ -699,11 +701,12 @@ def _cache_rows(what, X, heads, head_dim):
     return _CACHE_ROWS.pack(X.data_ptr(), lt if n > 1 else head_dim * heads, lh if h > 1 else head_dim)
 
 
-def oq_cache_write(pages, K, V, table, lens, start=None, kind="fp8"):
+def oq_cache_write(pages, K, V, table, lens, start=None, kind="fp8", page_size=None):
     """Quantizes keys and values of new tokens into the pages of their sequences.  pages: CUDA uint8 [pages, kv_heads, bytes of a
     block] (oq_cache_alloc); K, V: CUDA bf16 or fp32 [T, kv_heads, head_dim], any strides of multiples of 16 bytes, unit stride
     inside a head; table: int32 [sequences, pages]; lens: int32 [sequences], the new tokens included; start: int32 [sequences + 1]
-    or None for one sequence."""
+    or None for one sequence.  The tokens of a page follow from its bytes, kind and head_dim; page_size, where it is given, has to agree
+    (pages of head_dim 128 pass for pages of twice as many tokens of 64 without it)."""
     import torch
     if K.dim() != 3 or K.shape != V.shape or K.dtype != V.dtype:
         raise OqError(1, "oq_cache_write: K and V must be [T, kv_heads, head_dim] of one type")
@@ -712,7 +715,7 @@ def oq_cache_write(pages, K, V, table, lens, start=None, kind="fp8"):
         raise _off_device("oq_cache_write")
     code = _dtype_code(K.dtype, "oq_cache_write")
     n, heads, head_dim = K.shape
-    fields, at = _cache_fields("oq_cache_write", torch, pages, head_dim, kind, table, lens, start, device)
+    fields, at = _cache_fields("oq_cache_write", torch, pages, head_dim, kind, table, lens, start, device, page_size)
     if heads != fields[6]:
         raise OqError(1, "oq_cache_write: the pages are of another number of heads")
     if n > _INT_MAX:
@@ -724,13 +727,13 @@ def oq_cache_write(pages, K, V, table, lens, start=None, kind="fp8"):
         _check(rc)
 
 
-def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp8", out_k=None, out_v=None, out_dtype=None):
+def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp8", out_k=None, out_v=None, out_dtype=None, page_size=None):
     """Reads the last start[s + 1] - start[s] tokens of each sequence back.  total: tokens of all sequences together (the tensors'
     first size where out_k or out_v is given).  Returns (K, V) [total, kv_heads, head_dim] of out_dtype (bf16 or fp32, bf16 by default).
-    With out_k or out_v given, only what is given is read."""
+    With out_k or out_v given, only what is given is read.  page_size: see oq_cache_write."""
     import torch
     device = pages.get_device()
-    fields, at = _cache_fields("oq_cache_read", torch, pages, head_dim, kind, table, lens, start, device)
+    fields, at = _cache_fields("oq_cache_read", torch, pages, head_dim, kind, table, lens, start, device, page_size)
     heads = fields[6]
     if out_k is None and out_v is None:
         if total is None or not 0 <= total <= _INT_MAX:
@@ -757,9 +760,9 @@ def oq_cache_read(pages, head_dim, table, lens, start=None, total=None, kind="fp
 
 
 def oq_cache_attention(Q, pages, table, lens, q_start=None, kind="fp8", left=-1, right=0, sinks=0, scale=0.0, max_q=0, out=None,
-                       want_lse=False, workspace=None):
+                       want_lse=False, workspace=None, page_size=None):
     """Attention of new tokens over the pages of their sequences, which hold the new tokens' keys and values already.  Q: CUDA bf16
-    [T, heads, head_dim] (any strides of multiples of 8, unit stride inside a head); pages, table, lens, q_start: see oq_cache_write.  left, right,
+    [T, heads, head_dim] (any strides of multiples of 8, unit stride inside a head); pages, table, lens, q_start, page_size: see oq_cache_write.  left, right,
     sinks, max_q: see oq.h.  Returns out [T, heads, head_dim], or (out, lse fp32 [heads, T]) with want_lse.  workspace: CUDA uint8
     tensor, by default one is taken from torch's allocator when the call needs it."""
     import torch
@@ -768,7 +771,7 @@ def oq_cache_attention(Q, pages, table, lens, q_start=None, kind="fp8", left=-1,
         raise OqError(1, "oq_cache_attention: Q must be bf16 [T, heads, head_dim]")
     device = Q.get_device()
     n, heads, head_dim = qs
-    fields, at = _cache_fields("oq_cache_attention", torch, pages, head_dim, kind, table, lens, q_start, device)
+    fields, at = _cache_fields("oq_cache_attention", torch, pages, head_dim, kind, table, lens, q_start, device, page_size)
     qt, qh, qc = Q.stride()
     if out is None:
         out = Q.new_empty(qs)

@@ -525,3 +525,19 @@ def test_refusals():
     assert empty[0].shape == (0, 4, 64) and empty[1].shape == (4, 0)
     w(pages, k[:0], k[:0], table, lens)
     assert r(pages, 64, table, lens, None, 0)[0].shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("kind", ["fp8", "fp4"])
+def test_a_page_size_that_the_pages_do_not_have_is_refused(kind):
+    """Pages of 16 tokens of head_dim 128 are as long as pages of 32 of head_dim 64: who says what they hold is told."""
+    import torch
+    pages = B.oq_cache_alloc(4, 16, 2, 128, kind)
+    table, lens = _i32([[0, 1, 2, 3]]), _i32([20])
+    k = torch.zeros((20, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for call in (lambda **kw: B.oq_cache_write(pages, k, k, table, lens, kind=kind, **kw), lambda **kw: B.oq_cache_read(pages, 64, table, lens, None, 20, kind=kind, **kw),
+                 lambda **kw: B.oq_cache_attention(k, pages, table, lens, kind=kind, **kw)):
+        with pytest.raises(B.OqError) as e:
+            call(page_size=16)
+        assert e.value.code == 1
+        call(page_size=32)
+        call()

@@ -99,3 +99,13 @@ def test_the_command(kind, capsys, monkeypatch):
     al.main()
     line = json.loads(capsys.readouterr().out)
     assert line["cache"] == kind and line["chunk"] == 12 and line["ms_cache_attention"] > 0
+
+
+@pytest.mark.gpu
+def test_a_cache_of_another_head_dim_is_refused():
+    layer, x, pos, _, _ = al.make_layer("small", n_adapters=0)
+    cache = al.PagedCache(8, layer.heads, {64: 128, 128: 64}[layer.head_dim], 1, 256)
+    cache.extend([30])
+    cache.step()
+    with pytest.raises(B.OqError):
+        layer(x[:30], pos[:30], right=0, cache=cache)
