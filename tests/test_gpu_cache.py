@@ -541,3 +541,46 @@ def test_a_page_size_that_the_pages_do_not_have_is_refused(kind):
         assert e.value.code == 1
         call(page_size=32)
         call()
+
+
+@pytest.mark.parametrize("n_seqs", [33, 256])
+@pytest.mark.parametrize("most", [1, 12])
+def test_many_sequences_in_long_tables(n_seqs, most):
+    """More sequences than lanes where items are cut along their keys: short ones, some of thousands of keys, and one for the other kernel."""
+    g = np.random.default_rng(n_seqs + most)
+    new = g.integers(0, most + 1, n_seqs).tolist()
+    lens = [n + int(k) for n, k in zip(new, g.integers(0, 200, n_seqs))]
+    for s in (0, n_seqs // 2, n_seqs - 2):
+        lens[s] += 2500
+    new[-1] += 40
+    lens[-1] += 900
+    pool = Pool(lens, 16, 1, 64, "fp8", nan=True).fill(2)
+    q = _bf16((sum(new), 4, 64), 5, 0.1).cuda()
+    out, lse = _run(q, pool, new)
+    _verify(q, pool, new, out, lse)
+
+
+@pytest.mark.parametrize("mask", [dict(), dict(left=700, right=5, sinks=150)], ids=str)
+def test_more_blocks_of_chunks_than_lanes(mask):
+    """56 blocks of 256 rows of three sequences, cut along their keys, beside a single token."""
+    new, lens = [1100, 1, 500, 150], [1500, 2000, 1300, 150]
+    pool = Pool(lens, 64, 1, 64, "fp4", nan=True).fill(2)
+    q = _bf16((sum(new), 8, 64), 5, 0.1).cuda()
+    out, lse = _run(q, pool, new, **mask)
+    _verify(q, pool, new, out, lse, **mask)
+
+
+@pytest.mark.parametrize("max_q", [0, 1])
+def test_more_blocks_than_threads_of_a_plan_that_cuts(max_q):
+    """625 blocks of 256 rows (20000 of 8) over 2000 positions, cut along their keys."""
+    pool = Pool([2000], 64, 1, 64, "fp8", nan=True).fill(4)
+    pages, table, lens = pool.device()
+    q = _bf16((1, 8, 64), 5, 0.1).cuda()
+    many = q.expand(20000, 8, 64)                                # all queries alike
+    out, lse = B.oq_cache_attention(many, pages, table, lens, want_lse=True, max_q=max_q, right=-1)
+    _verify(many[:1], pool, [1], out[:1], lse[:, :1], right=-1)
+    # (rows differ by where a cut falls alone: twice what one of them may be off by)
+    ref, ref_lse, size = oc.attention(_f64(q), pool.pages, pool.table, pool.lens, [1], "fp8", right=-1)
+    err = (out.double() - out[:1].double()).abs().amax(0).cpu().numpy()
+    assert np.all(err <= 2 * (2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -11 + 1e-4) * size[0]))
+    assert np.all(np.abs(_f64(lse) - ref_lse) <= LSE * (1 + np.abs(ref_lse)))
