@@ -165,7 +165,9 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
   extern __shared__ unsigned char smem_dyn[];
   __shared__ __align__(8) unsigned long long bars[10 + 2 * SLOTS + 2 * STAGES];
   __shared__ Plan pm;
-  __shared__ int raw_keys[STAGES];        // what a stage holds: number of keys that exist, and the pieces of 16 whose page is missing in bits 8 .. 15
+  // what a stage holds: number of keys that exist; the pieces of 16 whose page is missing in bits 8 .. 15; from bit 16 and from bit 24 on, the first
+  // key between the sinks and the first window of the item, which no row sees, and the first one behind these
+  __shared__ uint32_t raw_keys[STAGES];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -457,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       if (round > 0) mbar_spin(kv_free(slot), (round - 1) & 1, &abort_flag, p.status, W_KVFREE);
       mbar_spin(raw_full(stage), raw_round & 1, &abort_flag, p.status, W_RAW);
       __syncwarp();
-      const int keys = raw_keys[stage];
+      const uint32_t keys = raw_keys[stage];
       uint32_t src = from + stage * S::RAW, src_scale = from_scale + stage * S::RAW, dst = to + slot * S::KV_TILE;
       int r = my_row;
 #pragma unroll 1
@@ -468,11 +470,11 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           load_shared16(src + (uint32_t)(i * H::RPI * F::ROW), raws[i]);
           scales[i] = load_shared1(src_scale + (uint32_t)(i * H::RPI * F::GROUPS));
         }
-        if (keys != BN) {                            // some keys do not exist: zeros, whatever lies in their places
+        if (keys != BN) {                            // some keys do not exist, or nobody sees them: zeros, whatever lies in their places
 #pragma unroll
           for (int i = 0; i < BATCH; ++i) {
-            const int row = r + i * H::RPI;
-            if (row >= (keys & 255) || ((keys >> (8 + row / PIECE)) & 1)) {
+            const uint32_t row = (uint32_t)(r + i * H::RPI);
+            if (row >= (keys & 255u) || ((keys >> (8 + row / PIECE)) & 1u) || (row >= ((keys >> 16) & 255u) && row < keys >> 24)) {
               raws[i][0] = raws[i][1] = raws[i][2] = raws[i][3] = 0u;
               scales[i] = 127u;
             }
@@ -616,7 +618,9 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
       }
       while (have && !abort_flag) {
         const uint32_t there = __ballot_sync(~0u, page >= 0);
-        const int exist = min(it.s.nk - it.key0(st.off + j), BN), at = pos & ((1 << p.c.shift) - 1);
+        const int k0 = it.key0(st.off + j), exist = min(it.s.nk - k0, BN), at = pos & ((1 << p.c.shift) - 1);
+        const int unseen = min(max(p.sinks - k0, 0), BN), seen = min(it.lo - k0, BN);
+        const uint32_t what = (uint32_t)exist | (~there & 255u) << 8 | (seen > unseen ? (uint32_t)unseen << 16 | (uint32_t)seen << 24 : 0u);
         const bool mine = page >= 0 && lane % run == 0;
         const uint32_t keys = (uint32_t)(min(PIECES - lane, run) * PIECE);
         const uint8_t* const block = mine ? block_of(p.c, page, it.head) : nullptr;
@@ -635,7 +639,7 @@ __global__ void __launch_bounds__(THREADS, 1) chunk_kernel(const __grid_constant
           if (round > 0) mbar_wait(raw_free(stage), (round - 1) & 1, &abort_flag, p.status, W_RAWFREE);
           __syncwarp();
           if (lane == 0) {
-            raw_keys[stage] = exist | (int)((~there & 255u) << 8);
+            raw_keys[stage] = what;
             mbar_expect_tx(raw_full(stage), pieces * (F::ROW + F::GROUPS));
           }
           __syncwarp();

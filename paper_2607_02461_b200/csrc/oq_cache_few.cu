@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
     const Item it = make_item<BM>(p, pm, st.head, st.block);
     const int first = st.off, end = (int)min((long long)it.tiles, st.off + st.count);
     // The warp's steps: 16 keys of each tile, where some row may see one of them and their page is there.  The 16 lie in one page, so all of
-    // a step's loads have one address and constants beside it; keys behind the sequence's end are in the page too, and are read (K's scores are
+    // a step's loads have one address and constants beside it; keys behind the sequence's end and in front of the window are in the page too, and are read (K's scores are
     // replaced and V's rows cleared).
     const int in_page = (1 << p.c.shift) - 1;
     int j = first;
@@ -277,14 +277,16 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       b[0] = transpose8(pack_f16(w[0], w[1]));
       b[1] = transpose8(pack_f16(w[2], w[3]));
       // --------------------------------------------- O^T += V^T P^T ---------------------------------------------
-      if (pos + 16 > it.s.nk) {                          // what lies behind the end may be anything
+      if (pos + 16 > it.s.nk || (pos < it.lo && pos + 16 > p.sinks)) {       // what lies behind the end, or in front of all windows, may be anything
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (pos + 2 * t + (e & 1) + 8 * (e >> 1) >= it.s.nk) {
+        for (int e = 0; e < 4; ++e) {
+          const int key = pos + 2 * t + (e & 1) + 8 * (e >> 1);
+          if (key >= it.s.nk || (key < it.lo && key >= p.sinks)) {
             v.scale[e] = 127u;
 #pragma unroll
             for (int w = 0; w < L::VW; ++w) v.w[e][w] = 0u;
           }
+        }
       }
       const uint32_t f0 = scale_pair(v.scale[0], v.scale[1]), f1 = scale_pair(v.scale[2], v.scale[3]);
 #pragma unroll

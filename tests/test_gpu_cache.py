@@ -584,3 +584,21 @@ def test_more_blocks_than_threads_of_a_plan_that_cuts(max_q):
     err = (out.double() - out[:1].double()).abs().amax(0).cpu().numpy()
     assert np.all(err <= 2 * (2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -11 + 1e-4) * size[0]))
     assert np.all(np.abs(_f64(lse) - ref_lse) <= LSE * (1 + np.abs(ref_lse)))
+
+
+@pytest.mark.parametrize("byte", [0x7F, 0xFF])
+@pytest.mark.parametrize("kind,d", [("fp8", 64), ("fp4", 128)])
+@pytest.mark.parametrize("nq", [1, 5, 60, 300])
+@pytest.mark.parametrize("nk", [500, 1000])                      # items whole and cut
+def test_places_that_nothing_was_written_to_outside_the_window(nk, nq, kind, d, byte):
+    """A request taken over with its window alone: what lies before that, in pages that are there, may be any bytes, such as elements or scales that decode to NaN."""
+    left, sinks = nk // 5 + 7, 20
+    pool = Pool([nk], 32, 2, d, kind).fill(3)
+    for p in range(sinks, nk - nq - left):
+        for part in [x for block in pool.pages[pool.table[0, p // 32]] for x in oc._parts(block, 32, d, kind)]:
+            part[p % 32] = byte
+    q = _bf16((nq, 4, d), 5, 0.1).cuda()
+    pool.table = pool.table[:, :-(-nk // 32)].copy()
+    for mask in (dict(left=left, sinks=sinks), dict(left=left, right=-1, sinks=sinks)):
+        out, lse = _run(q, pool, [nq], **mask)
+        _verify(q, pool, [nq], out, lse, **mask)
