@@ -378,8 +378,8 @@ int oq_attention(const oq_attention_args* args, void* workspace, size_t workspac
  *             tokens over, a read gives zeros, attention does not see them
  *
  * pages dev, 16-byte aligned; table dev int32 [n_seqs][ld_table], max_pages columns in use; lens dev int32 [n_seqs].  head_dim 64 or 128,
- * n_seqs <= 256, max_pages * page_size <= 2^30.  Pages may be shared by sequences (a common beginning); of tokens written to one place in one call any is kept, in
- * each of its values. */
+ * n_seqs <= 256, max_pages * page_size <= 2^30.  Pages may be shared by sequences (a common beginning).  Tokens
+ * that one call writes to one place have to be alike there: of different ones some values may be read back of each, and some with the other's scale. */
 enum { OQ_CACHE_FP8 = 8, OQ_CACHE_FP4 = 4 };
 typedef struct {
   void* pages;

@@ -602,3 +602,19 @@ def test_places_that_nothing_was_written_to_outside_the_window(nk, nq, kind, d, 
     for mask in (dict(left=left, sinks=sinks), dict(left=left, right=-1, sinks=sinks)):
         out, lse = _run(q, pool, [nq], **mask)
         _verify(q, pool, [nq], out, lse, **mask)
+
+
+@pytest.mark.parametrize("kind", ["fp8", "fp4"])
+def test_a_shared_beginning_written_by_all_of_its_sequences(kind):
+    """The same tokens to the same places from several sequences of one call, and further ones to pages of their own."""
+    import torch
+    lens = [100, 130, 64]
+    pool = Pool(lens, 32, 2, 64, kind)
+    pool.table[1, :2], pool.table[2, :2] = pool.table[0, :2], pool.table[0, :2]
+    pages, table, at = pool.device()
+    k, v = _bf16((64, 2, 64), 1), _bf16((64, 2, 64), 2)
+    k, v = (torch.cat([x for n in lens for x in (own, _bf16((n - 64, 2, 64), 3 + n))]).cuda() for own in (k, v))
+    for _ in range(3):
+        B.oq_cache_write(pages, k, v, table, at, _starts(lens), kind=kind)
+    oc.write(pool.pages, _f64(k), _f64(v), pool.table, lens, lens, 64, kind)
+    assert np.array_equal(pages.cpu().numpy(), pool.pages)
