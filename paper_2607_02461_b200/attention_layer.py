@@ -171,6 +171,8 @@ def main():
     ap.add_argument("--chunk", type=int, default=1560, help="tokens of a chunk, with --cache")
     ap.add_argument("--iters", type=int, default=10)
     a = ap.parse_args()
+    if a.chunk < 1:
+        ap.error("--chunk: at least one token")
     layer, x, pos, starts, adapters = make_layer(a.shape, a.adapters)
     left = a.window if a.window > 0 else -1
 

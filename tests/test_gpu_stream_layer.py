@@ -109,3 +109,11 @@ def test_a_cache_of_another_head_dim_is_refused():
     cache.step()
     with pytest.raises(B.OqError):
         layer(x[:30], pos[:30], right=0, cache=cache)
+
+
+@pytest.mark.parametrize("chunk", ["0", "-5"])
+def test_chunks_of_no_tokens_are_refused(chunk, capsys, monkeypatch):
+    monkeypatch.setattr("sys.argv", ["attention_layer", "--shape", "small", "--cache", "fp8", "--chunk", chunk])
+    with pytest.raises(SystemExit) as e:
+        al.main()
+    assert e.value.code == 2 and "at least one token" in capsys.readouterr().err
