@@ -11,84 +11,38 @@ namespace cache {
 
 constexpr int JOIN_WARPS = 8, JOIN_ROWS = JOIN_WARPS;
 
-// CTA (c, y): rows 8 y .. 8 y + 7 of the item that CTA c of the kernel before began and did not finish, if there is one.  Parts of a row are weighed by
-// l 2^(c (m - max m)).  The warps that a row has beside the others' take every so many parts each; the first ones are requested before their
-// weights are known.  (Four rows a warp, for more bytes on their way or fewer instructions: the same time with two parts a row, 2 to 8 us more with eighteen.)
-template <int BM, int D>
+// CTA (c, y): rows 8 y .. 8 y + 7 of the item that CTA c of the kernel before began and did not finish, if there is one.  The warps that a row has beside the others' take
+// every so many parts each.  (Four rows a warp, for more bytes on their way or fewer instructions: the same time with two parts a row, 2 to 8 us more with eighteen.)
+template <int D>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) cache_join_kernel(const __grid_constant__ AttnParams p) {
-  constexpr int N = D / 32, AHEAD = 4;
+  constexpr int N = D / 32;
   __shared__ float sums[JOIN_WARPS][D];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Cut cut = p.cuts[blockIdx.x];
-  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, cut.rows - row0), parts = cut.parts;
+  const int row0 = JOIN_ROWS * blockIdx.y, rows = min(JOIN_ROWS, cut.rows - row0);
   if (rows <= 0) return;
   int per_row = JOIN_WARPS;
   while (per_row > 1 && per_row * rows > JOIN_WARPS) per_row >>= 1;
   const int r = warp / per_row, share = warp % per_row;
-  const bool mine = r < rows;
-  const int row = row0 + (mine ? r : 0);
-  auto slot = [&](int i) { return (2ll * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * BM + row; };
-  float v[AHEAD][N];
-  auto load = [&](int i0) {
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s) {
-      const int i = i0 + s * per_row;
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[s][e] = i < parts ? p.part_o[slot(i) * D + N * lane + e] : 0.f;
-    }
-  };
-  load(share);
-  float top = -INFINITY, factor = 0.f, total = 0.f;
-  for (int i = lane; i < parts; i += 32) {
-    const float4 ml = p.part_ml[slot(i)];
-    top = fmaxf(top, ml.x);
-    factor = ml.z;
-  }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  factor = __shfl_sync(~0u, factor, 0);
-  auto weight = [&](const float4& ml) { return ml.y == 0.f ? 0.f : ml.y * (ml.x == top ? 1.f : exp2_fast((ml.x - top) * factor)); };
-  for (int i = lane; i < parts; i += 32) total += weight(p.part_ml[slot(i)]);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
-  const float inv = total == 0.f ? 0.f : 1.f / total;
-  float acc[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  for (int i0 = share; i0 < parts; i0 += AHEAD * per_row) {
-    if (i0 != share) load(i0);
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s) {
-      const int i = i0 + s * per_row;
-      if (i >= parts) continue;
-      const float w = weight(p.part_ml[slot(i)]) * inv;
-      if (w == 0.f) continue;
-#pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[s][e], acc[e]);
-    }
-  }
+  float acc[N], top, total, factor;
+  join_row<CHUNK_ROWS, D>(p, Parts{(int)blockIdx.x, cut.parts}, row0 + r, cut.rows, share, per_row, acc, top, total, factor);
   if (per_row > 1) {
 #pragma unroll
     for (int e = 0; e < N; ++e) sums[warp][N * lane + e] = acc[e];
     __syncthreads();
   }
-  if (!mine || share) return;
+  if (r >= rows || share) return;
   for (int w = 1; w < per_row; ++w)
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] += sums[warp + w][N * lane + e];
-  const int q = cut.r0 + row, tok = token_of(p, q), i = cut.q_base + tok, qh = cut.head * p.group + q - tok * p.group;
-  __nv_bfloat16* dst = p.out + (long long)i * p.ldo + qh * p.hdo + N * lane;
-#pragma unroll
-  for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);
-  if (lane == 0 && p.lse) p.lse[(long long)qh * p.total_q + i] = natural_lse(top, total, factor);
+  write_row<D>(p, cut.q_base, cut.head, cut.r0 + row0 + r, acc, top, total, factor);
 }
 
-template <int BM>
 static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas, (unsigned)(BM / JOIN_ROWS));
+  cfg.gridDim = dim3((unsigned)ctas, (unsigned)(CHUNK_ROWS / JOIN_ROWS));
   cfg.blockDim = dim3(32 * JOIN_WARPS);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -96,7 +50,7 @@ static cudaError_t launch_join(const AttnParams& p, int head_dim, int ctas, cuda
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return head_dim == 128 ? cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 128>, p) : cudaLaunchKernelEx(&cfg, cache_join_kernel<BM, 64>, p);
+  return head_dim == 128 ? cudaLaunchKernelEx(&cfg, cache_join_kernel<128>, p) : cudaLaunchKernelEx(&cfg, cache_join_kernel<64>, p);
 }
 
 static int sm_count() {
@@ -227,8 +181,7 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
   p.left = a->left < 0 ? -1 : (a->left > far ? far : a->left);
   p.right = a->right < 0 ? -1 : (a->right > far ? far : a->right);
   p.sinks = a->sinks > far ? far : a->sinks;
-  p.scale = a->scale > 0.f ? a->scale : (d == 128 ? 0.08838834764831845f : 0.125f);
-  p.scale_log2 = p.scale * 1.4426950408889634f;
+  p.scale_log2 = (a->scale > 0.f ? a->scale : (d == 128 ? 0.08838834764831845f : 0.125f)) * 1.4426950408889634f;
   p.status = device_status_word();
   if (!p.status) return fail(OQ_ERR_CUDA, "oq_cache_attention: cannot allocate the device status word");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -245,7 +198,7 @@ int oq_cache_attention(const oq_cache_attention_args* a, void* workspace, size_t
       p.cuts = nullptr;                              // nothing is cut
     }
     cudaError_t err = launch(p, a->cache.kind, d, ctas, st);
-    if (err == cudaSuccess && bytes && rows == CHUNK_ROWS) err = launch_join<CHUNK_ROWS>(p, d, ctas, st);
+    if (err == cudaSuccess && bytes && rows == CHUNK_ROWS) err = launch_join(p, d, ctas, st);
     return err;
   };
   if (ch.chunk) {

@@ -41,7 +41,7 @@ struct AttnParams {
   int row_min, row_max;                    // this kernel takes the sequences with row_min < rows <= row_max
   int whole;                               // items are not cut
   int left, right, sinks;
-  float scale, scale_log2;
+  float scale_log2;                        // scale / ln 2
   int* status;
 };
 
@@ -367,81 +367,62 @@ __device__ __forceinline__ float natural_lse(float m, float l, float c) {
   return l == 0.f ? -INFINITY : fmaf(m, c, log2f(l)) * 0.69314718055994531f;
 }
 
-// Rows row0 .. row0 + ROWS - 1 of an item (those from `rows` on stand in for the last) from the parts of CTAs q.first .. : by a warp, its parts share,
-// share + step, ... of them; lane l has coordinates N l .. of the results, and the rows' references and sums are returned.  Parts are weighed by
-// l 2^(c (m - max m)); the first ones are requested before their weights are known.
-template <int BM, int D, int ROWS>
-__device__ __forceinline__ void join_rows(const AttnParams& p, const Parts& q, int row0, int rows, int share, int step, float (&acc)[ROWS][D / 32], float (&top)[ROWS],
-                                          float (&total)[ROWS], float (&factor)[ROWS]) {
-  constexpr int N = D / 32, AHEAD = ROWS > 1 ? 2 : 4;
+// Row `row` of an item (one from `rows` on stands in for the last) from the parts of CTAs q.first .. : by a warp, its parts share, share + step, ... of them; lane l has
+// coordinates N l .. of the result, and the row's reference and sum are returned.  Parts are weighed by l 2^(c (m - max m)); the first ones are requested before their
+// weights are known.
+template <int BM, int D>
+__device__ __forceinline__ void join_row(const AttnParams& p, const Parts& q, int row, int rows, int share, int step, float (&acc)[D / 32], float& top, float& total,
+                                         float& factor) {
+  constexpr int N = D / 32, AHEAD = 4;
   const int lane = threadIdx.x & 31;
-  auto slot = [&](int i, int r) { return (2ll * (q.first + i) + (i == 0 ? 1 : 0)) * BM + min(row0 + r, rows - 1); };
-  float v[ROWS][AHEAD][N];
+  auto slot = [&](int i) { return (2ll * (q.first + i) + (i == 0 ? 1 : 0)) * BM + min(row, rows - 1); };
+  float v[AHEAD][N];
   auto load = [&](int i0) {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * step;
 #pragma unroll
-      for (int s = 0; s < AHEAD; ++s) {
-        const float* at = p.part_o + slot(min(i0 + s * step, q.parts - 1), r) * D + N * lane;
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const float2 x = __ldcg(reinterpret_cast<const float2*>(at + e));
-          v[r][s][e] = x.x;
-          v[r][s][e + 1] = x.y;
-        }
+      for (int e = 0; e < N; e += 2) {
+        const float2 x = i < q.parts ? __ldcg(reinterpret_cast<const float2*>(p.part_o + slot(i) * D + N * lane + e)) : make_float2(0.f, 0.f);
+        v[s][e] = x.x;
+        v[s][e + 1] = x.y;
       }
+    }
   };
   load(share);
-  float w[ROWS];                                     // of part `lane`, where there are no more than the lanes
-  float4 ml[ROWS];
+  const float4 ml = __ldcg(p.part_ml + slot(min(lane, q.parts - 1)));
+  top = ml.x;
+  factor = ml.z;
+  for (int i = lane + 32; i < q.parts; i += 32) top = fmaxf(top, __ldcg(p.part_ml + slot(i)).x);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    ml[r] = __ldcg(p.part_ml + slot(min(lane, q.parts - 1), r));
-    top[r] = ml[r].x;
-    factor[r] = ml[r].z;
-    total[r] = 0.f;
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  auto weight = [&](const float4& x) { return x.y == 0.f ? 0.f : x.y * (x.x == top ? 1.f : exp2_fast((x.x - top) * factor)); };
+  const float w = lane < q.parts ? weight(ml) : 0.f;
+  total = w;
+  for (int i = lane + 32; i < q.parts; i += 32) total += weight(__ldcg(p.part_ml + slot(i)));
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[r][e] = 0.f;
-  }
-  for (int i = lane + 32; i < q.parts; i += 32)
+  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(~0u, total, d);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __ldcg(p.part_ml + slot(i, r)).x);
-  auto weight = [&](const float4& x, int r) { return x.y == 0.f ? 0.f : x.y * (x.x == top[r] ? 1.f : exp2_fast((x.x - top[r]) * factor[r])); };
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], d));
-    w[r] = total[r] = lane < q.parts ? weight(ml[r], r) : 0.f;
-  }
-  for (int i = lane + 32; i < q.parts; i += 32)
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) total[r] += weight(__ldcg(p.part_ml + slot(i, r)), r);
-  float inv[ROWS];
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) total[r] += __shfl_xor_sync(~0u, total[r], d);
-    inv[r] = total[r] == 0.f ? 0.f : 1.f / total[r];
-  }
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
   for (int i0 = share; i0 < q.parts; i0 += AHEAD * step) {
     if (i0 != share) load(i0);
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int s = 0; s < AHEAD; ++s) {
+      const int i = i0 + s * step;
+      if (i >= q.parts) continue;
+      const float x = (i < 32 ? __shfl_sync(~0u, w, i) : weight(__ldcg(p.part_ml + slot(i)))) * inv;
+      if (x == 0.f) continue;
 #pragma unroll
-      for (int s = 0; s < AHEAD; ++s) {
-        const int i = i0 + s * step;
-        if (i >= q.parts) continue;
-        const float x = (i < 32 ? __shfl_sync(~0u, w[r], i) : weight(__ldcg(p.part_ml + slot(i, r)), r)) * inv[r];
-        if (x == 0.f) continue;
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[r][e] = fmaf(x, v[r][s][e], acc[r][e]);
-      }
+      for (int e = 0; e < N; ++e) acc[e] = fmaf(x, v[s][e], acc[e]);
+    }
   }
 }
+// Row r of a sequence whose queries begin at q_base, for a key and value head: its result, by a warp.
 template <int D>
-__device__ __forceinline__ void write_row(const AttnParams& p, const Item& it, int row, const float (&acc)[D / 32], float top, float total, float factor) {
+__device__ __forceinline__ void write_row(const AttnParams& p, int q_base, int kv_head, int r, const float (&acc)[D / 32], float top, float total, float factor) {
   constexpr int N = D / 32;
-  const int lane = threadIdx.x & 31, r = it.r0 + row, tok = token_of(p, r), i = it.s.q_base + tok, head = it.head * p.group + r - tok * p.group;
+  const int lane = threadIdx.x & 31, tok = token_of(p, r), i = q_base + tok, head = kv_head * p.group + r - tok * p.group;
   __nv_bfloat16* dst = p.out + (long long)i * p.ldo + head * p.hdo + N * lane;
 #pragma unroll
   for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(dst + e) = pack_bf16(acc[e], acc[e + 1]);

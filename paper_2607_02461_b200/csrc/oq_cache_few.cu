@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
       if (whole) {
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] *= inv;
-        write_row<D>(p, it, r, acc, top, total, c_s[r]);
+        write_row<D>(p, it.s.q_base, it.head, it.r0 + r, acc, top, total, c_s[r]);
       } else {
         float* dst = p.part_o + (slot * BM + r) * D + N * lane;
 #pragma unroll
@@ -375,9 +375,8 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
         int per_row = WARPS;
         while (per_row > 1 && per_row * it.rows > WARPS) per_row >>= 1;
         const int r = warp / per_row, share = warp % per_row;
-        float joined[1][N], top[1], total[1], factor[1];
-        join_rows<BM, D, 1>(p, q, r, it.rows, share, per_row, joined, top, total, factor);
-        float(&acc)[N] = joined[0];
+        float acc[N], top, total, factor;
+        join_row<BM, D>(p, q, r, it.rows, share, per_row, acc, top, total, factor);
 #pragma unroll
         for (int e = 0; e < N; ++e) part[warp * D + N * lane + e] = acc[e];
         __syncthreads();
@@ -385,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, FEW_CTAS) few_kernel(const __grid_con
           for (int w = 1; w < per_row; ++w)
 #pragma unroll
             for (int e = 0; e < N; ++e) acc[e] += part[(warp + w) * D + N * lane + e];
-          write_row<D>(p, it, r, acc, top[0], total[0], factor[0]);
+          write_row<D>(p, it.s.q_base, it.head, it.r0 + r, acc, top, total, factor);
         }
         __syncthreads();
       }
