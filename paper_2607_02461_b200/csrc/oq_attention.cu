@@ -162,33 +162,10 @@ __device__ __forceinline__ Item make_item(const Params& p, const int* prefix, in
   return it;
 }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // two fp32 lanes in one instruction
 __device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
   asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n mov.b64 c, {%5, %5};\n fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}"
       : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
-}
-__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
-  asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n mov.b64 d, {%0, %1};\n add.rn.f32x2 d, d, a;\n mov.b64 {%0, %1}, d;\n}"
-      : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1));
-}
-// bits 0 .. n-1 of a word, n clamped to 0 .. 32
-__device__ __forceinline__ uint32_t ones_below(int n) {
-  return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u);
 }
 
 __device__ __forceinline__ float natural_lse(const Params& p, float m, float l) {

@@ -16,6 +16,7 @@
 // one of them (2048 tokens over 16385: 416 us) and have a kernel of their own (380).
 #pragma once
 #include "oq_cache.cuh"
+#include "oq_sm100.cuh"
 
 namespace oq {
 namespace cache {
@@ -326,19 +327,9 @@ __device__ __forceinline__ void next_item(Stretch& st, const Item& it, int n) {
   next_item(st, n);
 }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
 

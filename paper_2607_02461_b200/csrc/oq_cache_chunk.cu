@@ -31,7 +31,6 @@
 #include <string>
 
 #include "oq_cache_attention.cuh"
-#include "oq_sm100.cuh"
 
 namespace oq {
 namespace cache {
@@ -62,11 +61,6 @@ struct Shape {
   static constexpr uint32_t SMEM = 1024 + 2 * Q_TILE + SLOTS * KV_TILE + STAGES * RAW;
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // two fp32 lanes in one instruction
 __device__ __forceinline__ uint64_t twice(float x) {
   uint64_t d;
@@ -76,12 +70,6 @@ __device__ __forceinline__ uint64_t twice(float x) {
 __device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, uint64_t b, uint64_t c) {
   asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n fma.rn.f32x2 d, a, %4, %5;\n mov.b64 {%0, %1}, d;\n}" : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "l"(b), "l"(c));
 }
-__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
-  asm("{\n .reg .b64 a, d;\n mov.b64 a, {%2, %3};\n mov.b64 d, {%0, %1};\n add.rn.f32x2 d, d, a;\n mov.b64 {%0, %1}, d;\n}"
-      : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1));
-}
-// bits 0 .. n-1 of a word, n clamped to 0 .. 32
-__device__ __forceinline__ uint32_t ones_below(int n) { return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u); }
 
 __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
