@@ -232,6 +232,13 @@ bool rows_meet(long long apart, long long tokens, long long heads, long long ld_
   } else {                                           // two sets, one behind the other
     const wide reach = all_heads + all_tokens - width;
     if (apart >= reach || -(wide)apart >= reach) return false;
+    // beside each other in the rows of one tensor, and dealt out between each other's heads
+    auto between = [&](long long ld, wide need) {
+      const long long at = (apart % ld + ld) % ld;
+      return at >= need && ld - at >= need;
+    };
+    if (ld_token && between(ld_token, all_heads)) return false;
+    if (ld_head && ld_token % ld_head == 0 && between(ld_head, width)) return false;
   }
   // else: rows dh heads and dt tokens from each other are apart + dh ld_head + dt ld_token apart; of the dt only those beside the quotient can be close
   for (long long dh = 1 - heads; dh < heads; ++dh) {
