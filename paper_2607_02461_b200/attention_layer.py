@@ -43,7 +43,8 @@ class _Projection:
 
 class PagedCache:
     """Keys and values of one layer for several requests, in 8 or 4 bits, in pages of one pool (see oq_cache_write).  The book-keeping is the
-    host's: extend() and forget() take pages from the pool and give them back, table and lens on the device follow in the next step()."""
+    host's: extend() and forget() take pages from the pool and give them back, table and lens on the device follow in the next step().  Positions
+    count from a request's first token on, so max_tokens bounds all that it ever has, the tokens whose pages were given back included."""
 
     def __init__(self, n_pages, kv_heads, head_dim, requests, max_tokens, page_size=64, kind="fp8", device="cuda"):
         self.pages = B.oq_cache_alloc(n_pages, page_size, kv_heads, head_dim, kind, device)

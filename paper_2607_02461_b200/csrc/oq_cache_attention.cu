@@ -70,10 +70,10 @@ static unsigned long long next_tag() {
 }
 
 // Items of up to so many tiles are not cut along their keys: joining the parts takes longer than the tiles do.  Measured at 1, 3, 20, 80 and 300 rows, 4 and 24 heads, one
-// sequence and eight: whole items are better in all of 20 at 256 keys and at 384, in 19 at 512, in 8 at 1024.  us, cut / whole: one token, 4 heads, 256 keys 9.1 / 6.8,
-// 512 keys 9.1 / 8.7, 1024 keys 9.1 / 12.5; eight sequences of 20 rows, 24 heads, 512 keys 28.9 / 21.2; 300 rows, 24 heads, 512 keys 30.9 / 24.0; the one that loses at
-// 512 keys, 80 rows, 4 heads: 14.6 / 16.6.  (At 1024 keys whole ones win where there are many items, eight sequences of 300 rows, 24 heads 101 / 87, if their lengths are
-// alike, which is not known here.)
+// sequence and eight: whole items are better in all of 20 at 256 keys, in 19 at 384, in 18 at 512, in 6 at 1024.  us, cut / whole: one token, 4 heads, 256 keys 8.4 / 6.2,
+// 512 keys 8.4 / 8.1, 1024 keys 8.6 / 11.9; eight sequences of 20 rows, 24 heads, 512 keys 28.1 / 20.7; 300 rows, 24 heads, 512 keys 30.2 / 24.5; those that lose, 4 heads:
+// 80 rows, 384 keys 13.5 / 14.9, 512 keys 13.8 / 16.8, 300 rows, 512 keys 21.0 / 23.1.  (At 1024 keys whole ones win where there are many items, eight sequences of 300 rows,
+// 24 heads 100 / 90, if their lengths are alike, which is not known here.)
 constexpr long long WHOLE_TILES = 4;
 
 // Which kernels run, with how many CTAs, and what their parts take.  Nothing is known here of the sequences but their number, the tokens of all

@@ -8,12 +8,12 @@
 // An item is a block of BM rows of one sequence and key and value head, with the tiles of 128 keys that some row of it sees (one, if
 // there are none).  All items, one after the other, are a line that is cut into as many equal stretches as there are CTAs, so the lengths may
 // be of any kind: they are on the device only, and every CTA finds its own stretch from them.  The line's units are tiles, and beside an item's tiles
-// as many units, in front of them, as it takes time to begin and end it (requests of a few tiles beside long ones: 113 us without them, 88 with).  Where a cut
+// as many units, in front of them, as it takes time to begin and end it (requests of a few tiles beside long ones: 113 us without them, 88 with, 85 with the present join).  Where a cut
 // falls among these the item begins in the stretch behind it.  An item that lies in one stretch is
 // finished there; of others each CTA writes its part.  A CTA has at most two such parts: part 0 of the item that its stretch begins inside of, and part 1 of
 // the one that begins in it and goes on behind it.  Of an item of few rows who writes the last part joins them (in the order of the keys, whoever it is, so
 // results do not depend on it): that saves a launch, 2 us of the 20 of four requests of five tokens.  The parts of an item of 256 rows are too long to be joined by what wrote
-// one of them (2048 tokens over 16385: 416 us) and have a kernel of their own (380).
+// one of them (2048 tokens over 16385: 416 us) and have a kernel of their own (381).
 #pragma once
 #include "oq_cache.cuh"
 #include "oq_sm100.cuh"
@@ -427,8 +427,8 @@ constexpr int FEW_ROWS = 8, CHUNK_ROWS = 256;      // rows of their items
 constexpr int FEW_OVERHEAD = 2, CHUNK_OVERHEAD = 4;       // what an item takes beside its tiles, in tiles
 constexpr int FEW_CTAS = 2;                         // of an SM
 // Rows up to which a sequence goes to the kernel for few, which reads the cache once for 8 of them where the other reads it once for 256 but takes
-// longer to begin.  us, kernel for few / for chunks, e4m3: 16384 keys x 40 heads, 8 rows 42 / 91, 16 rows 70 / 91, 24 rows 93 / 92, 32 rows 123 / 93;
-// 4096 keys x 8 heads, 24 rows 18 / 21, 40 rows 20 / 22, 64 rows 24 / 23; 16384 keys x 8 heads, 24 rows 29 / 34, 40 rows 37 / 35, 64 rows 51 / 38.
+// longer to begin.  us, kernel for few / for chunks, e4m3: 16384 keys x 40 heads, 8 rows 40 / 85, 16 rows 67 / 85, 24 rows 92 / 86, 32 rows 121 / 86;
+// 4096 keys x 8 heads, 24 rows 15 / 19, 40 rows 17 / 19, 64 rows 21 / 20; 16384 keys x 8 heads, 24 rows 28 / 31, 40 rows 37 / 31, 64 rows 51 / 33.
 constexpr int FEW_LIMIT = 24;
 
 }  // namespace cache

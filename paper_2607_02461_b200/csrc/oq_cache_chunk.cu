@@ -17,12 +17,12 @@
 //   4 warps                  convert: from a stage, 128 keys of K or V, to a slot of a second ring, fp16 in the tensor cores' order
 //   2 mma warps              one per 128 rows: S_t = Q_t K^T into tensor memory, O_t += P_t V with P_t from tensor memory
 //
-// Measured (B200, head_dim 128; device time of captured calls): 2048 tokens over 16385, 24 heads on 8, causal, e2m1 378 us = 1.02 PFLOP/s; a streamed frame of
-// 1560 tokens over 15600 of 32760, 40 heads, e4m3 531 us = 0.89; 4608 over 4608, 24 heads, e4m3 288 us = 0.91 (oq_attention on bf16 keys and values: 379, 471 and
-// 229 us, without a cache to keep, read back or move; head_dim 64 is bound by the exponentials, 0.60 PFLOP/s).  A step of 256 rows x 128 keys takes 3850 cycles, an
+// Measured (B200, head_dim 128; device time of captured calls): 2048 tokens over 16385, 24 heads on 8, causal, e2m1 381 us = 1.01 PFLOP/s; a streamed frame of
+// 1560 tokens over 15600 of 32760, 40 heads, e4m3 544 us = 0.87; 4608 over 4608, 24 heads, e4m3 299 us = 0.87 (oq_attention on bf16 keys and values on the same GPU: 376, 470 and
+// 221 us, without a cache to keep, read back or move; head_dim 64 is bound by the exponentials, 0.61 PFLOP/s).  A step of 256 rows x 128 keys takes 3850 cycles, an
 // item's begin and end as much as four of them.  What decoding costs: a copy of this kernel that stored nothing in the slots took 6 to 12 % less, one whose mma
 // warps did not wait for slots at all 25 % (the softmax and the products alone).  Other arrangements that were measured, beside the 512 us of the first form of the
-// 378: K and V loaded into the convert warps' registers 504; stages of half a tile, a slot more 476 beside 458; S read from tensor memory twice, 32 columns at a
+// 381: K and V loaded into the convert warps' registers 504; stages of half a tile, a slot more 476 beside 458; S read from tensor memory twice, 32 columns at a
 // time, for fewer registers 560 beside 458; the next turn at the exponentials given away a quarter earlier 462 beside 462, a half earlier 470; one copy of each
 // MMA sequence instead of two 422 beside 387; a row of queries loaded by 16 lanes instead of one 414 beside 390.
 //

@@ -13,9 +13,9 @@
 // 8 warps each take 16 keys of a tile of 128 and keep their own maximum, sum and O; they are put together at the end of an item.  A warp's
 // next keys are requested as soon as the present ones are decoded, its next values likewise; two CTAs an SM have 66 KB on their way.
 //
-// Measured (B200, device time of captured calls): one token over 32760 of 40 heads of 128 in e4m3 66 us = 5.2 TB/s, 0.80 of the copy rate (the loop alone runs at 0.95 of it;
+// Measured (B200, device time of captured calls): one token over 32760 of 40 heads of 128 in e4m3 65.6 us = 5.3 TB/s, 0.81 of the copy rate (the loop alone runs at 0.95 of it;
 // 5 us go by before the first keys arrive, as much at the end); in e2m1 57 us = 3.1 TB/s, bound by issue and latency: 410 instructions for 16 keys x 128 a warp, 145 of
-// them at half rate; 16 requests of one token, 17 to 16384 cached, 24 heads on 8, e2m1 38 us; four of five tokens 15 us.  With 16 rows a block (twice the sums and fragments,
+// them at half rate; 16 requests of one token, 17 to 16384 cached, 24 heads on 8, e2m1 37 us; four of five tokens 14.7 us.  With 16 rows a block (twice the sums and fragments,
 // spilled) the first took 270 us; loads that the compiler could move to their use 2 us more; one CTA an SM 87 us; three, with spills, 65 (e2m1); two sums of S in
 // turn, to halve its chain of products, no less.
 #include <string>
