@@ -409,7 +409,7 @@ int oq_cache_read(const oq_cache* cache, const oq_cache_rows* K, const oq_cache_
  * query i of a sequence with nq new and nk cached tokens stands at place p = i + nk - nq and sees key j iff
  *     j <= p + right (right < 0: no limit)   and   (j >= p - left (left < 0: no limit)  or  j < sinks)   and its page is there
  * out = sum_j softmax_j(scale * q . k_j) v_j, lse = log sum_j exp(scale * q . k_j); a query that sees nothing gets 0 and -inf.  A query that holds
- * NaN or an infinity gets NaN where it sees something.
+ * NaN or an infinity gets NaN where it sees something.  Places of a page that no query sees may hold any bytes.
  *   Q        dev bf16, strides in elements, multiples of 8, not negative; 16-byte aligned
  *   out      dev bf16, strides at least head_dim, no row over another; must not overlap Q or the pages.   lse dev fp32 [n_heads][total_q], or NULL
  *   q_start  dev int32 [n_seqs + 1] (see start above), NULL: one sequence.  Queries of no sequence are not written
